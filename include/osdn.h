@@ -255,6 +255,115 @@ int osdn_bwd_packed(const osdn_params *p, const void *q, const void *k, const vo
                     void *stream);
 
 /*
+ * Around the recurrence: the rows of queries, keys and values of a layer, each K adjacent elements of io_dtype (K in {64, 128, 256}),
+ * wherever the caller has them (slices of one projection's output, views): element (b, t, h, i) stands
+ * batch b + token t + head h + i elements behind data.  No two rows of an output may overlap.  Rows
+ * need no more alignment than their elements; rows that start on 16 bytes are read and written in one piece.
+ */
+typedef struct { void *data; int64_t batch, token, head; } osdn_rows;
+
+typedef enum { OSDN_NORM_NONE = 0, OSDN_NORM_RMS = 1, OSDN_NORM_L2 = 2 } osdn_norm;
+
+typedef struct {
+    int32_t B, T, Hq, Hk, K;        /* batch entries, tokens, heads of the queries and of the keys (and values), width */
+    int32_t io_dtype;               /* osdn_dtype of the rows (and of a cache) */
+    int32_t norm;                   /* osdn_norm: r = (sum x^2 / K + eps)^-1/2, (sum x^2 + eps)^-1/2, or 1 */
+    int32_t rotary_dim;             /* elements that turn, from the front of a row: 0, or a multiple of 16 up to K */
+    int32_t rotary_rows;            /* positions that the table has */
+    int32_t interleaved;            /* pairs that turn: 0: (i, i + rotary_dim / 2); 1: (2i, 2i + 1) */
+    float eps;                      /* > 0, finite (norm = NONE: not looked at) */
+} osdn_norm_params;
+
+/*
+ * Norm of queries and keys for each head, with the position rotation in the same pass.  A row x becomes
+ *     z = R(p) (w . x r),
+ * R(p): pair i of the first rotary_dim elements turned by the angle whose cosine and sine are rotary[p][i] and
+ * rotary[p][rotary_dim / 2 + i].  Computed in fp32, rounded once.  (norm = L2 without weights or rotation is
+ * what osdn_fwd expects of its caller's queries and keys.)
+ *   q, k              [B,T,Hq,K], [B,T,Hk,K]; Hq or Hk may be 0, then its arguments are not looked at
+ *   weight_q, weight_k [K] fp32 or NULL (=> ones)
+ *   rotary            [rotary_rows, rotary_dim] fp32, NULL iff rotary_dim == 0
+ *   positions         [B,T] int32 or NULL (=> t).  A negative position is a token that does not exist: its
+ *                     outputs (and gradients) are zero.  A position that the table does not have makes them NaN.
+ *   q_out, k_out      out; may be the input rows themselves (same pointer and strides)
+ * At most 2^31 - 1 rows.
+ */
+int osdn_qk_norm_fwd(const osdn_norm_params *p, const osdn_rows *q, const osdn_rows *k, const float *weight_q,
+                     const float *weight_k, const float *rotary, const int32_t *positions, const osdn_rows *q_out,
+                     const osdn_rows *k_out, void *stream);
+
+/*
+ * Backward of osdn_qk_norm_fwd from its inputs (nothing is kept by the forward pass):
+ *   dq_out, dk_out    gradients of q_out and k_out
+ *   dq, dk            out; may be the rows of dq_out and dk_out, or of q and k, themselves
+ *   dweight_q, dweight_k [K] fp32 out, summed over all tokens and heads in a fixed order; NULL where it is not wanted
+ *   workspace         osdn_qk_norm_bwd_workspace_bytes(p) bytes, 256-byte aligned; may be NULL where neither dweight is wanted
+ */
+size_t osdn_qk_norm_bwd_workspace_bytes(const osdn_norm_params *p);
+int osdn_qk_norm_bwd(const osdn_norm_params *p, const osdn_rows *q, const osdn_rows *k, const float *weight_q,
+                     const float *weight_k, const float *rotary, const int32_t *positions, const osdn_rows *dq_out,
+                     const osdn_rows *dk_out, const osdn_rows *dq, const osdn_rows *dk, float *dweight_q, float *dweight_k,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A paged cache of keys and values: n_pages pages of page_size tokens (a power of two).  The row of page g, slot s, head h of the
+ * keys starts k_page g + k_token s + k_head h elements behind k (likewise the values); rows start on 16 bytes.
+ * Token i of sequence n stands in page table[n][i / page_size], slot i % page_size; table entries
+ * outside [0, n_pages) are pages that are not there.
+ */
+typedef struct {
+    void *k, *v;                                    /* io_dtype */
+    int64_t k_page, k_token, k_head, v_page, v_token, v_head;
+    const int32_t *table;                           /* [n_seqs, max_pages], rows table_stride entries apart */
+    int64_t table_stride;
+    int32_t n_pages, page_size, n_seqs, max_pages;
+} osdn_cache;
+
+/*
+ * Append keys and values to a paged cache, and make the queries of the same tokens ready, in one pass: the row of a key is
+ * treated as by osdn_qk_norm_fwd and written to its place in the cache, the row of a value is copied to its own, the
+ * row of a query is treated as by osdn_qk_norm_fwd.
+ *   q, q_out          [B,T,Hq,K]; both NULL iff Hq == 0; q_out may be q
+ *   k, v              [B,T,Hk,K], Hk >= 1
+ *   positions         [B,T] int32: place of the token in its sequence, also what it is rotated by.  Negative: no token,
+ *                     nothing is appended and its query is zero
+ *   seq               [B,T] int32 or NULL (=> the batch entry): the sequence (row of the table) that the token belongs to
+ * A token whose sequence or page is not there is not appended.  Two tokens of one call with the same place: one of them
+ * is what the place holds.  Nothing else in the cache is touched.
+ */
+int osdn_paged_append(const osdn_norm_params *p, const osdn_cache *cache, const osdn_rows *q, const osdn_rows *k, const osdn_rows *v,
+                      const float *weight_q, const float *weight_k, const float *rotary, const int32_t *positions,
+                      const int32_t *seq, const osdn_rows *q_out, void *stream);
+
+typedef struct {
+    int32_t B, Hq, Hk, K;           /* queries (one token each), their heads, heads of the cache (Hq a multiple of it), width */
+    int32_t io_dtype;               /* osdn_dtype of q, o and the cache */
+    int32_t window;                 /* > 0: only the last so many tokens are seen; 0: all */
+    int32_t max_length;             /* no length is above it (the launch is sized by it) */
+    int32_t piece;                  /* scheduling: tokens of a piece, a multiple of 128; 0: the library decides */
+    float scale;                    /* multiplies the scores (usually K^-1/2) */
+} osdn_decode_params;
+
+/*
+ * Attention of one new token per sequence over a paged cache that holds it already.  Query head h reads head h Hk / Hq of the cache:
+ *     s_j = scale <q, k_j> for max(0, length - window) <= j < length,  m = max_j s_j,
+ *     lse = m + log sum_j e^(s_j - m),  o = sum_j e^(s_j - lse) v_j
+ * in fp32, but that with bf16 I/O the weights e^(s_j - m) are rounded to bf16 for the product with the values.
+ *   q, o              [B,Hq,K] (rows; token is not used); o may be q
+ *   lengths           [B] int32, tokens of the sequence in the cache; 0 (or less): none, o is zero and lse minus infinity
+ *   seq               [B] int32 or NULL (=> b): row of the table.  Several queries may read one sequence, each
+ *                     with its own length: drafted tokens, or a prompt token by token
+ *   lse               [B,Hq] fp32 or NULL
+ *   workspace         osdn_paged_decode_workspace_bytes(p) bytes, 256-byte aligned (may be NULL if that is 0)
+ * What a length hides is not looked at, whatever the cache holds there.  A length above max_length or above what a row of the
+ * table holds, a sequence or a page that is not there: o and lse are NaN, and nothing outside the cache is read.
+ */
+size_t osdn_paged_decode_workspace_bytes(const osdn_decode_params *p);
+int osdn_paged_decode(const osdn_decode_params *p, const osdn_cache *cache, const osdn_rows *q, const int32_t *lengths,
+                      const int32_t *seq, const osdn_rows *o, float *lse, void *workspace, size_t workspace_bytes,
+                      void *stream);
+
+/*
  * Diagnostic query for tests: the decisions of the projection's derivative (Section 4.5,
  * reverse sweep through the projected affine recurrence) that osdn_bwd took, as it left them
  * in the workspace.  Returns the byte offset, inside a workspace of a plain (not packed) batch

@@ -41,6 +41,27 @@ class OsdnParams(ctypes.Structure):
     ]
 
 
+class OsdnRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class OsdnNormParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "Hq", "Hk", "K", "io_dtype", "norm", "rotary_dim", "rotary_rows",
+                                              "interleaved")] + [("eps", ctypes.c_float)]
+
+
+class OsdnCache(ctypes.Structure):
+    _fields_ = ([("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+                + [(n, ctypes.c_int64) for n in ("k_page", "k_token", "k_head", "v_page", "v_token", "v_head")]
+                + [("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64)]
+                + [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "n_seqs", "max_pages")])
+
+
+class OsdnDecodeParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hk", "K", "io_dtype", "window", "max_length", "piece")] + [
+        ("scale", ctypes.c_float)]
+
+
 class OsdnError(RuntimeError):
     def __init__(self, status: int):
         self.status = status
@@ -82,6 +103,20 @@ def lib():
         L.osdn_bwd_packed.argtypes = [pp] + [vp] * 19 + [ip, ctypes.c_int32, vp, ctypes.c_size_t, vp]
         L.osdn_step.restype = ctypes.c_int
         L.osdn_step.argtypes = [pp, vp, vp, vp, fp, fp, fp, fp, fp, vp, fp, fp, vp]
+        np_, dp = ctypes.POINTER(OsdnNormParams), ctypes.POINTER(OsdnDecodeParams)
+        rp, cp = ctypes.POINTER(OsdnRows), ctypes.POINTER(OsdnCache)
+        L.osdn_qk_norm_fwd.restype = ctypes.c_int
+        L.osdn_qk_norm_fwd.argtypes = [np_, rp, rp, fp, fp, fp, vp, rp, rp, vp]
+        L.osdn_qk_norm_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.osdn_qk_norm_bwd_workspace_bytes.argtypes = [np_]
+        L.osdn_qk_norm_bwd.restype = ctypes.c_int
+        L.osdn_qk_norm_bwd.argtypes = [np_, rp, rp, fp, fp, fp, vp, rp, rp, rp, rp, fp, fp, vp, ctypes.c_size_t, vp]
+        L.osdn_paged_append.restype = ctypes.c_int
+        L.osdn_paged_append.argtypes = [np_, cp, rp, rp, rp, fp, fp, fp, vp, vp, rp, vp]
+        L.osdn_paged_decode_workspace_bytes.restype = ctypes.c_size_t
+        L.osdn_paged_decode_workspace_bytes.argtypes = [dp]
+        L.osdn_paged_decode.restype = ctypes.c_int
+        L.osdn_paged_decode.argtypes = [dp, cp, rp, vp, vp, rp, fp, vp, ctypes.c_size_t, vp]
         L.osdn_profile_enable.restype = None
         L.osdn_profile_enable.argtypes = [ctypes.c_int]
         L.osdn_profile_kernel_count.restype = ctypes.c_int
@@ -428,3 +463,194 @@ def precond_update(k, beta, retention=None, d_in=None, hp: Hyper = Hyper(), want
     ck = torch.empty(B, H, T // 64, K, dtype=torch.float32, device=k.device) if want_ckpt else None
     osdn_precond_update(p, k, beta, retention, d_in, kt, d_out, ck)
     return (kt, d_out, ck) if want_ckpt else (kt, d_out)
+
+
+# ------------------------------------------- queries, keys and values around the recurrence ----
+NORMS = {"none": 0, "rms": 1, "l2": 2}
+
+
+@dataclass
+class NormHyper:
+    norm: str = "l2"             # "l2": unit length (what the recurrence expects), "rms": unit mean square, "none"
+    eps: float = 1e-6            # added to the sum (mean) of squares
+    interleaved: bool = False    # rotation of the pairs (2i, 2i + 1); else (i, i + rotary_dim / 2)
+
+
+def make_norm_params(B, T, Hq, Hk, K, bf16: bool, hp: NormHyper = NormHyper(), rotary=None) -> OsdnNormParams:
+    if hp.norm not in NORMS:
+        raise ValueError(f"norm: expected one of {sorted(NORMS)}, got {hp.norm!r}")
+    rows, dim = (0, 0) if rotary is None else rotary.shape
+    return OsdnNormParams(B, T, Hq, Hk, K, OSDN_BF16 if bf16 else OSDN_F32, NORMS[hp.norm], dim, rows, int(bool(hp.interleaved)),
+                          hp.eps)
+
+
+def make_decode_params(B, Hq, Hk, K, bf16: bool, max_length: int, scale: float | None = None, window: int = 0,
+                       piece: int = 0) -> OsdnDecodeParams:
+    return OsdnDecodeParams(B, Hq, Hk, K, OSDN_BF16 if bf16 else OSDN_F32, int(window or 0), int(max_length), int(piece),
+                            float(K) ** -0.5 if scale is None else float(scale))
+
+
+def rotary_table(rows: int, dim: int, theta: float = 10000.0, device="cuda") -> torch.Tensor:
+    """The table of the rotation, [rows, dim] fp32: a position's cosines, then its sines (angle i: position theta^(-2 i / dim),
+    formed in 64 bits)."""
+    angle = torch.arange(rows, dtype=torch.float64)[:, None] * theta ** (-2.0 * torch.arange(dim // 2, dtype=torch.float64) / dim)
+    return torch.cat([angle.cos(), angle.sin()], dim=1).float().to(device)
+
+
+def alloc_paged_cache(n_pages: int, page_size: int, H: int, K: int, dtype=torch.bfloat16, device="cuda"):
+    """(k_cache, v_cache), [n_pages, page_size, H, K]: a page holds its tokens head after head, which is the order that
+    paged_decode reads (any order of pages, tokens and heads is taken)."""
+    return tuple(torch.empty(n_pages, H, page_size, K, dtype=dtype, device=device).transpose(1, 2) for _ in range(2))
+
+
+def _rows(t, dtype, shape, name):
+    """Rows of the last axis, wherever they stand: [B,T,H,K], or [B,H,K]."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name}: expected a CUDA/HIP torch tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected dtype {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"{name}: is on {t.device}, the current device is {torch._C._cuda_getDevice()}")
+    st = t.stride()
+    if st[-1] != 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    return OsdnRows(t.data_ptr(), st[0], st[1] if len(st) == 4 else 0, st[-2])
+
+
+def _cache(k_cache, v_cache, page_table, dtype, H, K):
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise TypeError("k_cache: expected a CUDA/HIP torch tensor [n_pages, page_size, H, K]")
+    n_pages, page_size = k_cache.shape[:2]
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        _rows(t, dtype, (n_pages, page_size, H, K), name)
+    if not isinstance(page_table, torch.Tensor) or not page_table.is_cuda or page_table.dtype != torch.int32:
+        raise TypeError("page_table: expected an int32 CUDA/HIP torch tensor")
+    if page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table: expected [n_seqs, max_pages] with adjacent entries of a row")
+    n_seqs, max_pages = page_table.shape
+    k, v = k_cache.stride(), v_cache.stride()
+    stride = page_table.stride(0) if n_seqs > 1 else max_pages
+    return OsdnCache(k_cache.data_ptr(), v_cache.data_ptr(), k[0], k[1], k[2], v[0], v[1], v[2], page_table.data_ptr(), stride,
+                     n_pages, page_size, n_seqs, max_pages)
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def _norm_rows(p, q, k, *more):
+    io = _io_torch_dtype(p)
+    sq, sk = (p.B, p.T, p.Hq, p.K), (p.B, p.T, p.Hk, p.K)
+    return [_rows(t, io, sk if name.startswith(("k", "v", "dk")) else sq, name) for t, name in ((q, "q"), (k, "k"), *more)]
+
+
+def _norm_shared(p, weight_q, weight_k, rotary, positions):
+    f32 = torch.float32
+    return (_ptr(weight_q, f32, (p.K,), "weight_q"), _ptr(weight_k, f32, (p.K,), "weight_k"),
+            _ptr(rotary, f32, (p.rotary_rows, p.rotary_dim), "rotary"), _ptr(positions, torch.int32, (p.B, p.T), "positions"))
+
+
+def osdn_qk_norm_fwd(params, q, k, weight_q, weight_k, rotary, positions, q_out, k_out, stream=None):
+    r = _norm_rows(params, q, k, (q_out, "q_out"), (k_out, "k_out"))
+    _check(lib().osdn_qk_norm_fwd(ctypes.byref(params), _ref(r[0]), _ref(r[1]), *_norm_shared(params, weight_q, weight_k, rotary, positions),
+                                  _ref(r[2]), _ref(r[3]), _stream_ptr(stream)))
+
+
+def osdn_qk_norm_bwd_workspace_bytes(params) -> int:
+    return int(lib().osdn_qk_norm_bwd_workspace_bytes(ctypes.byref(params)))
+
+
+def osdn_qk_norm_bwd(params, q, k, weight_q, weight_k, rotary, positions, dq_out, dk_out, dq, dk, dweight_q, dweight_k, workspace=None,
+                     stream=None):
+    p, f32 = params, torch.float32
+    r = _norm_rows(p, q, k, (dq_out, "dq_out"), (dk_out, "dk_out"), (dq, "dq"), (dk, "dk"))
+    _check(lib().osdn_qk_norm_bwd(
+        ctypes.byref(p), _ref(r[0]), _ref(r[1]), *_norm_shared(p, weight_q, weight_k, rotary, positions), *(_ref(x) for x in r[2:]),
+        _ptr(dweight_q, f32, (p.K,), "dweight_q"), _ptr(dweight_k, f32, (p.K,), "dweight_k"), _ptr(workspace, torch.uint8, None, "workspace"),
+        ctypes.c_size_t(0 if workspace is None else workspace.numel()), _stream_ptr(stream)))
+
+
+def osdn_paged_append(params, q, k, v, k_cache, v_cache, page_table, weight_q, weight_k, rotary, positions, seq, q_out, stream=None):
+    p = params
+    r = _norm_rows(p, q, k, (v, "v"), (q_out, "q_out"))
+    cache = _cache(k_cache, v_cache, page_table, _io_torch_dtype(p), p.Hk, p.K)
+    _check(lib().osdn_paged_append(
+        ctypes.byref(p), ctypes.byref(cache), *(_ref(x) for x in r[:3]), *_norm_shared(p, weight_q, weight_k, rotary, positions),
+        _ptr(seq, torch.int32, (p.B, p.T), "seq"), _ref(r[3]), _stream_ptr(stream)))
+
+
+def osdn_paged_decode_workspace_bytes(params) -> int:
+    return int(lib().osdn_paged_decode_workspace_bytes(ctypes.byref(params)))
+
+
+def osdn_paged_decode(params, q, k_cache, v_cache, page_table, lengths, seq, o, lse, workspace=None, stream=None):
+    p, i32 = params, torch.int32
+    io, rows = _io_torch_dtype(p), (p.B, p.Hq, p.K)
+    qr, orows = _rows(q, io, rows, "q"), _rows(o, io, rows, "o")
+    cache = _cache(k_cache, v_cache, page_table, io, p.Hk, p.K)
+    _check(lib().osdn_paged_decode(
+        ctypes.byref(p), ctypes.byref(cache), _ref(qr), _ptr(lengths, i32, (p.B,), "lengths"), _ptr(seq, i32, (p.B,), "seq"), _ref(orows),
+        _ptr(lse, torch.float32, (p.B, p.Hq), "lse"), _ptr(workspace, torch.uint8, None, "workspace"),
+        ctypes.c_size_t(0 if workspace is None else workspace.numel()), _stream_ptr(stream)))
+
+
+def _params_of(q, k, hp, rotary):
+    x = k if q is None else q
+    if not isinstance(x, torch.Tensor) or x.dim() != 4 or (q is not None and k is not None and (not isinstance(k, torch.Tensor) or k.dim() != 4)):
+        raise TypeError("expected rows [B,T,H,K] as CUDA/HIP torch tensors")
+    B, T, _, K = x.shape
+    return make_norm_params(B, T, 0 if q is None else q.shape[2], 0 if k is None else k.shape[2], K, x.dtype == torch.bfloat16, hp, rotary)
+
+
+def qk_norm(q, k, weight_q=None, weight_k=None, rotary=None, positions=None, hp: NormHyper = NormHyper()):
+    """Allocate outputs and call osdn_qk_norm_fwd (either of q and k may be None).  Returns (q_out, k_out)."""
+    p = _params_of(q, k, hp, rotary)
+    out = [None if x is None else x.new_empty(x.shape) for x in (q, k)]
+    osdn_qk_norm_fwd(p, q, k, weight_q, weight_k, rotary, positions, *out)
+    return tuple(out)
+
+
+def qk_norm_backward(q, k, dq_out, dk_out, weight_q=None, weight_k=None, rotary=None, positions=None, hp: NormHyper = NormHyper()):
+    """Allocate gradients and call osdn_qk_norm_bwd on the inputs of ``qk_norm``.  Returns a dict of dq, dk and, where there are
+    weights, dweight_q, dweight_k."""
+    p = _params_of(q, k, hp, rotary)
+    g = {"dq": None if q is None else q.new_empty(q.shape), "dk": None if k is None else k.new_empty(k.shape),
+         "dweight_q": None if weight_q is None else torch.empty_like(weight_q), "dweight_k": None if weight_k is None else torch.empty_like(weight_k)}
+    ws = None
+    if weight_q is not None or weight_k is not None:
+        ws = torch.empty(osdn_qk_norm_bwd_workspace_bytes(p), dtype=torch.uint8, device=(k if q is None else q).device)
+    osdn_qk_norm_bwd(p, q, k, weight_q, weight_k, rotary, positions, dq_out, dk_out, g["dq"], g["dk"], g["dweight_q"], g["dweight_k"], ws)
+    return g
+
+
+def paged_append(k, v, k_cache, v_cache, page_table, positions, seq=None, q=None, weight_q=None, weight_k=None, rotary=None,
+                 hp: NormHyper = NormHyper()):
+    """Append keys (normed and rotated) and values [B,T,Hk,K] to a paged cache [n_pages, page_size, Hk, K]; with q [B,T,Hq,K],
+    returns the queries normed and rotated alike, from the same launch."""
+    p = _params_of(q, k, hp, rotary)
+    q_out = None if q is None else q.new_empty(q.shape)
+    osdn_paged_append(p, q, k, v, k_cache, v_cache, page_table, weight_q, weight_k, rotary, positions, seq, q_out)
+    return q_out
+
+
+def paged_decode(q, k_cache, v_cache, page_table, lengths, seq=None, scale=None, window: int = 0, max_length=None, want_lse: bool = False,
+                 workspace=None):
+    """Attention of one new token per sequence, q [B,Hq,K], over a paged cache.  max_length: no length is above it (None: what a
+    row of the table can hold).  Returns o, or (o, lse)."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise TypeError("expected q [B,Hq,K] and a cache [n_pages, page_size, Hk, K] as CUDA/HIP torch tensors")
+    B, Hq, K = q.shape
+    if max_length is None:
+        max_length = min(page_table.shape[1] * k_cache.shape[1], 0x7fffff00)
+    p = make_decode_params(B, Hq, k_cache.shape[2], K, q.dtype == torch.bfloat16, max_length, scale, window)
+    o = q.new_empty(q.shape)
+    lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is None:
+        n = osdn_paged_decode_workspace_bytes(p)
+        workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    osdn_paged_decode(p, q, k_cache, v_cache, page_table, lengths, seq, o, lse, workspace)
+    return (o, lse) if want_lse else o

@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "libosdn.so")
 NATIVE = os.path.join(HERE, "_native" + sysconfig.get_config_var("EXT_SUFFIX"))     # (the name says for which Python)
 NATIVE_SOURCE = os.path.join(CSRC, "osdn_native.cpp")
 SOURCES = ["osdn_api.hip", "osdn_precond.hip", "osdn_precond_bwd.hip", "osdn_precond_gen.hip", "osdn_step.hip", "osdn_tables.hip",
-           "osdn_chunk_fwd.hip", "osdn_chunk_bwd.hip"]
+           "osdn_chunk_fwd.hip", "osdn_chunk_bwd.hip", "osdn_heads.hip", "osdn_paged.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -18,10 +18,11 @@ using namespace osdn;
 // only process-wide state the library has).  Not thread-safe; meant for benchmarks.
 enum { KID_PRECOND_FWD, KID_CHUNK_PREP, KID_STATE_FWD, KID_OUTPUT_FWD, KID_BWD_CHAIN,
        KID_BWD_POST, KID_PRECOND_MASK, KID_PRECOND_CHAIN, KID_PRECOND_POST, KID_STEP, KID_TABLES, KID_UNFOLD, KID_PRECOND_LIN,
-       KID_COUNT };
+       KID_QK_NORM, KID_QK_NORM_BWD, KID_PAGED_APPEND, KID_PAGED_DECODE, KID_COUNT };
 const char *const kKernelNames[KID_COUNT] = {"precond_fwd", "chunk_prep", "state_fwd", "output_fwd",
                                              "bwd_chain", "bwd_post", "precond_mask",
-                                             "precond_chain", "precond_post", "step", "tables", "unfold", "precond_lin"};
+                                             "precond_chain", "precond_post", "step", "tables", "unfold", "precond_lin",
+                                             "qk_norm", "qk_norm_bwd", "paged_append", "paged_decode"};
 struct Timed { int id; hipEvent_t e0, e1; };
 bool g_prof_on = false;
 std::vector<Timed> g_prof;
@@ -317,7 +318,8 @@ const char *osdn_strerror(int status) {
     switch (status) {
         case OSDN_OK: return "ok";
         case OSDN_ERR_NULL: return "a required pointer is NULL";
-        case OSDN_ERR_SHAPE: return "unsupported shape (chunk must be 64, K in {64,128}, V % 64 == 0, V <= 512, at most 64 tokens per osdn_step)";
+        case OSDN_ERR_SHAPE: return "unsupported shape (chunk must be 64, K in {64,128}, V % 64 == 0, V <= 512, at most 64 tokens per osdn_step; rows of an "
+                                     "attention layer: K in {64,128,256}, rotary_dim a multiple of 16, page_size a power of two, rows of a cache on 16 bytes)";
         case OSDN_ERR_DTYPE: return "io_dtype must be OSDN_F32 or OSDN_BF16";
         case OSDN_ERR_WORKSPACE: return "workspace too small or not 256-byte aligned";
         case OSDN_ERR_PARAM: return "invalid scalar parameter (eta < 0, eps <= 0 or non-finite)";
@@ -363,6 +365,178 @@ int osdn_step(const osdn_params *p, const void *q, const void *k, const void *v,
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool bf = p->io_dtype == OSDN_BF16;
     if (timed(KID_STEP, st, [&] { return launch_step(a, bf, st); }) != 0) return OSDN_ERR_SHAPE;
+    return launch_status();
+}
+
+// ---- queries, keys and values around the recurrence ----------------------------------------
+static int check_norm(const osdn_norm_params *p) {
+    if (!p) return OSDN_ERR_NULL;
+    if (p->io_dtype != OSDN_F32 && p->io_dtype != OSDN_BF16) return OSDN_ERR_DTYPE;
+    if (p->B < 1 || p->T < 1 || p->Hq < 0 || p->Hk < 0 || p->Hq > 65535 || p->Hk > 65535 || (p->Hq == 0 && p->Hk == 0)) return OSDN_ERR_SHAPE;
+    if (p->K != 64 && p->K != 128 && p->K != 256) return OSDN_ERR_SHAPE;
+    if (p->rotary_dim < 0 || p->rotary_dim > p->K || p->rotary_dim % 16 != 0 || (p->rotary_dim > 0 && p->rotary_rows < 1)) return OSDN_ERR_SHAPE;
+    const long long tokens = (long long)p->B * p->T;
+    if (tokens > 0x7fffffffLL || tokens * ((long long)p->Hq + 2 * p->Hk) > 0x7fffffffLL) return OSDN_ERR_SHAPE;
+    if (p->norm != OSDN_NORM_NONE && p->norm != OSDN_NORM_RMS && p->norm != OSDN_NORM_L2) return OSDN_ERR_PARAM;
+    if (p->norm != OSDN_NORM_NONE && (!(p->eps > 0.f) || !std::isfinite(p->eps))) return OSDN_ERR_PARAM;
+    if (p->interleaved != 0 && p->interleaved != 1) return OSDN_ERR_PARAM;
+    return OSDN_OK;
+}
+
+// A batch of rows of H heads: `on` tells whether it is there, `out` that it is written (no two rows at one place).  The rows' addresses
+// are those of their elements; clears `aligned` unless every row starts on 16 bytes.
+static int take_rows(const osdn_rows *r, long long B, long long T, long long H, size_t es, bool out, HeadRows &to, bool &aligned) {
+    if (H == 0) return OSDN_OK;
+    if (!r || !r->data) return OSDN_ERR_NULL;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(r->data);
+    if (at % es != 0) return OSDN_ERR_SHAPE;
+    if (out && ((B > 1 && r->batch == 0) || (T > 1 && r->token == 0) || (H > 1 && r->head == 0))) return OSDN_ERR_SHAPE;
+    const long long ve = 16 / (long long)es;
+    if (at % 16 != 0 || (B > 1 && r->batch % ve != 0) || (T > 1 && r->token % ve != 0) || (H > 1 && r->head % ve != 0)) aligned = false;
+    to = HeadRows{r->data, r->batch, r->token, r->head};
+    return OSDN_OK;
+}
+
+static int check_cache(const osdn_cache *c, int H, size_t es, int &shift) {
+    if (!c || !c->k || !c->v || !c->table) return OSDN_ERR_NULL;
+    if (c->n_pages < 1 || c->n_seqs < 1 || c->max_pages < 1 || c->page_size < 1 || (c->page_size & (c->page_size - 1)) != 0) return OSDN_ERR_SHAPE;
+    if (c->table_stride < 0 || (c->table_stride < c->max_pages && c->table_stride != 0)) return OSDN_ERR_SHAPE;
+    if ((c->n_pages > 1 && (c->k_page == 0 || c->v_page == 0)) || (c->page_size > 1 && (c->k_token == 0 || c->v_token == 0)) ||
+        (H > 1 && (c->k_head == 0 || c->v_head == 0)))
+        return OSDN_ERR_SHAPE;
+    const long long ve = 16 / (long long)es;
+    for (long long s : {c->k_page, c->k_token, c->k_head, c->v_page, c->v_token, c->v_head})
+        if (s < 0 || s % ve != 0) return OSDN_ERR_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) % 16 != 0 || reinterpret_cast<uintptr_t>(c->table) % 4 != 0) return OSDN_ERR_SHAPE;
+    shift = 0;
+    while ((1 << shift) < c->page_size) ++shift;
+    return OSDN_OK;
+}
+
+static HeadsArgs heads_args(const osdn_norm_params *p, const float *weight_q, const float *weight_k, const float *rotary, const int32_t *positions) {
+    HeadsArgs a{};
+    a.T = p->T; a.tokens = p->B * p->T; a.Hq = p->Hq; a.Hk = p->Hk; a.K = p->K;
+    a.norm = p->norm; a.mean = p->norm == OSDN_NORM_RMS ? 1.f / (float)p->K : 1.f; a.eps = p->eps;
+    a.rotary_dim = p->rotary_dim; a.rotary_rows = p->rotary_rows; a.interleaved = p->interleaved;
+    a.weight_q = weight_q; a.weight_k = weight_k; a.rotary = p->rotary_dim ? rotary : nullptr; a.positions = positions;
+    a.aligned = true;
+    return a;
+}
+
+int osdn_qk_norm_fwd(const osdn_norm_params *p, const osdn_rows *q, const osdn_rows *k, const float *weight_q, const float *weight_k,
+                     const float *rotary, const int32_t *positions, const osdn_rows *q_out, const osdn_rows *k_out, void *stream) {
+    int rc = check_norm(p);
+    if (rc != OSDN_OK) return rc;
+    if (p->rotary_dim && !rotary) return OSDN_ERR_NULL;
+    HeadsArgs a = heads_args(p, weight_q, weight_k, rotary, positions);
+    const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
+    if ((rc = take_rows(q, p->B, p->T, p->Hq, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(k, p->B, p->T, p->Hk, es, false, a.k, a.aligned)) != OSDN_OK ||
+        (rc = take_rows(q_out, p->B, p->T, p->Hq, es, true, a.q_out, a.aligned)) != OSDN_OK || (rc = take_rows(k_out, p->B, p->T, p->Hk, es, true, a.k_out, a.aligned)) != OSDN_OK)
+        return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (timed(KID_QK_NORM, st, [&] { return launch_heads_fwd(a, p->io_dtype == OSDN_BF16, st); }) != 0) return OSDN_ERR_SHAPE;
+    return launch_status();
+}
+
+size_t osdn_qk_norm_bwd_workspace_bytes(const osdn_norm_params *p) {
+    if (check_norm(p) != OSDN_OK) return 0;
+    return (size_t)heads_bwd_workgroups((long long)p->B * p->T) * 2 * p->K * sizeof(float);
+}
+
+int osdn_qk_norm_bwd(const osdn_norm_params *p, const osdn_rows *q, const osdn_rows *k, const float *weight_q, const float *weight_k,
+                     const float *rotary, const int32_t *positions, const osdn_rows *dq_out, const osdn_rows *dk_out, const osdn_rows *dq,
+                     const osdn_rows *dk, float *dweight_q, float *dweight_k, void *workspace, size_t workspace_bytes, void *stream) {
+    int rc = check_norm(p);
+    if (rc != OSDN_OK) return rc;
+    if (p->rotary_dim && !rotary) return OSDN_ERR_NULL;
+    HeadsArgs a = heads_args(p, weight_q, weight_k, rotary, positions);
+    const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
+    if ((rc = take_rows(q, p->B, p->T, p->Hq, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(k, p->B, p->T, p->Hk, es, false, a.k, a.aligned)) != OSDN_OK ||
+        (rc = take_rows(dq_out, p->B, p->T, p->Hq, es, false, a.dq_out, a.aligned)) != OSDN_OK ||
+        (rc = take_rows(dk_out, p->B, p->T, p->Hk, es, false, a.dk_out, a.aligned)) != OSDN_OK ||
+        (rc = take_rows(dq, p->B, p->T, p->Hq, es, true, a.dq, a.aligned)) != OSDN_OK || (rc = take_rows(dk, p->B, p->T, p->Hk, es, true, a.dk, a.aligned)) != OSDN_OK)
+        return rc;
+    if (dweight_q || dweight_k) {
+        rc = check_ws(workspace, workspace_bytes, osdn_qk_norm_bwd_workspace_bytes(p));
+        if (rc != OSDN_OK) return rc;
+        a.partial = static_cast<float *>(workspace);
+        a.dweight_q = dweight_q; a.dweight_k = dweight_k;
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (timed(KID_QK_NORM_BWD, st, [&] { return launch_heads_bwd(a, p->io_dtype == OSDN_BF16, st); }) != 0) return OSDN_ERR_SHAPE;
+    return launch_status();
+}
+
+int osdn_paged_append(const osdn_norm_params *p, const osdn_cache *cache, const osdn_rows *q, const osdn_rows *k, const osdn_rows *v,
+                      const float *weight_q, const float *weight_k, const float *rotary, const int32_t *positions, const int32_t *seq,
+                      const osdn_rows *q_out, void *stream) {
+    int rc = check_norm(p), shift = 0;
+    if (rc != OSDN_OK) return rc;
+    if (p->Hk < 1) return OSDN_ERR_SHAPE;
+    if ((p->rotary_dim && !rotary) || !positions) return OSDN_ERR_NULL;
+    const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
+    if ((rc = check_cache(cache, p->Hk, es, shift)) != OSDN_OK) return rc;
+    HeadsArgs a = heads_args(p, weight_q, weight_k, rotary, positions);
+    if ((rc = take_rows(q, p->B, p->T, p->Hq, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(k, p->B, p->T, p->Hk, es, false, a.k, a.aligned)) != OSDN_OK ||
+        (rc = take_rows(v, p->B, p->T, p->Hk, es, false, a.v, a.aligned)) != OSDN_OK || (rc = take_rows(q_out, p->B, p->T, p->Hq, es, true, a.q_out, a.aligned)) != OSDN_OK)
+        return rc;
+    a.append = true;
+    a.cache_k = HeadRows{cache->k, cache->k_page, cache->k_token, cache->k_head};
+    a.cache_v = HeadRows{cache->v, cache->v_page, cache->v_token, cache->v_head};
+    a.table = cache->table; a.table_stride = cache->table_stride; a.seq = seq;
+    a.n_pages = cache->n_pages; a.page_shift = shift; a.n_seqs = cache->n_seqs; a.max_pages = cache->max_pages;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (timed(KID_PAGED_APPEND, st, [&] { return launch_heads_fwd(a, p->io_dtype == OSDN_BF16, st); }) != 0) return OSDN_ERR_SHAPE;
+    return launch_status();
+}
+
+static int check_decode(const osdn_decode_params *p, int &head_tiles, int &piece, int &pieces) {
+    if (!p) return OSDN_ERR_NULL;
+    if (p->io_dtype != OSDN_F32 && p->io_dtype != OSDN_BF16) return OSDN_ERR_DTYPE;
+    if (p->B < 1 || p->B > 65535 || p->Hk < 1 || p->Hq < p->Hk || p->Hq % p->Hk != 0 || p->Hq > 65535) return OSDN_ERR_SHAPE;
+    if (p->K != 64 && p->K != 128 && p->K != 256) return OSDN_ERR_SHAPE;
+    if (p->max_length < 0 || p->max_length > 0x7fffff00) return OSDN_ERR_SHAPE;
+    if (!std::isfinite(p->scale) || p->window < 0 || p->piece < 0 || p->piece % DECODE_PIECE != 0) return OSDN_ERR_PARAM;
+    head_tiles = (p->Hq / p->Hk + 15) / 16;
+    const long long span = decode_span(p->max_length, p->window);
+    piece = p->piece ? p->piece : decode_piece((long long)p->B * p->Hk * head_tiles, span);
+    const long long n = (span + piece - 1) / piece;
+    if (n * DEC_THREADS >= (1ll << 32)) return OSDN_ERR_SHAPE;
+    pieces = n < 1 ? 1 : (int)n;
+    return OSDN_OK;
+}
+
+size_t osdn_paged_decode_workspace_bytes(const osdn_decode_params *p) {
+    int tiles, piece, pieces;
+    if (check_decode(p, tiles, piece, pieces) != OSDN_OK || pieces == 1) return 0;
+    return (size_t)p->B * p->Hq * pieces * (p->K + 2) * sizeof(float);
+}
+
+int osdn_paged_decode(const osdn_decode_params *p, const osdn_cache *cache, const osdn_rows *q, const int32_t *lengths, const int32_t *seq,
+                      const osdn_rows *o, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    DecodeArgs a{};
+    int rc = check_decode(p, a.head_tiles, a.piece, a.pieces);
+    if (rc != OSDN_OK) return rc;
+    if (!lengths) return OSDN_ERR_NULL;
+    const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
+    if ((rc = check_cache(cache, p->Hk, es, a.page_shift)) != OSDN_OK) return rc;
+    a.aligned = true;
+    if ((rc = take_rows(q, p->B, 1, p->Hq, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(o, p->B, 1, p->Hq, es, true, a.o, a.aligned)) != OSDN_OK) return rc;
+    const size_t rows = (size_t)p->B * p->Hq * a.pieces;
+    if (a.pieces > 1) {
+        rc = check_ws(workspace, workspace_bytes, rows * (p->K + 2) * sizeof(float));
+        if (rc != OSDN_OK) return rc;
+        a.part_o = static_cast<float *>(workspace);
+        a.part_ml = a.part_o + rows * p->K;
+    }
+    a.B = p->B; a.Hq = p->Hq; a.Hk = p->Hk; a.K = p->K; a.group = p->Hq / p->Hk;
+    a.scale = p->scale; a.window = p->window; a.max_length = p->max_length;
+    a.cache_k = HeadRows{cache->k, cache->k_page, cache->k_token, cache->k_head};
+    a.cache_v = HeadRows{cache->v, cache->v_page, cache->v_token, cache->v_head};
+    a.table = cache->table; a.table_stride = cache->table_stride; a.lengths = lengths; a.seq = seq; a.lse = lse;
+    a.n_pages = cache->n_pages; a.n_seqs = cache->n_seqs; a.max_pages = cache->max_pages;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (timed(KID_PAGED_DECODE, st, [&] { return launch_paged_decode(a, p->io_dtype == OSDN_BF16, st); }) != 0) return OSDN_ERR_SHAPE;
     return launch_status();
 }
 

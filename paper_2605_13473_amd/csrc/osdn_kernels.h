@@ -238,4 +238,49 @@ struct UnfoldArgs {
 };
 int launch_unfold(const UnfoldArgs &a, bool bf16_io, hipStream_t st);
 
+// Rows of the queries, keys and values of an attention layer, or of their gradients: element (b, t, h, i) stands batch b + token t + head h + i
+// elements behind data.  Of a cache: batch is the step from page to page and token that from slot to slot.
+struct HeadRows { void *data; long long batch, token, head; };
+
+// Norm and rotation of the rows of queries and keys (osdn_heads.hip)
+struct HeadsArgs {
+    int T, tokens, Hq, Hk, K;             // tokens: of all batch entries
+    int norm; float mean, eps;            // 1 / r^2 = mean sum x^2 + eps; norm == 0: r = 1
+    int rotary_dim, rotary_rows, interleaved;
+    bool aligned;                         // every row that is not a cache's starts on 16 bytes
+    HeadRows q, k, v, q_out, k_out;       // v: append alone
+    const float *weight_q, *weight_k;     // [K] or null
+    const float *rotary;                  // [rotary_rows, rotary_dim] or null
+    const int *positions;                 // [tokens] or null (a token's place in its batch entry)
+    // append
+    bool append;
+    HeadRows cache_k, cache_v;
+    const int *table, *seq;               // [n_seqs, max_pages], [tokens] or null (the batch entry)
+    long long table_stride;
+    int n_pages, page_shift, n_seqs, max_pages;
+    // backward
+    HeadRows dq_out, dk_out, dq, dk;
+    float *dweight_q, *dweight_k;         // [K] or null
+    float *partial;                       // [workgroups][2][K], null without weights
+    // set by the launcher: blocks of rows of a token, and how many wavefronts share them; tokens per step of the grid along y
+    int q_blocks, k_blocks, blocks, parts, tokens_y;
+};
+int launch_heads_fwd(HeadsArgs a, bool bf16_io, hipStream_t st);
+int launch_heads_bwd(HeadsArgs a, bool bf16_io, hipStream_t st);
+
+// Attention of one token per sequence over a paged cache (osdn_paged.hip)
+struct DecodeArgs {
+    int B, Hq, Hk, K, group, head_tiles;  // group: query heads of a key head; head_tiles: workgroups (of 16 query heads) that they take
+    float scale;
+    int window, max_length, piece, pieces;    // tokens of a piece; pieces of a sequence of max_length
+    HeadRows q, o, cache_k, cache_v;      // q, o: token unused
+    bool aligned;                         // every row of q and o starts on 16 bytes
+    const int *table, *seq, *lengths;     // [n_seqs, max_pages], [B] or null (the batch entry), [B]
+    long long table_stride;
+    int n_pages, page_shift, n_seqs, max_pages;
+    float *lse;                           // [B, Hq] or null
+    float *part_o, *part_ml;              // pieces > 1: [B, Hq, pieces, K] and [B, Hq, pieces, 2]
+};
+int launch_paged_decode(const DecodeArgs &a, bool bf16_io, hipStream_t st);
+
 }  // namespace osdn

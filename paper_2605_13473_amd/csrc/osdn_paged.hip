@@ -1,0 +1,304 @@
+// Attention of one new token for each of B sequences over a paged cache of keys and values.
+//
+// For a query q of one head, the cached rows j of its key head that it sees (max(0, length - window) <= j < length):
+//   s_j = scale <q, k_j>,  m = max_j s_j,  l = sum_j e^(s_j - m),  o = sum_j e^(s_j - m) v_j / l,  lse = m + log l
+//
+// Bound by memory: every visible key and value is read once, for all query heads that share it (up to 16 side by side: the columns
+// of a 16 x 16 matrix product, so that one query head costs what 16 do, 3 % of the matrix cores' time).  The visible tokens are cut into pieces;
+// a workgroup takes one piece of one key head, its four wavefronts take the piece's tiles in turn, each with a running
+// maximum and sum of its own, and join at the end; a second kernel joins the pieces, in their order.
+//
+// A wavefront's tile is TT tokens.  Keys go from memory to registers as the matrix product wants them (lane l: token l % 16, 16 bytes);
+// scores come out transposed, lane l with four tokens of head l % 16, which is how the second product (values transposed,
+// times the weights) takes its weights: its order of tokens is the same on both sides, so no lane has to pass any on.  Values are
+// transposed on their way through LDS.
+#include "osdn_kernels.h"
+
+#include <cfloat>
+
+namespace osdn {
+
+constexpr int DEC_T = DEC_THREADS, DEC_W = DEC_T / 64;
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ float max_xor16(float x) {
+    float y = x;
+    asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+    return fmaxf(x, y);
+}
+__device__ __forceinline__ float max_xor32(float x) {
+    float y = x;
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+    return fmaxf(x, y);
+}
+
+template <typename T, int K> struct DecodeTile {
+    static constexpr bool BF = sizeof(T) == 2;
+    static constexpr int TT = BF ? 32 : 16;             // tokens: the depth of the second product's matrix instruction, or four of them
+    static constexpr int SETS = TT / 16;                // 16-token products that make the scores
+    static constexpr int VE = 16 / sizeof(T);           // elements of a 16-byte vector
+    static constexpr int STEPS = K / (4 * VE);          // vectors of a row, per lane (four lanes share a row)
+    static constexpr int LDV = K + VE;                  // row of the values in LDS: 16 rows of one column start on 16 different quads of banks
+    static constexpr int OUT = K / 16;                  // 16-row tiles of the transposed result
+};
+
+// The rows of a tile that a lane loads: token 16 i + l % 16 of the tile, i < SETS
+template <typename T, int K> struct TileRows {
+    using D = DecodeTile<T, K>;
+    int page[D::SETS];
+    // tok: first token of the tile; rows outside [lo, hi) repeat a row inside
+    __device__ __forceinline__ void ask(const DecodeArgs &a, const int *row, int tok, int lo, int hi, int lane) {
+#pragma unroll
+        for (int i = 0; i < D::SETS; ++i) page[i] = row[max(lo, min(hi - 1, tok + 16 * i + (lane & 15))) >> a.page_shift];
+    }
+};
+
+template <typename T, int K>
+__global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
+    using D = DecodeTile<T, K>;
+    constexpr int TT = D::TT, VE = D::VE, STEPS = D::STEPS, LDV = D::LDV, OUT = D::OUT, LDO = K + 4;
+    __shared__ __align__(16) char lds[DEC_W * (TT * LDV * sizeof(T) > 16 * LDO * 4 ? TT * LDV * sizeof(T) : 16 * LDO * 4)];
+    __shared__ float ml[DEC_W][2][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
+    const int piece = blockIdx.x, kv = blockIdx.y / a.head_tiles, h0 = kv * a.group + 16 * (blockIdx.y % a.head_tiles), b = blockIdx.z;
+    const int heads = min(16, (kv + 1) * a.group - h0);
+    const int seq = a.seq ? a.seq[b] : b;
+    const int length = a.lengths[b];
+    // what the caller promised and did not keep makes the result NaN: nothing outside the cache is read
+    const bool bad_call = (unsigned)seq >= (unsigned)a.n_seqs || length > a.max_length || (length > 0 && (length - 1) >> a.page_shift >= a.max_pages);
+    const int lo = a.window > 0 && length > a.window ? length - a.window : 0;
+    const int first = lo & ~(TT - 1);                                   // pieces are cut from a multiple of the tile
+    const int begin = first + piece * a.piece;
+    if (!bad_call && begin >= length && piece > 0) return;              // (an empty sequence has one empty piece)
+    if (bad_call && piece > 0) return;
+    const int end = bad_call ? 0 : min(length, begin + a.piece);
+
+    // queries: lane l holds head l % 16
+    u32x4 q[STEPS];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        q[s] = u32x4{0u, 0u, 0u, 0u};
+        if (col < heads) {
+            const T *src = static_cast<const T *>(a.q.data) + b * a.q.batch + (h0 + col) * a.q.head + (4 * s + g) * VE;
+            if (a.aligned) {
+                q[s] = *reinterpret_cast<const u32x4 *>(src);
+            } else {
+                T v[VE];
+#pragma unroll
+                for (int e = 0; e < VE; ++e) v[e] = src[e];
+                q[s] = __builtin_bit_cast(u32x4, v);
+            }
+        }
+    }
+    const int *row = a.table + (bad_call ? 0 : seq * a.table_stride);
+    const T *kc = static_cast<const T *>(a.cache_k.data) + kv * a.cache_k.head + g * VE;
+    const T *vc = static_cast<const T *>(a.cache_v.data) + kv * a.cache_v.head + g * VE;
+    T *vs = reinterpret_cast<T *>(lds) + wave * TT * LDV;
+    const float scale2 = a.scale * LOG2E;
+    const int slots = (1 << a.page_shift) - 1;
+
+    float m = -FLT_MAX, l = 0.f;        // finite: a score of minus infinity then weighs nothing, also where there is no other
+    f32x4 o[OUT];
+#pragma unroll
+    for (int t = 0; t < OUT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    bool bad_page = false;
+
+    for (int tok = begin + wave * TT; tok < end; tok += DEC_W * TT) {
+        TileRows<T, K> rows;
+        rows.ask(a, row, tok, lo, end, lane);
+        u32x4 kr[D::SETS][STEPS], vr[D::SETS][STEPS];
+#pragma unroll
+        for (int i = 0; i < D::SETS; ++i) {
+            const int slot = max(lo, min(end - 1, tok + 16 * i + col)) & slots;
+            const bool ok = (unsigned)rows.page[i] < (unsigned)a.n_pages;
+            bad_page = bad_page || !ok;
+            const long long page = ok ? rows.page[i] : 0;
+            const T *kp = kc + page * a.cache_k.batch + slot * a.cache_k.token, *vp = vc + page * a.cache_v.batch + slot * a.cache_v.token;
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) kr[i][s] = *reinterpret_cast<const u32x4 *>(kp + 4 * VE * s);
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) vr[i][s] = *reinterpret_cast<const u32x4 *>(vp + 4 * VE * s);
+        }
+        // scores, transposed: p[i][r] is token 16 i + 4 g + r of head `col`
+        f32x4 p[D::SETS];
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < D::SETS; ++i) {
+            p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                if constexpr (D::BF) {
+                    p[i] = Mfma<bf16>::mma(__builtin_bit_cast(bf16x8, kr[i][s]), __builtin_bit_cast(bf16x8, q[s]), p[i]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[i] = Mfma<float>::mma(vec_get<float>(kr[i][s], e), vec_get<float>(q[s], e), p[i]);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int j = tok + 16 * i + 4 * g + r;
+                p[i][r] = j >= lo && j < end ? p[i][r] * scale2 : -INFINITY;
+                top = fmaxf(top, p[i][r]);
+            }
+        }
+        top = max_xor32(max_xor16(top));
+#pragma unroll
+        for (int i = 0; i < D::SETS; ++i)
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) *reinterpret_cast<u32x4 *>(vs + (16 * i + col) * LDV + (4 * s + g) * VE) = vr[i][s];
+        if (__any(top > m)) {
+            const float f = __builtin_amdgcn_exp2f(m - top);
+            l *= f;
+#pragma unroll
+            for (int t = 0; t < OUT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[t][r] *= f;
+            m = top;
+        }
+#pragma unroll
+        for (int i = 0; i < D::SETS; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                p[i][r] = __builtin_amdgcn_exp2f(p[i][r] - m);
+                l += p[i][r];
+            }
+        // o transposed += values transposed x weights
+        if constexpr (D::BF) {
+            typedef short v4s __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) v4s *lds_v4s;
+            bf16x8 w;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { w[r] = (bf16)p[0][r]; w[4 + r] = (bf16)p[D::SETS - 1][r]; }
+#pragma unroll
+            for (int t = 0; t < OUT; ++t) {
+                const bf16 *at = reinterpret_cast<const bf16 *>(vs) + (4 * g + (col >> 2)) * LDV + 16 * t + 4 * (col & 3);
+                const v4s a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at));
+                const v4s a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at + 16 * LDV));
+                o[t] = Mfma<bf16>::mma(__builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)), w, o[t]);
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < OUT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[t] = Mfma<float>::mma(to_f32(vs[(4 * g + r) * LDV + 16 * t + col]), p[0][r], o[t]);
+        }
+    }
+    // the four wavefronts join
+    l = add_xor32(add_xor16(l));
+    if (bad_call || __any(bad_page)) l = __builtin_nanf("");
+    if (g == 0) { ml[wave][0][col] = m; ml[wave][1][col] = l; }
+    __syncthreads();
+    float M = ml[0][0][col], L = 0.f;
+#pragma unroll
+    for (int u = 1; u < DEC_W; ++u) M = fmaxf(M, ml[u][0][col]);
+#pragma unroll
+    for (int u = 0; u < DEC_W; ++u) L = __builtin_fmaf(ml[u][1][col], __builtin_amdgcn_exp2f(ml[u][0][col] - M), L);
+    const float f = __builtin_amdgcn_exp2f(m - M);
+    float *os = reinterpret_cast<float *>(lds) + wave * 16 * LDO;
+#pragma unroll
+    for (int t = 0; t < OUT; ++t) {
+        f32x4 x = o[t];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] *= f;
+        *reinterpret_cast<f32x4 *>(os + col * LDO + 16 * t + 4 * g) = x;
+    }
+    if (wave == 0 && g == 0) { ml[0][0][col] = M; ml[0][1][col] = L; }
+    __syncthreads();
+    const bool whole = a.pieces == 1;
+    for (int i = threadIdx.x; i < heads * (K / 4); i += DEC_T) {
+        const int h = i / (K / 4), d = i % (K / 4) * 4;
+        f32x4 x = load4(reinterpret_cast<const float *>(lds) + h * LDO + d);
+#pragma unroll
+        for (int u = 1; u < DEC_W; ++u) {
+            const f32x4 y = load4(reinterpret_cast<const float *>(lds) + (u * 16 + h) * LDO + d);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] += y[r];
+        }
+        const size_t bh = (size_t)b * a.Hq + h0 + h;
+        if (whole) {
+            const float sum = ml[0][1][h], inv = sum == 0.f ? 0.f : 1.f / sum;
+            T *dst = static_cast<T *>(a.o.data) + b * a.o.batch + (h0 + h) * a.o.head + d;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] *= inv;
+            if (a.aligned) {
+                store4(dst, x);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) dst[r] = from_f32<T>(x[r]);
+            }
+            if (a.lse && d == 0) a.lse[bh] = sum == 0.f ? -INFINITY : __builtin_fmaf(ml[0][0][h], LN2, logf(sum));
+        } else {
+            store4(a.part_o + (bh * a.pieces + piece) * K + d, x);
+            if (d == 0) {
+                a.part_ml[(bh * a.pieces + piece) * 2] = ml[0][0][h];
+                a.part_ml[(bh * a.pieces + piece) * 2 + 1] = ml[0][1][h];
+            }
+        }
+    }
+}
+
+// The pieces of one query head, joined in a fixed order
+constexpr int JOIN_T = 256;
+template <typename T, int K>
+__global__ __launch_bounds__(JOIN_T) void decode_join_kernel(DecodeArgs a) {
+    constexpr int COLS = K / 4, ROWS = JOIN_T / COLS, TT = DecodeTile<T, K>::TT;
+    __shared__ float red[ROWS][K];
+    __shared__ float wmax[JOIN_T / 64], wsum[JOIN_T / 64];
+    const int h = blockIdx.x, b = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const size_t bh = (size_t)b * a.Hq + h;
+    const int length = a.lengths[b];
+    const int lo = a.window > 0 && length > a.window ? length - a.window : 0;
+    const int n = length > a.max_length ? 1 : max(1, (length - (lo & ~(TT - 1)) + a.piece - 1) / a.piece);
+    const float *ml = a.part_ml + bh * a.pieces * 2, *po = a.part_o + bh * a.pieces * K;
+    float M = -FLT_MAX;
+    for (int i = threadIdx.x; i < n; i += JOIN_T) M = fmaxf(M, ml[2 * i]);
+    M = max_xor32(max_xor16(M));
+    for (int x = 1; x < 16; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
+    if (lane == 0) wmax[wave] = M;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < JOIN_T / 64; ++u) M = fmaxf(M, wmax[u]);
+    float L = 0.f;
+    for (int i = threadIdx.x; i < n; i += JOIN_T) L = __builtin_fmaf(ml[2 * i + 1], __builtin_amdgcn_exp2f(ml[2 * i] - M), L);
+    L = wave_sum(L);
+    if (lane == 0) wsum[wave] = L;
+    const int c = threadIdx.x % COLS, r0 = threadIdx.x / COLS;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int i = r0; i < n; i += ROWS) {
+        const float f = __builtin_amdgcn_exp2f(ml[2 * i] - M);
+        const f32x4 y = load4(po + (size_t)i * K + 4 * c);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = __builtin_fmaf(y[r], f, x[r]);
+    }
+    *reinterpret_cast<f32x4 *>(&red[r0][4 * c]) = x;
+    __syncthreads();
+    L = 0.f;
+#pragma unroll
+    for (int u = 0; u < JOIN_T / 64; ++u) L += wsum[u];
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    for (int d = threadIdx.x; d < K; d += JOIN_T) {
+        float y = 0.f;
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) y += red[u][d];
+        static_cast<T *>(a.o.data)[b * a.o.batch + h * a.o.head + d] = from_f32<T>(y * inv);
+    }
+    if (a.lse && threadIdx.x == 0) a.lse[bh] = L == 0.f ? -INFINITY : __builtin_fmaf(M, LN2, logf(L));
+}
+
+namespace {
+template <typename T, int K> void decode_of(const DecodeArgs &a, hipStream_t st) {
+    hipLaunchKernelGGL((decode_kernel<T, K>), dim3(a.pieces, a.Hk * a.head_tiles, a.B), dim3(DEC_T), 0, st, a);
+    if (a.pieces > 1) hipLaunchKernelGGL((decode_join_kernel<T, K>), dim3(a.Hq, a.B), dim3(JOIN_T), 0, st, a);
+}
+}  // namespace
+
+int launch_paged_decode(const DecodeArgs &a, bool bf16_io, hipStream_t st) {
+    switch (a.K) {
+        case 64: bf16_io ? decode_of<bf16, 64>(a, st) : decode_of<float, 64>(a, st); return 0;
+        case 128: bf16_io ? decode_of<bf16, 128>(a, st) : decode_of<float, 128>(a, st); return 0;
+        case 256: bf16_io ? decode_of<bf16, 256>(a, st) : decode_of<float, 256>(a, st); return 0;
+        default: return -1;
+    }
+}
+
+}  // namespace osdn

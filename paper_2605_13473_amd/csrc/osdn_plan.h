@@ -231,4 +231,22 @@ inline bool solved_plan(const osdn_params *p, long long chains, int longest, boo
     return p->p1_solved > 0 || (p->p1_solved == 0 && chains * (quarter ? 4 : 8) <= NUM_CU);
 }
 
+// Blocks of rows (64 lanes of 16 bytes) that a wavefront of heads_fwd_kernel takes: four, one where that would leave the chip idle.
+inline int heads_blocks_per_wave(long long tokens, int blocks) { return tokens * blocks >= 4ll * NUM_CU * 8 ? 4 : 1; }
+// Workgroups of heads_bwd_kernel (four wavefronts, a token each at a time)
+inline int heads_bwd_workgroups(long long tokens) { return (int)(tokens < 4 * 1024 ? (tokens + 3) / 4 : 1024); }
+
+// Attention over a paged cache: tokens that a sequence of at most max_length may see, counted from a multiple of the tile of 32
+constexpr int DECODE_TILE = 32, DECODE_PIECE = 128, DEC_THREADS = 256;       // a piece: at least a tile for each of the workgroup's four wavefronts
+inline long long decode_span(int max_length, int window) {
+    const long long seen = window > 0 && window < max_length ? (long long)window + DECODE_TILE - 1 : max_length;
+    return seen < max_length ? seen : max_length;
+}
+// ... and the tokens of a piece, for `rows` (sequence, group of query heads) pairs
+inline int decode_piece(long long rows, long long span) {
+    const long long want = rows * span / (NUM_CU * 8);
+    const long long piece = (want + DECODE_PIECE - 1) / DECODE_PIECE * DECODE_PIECE;
+    return (int)(piece < DECODE_PIECE ? DECODE_PIECE : piece > 2048 ? 2048 : piece);
+}
+
 }  // namespace osdn
