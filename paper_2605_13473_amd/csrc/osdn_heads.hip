@@ -56,212 +56,271 @@ template <int LANES> __device__ __forceinline__ float row_sum(float x) {
     return x;
 }
 
-// The rotation of a lane's elements: z = x c + partner s (transposed: x c - partner s).  A lane that holds no pair leaves them alone.
-template <typename T, int K> struct Turn {
-    static constexpr int VE = HeadRow<T, K>::VE;
-    float c[VE], s[VE];
-    int from;                       // the lane that holds the partners, times 4 (adjacent pairs: this one)
-    bool on;
-    __device__ __forceinline__ void load(const float *row, int R, bool interleaved, int lane) {
-        const int l = lane & (HeadRow<T, K>::LANES - 1), e0 = l * VE, half = R / 2;
-        on = e0 < R;
+// The caller's fp32 arrays are aligned as floats are
+struct __attribute__((packed, aligned(4))) FloatQuad { float v[4]; };
+template <int N> __device__ __forceinline__ void load_floats(float (&x)[N], const float *p) {
+    static_assert(N % 2 == 0, "");
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const FloatQuad q = reinterpret_cast<const FloatQuad *>(p)[i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[4 * i + e] = q.v[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = p[e];
+    }
+}
+
+// The pairs that turn: none, (i, i + R / 2) or (2i, 2i + 1)
+enum { ROT_NONE = 0, ROT_HALF = 1, ROT_PAIRS = 2 };
+
+// The rotation of a lane's elements: z = y c + partner s (transposed: y c - partner s).  Elements that do not turn: c = 1, partner = 0.
+template <typename T, int K, int ROT> struct Turn {
+    static constexpr int VE = HeadRow<T, K>::VE, LANES = HeadRow<T, K>::LANES;
+    bool on;                        // the lane's elements turn
+    int from;                       // the lane that holds their partners
+    int i0;                         // the first one's pair
+    float sign;
+    __device__ __forceinline__ Turn(int R, int lane) {
+        const int e0 = (lane & (LANES - 1)) * VE, half = R / 2;
         const bool low = e0 < half;
-        const int i0 = !on ? 0 : interleaved ? e0 / 2 : low ? e0 : e0 - half;
-        from = 4 * (!on || interleaved ? lane : low ? lane + half / VE : lane - half / VE);
+        on = e0 < R;
+        from = ROT == ROT_PAIRS || !on ? lane : low ? lane + half / VE : lane - half / VE;
+        i0 = !on ? 0 : ROT == ROT_PAIRS ? e0 / 2 : low ? e0 : e0 - half;
+        sign = low ? -1.f : 1.f;
+    }
+    __device__ __forceinline__ void load(const float *row, int R, float (&c)[VE], float (&s)[VE]) const {
+        constexpr int N = ROT == ROT_PAIRS ? VE / 2 : VE;
+        float cs[N], sn[N];
+        load_floats(cs, row + i0);
+        load_floats(sn, row + R / 2 + i0);
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
-            const int i = i0 + (interleaved ? e / 2 : e);
-            c[e] = row[i];
-            const float sn = row[half + i];
-            s[e] = (interleaved ? (e & 1) == 0 : low) ? -sn : sn;
+            c[e] = on ? cs[ROT == ROT_PAIRS ? e / 2 : e] : 1.f;
+            s[e] = ROT == ROT_PAIRS ? ((e & 1) ? sn[e / 2] : -sn[e / 2]) : sn[e] * sign;
         }
     }
     // the partners of a lane's elements (every lane of the wavefront calls it)
-    __device__ __forceinline__ u32x4 partners(const u32x4 &raw, bool interleaved) const {
+    __device__ __forceinline__ void partners(const u32x4 &raw, float (&x)[VE]) const {
         u32x4 o;
-        if (interleaved) {
+        if constexpr (ROT == ROT_PAIRS) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) o[w] = sizeof(T) == 2 ? (raw[w] >> 16) | (raw[w] << 16) : raw[w ^ 1];
         } else {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) o[w] = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)raw[w]);
+            for (int w = 0; w < 4; ++w) o[w] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * from, (int)raw[w]);
         }
-        return o;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) o[w] = on ? o[w] : 0u;
+        unpack<T>(o, x);
     }
+    // what stands at the partners' places of a row that all lanes of a row hold (weights)
+    __device__ __forceinline__ int partner_element(int lane, int e) const { return ROT == ROT_PAIRS ? (lane & (LANES - 1)) * VE + (e ^ 1) : (from & (LANES - 1)) * VE + e; }
 };
 
-// Where a token's rows are and what becomes of them: -1 none (its outputs are zero), else its position
-__device__ __forceinline__ int token_position(const HeadsArgs &a, int t, size_t n) { return a.positions ? a.positions[n] : t; }
+// The weights of a lane's elements and of their partners, for queries (0) and keys (1); loaded once per wavefront
+template <typename T, int K, int ROT> struct Weights {
+    static constexpr int VE = HeadRow<T, K>::VE;
+    float own[2][VE], partner[2][VE];
+    __device__ __forceinline__ void load(const HeadsArgs &a, const Turn<T, K, ROT> &turn, int lane) {
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind) {
+            const float *w = kind == 0 ? a.weight_q : a.weight_k;
+            if (w) load_floats(own[kind], w + (lane & (HeadRow<T, K>::LANES - 1)) * VE);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                if (!w) own[kind][e] = 1.f;
+                if constexpr (ROT == ROT_PAIRS) partner[kind][e ^ 1] = own[kind][e];
+            }
+            if constexpr (ROT == ROT_HALF) {
+                if (w) load_floats(partner[kind], w + turn.partner_element(lane, 0));
+                else {
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) partner[kind][e] = 1.f;
+                }
+            }
+        }
+    }
+};
 
 template <typename T, bool VEC> __device__ __forceinline__ T *row_at(const HeadRows &r, int b, int t, int h) {
     return static_cast<T *>(r.data) + b * r.batch + t * r.token + h * r.head;
 }
 
-// NB blocks of rows per wavefront.  APPEND: keys go to the cache, values follow them unchanged.
-template <typename T, int K, bool VEC, bool ROT, int NB, bool APPEND>
+// A wavefront walks (token, part of its blocks of rows) pairs in steps of the grid; it has the loads of NB blocks in flight at a time.
+// APPEND: keys go to the cache, values follow them unchanged.
+template <typename T, int K, bool VEC, int ROT, bool APPEND>
 __global__ __launch_bounds__(HEADS_T) void heads_fwd_kernel(HeadsArgs a) {
     using HR = HeadRow<T, K>;
-    constexpr int VE = HR::VE, ROWS = HR::ROWS;
+    constexpr int VE = HR::VE, ROWS = HR::ROWS, NB = 4;
     const int lane = threadIdx.x & 63, sub = lane / HR::LANES, e0 = (lane % HR::LANES) * VE;
-    const unsigned item = __builtin_amdgcn_readfirstlane(blockIdx.x * (HEADS_T / 64) + (threadIdx.x >> 6));
-    const unsigned token = item / (unsigned)a.parts + blockIdx.y * (unsigned)a.tokens_y;
-    const int part = item % (unsigned)a.parts;
-    if (token >= (unsigned)a.tokens || item / (unsigned)a.parts >= (unsigned)a.tokens_y) return;
-    const int b = token / (unsigned)a.T, t = token % (unsigned)a.T;
+    const Turn<T, K, ROT> turn(a.rotary_dim, lane);
+    Weights<T, K, ROT> w;
+    w.load(a, turn, lane);
 
-    // a block of rows: 0 queries, 1 keys, 2 values
-    int kind[NB], h[NB];
-    bool live[NB];
-    u32x4 raw[NB];
-#pragma unroll
-    for (int i = 0; i < NB; ++i) {
-        const int blk = part * NB + i;
-        kind[i] = blk < a.q_blocks ? 0 : blk < a.q_blocks + a.k_blocks ? 1 : 2;
-        const int first = kind[i] == 0 ? 0 : kind[i] == 1 ? a.q_blocks : a.q_blocks + a.k_blocks;
-        h[i] = (blk - first) * ROWS + sub;
-        live[i] = blk < a.blocks && h[i] < (kind[i] == 0 ? a.Hq : a.Hk);
-        const HeadRows &src = kind[i] == 0 ? a.q : kind[i] == 1 ? a.k : a.v;
-        raw[i] = u32x4{0u, 0u, 0u, 0u};
-        if (live[i]) raw[i] = load_row<T, VEC>(row_at<const T, VEC>(src, b, t, h[i]) + e0);
-    }
-    const int pos = token_position(a, t, token);
-    const bool none = pos < 0;
-    const bool off_table = ROT && pos >= a.rotary_rows;
-    Turn<T, K> turn;
-    if constexpr (ROT) turn.load(a.rotary + (size_t)(none || off_table ? 0 : pos) * a.rotary_dim, a.rotary_dim, a.interleaved, lane);
-    T *page_k = nullptr, *page_v = nullptr;
-    if constexpr (APPEND) {
-        const int seq = a.seq ? a.seq[token] : b, col = pos >> a.page_shift;
-        if (!none && (unsigned)seq < (unsigned)a.n_seqs && col < a.max_pages) {
-            const int page = a.table[seq * a.table_stride + col];
-            const int slot = pos & ((1 << a.page_shift) - 1);
-            if ((unsigned)page < (unsigned)a.n_pages) {
-                page_k = static_cast<T *>(a.cache_k.data) + page * a.cache_k.batch + slot * a.cache_k.token;
-                page_v = static_cast<T *>(a.cache_v.data) + page * a.cache_v.batch + slot * a.cache_v.token;
+    const unsigned items = (unsigned)a.tokens * (unsigned)a.parts, stride = gridDim.x * (HEADS_T / 64);
+    for (unsigned item = __builtin_amdgcn_readfirstlane(blockIdx.x * (HEADS_T / 64) + (threadIdx.x >> 6)); item < items; item += stride) {
+        const unsigned token = item / (unsigned)a.parts;
+        const int part = item % (unsigned)a.parts, b = token / (unsigned)a.T, t = token % (unsigned)a.T;
+        const int blk_end = min(a.blocks, (part + 1) * a.per_part);
+        const int pos = a.positions ? a.positions[token] : t;
+        const bool none = pos < 0;
+        const bool off_table = ROT && pos >= a.rotary_rows;
+        float c[VE], s[VE];
+        if constexpr (ROT != ROT_NONE) turn.load(a.rotary + (size_t)(none || off_table ? 0 : pos) * a.rotary_dim, a.rotary_dim, c, s);
+        T *page_k = nullptr, *page_v = nullptr;
+        if constexpr (APPEND) {
+            const int seq = a.seq ? a.seq[token] : b, col = pos >> a.page_shift;
+            if (!none && (unsigned)seq < (unsigned)a.n_seqs && col < a.max_pages) {
+                const int page = a.table[seq * a.table_stride + col];
+                const int slot = pos & ((1 << a.page_shift) - 1);
+                if ((unsigned)page < (unsigned)a.n_pages) {
+                    page_k = static_cast<T *>(a.cache_k.data) + page * a.cache_k.batch + slot * a.cache_k.token;
+                    page_v = static_cast<T *>(a.cache_v.data) + page * a.cache_v.batch + slot * a.cache_v.token;
+                }
             }
         }
-    }
+        for (int blk0 = part * a.per_part; blk0 < blk_end; blk0 += NB) {
+            u32x4 raw[NB];
 #pragma unroll
-    for (int i = 0; i < NB; ++i) {
-        if (part * NB + i >= a.blocks) break;
-        if (APPEND && kind[i] == 2) {
-            if (live[i] && page_v) {
-                T *dst = page_v + h[i] * a.cache_v.head + e0;
-                *reinterpret_cast<u32x4 *>(dst) = raw[i];
+            for (int i = 0; i < NB; ++i) {
+                const int blk = blk0 + i, kind = blk < a.q_blocks ? 0 : blk < a.q_blocks + a.k_blocks ? 1 : 2;
+                const int h = (blk - (kind == 0 ? 0 : kind == 1 ? a.q_blocks : a.q_blocks + a.k_blocks)) * ROWS + sub;
+                const HeadRows &src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
+                raw[i] = u32x4{0u, 0u, 0u, 0u};
+                if (blk < blk_end && h < (kind == 0 ? a.Hq : a.Hk)) raw[i] = load_row<T, VEC>(row_at<const T, VEC>(src, b, t, h) + e0);
             }
-            continue;
-        }
-        float x[VE], z[VE];
-        unpack<T>(raw[i], x);
-        float r = 1.f;
-        if (a.norm != 0) {
-            float ss = 0.f;
 #pragma unroll
-            for (int e = 0; e < VE; ++e) ss = __builtin_fmaf(x[e], x[e], ss);
-            r = rsqrtf(__builtin_fmaf(row_sum<HR::LANES>(ss), a.mean, a.eps));
-        }
-        if (off_table) r = __builtin_nanf("");
-        const float *w = kind[i] == 0 ? a.weight_q : a.weight_k;
+            for (int i = 0; i < NB; ++i) {
+                const int blk = blk0 + i, kind = blk < a.q_blocks ? 0 : blk < a.q_blocks + a.k_blocks ? 1 : 2;
+                const int h = (blk - (kind == 0 ? 0 : kind == 1 ? a.q_blocks : a.q_blocks + a.k_blocks)) * ROWS + sub;
+                if (blk >= blk_end) break;
+                const bool live = h < (kind == 0 ? a.Hq : a.Hk);
+                if (APPEND && kind == 2) {
+                    if (live && page_v) *reinterpret_cast<u32x4 *>(page_v + h * a.cache_v.head + e0) = raw[i];
+                    continue;
+                }
+                float x[VE], z[VE];
+                unpack<T>(raw[i], x);
+                float r = 1.f;
+                if (a.norm != 0) {
+                    float ss = 0.f;
 #pragma unroll
-        for (int e = 0; e < VE; ++e) z[e] = x[e] * r;
-        if (w) {
+                    for (int e = 0; e < VE; ++e) ss = __builtin_fmaf(x[e], x[e], ss);
+                    r = rsqrtf(__builtin_fmaf(row_sum<HR::LANES>(ss), a.mean, a.eps));
+                }
+                if (off_table) r = __builtin_nanf("");
+                if constexpr (ROT == ROT_NONE) {
 #pragma unroll
-            for (int e = 0; e < VE; ++e) z[e] *= w[e0 + e];
-        }
-        if constexpr (ROT) {
-            float y[VE];
-            unpack<T>(turn.partners(raw[i], a.interleaved), y);
-            const int from = a.interleaved ? e0 : (turn.from / 4 % HR::LANES) * VE;
+                    for (int e = 0; e < VE; ++e) z[e] = x[e] * (r * (kind == 0 ? w.own[0][e] : w.own[1][e]));
+                } else {
+                    float y[VE];
+                    turn.partners(raw[i], y);
 #pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                float yp = y[e] * r;
-                if (w) yp *= w[from + (a.interleaved ? e ^ 1 : e)];
-                const float turned = __builtin_fmaf(z[e], turn.c[e], yp * turn.s[e]);
-                z[e] = turn.on ? turned : z[e];
+                    for (int e = 0; e < VE; ++e) {
+                        const float own = x[e] * (kind == 0 ? w.own[0][e] : w.own[1][e]), other = y[e] * (kind == 0 ? w.partner[0][e] : w.partner[1][e]);
+                        z[e] = r * __builtin_fmaf(own, c[e], other * s[e]);
+                    }
+                }
+                if (!live) continue;
+                if (none) {
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) z[e] = 0.f;
+                }
+                if (APPEND && kind == 1) {
+                    if (page_k) store_vec_t(page_k + h * a.cache_k.head + e0, z);
+                } else {
+                    store_row<T, VEC, VE>(row_at<T, VEC>(kind == 0 ? a.q_out : a.k_out, b, t, h) + e0, z);
+                }
             }
-        }
-        if (!live[i]) continue;
-        if (none) {
-#pragma unroll
-            for (int e = 0; e < VE; ++e) z[e] = 0.f;
-        }
-        if (APPEND && kind[i] == 1) {
-            if (page_k) store_vec_t(page_k + h[i] * a.cache_k.head + e0, z);
-        } else {
-            store_row<T, VEC, VE>(row_at<T, VEC>(kind[i] == 0 ? a.q_out : a.k_out, b, t, h[i]) + e0, z);
         }
     }
 }
 
-// Backward: a workgroup walks tokens in steps of the grid, so that the sums over rows of dw stay in registers until its end; its
-// partial sums go to a row of `partial` [gridDim.x][2][K], which heads_dw_kernel adds up in a fixed order.
-template <typename T, int K, bool VEC, bool ROT>
+// Backward: a wavefront walks tokens in steps of the grid, so that its sums over rows of dw stay in registers until the end; the
+// partial sums of a workgroup go to a row of `partial` [gridDim.x][2][K], which heads_dw_kernel adds up in a fixed order.
+template <typename T, int K, bool VEC, int ROT>
 __global__ __launch_bounds__(HEADS_T) void heads_bwd_kernel(HeadsArgs a) {
     using HR = HeadRow<T, K>;
-    constexpr int VE = HR::VE, ROWS = HR::ROWS, WAVES = HEADS_T / 64;
+    constexpr int VE = HR::VE, ROWS = HR::ROWS, WAVES = HEADS_T / 64, NB = 2;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / HR::LANES, e0 = (lane % HR::LANES) * VE;
-    float dw[2][VE];
+    const Turn<T, K, ROT> turn(a.rotary_dim, lane);
+    float w[2][VE], dw[2][VE];
 #pragma unroll
-    for (int e = 0; e < VE; ++e) dw[0][e] = dw[1][e] = 0.f;
+    for (int kind = 0; kind < 2; ++kind) {
+        const float *src = kind == 0 ? a.weight_q : a.weight_k;
+        if (src) load_floats(w[kind], src + e0);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+            if (!src) w[kind][e] = 1.f;
+            dw[kind][e] = 0.f;
+        }
+    }
 
     for (unsigned token = __builtin_amdgcn_readfirstlane(blockIdx.x * WAVES + wave); token < (unsigned)a.tokens; token += gridDim.x * WAVES) {
         const int b = token / (unsigned)a.T, t = token % (unsigned)a.T;
-        const int pos = token_position(a, t, token);
+        const int pos = a.positions ? a.positions[token] : t;
         const bool none = pos < 0;
         const bool off_table = ROT && pos >= a.rotary_rows;
-        Turn<T, K> turn;
-        if constexpr (ROT) turn.load(a.rotary + (size_t)(none || off_table ? 0 : pos) * a.rotary_dim, a.rotary_dim, a.interleaved, lane);
+        float c[VE], s[VE];
+        if constexpr (ROT != ROT_NONE) turn.load(a.rotary + (size_t)(none || off_table ? 0 : pos) * a.rotary_dim, a.rotary_dim, c, s);
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind) {
             const HeadRows &xs = kind == 0 ? a.q : a.k, &zs = kind == 0 ? a.dq_out : a.dk_out, &ds = kind == 0 ? a.dq : a.dk;
             const int H = kind == 0 ? a.Hq : a.Hk;
-            const float *w = kind == 0 ? a.weight_q : a.weight_k;
-            for (int h0 = 0; h0 < H; h0 += ROWS) {
-                const int h = h0 + sub;
-                const bool live = h < H;
-                u32x4 rx = {0u, 0u, 0u, 0u}, rz = {0u, 0u, 0u, 0u};
-                if (live) {
-                    rx = load_row<T, VEC>(row_at<const T, VEC>(xs, b, t, h) + e0);
-                    rz = load_row<T, VEC>(row_at<const T, VEC>(zs, b, t, h) + e0);
-                }
-                float x[VE], dy[VE], g[VE];
-                unpack<T>(rx, x);
-                unpack<T>(rz, dy);
-                if constexpr (ROT) {
-                    float p[VE];
-                    unpack<T>(turn.partners(rz, a.interleaved), p);
+            for (int h0 = 0; h0 < H; h0 += NB * ROWS) {
+                u32x4 rx[NB], rz[NB];
 #pragma unroll
-                    for (int e = 0; e < VE; ++e) {
-                        const float turned = __builtin_fmaf(dy[e], turn.c[e], -(p[e] * turn.s[e]));
-                        dy[e] = turn.on ? turned : dy[e];
+                for (int i = 0; i < NB; ++i) {
+                    const int h = h0 + i * ROWS + sub;
+                    rx[i] = rz[i] = u32x4{0u, 0u, 0u, 0u};
+                    if (h < H) {
+                        rx[i] = load_row<T, VEC>(row_at<const T, VEC>(xs, b, t, h) + e0);
+                        rz[i] = load_row<T, VEC>(row_at<const T, VEC>(zs, b, t, h) + e0);
                     }
                 }
-                float r = 1.f, ss = 0.f, gx = 0.f;
 #pragma unroll
-                for (int e = 0; e < VE; ++e) {
-                    g[e] = w ? dy[e] * w[e0 + e] : dy[e];
-                    ss = __builtin_fmaf(x[e], x[e], ss);
-                    gx = __builtin_fmaf(g[e], x[e], gx);
-                }
-                if (a.norm != 0) {
-                    r = rsqrtf(__builtin_fmaf(row_sum<HR::LANES>(ss), a.mean, a.eps));
-                    gx = row_sum<HR::LANES>(gx) * (r * r * a.mean);
-                } else {
-                    gx = 0.f;
-                }
-                if (off_table) r = __builtin_nanf("");
-                if (none || !live) {
+                for (int i = 0; i < NB; ++i) {
+                    const int h = h0 + i * ROWS + sub;
+                    if (h0 + i * ROWS >= H) break;
+                    float x[VE], dy[VE], g[VE];
+                    unpack<T>(rx[i], x);
+                    unpack<T>(rz[i], dy);
+                    if constexpr (ROT != ROT_NONE) {
+                        float y[VE];
+                        turn.partners(rz[i], y);
 #pragma unroll
-                    for (int e = 0; e < VE; ++e) g[e] = x[e] = dy[e] = 0.f;
-                    gx = r = 0.f;
-                }
-                float dx[VE];
+                        for (int e = 0; e < VE; ++e) dy[e] = __builtin_fmaf(dy[e], c[e], -(y[e] * s[e]));
+                    }
+                    float r = 1.f, ss = 0.f, gx = 0.f;
 #pragma unroll
-                for (int e = 0; e < VE; ++e) {
-                    dx[e] = r * __builtin_fmaf(-gx, x[e], g[e]);
-                    dw[kind][e] = __builtin_fmaf(dy[e] * r, x[e], dw[kind][e]);
+                    for (int e = 0; e < VE; ++e) {
+                        g[e] = dy[e] * w[kind][e];
+                        ss = __builtin_fmaf(x[e], x[e], ss);
+                        gx = __builtin_fmaf(g[e], x[e], gx);
+                    }
+                    if (a.norm != 0) {
+                        r = rsqrtf(__builtin_fmaf(row_sum<HR::LANES>(ss), a.mean, a.eps));
+                        gx = row_sum<HR::LANES>(gx) * (r * r * a.mean);
+                    } else {
+                        gx = 0.f;
+                    }
+                    if (off_table) r = __builtin_nanf("");
+                    if (none || h >= H) {
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) g[e] = x[e] = dy[e] = 0.f;
+                        gx = r = 0.f;
+                    }
+                    float dx[VE];
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) {
+                        dx[e] = r * __builtin_fmaf(-gx, x[e], g[e]);
+                        dw[kind][e] = __builtin_fmaf(dy[e] * r, x[e], dw[kind][e]);
+                    }
+                    if (h < H) store_row<T, VEC, VE>(row_at<T, VEC>(ds, b, t, h) + e0, dx);
                 }
-                if (live) store_row<T, VEC, VE>(row_at<T, VEC>(ds, b, t, h) + e0, dx);
             }
         }
     }
@@ -305,61 +364,43 @@ __global__ __launch_bounds__(DW_T) void heads_dw_kernel(const float *partial, in
 }
 
 namespace {
-template <typename T, int K, bool VEC, bool ROT> void fwd_parts(HeadsArgs &a, int nb, hipStream_t st) {
-    auto go = [&](auto kernel, int n) {
-        a.parts = (a.blocks + n - 1) / n;
-        // (a grid has fewer than 2^32 threads along x: more tokens than that go along y)
-        const long long most = (1ll << 25) / a.parts, rows = a.tokens < most ? a.tokens : most;
-        a.tokens_y = (int)rows;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((rows * a.parts + HEADS_T / 64 - 1) / (HEADS_T / 64)), (unsigned)((a.tokens + rows - 1) / rows)), dim3(HEADS_T), 0, st, a);
-    };
-    if (a.append) {
-        if (VEC && nb > 1) go(heads_fwd_kernel<T, K, VEC, ROT, VEC ? 4 : 1, true>, 4);
-        else go(heads_fwd_kernel<T, K, VEC, ROT, 1, true>, 1);
-    } else {
-        if (VEC && nb > 1) go(heads_fwd_kernel<T, K, VEC, ROT, VEC ? 4 : 1, false>, 4);
-        else go(heads_fwd_kernel<T, K, VEC, ROT, 1, false>, 1);
-    }
-}
-template <typename T, int K> void set_blocks(HeadsArgs &a) {
+template <typename T, int K, bool VEC, int ROT> void fwd_of(HeadsArgs a, hipStream_t st) {
     constexpr int ROWS = HeadRow<T, K>::ROWS;
     a.q_blocks = (a.Hq + ROWS - 1) / ROWS;
     a.k_blocks = (a.Hk + ROWS - 1) / ROWS;
     a.blocks = a.q_blocks + a.k_blocks * (a.append ? 2 : 1);
+    a.per_part = heads_blocks_per_wave(a.tokens, a.blocks);
+    a.parts = (a.blocks + a.per_part - 1) / a.per_part;
+    const dim3 g((unsigned)heads_fwd_workgroups((long long)a.tokens * a.parts)), t(HEADS_T);
+    if (a.append) hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, true>), g, t, 0, st, a);
+    else hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, false>), g, t, 0, st, a);
 }
-template <typename T, int K> void fwd_of(HeadsArgs &a, hipStream_t st) {
-    set_blocks<T, K>(a);
-    const int nb = heads_blocks_per_wave(a.tokens, a.blocks);
-    if (a.aligned) a.rotary ? fwd_parts<T, K, true, true>(a, nb, st) : fwd_parts<T, K, true, false>(a, nb, st);
-    else a.rotary ? fwd_parts<T, K, false, true>(a, nb, st) : fwd_parts<T, K, false, false>(a, nb, st);
-}
-template <typename T, int K> void bwd_of(HeadsArgs &a, hipStream_t st) {
-    const dim3 g((unsigned)heads_bwd_workgroups(a.tokens)), t(HEADS_T);
-    if (a.aligned) {
-        if (a.rotary) hipLaunchKernelGGL((heads_bwd_kernel<T, K, true, true>), g, t, 0, st, a);
-        else hipLaunchKernelGGL((heads_bwd_kernel<T, K, true, false>), g, t, 0, st, a);
-    } else {
-        if (a.rotary) hipLaunchKernelGGL((heads_bwd_kernel<T, K, false, true>), g, t, 0, st, a);
-        else hipLaunchKernelGGL((heads_bwd_kernel<T, K, false, false>), g, t, 0, st, a);
-    }
+template <typename T, int K, bool VEC, int ROT> void bwd_of(const HeadsArgs &a, hipStream_t st) {
+    const int n = heads_bwd_workgroups(a.tokens);
+    hipLaunchKernelGGL((heads_bwd_kernel<T, K, VEC, ROT>), dim3((unsigned)n), dim3(HEADS_T), 0, st, a);
     if (a.partial)
-        hipLaunchKernelGGL(heads_dw_kernel, dim3(2 * K / DW_COLS), dim3(DW_T), 0, st, a.partial, (int)g.x, K, a.dweight_q, a.dweight_k);
+        hipLaunchKernelGGL(heads_dw_kernel, dim3(2 * K / DW_COLS), dim3(DW_T), 0, st, a.partial, n, K, a.dweight_q, a.dweight_k);
 }
-template <typename F> int by_width(int K, bool bf16_io, F &&f) {
-    switch (K) {
-        case 64: bf16_io ? f(bf16{}, std::integral_constant<int, 64>{}) : f(float{}, std::integral_constant<int, 64>{}); return 0;
-        case 128: bf16_io ? f(bf16{}, std::integral_constant<int, 128>{}) : f(float{}, std::integral_constant<int, 128>{}); return 0;
-        case 256: bf16_io ? f(bf16{}, std::integral_constant<int, 256>{}) : f(float{}, std::integral_constant<int, 256>{}); return 0;
+template <typename T, int K, bool VEC> void by_rotation(const HeadsArgs &a, bool backward, hipStream_t st) {
+    if (!a.rotary) backward ? bwd_of<T, K, VEC, ROT_NONE>(a, st) : fwd_of<T, K, VEC, ROT_NONE>(a, st);
+    else if (a.interleaved) backward ? bwd_of<T, K, VEC, ROT_PAIRS>(a, st) : fwd_of<T, K, VEC, ROT_PAIRS>(a, st);
+    else backward ? bwd_of<T, K, VEC, ROT_HALF>(a, st) : fwd_of<T, K, VEC, ROT_HALF>(a, st);
+}
+template <typename T> int by_width(const HeadsArgs &a, bool backward, hipStream_t st) {
+    auto go = [&](auto k) {
+        a.aligned ? by_rotation<T, decltype(k)::value, true>(a, backward, st) : by_rotation<T, decltype(k)::value, false>(a, backward, st);
+        return 0;
+    };
+    switch (a.K) {
+        case 64: return go(std::integral_constant<int, 64>{});
+        case 128: return go(std::integral_constant<int, 128>{});
+        case 256: return go(std::integral_constant<int, 256>{});
         default: return -1;
     }
 }
 }  // namespace
 
-int launch_heads_fwd(HeadsArgs a, bool bf16_io, hipStream_t st) {
-    return by_width(a.K, bf16_io, [&](auto t, auto k) { fwd_of<decltype(t), decltype(k)::value>(a, st); });
-}
-int launch_heads_bwd(HeadsArgs a, bool bf16_io, hipStream_t st) {
-    return by_width(a.K, bf16_io, [&](auto t, auto k) { bwd_of<decltype(t), decltype(k)::value>(a, st); });
-}
+int launch_heads_fwd(const HeadsArgs &a, bool bf16_io, hipStream_t st) { return bf16_io ? by_width<bf16>(a, false, st) : by_width<float>(a, false, st); }
+int launch_heads_bwd(const HeadsArgs &a, bool bf16_io, hipStream_t st) { return bf16_io ? by_width<bf16>(a, true, st) : by_width<float>(a, true, st); }
 
 }  // namespace osdn

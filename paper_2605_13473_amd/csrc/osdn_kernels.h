@@ -262,11 +262,11 @@ struct HeadsArgs {
     HeadRows dq_out, dk_out, dq, dk;
     float *dweight_q, *dweight_k;         // [K] or null
     float *partial;                       // [workgroups][2][K], null without weights
-    // set by the launcher: blocks of rows of a token, and how many wavefronts share them; tokens per step of the grid along y
-    int q_blocks, k_blocks, blocks, parts, tokens_y;
+    // set by the launcher: blocks of rows of a token, how many wavefronts share them, blocks of each
+    int q_blocks, k_blocks, blocks, parts, per_part;
 };
-int launch_heads_fwd(HeadsArgs a, bool bf16_io, hipStream_t st);
-int launch_heads_bwd(HeadsArgs a, bool bf16_io, hipStream_t st);
+int launch_heads_fwd(const HeadsArgs &a, bool bf16_io, hipStream_t st);
+int launch_heads_bwd(const HeadsArgs &a, bool bf16_io, hipStream_t st);
 
 // Attention of one token per sequence over a paged cache (osdn_paged.hip)
 struct DecodeArgs {

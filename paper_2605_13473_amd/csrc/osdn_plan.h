@@ -231,9 +231,14 @@ inline bool solved_plan(const osdn_params *p, long long chains, int longest, boo
     return p->p1_solved > 0 || (p->p1_solved == 0 && chains * (quarter ? 4 : 8) <= NUM_CU);
 }
 
-// Blocks of rows (64 lanes of 16 bytes) that a wavefront of heads_fwd_kernel takes: four, one where that would leave the chip idle.
-inline int heads_blocks_per_wave(long long tokens, int blocks) { return tokens * blocks >= 4ll * NUM_CU * 8 ? 4 : 1; }
-// Workgroups of heads_bwd_kernel (four wavefronts, a token each at a time)
+// Blocks of rows (64 lanes of 16 bytes) of a token that one wavefront of heads_fwd_kernel takes: all of them, or as few as it takes to give every CU
+// eight wavefronts.
+inline int heads_blocks_per_wave(long long tokens, int blocks) {
+    const long long per = tokens * blocks / (NUM_CU * 8);
+    return (int)(per < 1 ? 1 : per > blocks ? blocks : per);
+}
+// Workgroups (four wavefronts) for so many (token, part) pairs
+inline int heads_fwd_workgroups(long long items) { return (int)(items < 4 * 4096 ? (items + 3) / 4 : 4096); }
 inline int heads_bwd_workgroups(long long tokens) { return (int)(tokens < 4 * 1024 ? (tokens + 3) / 4 : 1024); }
 
 // Attention over a paged cache: tokens that a sequence of at most max_length may see, counted from a multiple of the tile of 32
