@@ -355,6 +355,7 @@ typedef struct {
  *                     with its own length: drafted tokens, or a prompt token by token
  *   lse               [B,Hq] fp32 or NULL
  *   workspace         osdn_paged_decode_workspace_bytes(p) bytes, 256-byte aligned (may be NULL if that is 0)
+ * B Hq is below 2^21, and the pieces of all sequences of max_length below 2^24.
  * What a length hides is not looked at, whatever the cache holds there.  A length above max_length or above what a row of the
  * table holds, a sequence or a page that is not there: o and lse are NaN, and nothing outside the cache is read.
  */

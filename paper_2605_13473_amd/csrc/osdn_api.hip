@@ -493,15 +493,17 @@ int osdn_paged_append(const osdn_norm_params *p, const osdn_cache *cache, const 
 static int check_decode(const osdn_decode_params *p, int &head_tiles, int &piece, int &pieces) {
     if (!p) return OSDN_ERR_NULL;
     if (p->io_dtype != OSDN_F32 && p->io_dtype != OSDN_BF16) return OSDN_ERR_DTYPE;
-    if (p->B < 1 || p->B > 65535 || p->Hk < 1 || p->Hq < p->Hk || p->Hq % p->Hk != 0 || p->Hq > 65535) return OSDN_ERR_SHAPE;
+    if (p->B < 1 || p->B > 65535 || p->Hk < 1 || p->Hq < p->Hk || p->Hq % p->Hk != 0 || (long long)p->B * p->Hq >= 1 << 21) return OSDN_ERR_SHAPE;
     if (p->K != 64 && p->K != 128 && p->K != 256) return OSDN_ERR_SHAPE;
     if (p->max_length < 0 || p->max_length > 0x7fffff00) return OSDN_ERR_SHAPE;
     if (!std::isfinite(p->scale) || p->window < 0 || p->piece < 0 || p->piece % DECODE_PIECE != 0) return OSDN_ERR_PARAM;
     head_tiles = (p->Hq / p->Hk + 15) / 16;
     const long long span = decode_span(p->max_length, p->window);
-    piece = p->piece ? p->piece : decode_piece((long long)p->B * p->Hk * head_tiles, span);
+    const long long rows = (long long)p->B * p->Hk * head_tiles, most = ((1ll << 32) / DEC_THREADS - 1) / rows;      // (a launch has fewer than 2^32 threads)
+    piece = p->piece ? p->piece : decode_piece(p->B, rows, span, p->io_dtype == OSDN_BF16);
+    while (!p->piece && (span + piece - 1) / piece > most) piece *= 2;          // (most is 7 at least, and span below 2^31)
     const long long n = (span + piece - 1) / piece;
-    if (n * DEC_THREADS >= (1ll << 32)) return OSDN_ERR_SHAPE;
+    if (n > most) return OSDN_ERR_SHAPE;
     pieces = n < 1 ? 1 : (int)n;
     return OSDN_OK;
 }

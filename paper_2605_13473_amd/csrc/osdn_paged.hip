@@ -60,7 +60,12 @@ __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
     __shared__ __align__(16) char lds[DEC_W * (TT * LDV * sizeof(T) > 16 * LDO * 4 ? TT * LDV * sizeof(T) : 16 * LDO * 4)];
     __shared__ float ml[DEC_W][2][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
-    const int piece = blockIdx.x, kv = blockIdx.y / a.head_tiles, h0 = kv * a.group + 16 * (blockIdx.y % a.head_tiles), b = blockIdx.z;
+    // The pieces of a (sequence, group of heads) are neighbours in the launch (neighbouring heads side by side, 64 sequences of up to 8192
+    // tokens whose pages hold a token's heads together: 240 us, so 203).  Workgroups are dealt to the XCDs in turn, so the pieces are turned
+    // from one group to the next: else, with uneven lengths, the XCDs with the last pieces would have nothing to do (309 us).
+    const unsigned at = blockIdx.x / (unsigned)a.pieces, groups = a.Hk * a.head_tiles;
+    const int piece = (blockIdx.x + at + at / 4) % (unsigned)a.pieces, b = at / groups, kt = at % groups;
+    const int kv = kt / a.head_tiles, h0 = kv * a.group + 16 * (kt % a.head_tiles);
     const int heads = min(16, (kv + 1) * a.group - h0);
     const int seq = a.seq ? a.seq[b] : b;
     const int length = a.lengths[b];
@@ -71,7 +76,7 @@ __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
     const int begin = first + piece * a.piece;
     if (!bad_call && begin >= length && piece > 0) return;              // (an empty sequence has one empty piece)
     if (bad_call && piece > 0) return;
-    const int end = bad_call ? 0 : min(length, begin + a.piece);
+    const int end = bad_call ? 0 : length - begin < a.piece ? length : begin + a.piece;
 
     // queries: lane l holds head l % 16
     u32x4 q[STEPS];
@@ -237,58 +242,78 @@ __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
     }
 }
 
-// The pieces of one query head, joined in a fixed order
-constexpr int JOIN_T = 256;
-template <typename T, int K>
-__global__ __launch_bounds__(JOIN_T) void decode_join_kernel(DecodeArgs a) {
-    constexpr int COLS = K / 4, ROWS = JOIN_T / COLS, TT = DecodeTile<T, K>::TT;
-    __shared__ float red[ROWS][K];
-    __shared__ float wmax[JOIN_T / 64], wsum[JOIN_T / 64];
-    const int h = blockIdx.x, b = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const size_t bh = (size_t)b * a.Hq + h;
+// The pieces of the query heads, joined in a fixed order.  A wavefront (WG: a workgroup, its four wavefronts a quarter of the pieces each) joins JC columns
+// of one head: a lane four columns of every (64 / (JC / 4))-th piece.
+template <typename T, int K, int JC, bool WG>
+__global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
+    constexpr int QUADS = JC / 4, ROWS = 64 / QUADS, TT = DecodeTile<T, K>::TT, WAVES = WG ? 4 : 1;
+    __shared__ float red[4][JC], sums[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const unsigned item = WG ? blockIdx.x : blockIdx.x * 4 + wave;
+    const unsigned bh = item / (K / JC);
+    const int c0 = item % (K / JC) * JC + lane % QUADS * 4;
+    if (!WG && bh >= (unsigned)a.B * a.Hq) return;
+    const int b = bh / (unsigned)a.Hq, h = bh % (unsigned)a.Hq;
     const int length = a.lengths[b];
     const int lo = a.window > 0 && length > a.window ? length - a.window : 0;
     const int n = length > a.max_length ? 1 : max(1, (length - (lo & ~(TT - 1)) + a.piece - 1) / a.piece);
-    const float *ml = a.part_ml + bh * a.pieces * 2, *po = a.part_o + bh * a.pieces * K;
+    const float *ml = a.part_ml + (size_t)bh * a.pieces * 2, *po = a.part_o + (size_t)bh * a.pieces * K + c0;
     float M = -FLT_MAX;
-    for (int i = threadIdx.x; i < n; i += JOIN_T) M = fmaxf(M, ml[2 * i]);
+    for (int i = lane; i < n; i += 64) M = fmaxf(M, ml[2 * i]);
     M = max_xor32(max_xor16(M));
-    for (int x = 1; x < 16; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
-    if (lane == 0) wmax[wave] = M;
-    __syncthreads();
 #pragma unroll
-    for (int u = 0; u < JOIN_T / 64; ++u) M = fmaxf(M, wmax[u]);
+    for (int x = 1; x < 16; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
     float L = 0.f;
-    for (int i = threadIdx.x; i < n; i += JOIN_T) L = __builtin_fmaf(ml[2 * i + 1], __builtin_amdgcn_exp2f(ml[2 * i] - M), L);
-    L = wave_sum(L);
-    if (lane == 0) wsum[wave] = L;
-    const int c = threadIdx.x % COLS, r0 = threadIdx.x / COLS;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    for (int i = r0; i < n; i += ROWS) {
+#pragma unroll 4
+    for (int i = (WG ? wave * ROWS : 0) + lane / QUADS; i < n; i += ROWS * WAVES) {
         const float f = __builtin_amdgcn_exp2f(ml[2 * i] - M);
-        const f32x4 y = load4(po + (size_t)i * K + 4 * c);
+        const f32x4 y = load4(po + (size_t)i * K);
+        L = __builtin_fmaf(ml[2 * i + 1], f, L);
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] = __builtin_fmaf(y[r], f, x[r]);
     }
-    *reinterpret_cast<f32x4 *>(&red[r0][4 * c]) = x;
-    __syncthreads();
-    L = 0.f;
 #pragma unroll
-    for (int u = 0; u < JOIN_T / 64; ++u) L += wsum[u];
-    const float inv = L == 0.f ? 0.f : 1.f / L;
-    for (int d = threadIdx.x; d < K; d += JOIN_T) {
-        float y = 0.f;
+    for (int s = QUADS; s < 64; s <<= 1) {
+        L += __shfl_xor(L, s, 64);
 #pragma unroll
-        for (int u = 0; u < ROWS; ++u) y += red[u][d];
-        static_cast<T *>(a.o.data)[b * a.o.batch + h * a.o.head + d] = from_f32<T>(y * inv);
+        for (int r = 0; r < 4; ++r) x[r] += __shfl_xor(x[r], s, 64);
     }
-    if (a.lse && threadIdx.x == 0) a.lse[bh] = L == 0.f ? -INFINITY : __builtin_fmaf(M, LN2, logf(L));
+    if constexpr (WG) {
+        if (lane < QUADS) *reinterpret_cast<f32x4 *>(&red[wave][4 * lane]) = x;
+        if (lane == 0) sums[wave] = L;
+        __syncthreads();
+        if (wave != 0) return;
+        L = sums[0] + sums[1] + sums[2] + sums[3];
+        x = load4(&red[0][lane % QUADS * 4]);
+#pragma unroll
+        for (int u = 1; u < 4; ++u) {
+            const f32x4 y = load4(&red[u][lane % QUADS * 4]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] += y[r];
+        }
+    }
+    if (lane >= QUADS) return;
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    T *dst = static_cast<T *>(a.o.data) + b * a.o.batch + h * a.o.head + c0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] *= inv;
+    if (a.aligned) {
+        store4(dst, x);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) dst[r] = from_f32<T>(x[r]);
+    }
+    if (a.lse && c0 == 0) a.lse[bh] = L == 0.f ? -INFINITY : __builtin_fmaf(M, LN2, logf(L));
 }
 
 namespace {
 template <typename T, int K> void decode_of(const DecodeArgs &a, hipStream_t st) {
-    hipLaunchKernelGGL((decode_kernel<T, K>), dim3(a.pieces, a.Hk * a.head_tiles, a.B), dim3(DEC_T), 0, st, a);
-    if (a.pieces > 1) hipLaunchKernelGGL((decode_join_kernel<T, K>), dim3(a.Hq, a.B), dim3(JOIN_T), 0, st, a);
+    hipLaunchKernelGGL((decode_kernel<T, K>), dim3((unsigned)a.pieces * a.Hk * a.head_tiles * a.B), dim3(DEC_T), 0, st, a);
+    if (a.pieces == 1) return;
+    const unsigned heads = (unsigned)a.B * a.Hq;
+    if (a.pieces > 16) hipLaunchKernelGGL((decode_join_kernel<T, K, 32, true>), dim3(heads * (K / 32)), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((decode_join_kernel<T, K, 64, false>), dim3((heads * (K / 64) + 3) / 4), dim3(256), 0, st, a);
 }
 }  // namespace
 

@@ -247,11 +247,15 @@ inline long long decode_span(int max_length, int window) {
     const long long seen = window > 0 && window < max_length ? (long long)window + DECODE_TILE - 1 : max_length;
     return seen < max_length ? seen : max_length;
 }
-// ... and the tokens of a piece, for `rows` (sequence, group of query heads) pairs
-inline int decode_piece(long long rows, long long span) {
-    const long long want = rows * span / (NUM_CU * 8);
-    const long long piece = (want + DECODE_PIECE - 1) / DECODE_PIECE * DECODE_PIECE;
-    return (int)(piece < DECODE_PIECE ? DECODE_PIECE : piece > 2048 ? 2048 : piece);
+// ... and the tokens of a piece, for B sequences and `rows` (sequence, group of query heads) pairs: two workgroups a CU (fp32, whose products
+// take more of the time: four), not above 512 tokens where the lengths may differ, which only small pieces even out.  us, pieces of
+// 128, 256, 512, 1024 and 2048 tokens, K = 128 in bf16 unless said: 1 x 131072 x 8 heads 127, 117, 107, 103, 99; 4 x 32768 x 1 21.7, 19.6, 19.8, 26.9, 45.3;
+// 32 x 1000 x 4 20.2, 18.5, 19.3, 23.6; fp32 K = 64, 8 x 4096 x 8 32.5, 31.6, 37.4, 52.9; uneven lengths, 64 x 8192 x 8 237, 220,
+// 208, 219, 257, 512 x 4096 x 4 511, 438, 408, 421, 460; even ones, 16 x 4096 x 16 104, 101, 100, 99, 98.
+inline int decode_piece(int B, long long rows, long long span, bool bf16) {
+    const long long want = rows * span / (NUM_CU * (bf16 ? 2 : 4));
+    const long long piece = (want + DECODE_PIECE - 1) / DECODE_PIECE * DECODE_PIECE, most = B > 1 ? 512 : 2048;
+    return (int)(piece < DECODE_PIECE ? DECODE_PIECE : piece > most ? most : piece);
 }
 
 }  // namespace osdn

@@ -112,7 +112,8 @@ def test_append_needs_keys_values_and_positions():
 
 
 BAD_DECODE = [
-    (dict(io_dtype=7), DTYPE), (dict(B=0), SHAPE), (dict(B=65536), SHAPE), (dict(Hk=0), SHAPE), (dict(Hq=2), SHAPE), (dict(Hq=10), SHAPE), (dict(K=96), SHAPE), (dict(max_length=-1), SHAPE),
+    (dict(io_dtype=7), DTYPE), (dict(B=0), SHAPE), (dict(B=65536), SHAPE), (dict(Hk=0), SHAPE), (dict(Hq=2), SHAPE), (dict(Hq=10), SHAPE), (dict(K=96), SHAPE), (dict(max_length=-1), SHAPE), (dict(B=65535, Hq=64), SHAPE),
+    (dict(max_length=2 ** 31 - 1), SHAPE), (dict(B=100, max_length=2 ** 30, piece=128), SHAPE),
     (dict(window=-1), PARAM), (dict(piece=64), PARAM), (dict(piece=-128), PARAM), (dict(scale=float("nan")), PARAM), (dict(scale=float("inf")), PARAM),
 ]
 
