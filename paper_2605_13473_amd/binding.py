@@ -23,6 +23,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libosdn.so")
 _lib = None
 _step_native = None        # _native.step, once the library is loaded (None: no module that fits it)
+_rows_native = None        # _native, for the operators around the recurrence
 
 OSDN_F32, OSDN_BF16 = 0, 1
 
@@ -70,7 +71,7 @@ class OsdnError(RuntimeError):
 
 def lib():
     """Load libosdn.so (built in-tree by ``build.py``); raises if it is not there."""
-    global _lib, _step_native
+    global _lib, _step_native, _rows_native
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise FileNotFoundError(
@@ -128,8 +129,11 @@ def lib():
         try:
             from . import _native
             _native.bind(ctypes.cast(L.osdn_step, vp).value, ctypes.sizeof(OsdnParams), torch.__version__)
-            _step_native = _native.step
-        except (ImportError, TypeError) as e:       # (TypeError: one of an earlier interface)
+            _native.bind_rows(*(ctypes.cast(f, vp).value for f in (
+                L.osdn_qk_norm_fwd, L.osdn_qk_norm_bwd, L.osdn_qk_norm_bwd_workspace_bytes, L.osdn_paged_append, L.osdn_paged_decode,
+                L.osdn_paged_decode_workspace_bytes)), *(ctypes.sizeof(c) for c in (OsdnRows, OsdnNormParams, OsdnCache, OsdnDecodeParams)))
+            _step_native, _rows_native = _native.step, _native
+        except (ImportError, TypeError, AttributeError) as e:       # (TypeError, AttributeError: one of an earlier interface)
             warnings.warn(f"no extension module ({e}): step goes through Python, at twice the time of a small call; "
                           "run python -m paper_2605_13473_amd.build", RuntimeWarning, stacklevel=2)
     return _lib
@@ -606,8 +610,24 @@ def _params_of(q, k, hp, rotary):
     return make_norm_params(B, T, 0 if q is None else q.shape[2], 0 if k is None else k.shape[2], K, x.dtype == torch.bfloat16, hp, rotary)
 
 
+def _native_call(name, like, *args):
+    """The call through the extension module: its results, or None for what it leaves to the code below."""
+    if _lib is None:
+        lib()
+    if _rows_native is None or not isinstance(like, torch.Tensor) or not like.is_cuda:
+        return None
+    dev = torch._C._cuda_getDevice()
+    r = getattr(_rows_native, name)(*args, dev, torch._C._cuda_getCurrentRawStream(dev))
+    if type(r) is int:
+        _check(r)
+    return r
+
+
 def qk_norm(q, k, weight_q=None, weight_k=None, rotary=None, positions=None, hp: NormHyper = NormHyper()):
     """Allocate outputs and call osdn_qk_norm_fwd (either of q and k may be None).  Returns (q_out, k_out)."""
+    r = _native_call("qk_norm", k if q is None else q, q, k, weight_q, weight_k, rotary, positions, hp)
+    if r is not None:
+        return r
     p = _params_of(q, k, hp, rotary)
     out = [None if x is None else x.new_empty(x.shape) for x in (q, k)]
     osdn_qk_norm_fwd(p, q, k, weight_q, weight_k, rotary, positions, *out)
@@ -617,6 +637,9 @@ def qk_norm(q, k, weight_q=None, weight_k=None, rotary=None, positions=None, hp:
 def qk_norm_backward(q, k, dq_out, dk_out, weight_q=None, weight_k=None, rotary=None, positions=None, hp: NormHyper = NormHyper()):
     """Allocate gradients and call osdn_qk_norm_bwd on the inputs of ``qk_norm``.  Returns a dict of dq, dk and, where there are
     weights, dweight_q, dweight_k."""
+    r = _native_call("qk_norm_backward", k if q is None else q, q, k, dq_out, dk_out, weight_q, weight_k, rotary, positions, hp)
+    if r is not None:
+        return dict(zip(("dq", "dk", "dweight_q", "dweight_k"), r))
     p = _params_of(q, k, hp, rotary)
     g = {"dq": None if q is None else q.new_empty(q.shape), "dk": None if k is None else k.new_empty(k.shape),
          "dweight_q": None if weight_q is None else torch.empty_like(weight_q), "dweight_k": None if weight_k is None else torch.empty_like(weight_k)}
@@ -631,6 +654,9 @@ def paged_append(k, v, k_cache, v_cache, page_table, positions, seq=None, q=None
                  hp: NormHyper = NormHyper()):
     """Append keys (normed and rotated) and values [B,T,Hk,K] to a paged cache [n_pages, page_size, Hk, K]; with q [B,T,Hq,K],
     returns the queries normed and rotated alike, from the same launch."""
+    r = _native_call("paged_append", k, k, v, k_cache, v_cache, page_table, positions, seq, q, weight_q, weight_k, rotary, hp)
+    if r is not None:
+        return r[0]
     p = _params_of(q, k, hp, rotary)
     q_out = None if q is None else q.new_empty(q.shape)
     osdn_paged_append(p, q, k, v, k_cache, v_cache, page_table, weight_q, weight_k, rotary, positions, seq, q_out)
@@ -641,6 +667,9 @@ def paged_decode(q, k_cache, v_cache, page_table, lengths, seq=None, scale=None,
                  workspace=None):
     """Attention of one new token per sequence, q [B,Hq,K], over a paged cache.  max_length: no length is above it (None: what a
     row of the table can hold).  Returns o, or (o, lse)."""
+    r = _native_call("paged_decode", q, q, k_cache, v_cache, page_table, lengths, seq, workspace, scale, window, max_length, want_lse)
+    if r is not None:
+        return r if want_lse else r[0]
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
         raise TypeError("expected q [B,Hq,K] and a cache [n_pages, page_size, Hk, K] as CUDA/HIP torch tensors")
     B, Hq, K = q.shape
