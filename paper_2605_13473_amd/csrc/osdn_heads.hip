@@ -349,18 +349,19 @@ __global__ __launch_bounds__(HEADS_T) void heads_bwd_kernel(HeadsArgs a) {
 // dw = sum of the n rows of partial [n][2][K]: 16 columns a workgroup, its 64 groups of 16 lanes add up every 64th row
 constexpr int DW_COLS = 16, DW_T = 1024, DW_ROWS = DW_T / DW_COLS;
 __global__ __launch_bounds__(DW_T) void heads_dw_kernel(const float *partial, int n, int K, float *dwq, float *dwk) {
-    __shared__ float s[DW_ROWS][DW_COLS + 1];
-    const int col = threadIdx.x % DW_COLS, row = threadIdx.x / DW_COLS, c = blockIdx.x * DW_COLS + col;
+    __shared__ float s[DW_T / 64][DW_COLS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane % DW_COLS, c = blockIdx.x * DW_COLS + col;
     float v = 0.f;
-    for (int i = row; i < n; i += DW_ROWS) v += partial[(size_t)i * 2 * K + c];
-    s[row][col] = v;
+#pragma unroll 8
+    for (int i = threadIdx.x / DW_COLS; i < n; i += DW_ROWS) v += partial[(size_t)i * 2 * K + c];
+    v = add_xor32(add_xor16(v));
+    if (lane < DW_COLS) s[wave][col] = v;
     __syncthreads();
-    if (row == 0) {
-        v = 0.f;
-        for (int i = 0; i < DW_ROWS; ++i) v += s[i][col];
-        float *dst = c < K ? dwq : dwk;
-        if (dst) dst[c < K ? c : c - K] = v;
-    }
+    if (wave != 0) return;
+    v = (s[lane / DW_COLS][col] + s[lane / DW_COLS + 4][col]) + (s[lane / DW_COLS + 8][col] + s[lane / DW_COLS + 12][col]);
+    v = add_xor32(add_xor16(v));
+    float *dst = c < K ? dwq : dwk;
+    if (lane < DW_COLS && dst) dst[c < K ? c : c - K] = v;
 }
 
 namespace {

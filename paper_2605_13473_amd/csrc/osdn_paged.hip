@@ -42,14 +42,32 @@ template <typename T, int K> struct DecodeTile {
     static constexpr int OUT = K / 16;                  // 16-row tiles of the transposed result
 };
 
-// The rows of a tile that a lane loads: token 16 i + l % 16 of the tile, i < SETS
-template <typename T, int K> struct TileRows {
+// The rows of a tile that a lane loads, token 16 i + l % 16 of the tile, on their way: first their pages, then the rows
+template <typename T, int K> struct TileLoads {
     using D = DecodeTile<T, K>;
     int page[D::SETS];
-    // tok: first token of the tile; rows outside [lo, hi) repeat a row inside
-    __device__ __forceinline__ void ask(const DecodeArgs &a, const int *row, int tok, int lo, int hi, int lane) {
+    u32x4 k[D::SETS][D::STEPS], v[D::SETS][D::STEPS];
+    // pages of the tile at token tok, as far as the table goes (whatever the length: it need not be known yet)
+    __device__ __forceinline__ void ask(const DecodeArgs &a, const int *row, int tok, int lane) {
 #pragma unroll
-        for (int i = 0; i < D::SETS; ++i) page[i] = row[max(lo, min(hi - 1, tok + 16 * i + (lane & 15))) >> a.page_shift];
+        for (int i = 0; i < D::SETS; ++i) page[i] = row[min((tok + 16 * i + (lane & 15)) >> a.page_shift, a.max_pages - 1)];
+    }
+    // the rows (of a token outside [lo, hi): whatever stands there); true: a token inside has no page
+    __device__ __forceinline__ bool load(const DecodeArgs &a, const T *kc, const T *vc, int tok, int lo, int hi, int lane) {
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < D::SETS; ++i) {
+            const int j = tok + 16 * i + (lane & 15), slot = j & ((1 << a.page_shift) - 1);
+            const bool ok = (unsigned)page[i] < (unsigned)a.n_pages;
+            bad = bad || (!ok && j >= lo && j < hi);
+            const long long g = ok ? page[i] : 0;
+            const T *kp = kc + g * a.cache_k.batch + slot * a.cache_k.token, *vp = vc + g * a.cache_v.batch + slot * a.cache_v.token;
+#pragma unroll
+            for (int s = 0; s < D::STEPS; ++s) k[i][s] = *reinterpret_cast<const u32x4 *>(kp + 4 * D::VE * s);
+#pragma unroll
+            for (int s = 0; s < D::STEPS; ++s) v[i][s] = *reinterpret_cast<const u32x4 *>(vp + 4 * D::VE * s);
+        }
+        return bad;
     }
 };
 
@@ -58,7 +76,7 @@ __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
     using D = DecodeTile<T, K>;
     constexpr int TT = D::TT, VE = D::VE, STEPS = D::STEPS, LDV = D::LDV, OUT = D::OUT, LDO = K + 4;
     __shared__ __align__(16) char lds[DEC_W * (TT * LDV * sizeof(T) > 16 * LDO * 4 ? TT * LDV * sizeof(T) : 16 * LDO * 4)];
-    __shared__ float ml[DEC_W][2][16];
+    __shared__ float ml[DEC_W][2][16], all[2][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     // The pieces of a (sequence, group of heads) are neighbours in the launch (neighbouring heads side by side, 64 sequences of up to 8192
     // tokens whose pages hold a token's heads together: 240 us, so 203).  Workgroups are dealt to the XCDs in turn, so the pieces are turned
@@ -68,16 +86,15 @@ __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
     const int kv = kt / a.head_tiles, h0 = kv * a.group + 16 * (kt % a.head_tiles);
     const int heads = min(16, (kv + 1) * a.group - h0);
     const int seq = a.seq ? a.seq[b] : b;
+    const bool no_seq = (unsigned)seq >= (unsigned)a.n_seqs;
+    const int *row = a.table + (no_seq ? 0 : seq * a.table_stride);
     const int length = a.lengths[b];
-    // what the caller promised and did not keep makes the result NaN: nothing outside the cache is read
-    const bool bad_call = (unsigned)seq >= (unsigned)a.n_seqs || length > a.max_length || (length > 0 && (length - 1) >> a.page_shift >= a.max_pages);
-    const int lo = a.window > 0 && length > a.window ? length - a.window : 0;
-    const int first = lo & ~(TT - 1);                                   // pieces are cut from a multiple of the tile
-    const int begin = first + piece * a.piece;
-    if (!bad_call && begin >= length && piece > 0) return;              // (an empty sequence has one empty piece)
-    if (bad_call && piece > 0) return;
-    const int end = bad_call ? 0 : length - begin < a.piece ? length : begin + a.piece;
-
+    int lo = 0;
+    if (a.window > 0 && length > a.window) lo = length - a.window;
+    const int begin = (lo & ~(TT - 1)) + piece * a.piece;               // (pieces are cut from a multiple of the tile)
+    constexpr int STRIDE = DEC_W * TT;
+    TileLoads<T, K> x;
+    x.ask(a, row, begin + wave * TT, lane);
     // queries: lane l holds head l % 16
     u32x4 q[STEPS];
 #pragma unroll
@@ -95,12 +112,15 @@ __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
             }
         }
     }
-    const int *row = a.table + (bad_call ? 0 : seq * a.table_stride);
+    // what the caller promised and did not keep makes the result NaN: nothing outside the cache is read
+    const bool bad_call = no_seq || length > a.max_length || (length > 0 && (length - 1) >> a.page_shift >= a.max_pages);
+    if (piece > 0 && (bad_call || begin >= length)) return;             // (an empty sequence has one empty piece)
+    const int end = bad_call ? 0 : length - begin < a.piece ? length : begin + a.piece;
+
     const T *kc = static_cast<const T *>(a.cache_k.data) + kv * a.cache_k.head + g * VE;
     const T *vc = static_cast<const T *>(a.cache_v.data) + kv * a.cache_v.head + g * VE;
     T *vs = reinterpret_cast<T *>(lds) + wave * TT * LDV;
     const float scale2 = a.scale * LOG2E;
-    const int slots = (1 << a.page_shift) - 1;
 
     float m = -FLT_MAX, l = 0.f;        // finite: a score of minus infinity then weighs nothing, also where there is no other
     f32x4 o[OUT];
@@ -108,49 +128,68 @@ __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
     for (int t = 0; t < OUT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     bool bad_page = false;
 
-    for (int tok = begin + wave * TT; tok < end; tok += DEC_W * TT) {
-        TileRows<T, K> rows;
-        rows.ask(a, row, tok, lo, end, lane);
-        u32x4 kr[D::SETS][STEPS], vr[D::SETS][STEPS];
-#pragma unroll
-        for (int i = 0; i < D::SETS; ++i) {
-            const int slot = max(lo, min(end - 1, tok + 16 * i + col)) & slots;
-            const bool ok = (unsigned)rows.page[i] < (unsigned)a.n_pages;
-            bad_page = bad_page || !ok;
-            const long long page = ok ? rows.page[i] : 0;
-            const T *kp = kc + page * a.cache_k.batch + slot * a.cache_k.token, *vp = vc + page * a.cache_v.batch + slot * a.cache_v.token;
-#pragma unroll
-            for (int s = 0; s < STEPS; ++s) kr[i][s] = *reinterpret_cast<const u32x4 *>(kp + 4 * VE * s);
-#pragma unroll
-            for (int s = 0; s < STEPS; ++s) vr[i][s] = *reinterpret_cast<const u32x4 *>(vp + 4 * VE * s);
-        }
+    // The rows of the next tile are asked for when this one's are in the matrix products' registers and in LDS, its pages a tile earlier
+    int tok = begin + wave * TT;
+    if (tok < end) {
+        bad_page = x.load(a, kc, vc, tok, lo, end, lane);
+        x.ask(a, row, tok + STRIDE, lane);
+    }
+    while (tok < end) {
         // scores, transposed: p[i][r] is token 16 i + 4 g + r of head `col`
         f32x4 p[D::SETS];
         float top = m;
+        const bool whole = tok >= lo && tok + TT <= end;
 #pragma unroll
         for (int i = 0; i < D::SETS; ++i) {
             p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
                 if constexpr (D::BF) {
-                    p[i] = Mfma<bf16>::mma(__builtin_bit_cast(bf16x8, kr[i][s]), __builtin_bit_cast(bf16x8, q[s]), p[i]);
+                    p[i] = Mfma<bf16>::mma(__builtin_bit_cast(bf16x8, x.k[i][s]), __builtin_bit_cast(bf16x8, q[s]), p[i]);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) p[i] = Mfma<float>::mma(vec_get<float>(kr[i][s], e), vec_get<float>(q[s], e), p[i]);
+                    for (int e = 0; e < 4; ++e) p[i] = Mfma<float>::mma(vec_get<float>(x.k[i][s], e), vec_get<float>(q[s], e), p[i]);
                 }
             }
+        }
+        if (!whole) {               // what is not seen has no weight, and must not be infinite or NaN either
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int j = tok + 16 * i + 4 * g + r;
-                p[i][r] = j >= lo && j < end ? p[i][r] * scale2 : -INFINITY;
-                top = fmaxf(top, p[i][r]);
+            for (int i = 0; i < D::SETS; ++i) {
+                const int j = tok + 16 * i + col;
+                const bool seen = j >= lo && j < end;
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) x.v[i][s][w] = seen ? x.v[i][s][w] : 0u;
             }
         }
-        top = max_xor32(max_xor16(top));
 #pragma unroll
         for (int i = 0; i < D::SETS; ++i)
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) *reinterpret_cast<u32x4 *>(vs + (16 * i + col) * LDV + (4 * s + g) * VE) = vr[i][s];
+            for (int s = 0; s < STEPS; ++s) *reinterpret_cast<u32x4 *>(vs + (16 * i + col) * LDV + (4 * s + g) * VE) = x.v[i][s];
+        const int next = tok + STRIDE;
+        if (next < end) {
+            bad_page = x.load(a, kc, vc, next, lo, end, lane) || bad_page;
+            x.ask(a, row, next + STRIDE, lane);
+        }
+#pragma unroll
+        for (int i = 0; i < D::SETS; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) p[i][r] *= scale2;
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < D::SETS; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int j = tok + 16 * i + 4 * g + r;
+                    p[i][r] = j >= lo && j < end ? p[i][r] : -INFINITY;
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < D::SETS; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, p[i][r]);
+        top = max_xor32(max_xor16(top));
         if (__any(top > m)) {
             const float f = __builtin_amdgcn_exp2f(m - top);
             l *= f;
@@ -187,6 +226,7 @@ __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) o[t] = Mfma<float>::mma(to_f32(vs[(4 * g + r) * LDV + 16 * t + col]), p[0][r], o[t]);
         }
+        tok = next;
     }
     // the four wavefronts join
     l = add_xor32(add_xor16(l));
@@ -207,9 +247,9 @@ __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
         for (int r = 0; r < 4; ++r) x[r] *= f;
         *reinterpret_cast<f32x4 *>(os + col * LDO + 16 * t + 4 * g) = x;
     }
-    if (wave == 0 && g == 0) { ml[0][0][col] = M; ml[0][1][col] = L; }
+    if (wave == 0 && g == 0) { all[0][col] = M; all[1][col] = L; }
     __syncthreads();
-    const bool whole = a.pieces == 1;
+    const bool alone = a.pieces == 1;
     for (int i = threadIdx.x; i < heads * (K / 4); i += DEC_T) {
         const int h = i / (K / 4), d = i % (K / 4) * 4;
         f32x4 x = load4(reinterpret_cast<const float *>(lds) + h * LDO + d);
@@ -220,8 +260,8 @@ __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
             for (int r = 0; r < 4; ++r) x[r] += y[r];
         }
         const size_t bh = (size_t)b * a.Hq + h0 + h;
-        if (whole) {
-            const float sum = ml[0][1][h], inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (alone) {
+            const float sum = all[1][h], inv = sum == 0.f ? 0.f : 1.f / sum;
             T *dst = static_cast<T *>(a.o.data) + b * a.o.batch + (h0 + h) * a.o.head + d;
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[r] *= inv;
@@ -231,12 +271,12 @@ __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) dst[r] = from_f32<T>(x[r]);
             }
-            if (a.lse && d == 0) a.lse[bh] = sum == 0.f ? -INFINITY : __builtin_fmaf(ml[0][0][h], LN2, logf(sum));
+            if (a.lse && d == 0) a.lse[bh] = sum == 0.f ? -INFINITY : __builtin_fmaf(all[0][h], LN2, logf(sum));
         } else {
             store4(a.part_o + (bh * a.pieces + piece) * K + d, x);
             if (d == 0) {
-                a.part_ml[(bh * a.pieces + piece) * 2] = ml[0][0][h];
-                a.part_ml[(bh * a.pieces + piece) * 2 + 1] = ml[0][1][h];
+                a.part_ml[(bh * a.pieces + piece) * 2] = all[0][h];
+                a.part_ml[(bh * a.pieces + piece) * 2 + 1] = all[1][h];
             }
         }
     }
@@ -258,6 +298,12 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
     const int lo = a.window > 0 && length > a.window ? length - a.window : 0;
     const int n = length > a.max_length ? 1 : max(1, (length - (lo & ~(TT - 1)) + a.piece - 1) / a.piece);
     const float *ml = a.part_ml + (size_t)bh * a.pieces * 2, *po = a.part_o + (size_t)bh * a.pieces * K + c0;
+    // the first four of a lane's pieces are on their way before the maximum is known
+    constexpr int STEP = ROWS * WAVES, AHEAD = 4;
+    const int first = (WG ? wave * ROWS : 0) + lane / QUADS;
+    f32x4 ahead[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) ahead[u] = load4(po + (size_t)min(first + u * STEP, n - 1) * K);
     float M = -FLT_MAX;
     for (int i = lane; i < n; i += 64) M = fmaxf(M, ml[2 * i]);
     M = max_xor32(max_xor16(M));
@@ -265,14 +311,17 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
     for (int x = 1; x < 16; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
     float L = 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int i = (WG ? wave * ROWS : 0) + lane / QUADS; i < n; i += ROWS * WAVES) {
+    auto add = [&](int i, const f32x4 &y) {
         const float f = __builtin_amdgcn_exp2f(ml[2 * i] - M);
-        const f32x4 y = load4(po + (size_t)i * K);
         L = __builtin_fmaf(ml[2 * i + 1], f, L);
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] = __builtin_fmaf(y[r], f, x[r]);
-    }
+    };
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+        if (first + u * STEP < n) add(first + u * STEP, ahead[u]);
+#pragma unroll 4
+    for (int i = first + AHEAD * STEP; i < n; i += STEP) add(i, load4(po + (size_t)i * K));
 #pragma unroll
     for (int s = QUADS; s < 64; s <<= 1) {
         L += __shfl_xor(L, s, 64);
