@@ -154,7 +154,7 @@ template <typename T, bool VEC> __device__ __forceinline__ T *row_at(const HeadR
 template <typename T, int K, bool VEC, int ROT, bool APPEND>
 __global__ __launch_bounds__(HEADS_T) void heads_fwd_kernel(HeadsArgs a) {
     using HR = HeadRow<T, K>;
-    constexpr int VE = HR::VE, ROWS = HR::ROWS, NB = 4;
+    constexpr int VE = HR::VE, ROWS = HR::ROWS, NB = 2;
     const int lane = threadIdx.x & 63, sub = lane / HR::LANES, e0 = (lane % HR::LANES) * VE;
     const Turn<T, K, ROT> turn(a.rotary_dim, lane);
     Weights<T, K, ROT> w;
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(HEADS_T) void heads_fwd_kernel(HeadsArgs a) {
 template <typename T, int K, bool VEC, int ROT>
 __global__ __launch_bounds__(HEADS_T) void heads_bwd_kernel(HeadsArgs a) {
     using HR = HeadRow<T, K>;
-    constexpr int VE = HR::VE, ROWS = HR::ROWS, WAVES = HEADS_T / 64, NB = 2;
+    constexpr int VE = HR::VE, ROWS = HR::ROWS, WAVES = HEADS_T / 64, NB = 4;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / HR::LANES, e0 = (lane % HR::LANES) * VE;
     const Turn<T, K, ROT> turn(a.rotary_dim, lane);
     float w[2][VE], dw[2][VE];
@@ -266,61 +266,63 @@ __global__ __launch_bounds__(HEADS_T) void heads_bwd_kernel(HeadsArgs a) {
         const bool off_table = ROT && pos >= a.rotary_rows;
         float c[VE], s[VE];
         if constexpr (ROT != ROT_NONE) turn.load(a.rotary + (size_t)(none || off_table ? 0 : pos) * a.rotary_dim, a.rotary_dim, c, s);
+        for (int blk0 = 0; blk0 < a.blocks; blk0 += NB) {
+            u32x4 rx[NB], rz[NB];
 #pragma unroll
-        for (int kind = 0; kind < 2; ++kind) {
-            const HeadRows &xs = kind == 0 ? a.q : a.k, &zs = kind == 0 ? a.dq_out : a.dk_out, &ds = kind == 0 ? a.dq : a.dk;
-            const int H = kind == 0 ? a.Hq : a.Hk;
-            for (int h0 = 0; h0 < H; h0 += NB * ROWS) {
-                u32x4 rx[NB], rz[NB];
-#pragma unroll
-                for (int i = 0; i < NB; ++i) {
-                    const int h = h0 + i * ROWS + sub;
-                    rx[i] = rz[i] = u32x4{0u, 0u, 0u, 0u};
-                    if (h < H) {
-                        rx[i] = load_row<T, VEC>(row_at<const T, VEC>(xs, b, t, h) + e0);
-                        rz[i] = load_row<T, VEC>(row_at<const T, VEC>(zs, b, t, h) + e0);
-                    }
+            for (int i = 0; i < NB; ++i) {
+                const int blk = blk0 + i;
+                const bool query = blk < a.q_blocks;
+                const int h = (query ? blk : blk - a.q_blocks) * ROWS + sub;
+                rx[i] = rz[i] = u32x4{0u, 0u, 0u, 0u};
+                if (h < (query ? a.Hq : a.Hk)) {
+                    rx[i] = load_row<T, VEC>(row_at<const T, VEC>(query ? a.q : a.k, b, t, h) + e0);
+                    rz[i] = load_row<T, VEC>(row_at<const T, VEC>(query ? a.dq_out : a.dk_out, b, t, h) + e0);
                 }
+            }
 #pragma unroll
-                for (int i = 0; i < NB; ++i) {
-                    const int h = h0 + i * ROWS + sub;
-                    if (h0 + i * ROWS >= H) break;
-                    float x[VE], dy[VE], g[VE];
-                    unpack<T>(rx[i], x);
-                    unpack<T>(rz[i], dy);
-                    if constexpr (ROT != ROT_NONE) {
-                        float y[VE];
-                        turn.partners(rz[i], y);
+            for (int i = 0; i < NB; ++i) {
+                const int blk = blk0 + i;
+                const bool query = blk < a.q_blocks;
+                const int h = (query ? blk : blk - a.q_blocks) * ROWS + sub;
+                if (blk >= a.blocks) break;
+                const bool live = h < (query ? a.Hq : a.Hk);
+                float x[VE], dy[VE], g[VE];
+                unpack<T>(rx[i], x);
+                unpack<T>(rz[i], dy);
+                if constexpr (ROT != ROT_NONE) {
+                    float y[VE];
+                    turn.partners(rz[i], y);
 #pragma unroll
-                        for (int e = 0; e < VE; ++e) dy[e] = __builtin_fmaf(dy[e], c[e], -(y[e] * s[e]));
-                    }
-                    float r = 1.f, ss = 0.f, gx = 0.f;
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) {
-                        g[e] = dy[e] * w[kind][e];
-                        ss = __builtin_fmaf(x[e], x[e], ss);
-                        gx = __builtin_fmaf(g[e], x[e], gx);
-                    }
-                    if (a.norm != 0) {
-                        r = rsqrtf(__builtin_fmaf(row_sum<HR::LANES>(ss), a.mean, a.eps));
-                        gx = row_sum<HR::LANES>(gx) * (r * r * a.mean);
-                    } else {
-                        gx = 0.f;
-                    }
-                    if (off_table) r = __builtin_nanf("");
-                    if (none || h >= H) {
-#pragma unroll
-                        for (int e = 0; e < VE; ++e) g[e] = x[e] = dy[e] = 0.f;
-                        gx = r = 0.f;
-                    }
-                    float dx[VE];
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) {
-                        dx[e] = r * __builtin_fmaf(-gx, x[e], g[e]);
-                        dw[kind][e] = __builtin_fmaf(dy[e] * r, x[e], dw[kind][e]);
-                    }
-                    if (h < H) store_row<T, VEC, VE>(row_at<T, VEC>(ds, b, t, h) + e0, dx);
+                    for (int e = 0; e < VE; ++e) dy[e] = __builtin_fmaf(dy[e], c[e], -(y[e] * s[e]));
                 }
+                float r = 1.f, ss = 0.f, gx = 0.f;
+#pragma unroll
+                for (int e = 0; e < VE; ++e) {
+                    g[e] = dy[e] * (query ? w[0][e] : w[1][e]);
+                    ss = __builtin_fmaf(x[e], x[e], ss);
+                    gx = __builtin_fmaf(g[e], x[e], gx);
+                }
+                if (a.norm != 0) {
+                    r = rsqrtf(__builtin_fmaf(row_sum<HR::LANES>(ss), a.mean, a.eps));
+                    gx = row_sum<HR::LANES>(gx) * (r * r * a.mean);
+                } else {
+                    gx = 0.f;
+                }
+                if (off_table) r = __builtin_nanf("");
+                if (none || !live) {
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) g[e] = x[e] = dy[e] = 0.f;
+                    gx = r = 0.f;
+                }
+                float dx[VE];
+#pragma unroll
+                for (int e = 0; e < VE; ++e) {
+                    dx[e] = r * __builtin_fmaf(-gx, x[e], g[e]);
+                    const float term = dy[e] * r;
+                    if (query) dw[0][e] = __builtin_fmaf(term, x[e], dw[0][e]);
+                    else dw[1][e] = __builtin_fmaf(term, x[e], dw[1][e]);
+                }
+                if (live) store_row<T, VEC, VE>(row_at<T, VEC>(query ? a.dq : a.dk, b, t, h) + e0, dx);
             }
         }
     }
@@ -365,18 +367,22 @@ __global__ __launch_bounds__(DW_T) void heads_dw_kernel(const float *partial, in
 }
 
 namespace {
-template <typename T, int K, bool VEC, int ROT> void fwd_of(HeadsArgs a, hipStream_t st) {
+template <typename T, int K> void count_blocks(HeadsArgs &a) {
     constexpr int ROWS = HeadRow<T, K>::ROWS;
     a.q_blocks = (a.Hq + ROWS - 1) / ROWS;
     a.k_blocks = (a.Hk + ROWS - 1) / ROWS;
     a.blocks = a.q_blocks + a.k_blocks * (a.append ? 2 : 1);
+}
+template <typename T, int K, bool VEC, int ROT> void fwd_of(HeadsArgs a, hipStream_t st) {
+    count_blocks<T, K>(a);
     a.per_part = heads_blocks_per_wave(a.tokens, a.blocks);
     a.parts = (a.blocks + a.per_part - 1) / a.per_part;
     const dim3 g((unsigned)heads_fwd_workgroups((long long)a.tokens * a.parts)), t(HEADS_T);
     if (a.append) hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, true>), g, t, 0, st, a);
     else hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, false>), g, t, 0, st, a);
 }
-template <typename T, int K, bool VEC, int ROT> void bwd_of(const HeadsArgs &a, hipStream_t st) {
+template <typename T, int K, bool VEC, int ROT> void bwd_of(HeadsArgs a, hipStream_t st) {
+    count_blocks<T, K>(a);
     const int n = heads_bwd_workgroups(a.tokens);
     hipLaunchKernelGGL((heads_bwd_kernel<T, K, VEC, ROT>), dim3((unsigned)n), dim3(HEADS_T), 0, st, a);
     if (a.partial)

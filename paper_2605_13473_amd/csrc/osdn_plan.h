@@ -238,7 +238,7 @@ inline int heads_blocks_per_wave(long long tokens, int blocks) {
     return (int)(per < 1 ? 1 : per > blocks ? blocks : per);
 }
 // Workgroups (four wavefronts) for so many (token, part) pairs
-inline int heads_fwd_workgroups(long long items) { return (int)(items < 4 * 4096 ? (items + 3) / 4 : 4096); }
+inline int heads_fwd_workgroups(long long items) { return (int)(items < 4 * 16384 ? (items + 3) / 4 : 16384); }
 inline int heads_bwd_workgroups(long long tokens) { return (int)(tokens < 4 * 1024 ? (tokens + 3) / 4 : 1024); }
 
 // Attention over a paged cache: tokens that a sequence of at most max_length may see, counted from a multiple of the tile of 32
