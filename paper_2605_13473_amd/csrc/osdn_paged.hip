@@ -71,6 +71,12 @@ template <typename T, int K> struct TileLoads {
     }
 };
 
+// Pieces of a sequence; a length that must not be has one, whose sum is NaN (so is that of the first piece where the sequence or its pages are not
+// there: the others are then not written, and whatever stands in their place is joined to it)
+template <typename T, int K> __device__ __forceinline__ int pieces_of(const DecodeArgs &a, int length, int lo) {
+    return length > a.max_length ? 1 : (length - (lo & ~(DecodeTile<T, K>::TT - 1)) + a.piece - 1) / a.piece;
+}
+
 template <typename T, int K>
 __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
     using D = DecodeTile<T, K>;
@@ -249,7 +255,7 @@ __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
     }
     if (wave == 0 && g == 0) { all[0][col] = M; all[1][col] = L; }
     __syncthreads();
-    const bool alone = a.pieces == 1;
+    const bool alone = pieces_of<T, K>(a, length, lo) <= 1;             // (nothing to join)
     for (int i = threadIdx.x; i < heads * (K / 4); i += DEC_T) {
         const int h = i / (K / 4), d = i % (K / 4) * 4;
         f32x4 x = load4(reinterpret_cast<const float *>(lds) + h * LDO + d);
@@ -286,7 +292,7 @@ __global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
 // of one head: a lane four columns of every (64 / (JC / 4))-th piece.
 template <typename T, int K, int JC, bool WG>
 __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
-    constexpr int QUADS = JC / 4, ROWS = 64 / QUADS, TT = DecodeTile<T, K>::TT, WAVES = WG ? 4 : 1;
+    constexpr int QUADS = JC / 4, ROWS = 64 / QUADS, WAVES = WG ? 4 : 1;
     __shared__ float red[4][JC], sums[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const unsigned item = WG ? blockIdx.x : blockIdx.x * 4 + wave;
@@ -296,7 +302,8 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
     const int b = bh / (unsigned)a.Hq, h = bh % (unsigned)a.Hq;
     const int length = a.lengths[b];
     const int lo = a.window > 0 && length > a.window ? length - a.window : 0;
-    const int n = length > a.max_length ? 1 : max(1, (length - (lo & ~(TT - 1)) + a.piece - 1) / a.piece);
+    const int n = pieces_of<T, K>(a, length, lo);
+    if (n <= 1) return;                 // decode_kernel has written it
     const float *ml = a.part_ml + (size_t)bh * a.pieces * 2, *po = a.part_o + (size_t)bh * a.pieces * K + c0;
     // the first four of a lane's pieces are on their way before the maximum is known
     constexpr int STEP = ROWS * WAVES, AHEAD = 4;

@@ -247,14 +247,20 @@ inline long long decode_span(int max_length, int window) {
     const long long seen = window > 0 && window < max_length ? (long long)window + DECODE_TILE - 1 : max_length;
     return seen < max_length ? seen : max_length;
 }
-// ... and the tokens of a piece, for B sequences and `rows` (sequence, group of query heads) pairs: two workgroups a CU (fp32, whose products
-// take more of the time: four), not above 512 tokens where the lengths may differ, which only small pieces even out.  us, pieces of
-// 128, 256, 512, 1024 and 2048 tokens, K = 128 in bf16 unless said: 1 x 131072 x 8 heads 127, 117, 107, 103, 99; 4 x 32768 x 1 21.7, 19.6, 19.8, 26.9, 45.3;
-// 32 x 1000 x 4 20.2, 18.5, 19.3, 23.6; fp32 K = 64, 8 x 4096 x 8 32.5, 31.6, 37.4, 52.9; uneven lengths, 64 x 8192 x 8 237, 220,
-// 208, 219, 257, 512 x 4096 x 4 511, 438, 408, 421, 460; even ones, 16 x 4096 x 16 104, 101, 100, 99, 98.
+// ... and the tokens of a piece, for B sequences and `rows` (sequence, group of query heads) pairs.  us, K = 128 in bf16 and four heads of the
+// cache unless said, "even" where all lengths are the same, "uneven" where they are spread from 1 to the longest:
+//  - one piece, and no second kernel, for short sequences and where the rows alone fill the chip: pieces of 128, 256, 512 tokens and one, 256 even ones
+//    of 1000 116, 109, 105, 95, 64 of 500 20.9, 20.2, -, 16.9; uneven 512 of 1000 127, 121, 123, 105, 64 of 2000 38.3, 36.2, 37.2, 37.6; fp32, 64 x 8 of 1500
+//    79, 78, 82, 71; 1 of 200 9.0 and 8.1; but 1 of 500 9.3 and 12.2.
+//  - else two workgroups a CU (fp32, whose products take more of the time: four).  Pieces of 128, 256, 512, 1024 and 2048: 1 x 131072 x 8
+//    heads 122, 112, 105, 100, 99; 4 x 32768 x 1 21.2, 19.3, 19.3, 22.8, 36.5; 32 x 1000 x 4 19.4, 18.9, 20.3, 21.6; fp32 K = 64, 8 x 4096 x 8 32.0,
+//    31.3, 30.6, 37.2, 57.2.
+//  - but small enough to even out lengths that may differ: uneven 64 x 8192 x 8 245, 214, 200, 206, 229, 16 x 4096 27.5, 25.3, 26.8, 27.8, 39.4; with many
+//    rows larger ones do, uneven 512 x 4096 524, 422, 405, 401, 419, even 256 x 4096 444, 409, 394, 378, 371.
 inline int decode_piece(int B, long long rows, long long span, bool bf16) {
-    const long long want = rows * span / (NUM_CU * (bf16 ? 2 : 4));
-    const long long piece = (want + DECODE_PIECE - 1) / DECODE_PIECE * DECODE_PIECE, most = B > 1 ? 512 : 2048;
+    const bool one = span <= 256 || (rows >= NUM_CU && span <= 2048);
+    const long long want = one ? span : rows * span / (NUM_CU * (bf16 ? 2 : 4)), most = one || B == 1 ? 2048 : rows >= 4 * NUM_CU ? 1024 : 512;
+    const long long piece = (want + DECODE_PIECE - 1) / DECODE_PIECE * DECODE_PIECE;
     return (int)(piece < DECODE_PIECE ? DECODE_PIECE : piece > most ? most : piece);
 }
 
