@@ -493,7 +493,7 @@ int osdn_paged_append(const osdn_norm_params *p, const osdn_cache *cache, const 
 static int check_decode(const osdn_decode_params *p, int &head_tiles, int &piece, int &pieces) {
     if (!p) return OSDN_ERR_NULL;
     if (p->io_dtype != OSDN_F32 && p->io_dtype != OSDN_BF16) return OSDN_ERR_DTYPE;
-    if (p->B < 1 || p->B > 65535 || p->Hk < 1 || p->Hq < p->Hk || p->Hq % p->Hk != 0 || (long long)p->B * p->Hq >= 1 << 21) return OSDN_ERR_SHAPE;
+    if (p->B < 1 || p->B > 65535 || p->Hk < 1 || p->Hq < p->Hk || p->Hq % p->Hk != 0 || p->Hq > 65535 || (long long)p->B * p->Hq >= 1 << 21) return OSDN_ERR_SHAPE;
     if (p->K != 64 && p->K != 128 && p->K != 256) return OSDN_ERR_SHAPE;
     if (p->max_length < 0 || p->max_length > 0x7fffff00) return OSDN_ERR_SHAPE;
     if (!std::isfinite(p->scale) || p->window < 0 || p->piece < 0 || p->piece % DECODE_PIECE != 0) return OSDN_ERR_PARAM;

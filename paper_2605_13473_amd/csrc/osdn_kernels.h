@@ -247,6 +247,7 @@ struct HeadsArgs {
     int T, tokens, Hq, Hk, K;             // tokens: of all batch entries
     int norm; float mean, eps;            // 1 / r^2 = mean sum x^2 + eps; norm == 0: r = 1
     int rotary_dim, rotary_rows, interleaved;
+    int q_blocks, k_blocks, blocks, parts, per_part;      // set by the launcher: blocks of rows of a token, how many wavefronts share them, blocks of each
     bool aligned;                         // every row that is not a cache's starts on 16 bytes
     HeadRows q, k, v, q_out, k_out;       // v: append alone
     const float *weight_q, *weight_k;     // [K] or null
@@ -262,8 +263,6 @@ struct HeadsArgs {
     HeadRows dq_out, dk_out, dq, dk;
     float *dweight_q, *dweight_k;         // [K] or null
     float *partial;                       // [workgroups][2][K], null without weights
-    // set by the launcher: blocks of rows of a token, how many wavefronts share them, blocks of each
-    int q_blocks, k_blocks, blocks, parts, per_part;
 };
 int launch_heads_fwd(const HeadsArgs &a, bool bf16_io, hipStream_t st);
 int launch_heads_bwd(const HeadsArgs &a, bool bf16_io, hipStream_t st);

@@ -231,14 +231,17 @@ inline bool solved_plan(const osdn_params *p, long long chains, int longest, boo
     return p->p1_solved > 0 || (p->p1_solved == 0 && chains * (quarter ? 4 : 8) <= NUM_CU);
 }
 
-// Blocks of rows (64 lanes of 16 bytes) of a token that one wavefront of heads_fwd_kernel takes: all of them, or as few as it takes to give every CU
-// eight wavefronts.
+// Blocks of rows (64 lanes of 16 bytes) of a token that one wavefront of heads_fwd_kernel takes: all of them where every CU then has sixteen wavefronts,
+// else as many pairs as leave it sixteen (its loads go in pairs), and one by one below eight.  us, from eight wavefronts with any number and from
+// sixteen: 1531 tokens of 8 blocks 8.5 and 7.5, 800 of 12 9.7 and 9.0, fp32 1500 of 8 8.6 and 7.7; 4000 of 2 one by one 8.4, as a pair 7.3.
 inline int heads_blocks_per_wave(long long tokens, int blocks) {
-    const long long per = tokens * blocks / (NUM_CU * 8);
-    return (int)(per < 1 ? 1 : per > blocks ? blocks : per);
+    if (tokens * blocks < 2 * 8 * NUM_CU) return 1;
+    const long long pairs = tokens * blocks / (2 * 16 * NUM_CU);
+    return (int)(pairs < 1 ? 2 : 2 * pairs > blocks ? blocks : 2 * pairs);
 }
-// Workgroups (four wavefronts) for so many (token, part) pairs
+// Workgroups (four wavefronts) for so many (token, part) pairs: 65536 tokens appended with up to 2048, 4096 and 16384 of them 190, 180 and 173 us
 inline int heads_fwd_workgroups(long long items) { return (int)(items < 4 * 16384 ? (items + 3) / 4 : 16384); }
+// ... of heads_bwd_kernel, each with a row of partial sums: 2 x 8192 x (32 + 8) heads with 1024 and 2048 178 and 179 us (both passes), 4 x 2048 x (16 + 4) of 64 33 and 36
 inline int heads_bwd_workgroups(long long tokens) { return (int)(tokens < 4 * 1024 ? (tokens + 3) / 4 : 1024); }
 
 // Attention over a paged cache: tokens that a sequence of at most max_length may see, counted from a multiple of the tile of 32
