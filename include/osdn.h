@@ -340,7 +340,8 @@ typedef struct {
     int32_t io_dtype;               /* osdn_dtype of q, o and the cache */
     int32_t window;                 /* > 0: only the last so many tokens are seen; 0: all */
     int32_t max_length;             /* no length is above it (the launch is sized by it) */
-    int32_t piece;                  /* scheduling: tokens of a piece, a multiple of 128; 0: the library decides */
+    int32_t shares;                 /* scheduling: > 0 (up to 65535): cut the tokens among so many workgroups; -1: a workgroup for each
+                                       sequence and group of query heads; 0: the library decides */
     float scale;                    /* multiplies the scores (usually K^-1/2) */
 } osdn_decode_params;
 
@@ -355,7 +356,7 @@ typedef struct {
  *                     with its own length: drafted tokens, or a prompt token by token
  *   lse               [B,Hq] fp32 or NULL
  *   workspace         osdn_paged_decode_workspace_bytes(p) bytes, 256-byte aligned (may be NULL if that is 0)
- * B Hq is below 2^21, and the pieces of all sequences of max_length below 2^24.
+ * B Hq is below 2^21, and B Hk max_length / 128 (with more than 16 query heads a key head as many times that) below 2^31.
  * What a length hides is not looked at, whatever the cache holds there.  A length above max_length or above what a row of the
  * table holds, a sequence or a page that is not there: o and lse are NaN, and nothing outside the cache is read.
  */

@@ -59,7 +59,7 @@ class OsdnCache(ctypes.Structure):
 
 
 class OsdnDecodeParams(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hk", "K", "io_dtype", "window", "max_length", "piece")] + [
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hk", "K", "io_dtype", "window", "max_length", "shares")] + [
         ("scale", ctypes.c_float)]
 
 
@@ -489,8 +489,8 @@ def make_norm_params(B, T, Hq, Hk, K, bf16: bool, hp: NormHyper = NormHyper(), r
 
 
 def make_decode_params(B, Hq, Hk, K, bf16: bool, max_length: int, scale: float | None = None, window: int = 0,
-                       piece: int = 0) -> OsdnDecodeParams:
-    return OsdnDecodeParams(B, Hq, Hk, K, OSDN_BF16 if bf16 else OSDN_F32, int(window or 0), int(max_length), int(piece),
+                       shares: int = 0) -> OsdnDecodeParams:
+    return OsdnDecodeParams(B, Hq, Hk, K, OSDN_BF16 if bf16 else OSDN_F32, int(window or 0), int(max_length), int(shares),
                             float(K) ** -0.5 if scale is None else float(scale))
 
 

@@ -490,46 +490,46 @@ int osdn_paged_append(const osdn_norm_params *p, const osdn_cache *cache, const 
     return launch_status();
 }
 
-static int check_decode(const osdn_decode_params *p, int &head_tiles, int &piece, int &pieces) {
+static int check_decode(const osdn_decode_params *p, DecodeArgs &a, size_t &bytes) {
     if (!p) return OSDN_ERR_NULL;
     if (p->io_dtype != OSDN_F32 && p->io_dtype != OSDN_BF16) return OSDN_ERR_DTYPE;
     if (p->B < 1 || p->B > 65535 || p->Hk < 1 || p->Hq < p->Hk || p->Hq % p->Hk != 0 || p->Hq > 65535 || (long long)p->B * p->Hq >= 1 << 21) return OSDN_ERR_SHAPE;
     if (p->K != 64 && p->K != 128 && p->K != 256) return OSDN_ERR_SHAPE;
     if (p->max_length < 0 || p->max_length > 0x7fffff00) return OSDN_ERR_SHAPE;
-    if (!std::isfinite(p->scale) || p->window < 0 || p->piece < 0 || p->piece % DECODE_PIECE != 0) return OSDN_ERR_PARAM;
-    head_tiles = (p->Hq / p->Hk + 15) / 16;
-    const long long span = decode_span(p->max_length, p->window);
-    const long long rows = (long long)p->B * p->Hk * head_tiles, most = ((1ll << 32) / DEC_THREADS - 1) / rows;      // (a launch has fewer than 2^32 threads)
-    piece = p->piece ? p->piece : decode_piece(p->B, rows, span, p->io_dtype == OSDN_BF16);
-    while (!p->piece && (span + piece - 1) / piece > most) piece *= 2;          // (most is 7 at least, and span below 2^31)
-    const long long n = (span + piece - 1) / piece;
-    if (n > most) return OSDN_ERR_SHAPE;
-    pieces = n < 1 ? 1 : (int)n;
+    if (!std::isfinite(p->scale) || p->window < 0 || p->shares < -1 || p->shares > 65535) return OSDN_ERR_PARAM;
+    a.head_tiles = (p->Hq / p->Hk + 15) / 16;
+    a.part_heads = p->Hq / p->Hk < 16 ? p->Hq / p->Hk : 16;
+    const long long rows = (long long)p->B * p->Hk * a.head_tiles, units = decode_units(p->max_length, p->window);
+    if (rows * units > 0x7fffffffLL) return OSDN_ERR_SHAPE;            // (units are counted in 32 bits)
+    a.shares = p->shares == -1 ? 0 : p->shares ? p->shares : decode_shares(rows, units, p->K, p->io_dtype == OSDN_BF16);
+    bytes = !a.shares ? 0 : (size_t)a.shares * 2 * a.part_heads * (p->K + 2) * sizeof(float) + (size_t)rows * 2 * sizeof(int);
     return OSDN_OK;
 }
 
 size_t osdn_paged_decode_workspace_bytes(const osdn_decode_params *p) {
-    int tiles, piece, pieces;
-    if (check_decode(p, tiles, piece, pieces) != OSDN_OK || pieces == 1) return 0;
-    return (size_t)p->B * p->Hq * pieces * (p->K + 2) * sizeof(float);
+    DecodeArgs a{};
+    size_t bytes;
+    return check_decode(p, a, bytes) == OSDN_OK ? bytes : 0;
 }
 
 int osdn_paged_decode(const osdn_decode_params *p, const osdn_cache *cache, const osdn_rows *q, const int32_t *lengths, const int32_t *seq,
                       const osdn_rows *o, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
     DecodeArgs a{};
-    int rc = check_decode(p, a.head_tiles, a.piece, a.pieces);
+    size_t bytes = 0;
+    int rc = check_decode(p, a, bytes);
     if (rc != OSDN_OK) return rc;
     if (!lengths) return OSDN_ERR_NULL;
     const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
     if ((rc = check_cache(cache, p->Hk, es, a.page_shift)) != OSDN_OK) return rc;
     a.aligned = true;
     if ((rc = take_rows(q, p->B, 1, p->Hq, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(o, p->B, 1, p->Hq, es, true, a.o, a.aligned)) != OSDN_OK) return rc;
-    const size_t rows = (size_t)p->B * p->Hq * a.pieces;
-    if (a.pieces > 1) {
-        rc = check_ws(workspace, workspace_bytes, rows * (p->K + 2) * sizeof(float));
+    if (a.shares) {
+        rc = check_ws(workspace, workspace_bytes, bytes);
         if (rc != OSDN_OK) return rc;
+        const size_t parts = (size_t)a.shares * 2 * a.part_heads;
         a.part_o = static_cast<float *>(workspace);
-        a.part_ml = a.part_o + rows * p->K;
+        a.part_ml = a.part_o + parts * p->K;
+        a.info = reinterpret_cast<int *>(a.part_ml + parts * 2);
     }
     a.B = p->B; a.Hq = p->Hq; a.Hk = p->Hk; a.K = p->K; a.group = p->Hq / p->Hk;
     a.scale = p->scale; a.window = p->window; a.max_length = p->max_length;

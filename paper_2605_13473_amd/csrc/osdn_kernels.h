@@ -269,16 +269,19 @@ int launch_heads_bwd(const HeadsArgs &a, bool bf16_io, hipStream_t st);
 
 // Attention of one token per sequence over a paged cache (osdn_paged.hip)
 struct DecodeArgs {
-    int B, Hq, Hk, K, group, head_tiles;  // group: query heads of a key head; head_tiles: workgroups (of 16 query heads) that they take
+    int B, Hq, Hk, K, group, head_tiles;  // group: query heads of a key head; head_tiles: rows (of up to 16 query heads) that they make
     float scale;
-    int window, max_length, piece, pieces;    // tokens of a piece; pieces of a sequence of max_length
+    int window, max_length;
+    int shares, part_heads;               // shares: workgroups that the tokens are cut among, 0: one for each row; part_heads: heads of a row, at most
     HeadRows q, o, cache_k, cache_v;      // q, o: token unused
     bool aligned;                         // every row of q and o starts on 16 bytes
     const int *table, *seq, *lengths;     // [n_seqs, max_pages], [B] or null (the batch entry), [B]
     long long table_stride;
     int n_pages, page_shift, n_seqs, max_pages;
     float *lse;                           // [B, Hq] or null
-    float *part_o, *part_ml;              // pieces > 1: [B, Hq, pieces, K] and [B, Hq, pieces, 2]
+    // shares > 0: two parts of each, [shares, 2, part_heads, K] and (maximum, sum) [shares, 2, part_heads, 2]; the first part and how many, of each row
+    float *part_o, *part_ml;
+    int *info;
 };
 int launch_paged_decode(const DecodeArgs &a, bool bf16_io, hipStream_t st);
 

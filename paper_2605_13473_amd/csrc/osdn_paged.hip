@@ -4,9 +4,12 @@
 //   s_j = scale <q, k_j>,  m = max_j s_j,  l = sum_j e^(s_j - m),  o = sum_j e^(s_j - m) v_j / l,  lse = m + log l
 //
 // Bound by memory: every visible key and value is read once, for all query heads that share it (up to 16 side by side: the columns
-// of a 16 x 16 matrix product, so that one query head costs what 16 do, 3 % of the matrix cores' time).  The visible tokens are cut into pieces;
-// a workgroup takes one piece of one key head, its four wavefronts take the piece's tiles in turn, each with a running
-// maximum and sum of its own, and join at the end; a second kernel joins the pieces, in their order.
+// of a 16 x 16 matrix product, so that one query head costs what 16 do, 3 % of the matrix cores' time).  The visible tokens of all
+// rows (a row: a sequence and a group of up to 16 query heads of one key head) make one list that is cut into even shares, one a
+// workgroup, whatever the lengths; a share is a part of a row, or the end of one, whole ones and the beginning of the last.  The four wavefronts of
+// a workgroup take a row's tiles in turn, each with a running maximum and sum of its own, and join at its end; rows that a share does
+// not hold whole go to a second kernel, which joins their parts in their order.  2.1 GB of keys and values of 512 sequences of 1 to 4096
+// tokens: 380 us, 5.6 TB/s (cut into pieces of 1024 tokens, a workgroup each, 401); 0.54 GB of one sequence 99 us, 5.4 TB/s.
 //
 // A wavefront's tile is TT tokens.  Keys go from memory to registers as the matrix product wants them (lane l: token l % 16, 16 bytes);
 // scores come out transposed, lane l with four tokens of head l % 16, which is how the second product (values transposed,
@@ -34,12 +37,13 @@ __device__ __forceinline__ float max_xor32(float x) {
 
 template <typename T, int K> struct DecodeTile {
     static constexpr bool BF = sizeof(T) == 2;
-    static constexpr int TT = BF ? 32 : 16;             // tokens: the depth of the second product's matrix instruction, or four of them
+    static constexpr int TT = BF && K <= 128 ? 32 : 16; // tokens: the depth of the second product's matrix instruction (fp32: four of them; wide rows: half, for the registers)
     static constexpr int SETS = TT / 16;                // 16-token products that make the scores
     static constexpr int VE = 16 / sizeof(T);           // elements of a 16-byte vector
     static constexpr int STEPS = K / (4 * VE);          // vectors of a row, per lane (four lanes share a row)
     static constexpr int LDV = K + VE;                  // row of the values in LDS: 16 rows of one column start on 16 different quads of banks
     static constexpr int OUT = K / 16;                  // 16-row tiles of the transposed result
+    static constexpr int PER_CU = K == 64 ? 4 : K == 128 ? (BF ? 3 : 2) : BF ? 2 : 1;      // workgroups that a CU's registers hold
 };
 
 // The rows of a tile that a lane loads, token 16 i + l % 16 of the tile, on their way: first their pages, then the rows
@@ -77,226 +81,306 @@ __device__ __forceinline__ void ask_arguments(const DecodeArgs &a) {
     asm volatile("" ::"s"(a.B), "s"(a.q.token), "s"(a.cache_k.data), "s"(a.cache_v.token), "s"(a.table_stride), "s"(a.part_ml));
 }
 
-// Pieces of a sequence; a length that must not be has one, whose sum is NaN (so is that of the first piece where the sequence or its pages are not
-// there: the others are then not written, and whatever stands in their place is joined to it)
-template <typename T, int K> __device__ __forceinline__ int pieces_of(const DecodeArgs &a, int length, int lo) {
-    return length > a.max_length ? 1 : (length - (lo & ~(DecodeTile<T, K>::TT - 1)) + a.piece - 1) / a.piece;
+// What the caller promised and did not keep makes the result NaN: nothing outside the cache is read
+__device__ __forceinline__ bool broken(const DecodeArgs &a, int length, int seq) {
+    return (unsigned)seq >= (unsigned)a.n_seqs || length > a.max_length || (length > 0 && (length - 1) >> a.page_shift >= a.max_pages);
+}
+__device__ __forceinline__ int first_seen(const DecodeArgs &a, int length) { return a.window > 0 && length > a.window ? length - a.window : 0; }
+// Units of DECODE_UNIT tokens, from a multiple of DECODE_TILE on, of each row of sequence b; one where there is nothing to see, so that its zeros
+// (or NaN) are written
+__device__ __forceinline__ int units_of(const DecodeArgs &a, int b) {
+    const int length = a.lengths[b], seq = a.seq ? a.seq[b] : b;
+    if (length <= 0 || broken(a, length, seq)) return 1;
+    return (length - (first_seen(a, length) & ~(DECODE_TILE - 1)) + DECODE_UNIT - 1) / DECODE_UNIT;
 }
 
-template <typename T, int K>
-__global__ __launch_bounds__(DEC_T) void decode_kernel(DecodeArgs a) {
+// The even shares of n units among W workgroups: the first n % W have one more
+struct Shares {
+    int q, rem;
+    __device__ __forceinline__ Shares(int n, int W) : q(n / W), rem(n % W) {}
+    __device__ __forceinline__ int begin(int w) const { return w * q + min(w, rem); }
+    __device__ __forceinline__ int owner(int unit) const { return unit < rem * (q + 1) ? unit / (q + 1) : rem + (unit - rem * (q + 1)) / q; }
+};
+
+// SHARED: even shares; else a workgroup takes one row, whole (short rows, or many: no search and no second kernel)
+template <typename T, int K, bool SHARED>
+__global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kernel(DecodeArgs a) {
     using D = DecodeTile<T, K>;
-    constexpr int TT = D::TT, VE = D::VE, STEPS = D::STEPS, LDV = D::LDV, OUT = D::OUT, LDO = K + 4;
+    constexpr int TT = D::TT, VE = D::VE, STEPS = D::STEPS, LDV = D::LDV, OUT = D::OUT, LDO = K + 4, STRIDE = DEC_W * TT;
     __shared__ __align__(16) char lds[DEC_W * (TT * LDV * sizeof(T) > 16 * LDO * 4 ? TT * LDV * sizeof(T) : 16 * LDO * 4)];
     __shared__ float ml[DEC_W][2][16], all[2][16];
+    __shared__ int found[2], sums[DEC_W];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     ask_arguments(a);
-    // The pieces of a (sequence, group of heads) are neighbours in the launch (neighbouring heads side by side, 64 sequences of up to 8192
-    // tokens whose pages hold a token's heads together: 240 us, so 203).  Workgroups are dealt to the XCDs in turn, so the pieces are turned
-    // from one group to the next: else, with uneven lengths, the XCDs with the last pieces would have nothing to do (309 us).
-    const unsigned kt = blockIdx.y, b = blockIdx.z, at = kt + gridDim.y * b;
-    const int piece = (blockIdx.x + at + at / 4) % gridDim.x;
-    const int kv = a.head_tiles == 1 ? kt : kt / (unsigned)a.head_tiles, h0 = kv * a.group + 16 * (kt - kv * a.head_tiles);
-    const int heads = min(16, (kv + 1) * a.group - h0);
-    const int seq = a.seq ? a.seq[b] : b;
-    const bool no_seq = (unsigned)seq >= (unsigned)a.n_seqs;
-    const int *row = a.table + (no_seq ? 0 : seq * a.table_stride);
-    const int length = a.lengths[b];
-    int lo = 0;
-    if (a.window > 0 && length > a.window) lo = length - a.window;
-    const int begin = (lo & ~(TT - 1)) + piece * a.piece;               // (pieces are cut from a multiple of the tile)
-    constexpr int STRIDE = DEC_W * TT;
-    TileLoads<T, K> x;
-    x.ask(a, row, begin + wave * TT, lane);
-    // queries: lane l holds head l % 16
-    u32x4 q[STEPS];
+    const int rows = a.Hk * a.head_tiles, w = blockIdx.x;          // rows of a sequence
+    // This workgroup's share: units [at, until), the first of them of sequence b, whose units start at `base`
+    int b, base, at, until, total = 0;
+    if constexpr (!SHARED) {
+        b = w / (unsigned)rows;
+        base = 0;
+        const int u = units_of(a, b);
+        at = (w - b * rows) * u;
+        until = at + u;
+    } else {
+        if (a.B == 1) {
+            total = units_of(a, 0) * rows;
+            b = base = 0;
+        } else {                        // where the share begins: a sum over the sequences before it, a run of them a thread
+            const int run = (a.B + DEC_T - 1) / DEC_T, i0 = threadIdx.x * run, i1 = min(a.B, i0 + run);
+            int mine = 0;
+            for (int i = i0; i < i1; ++i) mine += units_of(a, i);
+            int upto = mine;
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-        q[s] = u32x4{0u, 0u, 0u, 0u};
-        if (col < heads) {
-            const T *src = static_cast<const T *>(a.q.data) + b * a.q.batch + (h0 + col) * a.q.head + (4 * s + g) * VE;
-            if (a.aligned) {
-                q[s] = *reinterpret_cast<const u32x4 *>(src);
-            } else {
-                T v[VE];
-#pragma unroll
-                for (int e = 0; e < VE; ++e) v[e] = src[e];
-                q[s] = __builtin_bit_cast(u32x4, v);
+            for (int x = 1; x < 64; x <<= 1) {
+                const int y = __shfl_up(upto, x, 64);
+                if (lane >= x) upto += y;
             }
+            if (lane == 63) sums[wave] = upto;
+            __syncthreads();
+            int before = upto - mine;
+#pragma unroll
+            for (int u = 0; u < DEC_W; ++u) {
+                if (u < wave) before += sums[u];
+                total += sums[u];
+            }
+            total = __builtin_amdgcn_readfirstlane(total) * rows;
+            const int start = Shares(total, a.shares).begin(w);
+            if (start >= before * rows && start < (before + mine) * rows) {
+                int i = i0, u = units_of(a, i);
+                while (start >= (before + u) * rows) {
+                    before += u;
+                    u = units_of(a, ++i);
+                }
+                found[0] = i;
+                found[1] = before * rows;
+            }
+            __syncthreads();
+            b = __builtin_amdgcn_readfirstlane(found[0]);
+            base = __builtin_amdgcn_readfirstlane(found[1]);
         }
+        const Shares share(total, a.shares);
+        at = share.begin(w);
+        until = share.begin(w + 1);
+        if (at >= until) return;
     }
-    // what the caller promised and did not keep makes the result NaN: nothing outside the cache is read
-    const bool bad_call = no_seq || length > a.max_length || (length > 0 && (length - 1) >> a.page_shift >= a.max_pages);
-    if (piece > 0 && (bad_call || begin >= length)) return;             // (an empty sequence has one empty piece)
-    const int end = bad_call ? 0 : length - begin < a.piece ? length : begin + a.piece;
+    const int share_begin = at;
 
-    const T *kc = static_cast<const T *>(a.cache_k.data) + kv * a.cache_k.head + g * VE;
-    const T *vc = static_cast<const T *>(a.cache_v.data) + kv * a.cache_v.head + g * VE;
-    T *vs = reinterpret_cast<T *>(lds) + wave * TT * LDV;
-    const float scale2 = a.scale * LOG2E;
-
-    float m = -FLT_MAX, l = 0.f;        // finite: a score of minus infinity then weighs nothing, also where there is no other
-    f32x4 o[OUT];
+    do {
+        const int units = units_of(a, b), kt = (at - base) / units, u0 = at - base - kt * units, u1 = min(units, u0 + until - at);
+        const int kv = a.head_tiles == 1 ? kt : kt / a.head_tiles, h0 = kv * a.group + 16 * (kt - kv * a.head_tiles);
+        const int heads = min(16, (kv + 1) * a.group - h0);
+        const int seq = a.seq ? a.seq[b] : b, length = a.lengths[b], lo = first_seen(a, length);
+        const bool bad_call = broken(a, length, seq);
+        const int *row = a.table + (bad_call ? 0 : seq * a.table_stride);
+        const int begin = (lo & ~(DECODE_TILE - 1)) + u0 * DECODE_UNIT;
+        const int end = bad_call ? 0 : u1 == units ? length : begin + (u1 - u0) * DECODE_UNIT;
+        TileLoads<T, K> x;
+        x.ask(a, row, begin + wave * TT, lane);
+        // queries: lane l holds head l % 16
+        u32x4 q[STEPS];
 #pragma unroll
-    for (int t = 0; t < OUT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    bool bad_page = false;
-
-    // The rows of the next tile are asked for when this one's are in the matrix products' registers and in LDS, its pages a tile earlier
-    int tok = begin + wave * TT;
-    if (tok < end) {
-        bad_page = x.load(a, kc, vc, tok, lo, end, lane);
-        x.ask(a, row, tok + STRIDE, lane);
-    }
-    while (tok < end) {
-        // scores, transposed: p[i][r] is token 16 i + 4 g + r of head `col`
-        f32x4 p[D::SETS];
-        float top = m;
-        const bool whole = tok >= lo && tok + TT <= end;
-#pragma unroll
-        for (int i = 0; i < D::SETS; ++i) {
-            p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-                if constexpr (D::BF) {
-                    p[i] = Mfma<bf16>::mma(__builtin_bit_cast(bf16x8, x.k[i][s]), __builtin_bit_cast(bf16x8, q[s]), p[i]);
+        for (int s = 0; s < STEPS; ++s) {
+            q[s] = u32x4{0u, 0u, 0u, 0u};
+            if (col < heads) {
+                const T *src = static_cast<const T *>(a.q.data) + b * a.q.batch + (h0 + col) * a.q.head + (4 * s + g) * VE;
+                if (a.aligned) {
+                    q[s] = *reinterpret_cast<const u32x4 *>(src);
                 } else {
+                    T v[VE];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) p[i] = Mfma<float>::mma(vec_get<float>(x.k[i][s], e), vec_get<float>(q[s], e), p[i]);
+                    for (int e = 0; e < VE; ++e) v[e] = src[e];
+                    q[s] = __builtin_bit_cast(u32x4, v);
                 }
             }
         }
-        if (!whole) {               // what is not seen has no weight, and must not be infinite or NaN either
+        const T *kc = static_cast<const T *>(a.cache_k.data) + kv * a.cache_k.head + g * VE;
+        const T *vc = static_cast<const T *>(a.cache_v.data) + kv * a.cache_v.head + g * VE;
+        T *vs = reinterpret_cast<T *>(lds) + wave * TT * LDV;
+        const float scale2 = a.scale * LOG2E;
+
+        float m = -FLT_MAX, l = 0.f;        // finite: a score of minus infinity then weighs nothing, also where there is no other
+        f32x4 o[OUT];
+#pragma unroll
+        for (int t = 0; t < OUT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        bool bad_page = false;
+
+        // The rows of the next tile are asked for when this one's are in the matrix products' registers and in LDS, its pages a tile earlier
+        int tok = begin + wave * TT;
+        if (tok < end) {
+            bad_page = x.load(a, kc, vc, tok, lo, end, lane);
+            x.ask(a, row, tok + STRIDE, lane);
+        }
+        while (tok < end) {
+            // scores, transposed: p[i][r] is token 16 i + 4 g + r of head `col`
+            f32x4 p[D::SETS];
+            float top = m;
+            const bool whole = tok >= lo && tok + TT <= end;
 #pragma unroll
             for (int i = 0; i < D::SETS; ++i) {
-                const int j = tok + 16 * i + col;
-                const bool seen = j >= lo && j < end;
+                p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s)
+                for (int s = 0; s < STEPS; ++s) {
+                    if constexpr (D::BF) {
+                        p[i] = Mfma<bf16>::mma(__builtin_bit_cast(bf16x8, x.k[i][s]), __builtin_bit_cast(bf16x8, q[s]), p[i]);
+                    } else {
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) x.v[i][s][w] = seen ? x.v[i][s][w] : 0u;
+                        for (int e = 0; e < 4; ++e) p[i] = Mfma<float>::mma(vec_get<float>(x.k[i][s], e), vec_get<float>(q[s], e), p[i]);
+                    }
+                }
             }
-        }
+            if (!whole) {               // what is not seen has no weight, and must not be infinite or NaN either
 #pragma unroll
-        for (int i = 0; i < D::SETS; ++i)
+                for (int i = 0; i < D::SETS; ++i) {
+                    const int j = tok + 16 * i + col;
+                    const bool seen = j >= lo && j < end;
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) *reinterpret_cast<u32x4 *>(vs + (16 * i + col) * LDV + (4 * s + g) * VE) = x.v[i][s];
-        const int next = tok + STRIDE;
-        if (next < end) {
-            bad_page = x.load(a, kc, vc, next, lo, end, lane) || bad_page;
-            x.ask(a, row, next + STRIDE, lane);
-        }
+                    for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-        for (int i = 0; i < D::SETS; ++i)
+                        for (int w = 0; w < 4; ++w) x.v[i][s][w] = seen ? x.v[i][s][w] : 0u;
+                }
+            }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) p[i][r] *= scale2;
-        if (!whole) {
+            for (int i = 0; i < D::SETS; ++i)
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) *reinterpret_cast<u32x4 *>(vs + (16 * i + col) * LDV + (4 * s + g) * VE) = x.v[i][s];
+            const int next = tok + STRIDE;
+            if (next < end) {
+                bad_page = x.load(a, kc, vc, next, lo, end, lane) || bad_page;
+                x.ask(a, row, next + STRIDE, lane);
+            }
+#pragma unroll
+            for (int i = 0; i < D::SETS; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[i][r] *= scale2;
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < D::SETS; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int j = tok + 16 * i + 4 * g + r;
+                        p[i][r] = j >= lo && j < end ? p[i][r] : -INFINITY;
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < D::SETS; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top = fmaxf(top, p[i][r]);
+            top = max_xor32(max_xor16(top));
+            if (__any(top > m)) {
+                const float f = __builtin_amdgcn_exp2f(m - top);
+                l *= f;
+#pragma unroll
+                for (int t = 0; t < OUT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[t][r] *= f;
+                m = top;
+            }
 #pragma unroll
             for (int i = 0; i < D::SETS; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int j = tok + 16 * i + 4 * g + r;
-                    p[i][r] = j >= lo && j < end ? p[i][r] : -INFINITY;
+                    p[i][r] = __builtin_amdgcn_exp2f(p[i][r] - m);
+                    l += p[i][r];
                 }
-        }
+            // o transposed += values transposed x weights
+            if constexpr (D::BF) {
+                typedef short v4s __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) v4s *lds_v4s;
+                bf16x4 w[D::SETS];
 #pragma unroll
-        for (int i = 0; i < D::SETS; ++i)
+                for (int i = 0; i < D::SETS; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, p[i][r]);
-        top = max_xor32(max_xor16(top));
-        if (__any(top > m)) {
-            const float f = __builtin_amdgcn_exp2f(m - top);
-            l *= f;
+                    for (int r = 0; r < 4; ++r) w[i][r] = (bf16)p[i][r];
 #pragma unroll
-            for (int t = 0; t < OUT; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) o[t][r] *= f;
-            m = top;
-        }
-#pragma unroll
-        for (int i = 0; i < D::SETS; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                p[i][r] = __builtin_amdgcn_exp2f(p[i][r] - m);
-                l += p[i][r];
-            }
-        // o transposed += values transposed x weights
-        if constexpr (D::BF) {
-            typedef short v4s __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) v4s *lds_v4s;
-            bf16x8 w;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) { w[r] = (bf16)p[0][r]; w[4 + r] = (bf16)p[D::SETS - 1][r]; }
-#pragma unroll
-            for (int t = 0; t < OUT; ++t) {
-                const bf16 *at = reinterpret_cast<const bf16 *>(vs) + (4 * g + (col >> 2)) * LDV + 16 * t + 4 * (col & 3);
-                const v4s a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at));
-                const v4s a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at + 16 * LDV));
-                o[t] = Mfma<bf16>::mma(__builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)), w, o[t]);
-            }
-        } else {
-#pragma unroll
-            for (int t = 0; t < OUT; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) o[t] = Mfma<float>::mma(to_f32(vs[(4 * g + r) * LDV + 16 * t + col]), p[0][r], o[t]);
-        }
-        tok = next;
-    }
-    // the four wavefronts join
-    l = add_xor32(add_xor16(l));
-    if (bad_call || __any(bad_page)) l = __builtin_nanf("");
-    if (g == 0) { ml[wave][0][col] = m; ml[wave][1][col] = l; }
-    __syncthreads();
-    float M = ml[0][0][col], L = 0.f;
-#pragma unroll
-    for (int u = 1; u < DEC_W; ++u) M = fmaxf(M, ml[u][0][col]);
-#pragma unroll
-    for (int u = 0; u < DEC_W; ++u) L = __builtin_fmaf(ml[u][1][col], __builtin_amdgcn_exp2f(ml[u][0][col] - M), L);
-    const float f = __builtin_amdgcn_exp2f(m - M);
-    float *os = reinterpret_cast<float *>(lds) + wave * 16 * LDO;
-#pragma unroll
-    for (int t = 0; t < OUT; ++t) {
-        f32x4 x = o[t];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] *= f;
-        *reinterpret_cast<f32x4 *>(os + col * LDO + 16 * t + 4 * g) = x;
-    }
-    if (wave == 0 && g == 0) { all[0][col] = M; all[1][col] = L; }
-    __syncthreads();
-    const bool alone = pieces_of<T, K>(a, length, lo) <= 1;             // (nothing to join)
-    for (int i = threadIdx.x; i < heads * (K / 4); i += DEC_T) {
-        const int h = i / (K / 4), d = i % (K / 4) * 4;
-        f32x4 x = load4(reinterpret_cast<const float *>(lds) + h * LDO + d);
-#pragma unroll
-        for (int u = 1; u < DEC_W; ++u) {
-            const f32x4 y = load4(reinterpret_cast<const float *>(lds) + (u * 16 + h) * LDO + d);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] += y[r];
-        }
-        const size_t bh = (size_t)b * a.Hq + h0 + h;
-        if (alone) {
-            const float sum = all[1][h], inv = sum == 0.f ? 0.f : 1.f / sum;
-            T *dst = static_cast<T *>(a.o.data) + b * a.o.batch + (h0 + h) * a.o.head + d;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] *= inv;
-            if (a.aligned) {
-                store4(dst, x);
+                for (int t = 0; t < OUT; ++t) {
+                    const bf16 *at = reinterpret_cast<const bf16 *>(vs) + (4 * g + (col >> 2)) * LDV + 16 * t + 4 * (col & 3);
+                    const v4s a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at));
+                    if constexpr (D::SETS == 2) {
+                        const v4s a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at + 16 * LDV));
+                        o[t] = Mfma<bf16>::mma(__builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)),
+                                               __builtin_shufflevector(w[0], w[D::SETS - 1], 0, 1, 2, 3, 4, 5, 6, 7), o[t]);
+                    } else {
+                        o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0, __builtin_bit_cast(v4s, w[0]), o[t], 0, 0, 0);
+                    }
+                }
             } else {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) dst[r] = from_f32<T>(x[r]);
+                for (int t = 0; t < OUT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[t] = Mfma<float>::mma(to_f32(vs[(4 * g + r) * LDV + 16 * t + col]), p[0][r], o[t]);
             }
-            if (a.lse && d == 0) a.lse[bh] = sum == 0.f ? -INFINITY : __builtin_fmaf(all[0][h], LN2, logf(sum));
-        } else {
-            store4(a.part_o + (bh * a.pieces + piece) * K + d, x);
-            if (d == 0) {
-                a.part_ml[(bh * a.pieces + piece) * 2] = all[0][h];
-                a.part_ml[(bh * a.pieces + piece) * 2 + 1] = all[1][h];
+            tok = next;
+        }
+        // the four wavefronts join
+        l = add_xor32(add_xor16(l));
+        if (bad_call || __any(bad_page)) l = __builtin_nanf("");
+        if (g == 0) { ml[wave][0][col] = m; ml[wave][1][col] = l; }
+        __syncthreads();
+        float M = ml[0][0][col], L = 0.f;
+#pragma unroll
+        for (int u = 1; u < DEC_W; ++u) M = fmaxf(M, ml[u][0][col]);
+#pragma unroll
+        for (int u = 0; u < DEC_W; ++u) L = __builtin_fmaf(ml[u][1][col], __builtin_amdgcn_exp2f(ml[u][0][col] - M), L);
+        const float f = __builtin_amdgcn_exp2f(m - M);
+        float *os = reinterpret_cast<float *>(lds) + wave * 16 * LDO;
+#pragma unroll
+        for (int t = 0; t < OUT; ++t) {
+            f32x4 x = o[t];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] *= f;
+            *reinterpret_cast<f32x4 *>(os + col * LDO + 16 * t + 4 * g) = x;
+        }
+        if (wave == 0 && g == 0) { all[0][col] = M; all[1][col] = L; }
+        __syncthreads();
+        const bool alone = !SHARED || u1 - u0 == units;                     // (nothing to join)
+        const size_t slot = 2 * (size_t)w + (at == share_begin ? 0 : 1);    // a share has at most two rows that are not whole: its first and its last
+        if (SHARED && u0 == 0 && threadIdx.x == 0) {
+            const int last = alone ? w : Shares(total, a.shares).owner(at + units - 1);
+            a.info[((size_t)b * rows + kt) * 2] = (int)slot;
+            a.info[((size_t)b * rows + kt) * 2 + 1] = last - w + 1;
+        }
+        for (int i = threadIdx.x; i < heads * (K / 4); i += DEC_T) {
+            const int h = i / (K / 4), d = i % (K / 4) * 4;
+            f32x4 x = load4(reinterpret_cast<const float *>(lds) + h * LDO + d);
+#pragma unroll
+            for (int u = 1; u < DEC_W; ++u) {
+                const f32x4 y = load4(reinterpret_cast<const float *>(lds) + (u * 16 + h) * LDO + d);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] += y[r];
+            }
+            const size_t bh = (size_t)b * a.Hq + h0 + h;
+            if (alone) {
+                const float sum = all[1][h], inv = sum == 0.f ? 0.f : 1.f / sum;
+                T *dst = static_cast<T *>(a.o.data) + b * a.o.batch + (h0 + h) * a.o.head + d;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] *= inv;
+                if (a.aligned) {
+                    store4(dst, x);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) dst[r] = from_f32<T>(x[r]);
+                }
+                if (a.lse && d == 0) a.lse[bh] = sum == 0.f ? -INFINITY : __builtin_fmaf(all[0][h], LN2, logf(sum));
+            } else {
+                const size_t to = slot * a.part_heads + h;
+                store4(a.part_o + to * K + d, x);
+                if (d == 0) {
+                    a.part_ml[to * 2] = all[0][h];
+                    a.part_ml[to * 2 + 1] = all[1][h];
+                }
             }
         }
-    }
+        at += u1 - u0;
+        if (at == base + rows * units) {
+            base = at;
+            ++b;
+        }
+        if (SHARED && at < until) __syncthreads();         // (the next row's values take the place of these sums)
+    } while (SHARED && at < until);
 }
 
-// The pieces of the query heads, joined in a fixed order.  A wavefront (WG: a workgroup, its four wavefronts a quarter of the pieces each) joins JC columns
-// of one head: a lane four columns of every (64 / (JC / 4))-th piece.
+// The parts of the query heads, joined in their order.  A wavefront (WG: a workgroup, its four wavefronts a quarter of the parts each) joins JC columns
+// of one head: a lane four columns of every (64 / (JC / 4))-th part.
 template <typename T, int K, int JC, bool WG>
 __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
     constexpr int QUADS = JC / 4, ROWS = 64 / QUADS, WAVES = WG ? 4 : 1;
@@ -308,27 +392,29 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
     const int c0 = item % (K / JC) * JC + lane % QUADS * 4;
     if (!WG && bh >= (unsigned)a.B * a.Hq) return;
     const int b = bh / (unsigned)a.Hq, h = bh % (unsigned)a.Hq;
-    const int length = a.lengths[b];
-    const int lo = a.window > 0 && length > a.window ? length - a.window : 0;
-    const int n = pieces_of<T, K>(a, length, lo);
+    // its row, the slot of the first part and how many there are: the parts after the first are each the first of their share
+    const int kv = h / (unsigned)a.group, in = h - kv * a.group, hh = in & 15;
+    const int *info = a.info + ((size_t)bh / a.Hq * a.Hk * a.head_tiles + kv * a.head_tiles + (in >> 4)) * 2;
+    const int first_slot = info[0], n = info[1];
     if (n <= 1) return;                 // decode_kernel has written it
-    const float *ml = a.part_ml + (size_t)bh * a.pieces * 2, *po = a.part_o + (size_t)bh * a.pieces * K + c0;
-    // the first four of a lane's pieces are on their way before the maximum is known
+    auto place = [&](int i) { return (size_t)(i == 0 ? first_slot : (first_slot & ~1) + 2 * i) * a.part_heads + hh; };
+    const float *ml = a.part_ml, *po = a.part_o + c0;
+    // the first four of a lane's parts are on their way before the maximum is known
     constexpr int STEP = ROWS * WAVES, AHEAD = 4;
     const int first = (WG ? wave * ROWS : 0) + lane / QUADS;
     f32x4 ahead[AHEAD];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) ahead[u] = load4(po + (size_t)min(first + u * STEP, n - 1) * K);
+    for (int u = 0; u < AHEAD; ++u) ahead[u] = load4(po + place(min(first + u * STEP, n - 1)) * K);
     float M = -FLT_MAX;
-    for (int i = lane; i < n; i += 64) M = fmaxf(M, ml[2 * i]);
+    for (int i = lane; i < n; i += 64) M = fmaxf(M, ml[2 * place(i)]);
     M = max_xor32(max_xor16(M));
 #pragma unroll
     for (int x = 1; x < 16; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
     float L = 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
     auto add = [&](int i, const f32x4 &y) {
-        const float f = __builtin_amdgcn_exp2f(ml[2 * i] - M);
-        L = __builtin_fmaf(ml[2 * i + 1], f, L);
+        const float f = __builtin_amdgcn_exp2f(ml[2 * place(i)] - M);
+        L = __builtin_fmaf(ml[2 * place(i) + 1], f, L);
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] = __builtin_fmaf(y[r], f, x[r]);
     };
@@ -336,7 +422,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
     for (int u = 0; u < AHEAD; ++u)
         if (first + u * STEP < n) add(first + u * STEP, ahead[u]);
 #pragma unroll 4
-    for (int i = first + AHEAD * STEP; i < n; i += STEP) add(i, load4(po + (size_t)i * K));
+    for (int i = first + AHEAD * STEP; i < n; i += STEP) add(i, load4(po + place(i) * K));
 #pragma unroll
     for (int s = QUADS; s < 64; s <<= 1) {
         L += __shfl_xor(L, s, 64);
@@ -373,10 +459,14 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
 
 namespace {
 template <typename T, int K> void decode_of(const DecodeArgs &a, hipStream_t st) {
-    hipLaunchKernelGGL((decode_kernel<T, K>), dim3(a.pieces, a.Hk * a.head_tiles, a.B), dim3(DEC_T), 0, st, a);
-    if (a.pieces == 1) return;
-    const unsigned heads = (unsigned)a.B * a.Hq;
-    if (a.pieces > 16) hipLaunchKernelGGL((decode_join_kernel<T, K, 32, true>), dim3(heads * (K / 32)), dim3(256), 0, st, a);
+    const unsigned rows = (unsigned)a.B * a.Hk * a.head_tiles, heads = (unsigned)a.B * a.Hq;
+    if (!a.shares) {
+        hipLaunchKernelGGL((decode_kernel<T, K, false>), dim3(rows), dim3(DEC_T), 0, st, a);
+        return;
+    }
+    hipLaunchKernelGGL((decode_kernel<T, K, true>), dim3(a.shares), dim3(DEC_T), 0, st, a);
+    // (many parts of few rows: a workgroup each, as the loads of a row are then what takes the time)
+    if ((unsigned)a.shares > 16 * rows) hipLaunchKernelGGL((decode_join_kernel<T, K, 32, true>), dim3(heads * (K / 32)), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((decode_join_kernel<T, K, 64, false>), dim3((heads * (K / 64) + 3) / 4), dim3(256), 0, st, a);
 }
 }  // namespace

@@ -245,26 +245,28 @@ inline int heads_fwd_workgroups(long long items) { return (int)(items < 4 * 1638
 inline int heads_bwd_workgroups(long long tokens) { return (int)(tokens < 4 * 1024 ? (tokens + 3) / 4 : 1024); }
 
 // Attention over a paged cache: tokens that a sequence of at most max_length may see, counted from a multiple of the tile of 32
-constexpr int DECODE_TILE = 32, DECODE_PIECE = 128, DEC_THREADS = 256;       // a piece: at least a tile for each of the workgroup's four wavefronts
+constexpr int DECODE_TILE = 32, DECODE_UNIT = 128, DEC_THREADS = 256;       // a unit: a tile for each of the workgroup's four wavefronts (K = 256 and fp32: two)
 inline long long decode_span(int max_length, int window) {
     const long long seen = window > 0 && window < max_length ? (long long)window + DECODE_TILE - 1 : max_length;
     return seen < max_length ? seen : max_length;
 }
-// ... and the tokens of a piece, for B sequences and `rows` (sequence, group of query heads) pairs.  us, K = 128 in bf16 and four heads of the
-// cache unless said, "even" where all lengths are the same, "uneven" where they are spread from 1 to the longest:
-//  - one piece, and no second kernel, for short sequences and where the rows alone fill the chip: pieces of 128, 256, 512 tokens and one, 256 even ones
-//    of 1000 116, 109, 105, 95, 64 of 500 20.9, 20.2, -, 16.9; uneven 512 of 1000 127, 121, 123, 105, 64 of 2000 38.3, 36.2, 37.2, 37.6; fp32, 64 x 8 of 1500
-//    79, 78, 82, 71; 1 of 200 9.0 and 8.1; but 1 of 500 9.3 and 12.2.
-//  - else two workgroups a CU (fp32, whose products take more of the time: four).  Pieces of 128, 256, 512, 1024 and 2048: 1 x 131072 x 8
-//    heads 122, 112, 105, 100, 99; 4 x 32768 x 1 21.2, 19.3, 19.3, 22.8, 36.5; 32 x 1000 x 4 19.4, 18.9, 20.3, 21.6; fp32 K = 64, 8 x 4096 x 8 32.0,
-//    31.3, 30.6, 37.2, 57.2.
-//  - but small enough to even out lengths that may differ: uneven 64 x 8192 x 8 245, 214, 200, 206, 229, 16 x 4096 27.5, 25.3, 26.8, 27.8, 39.4; with many
-//    rows larger ones do, uneven 512 x 4096 524, 422, 405, 401, 419, even 256 x 4096 444, 409, 394, 378, 371.
-inline int decode_piece(int B, long long rows, long long span, bool bf16) {
-    const bool one = span <= 256 || (rows >= NUM_CU && span <= 2048);
-    const long long want = one ? span : rows * span / (NUM_CU * (bf16 ? 2 : 4)), most = one || B == 1 ? 2048 : rows >= 4 * NUM_CU ? 1024 : 512;
-    const long long piece = (want + DECODE_PIECE - 1) / DECODE_PIECE * DECODE_PIECE;
-    return (int)(piece < DECODE_PIECE ? DECODE_PIECE : piece > most ? most : piece);
+inline long long decode_units(int max_length, int window) {
+    const long long units = (decode_span(max_length, window) + DECODE_UNIT - 1) / DECODE_UNIT;
+    return units < 1 ? 1 : units;
+}
+// ... and the shares that they are cut into for `rows` (sequence, group of query heads) pairs, 0: a row each and no second kernel.  us, four heads of the
+// cache of K = 128 in bf16 unless said; "uneven": lengths spread from 1 to the longest.
+//  - a row each for short rows, and for up to 1024 tokens where the rows fill the chip, against 512 shares: 1 x 300 tokens 9.3 and 10.3, 256 x 300
+//    35.7 and 39.7, uneven 512 x 300 41 and 56; 64 x 1000 32.2 and 33.3, uneven 512 x 1000 108 and 116; but 1 x 500 12.0 and 10.3, 16 x 500 14.0 and 12.8,
+//    uneven 256 x 2000 125 and 114, 512 x 4096 429 and 380.
+//  - two shares a CU, which start and end together whatever the lengths.  With 256, 512, 768 and 1024: 1 x 131072 x 8 heads 99.8, 99.5, 99.9, 101;
+//    uneven 512 x 4096 392, 379, 382, 383, 64 x 8192 x 8 199, 186, 187, 188; 16 x 4096 x 8, K = 256, 100, 104, 121, 106; fp32 115, 102, 119, 102.  With 384 and
+//    640, half a share a CU more or less, 434 and 414 for the first of the uneven ones.  K = 64, three: uneven 64 x 4096 x 8 72.5, 63.5, 57.8, 62.7; fp32
+//    and K = 256, whose registers hold one workgroup, one: 8 x 4096 63.5, 68.4, 74.0, 79.4.
+inline int decode_shares(long long rows, long long units, int K, bool bf16) {
+    if (units <= 3 || (rows >= NUM_CU && units <= 8)) return 0;
+    const long long most = NUM_CU * (K == 64 ? 3 : K == 256 && !bf16 ? 1 : 2);
+    return (int)(rows * units < most ? rows * units : most);
 }
 
 }  // namespace osdn

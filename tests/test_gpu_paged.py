@@ -58,26 +58,26 @@ DECODE = [
     dict(lengths=[300, 77, 5, 0], Hq=8, Hk=2, K=128, page=16, window=50),
     dict(lengths=[2000, 1999, 40], Hq=7, Hk=1, K=64, page=2, window=1000, io="f32"),
     dict(lengths=[2000, 1999, 40], Hq=16, Hk=1, K=256, page=1024, window=33),
-    dict(lengths=[5000, 4096, 4097, 1], Hq=4, Hk=1, K=64, page=256, piece=128),
-    dict(lengths=[5000, 4096, 4097, 1], Hq=4, Hk=1, K=128, page=64, piece=1024),
+    dict(lengths=[5000, 4096, 4097, 1], Hq=4, Hk=1, K=64, page=256, shares=33),
+    dict(lengths=[5000, 4096, 4097, 1], Hq=4, Hk=1, K=128, page=64, shares=7),
     dict(lengths=[130] * 70, Hq=2, Hk=2, K=64, page=32),
     dict(lengths=[20000], Hq=2, Hk=1, K=128, page=64),
 ]
 
 
-def make_decode(lengths, Hq, Hk, K, page, io="bf16", order="head", window=0, piece=0, seed=2, spread=2.0):
+def make_decode(lengths, Hq, Hk, K, page, io="bf16", order="head", window=0, shares=0, seed=2, spread=2.0):
     g = torch.Generator(device="cuda").manual_seed(seed)
     dt = torch.bfloat16 if io == "bf16" else torch.float32
     table, n_pages = make_table(lengths, page, extra=2, seed=seed)
     kc, vc = (make_cache(g, n_pages, page, Hk, K, dt, order) for _ in range(2))
     return dict(q=(spread * rnd(g, len(lengths), Hq, K)).to(dt), kc=kc, vc=vc, table=table.cuda(), lengths=torch.tensor(lengths, dtype=torch.int32, device="cuda"),
-                window=window, piece=piece, longest=max(max(lengths), 0))
+                window=window, shares=shares, longest=max(max(lengths), 0))
 
 
 def call(x, seq=None, max_length=None, scale=None, **kw):
     B, Hq, K = x["q"].shape
     p = ob.make_decode_params(B, Hq, x["kc"].shape[2], K, x["q"].dtype == torch.bfloat16, x["longest"] if max_length is None else max_length, scale,
-                              x["window"], x["piece"])
+                              x["window"], x["shares"])
     n = ob.osdn_paged_decode_workspace_bytes(p)
     ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda") if n else None            # (fp32 NaN: nothing in it is read before it is written)
     o, lse = torch.empty_like(x["q"]), torch.empty(B, Hq, device="cuda")
@@ -118,7 +118,9 @@ def test_decode(case):
             c.masked_fill_(~shown.cuda()[..., None, None], poison)
         o2, lse2 = call(x)
         assert torch.equal(o, o2) and torch.equal(lse, lse2)
-    # a launch sized for more than is there joins other pieces: the same answer
+    # a launch sized for more than is there, and other cuts: the same answer
+    for shares in (-1, 1, 3, 1000):
+        compare(x, *call(dict(x, shares=shares)))
     compare(x, *call(x, max_length=x["longest"] + 777 if x["longest"] + 777 <= x["table"].shape[1] * page else x["longest"]))
 
 
@@ -151,7 +153,7 @@ def test_several_queries_of_one_sequence():
 
 @pytest.mark.parametrize("spread,scale", [(300.0, 0.5), (1e-3, 0.125), (2.0, -0.2), (2.0, 0.0)])
 def test_scores_far_apart_and_equal(spread, scale):
-    x = make_decode([600, 45], 4, 1, 64, 32, io="f32", spread=spread, piece=128)
+    x = make_decode([600, 45], 4, 1, 64, 32, io="f32", spread=spread, shares=33)
     o, lse = call(x, scale=scale)
     compare(x, o, lse, scale=scale)
 
@@ -187,8 +189,8 @@ def test_decode_says_so_when_promises_are_not_kept():
     assert bool(o[1:3].isnan().all()) and torch.equal(o[3].isfinite(), torch.ones_like(o[3], dtype=torch.bool))
     x = make_decode([40], 4, 2, 128, 16)
     x["table"] = x["table"][:, :2].contiguous()         # a table of two pages for forty tokens
-    for piece in (0, 128):
-        o, lse = call(dict(x, piece=piece), max_length=400)
+    for shares in (0, -1, 5):
+        o, lse = call(dict(x, shares=shares), max_length=400)
         assert bool(o.isnan().all()) and bool(lse.isnan().all())
 
 

@@ -113,8 +113,8 @@ def test_append_needs_keys_values_and_positions():
 
 BAD_DECODE = [
     (dict(io_dtype=7), DTYPE), (dict(B=0), SHAPE), (dict(B=65536), SHAPE), (dict(Hk=0), SHAPE), (dict(Hq=2), SHAPE), (dict(Hq=10), SHAPE), (dict(K=96), SHAPE), (dict(max_length=-1), SHAPE), (dict(B=65535, Hq=64), SHAPE),
-    (dict(max_length=2 ** 31 - 1), SHAPE), (dict(B=100, max_length=2 ** 30, piece=128), SHAPE),
-    (dict(window=-1), PARAM), (dict(piece=64), PARAM), (dict(piece=-128), PARAM), (dict(scale=float("nan")), PARAM), (dict(scale=float("inf")), PARAM),
+    (dict(max_length=2 ** 31 - 1), SHAPE), (dict(B=100, Hk=8, max_length=2 ** 30), SHAPE),
+    (dict(window=-1), PARAM), (dict(shares=-2), PARAM), (dict(shares=65536), PARAM), (dict(scale=float("nan")), PARAM), (dict(scale=float("inf")), PARAM),
 ]
 
 
@@ -133,7 +133,7 @@ def test_decode_pointers_and_workspace():
     none = ctypes.POINTER(ob.OsdnRows)()
     p = ob.make_decode_params(2, 8, 4, 64, True, 100000)
     n = ob.osdn_paged_decode_workspace_bytes(p)
-    assert n > 0 and n % (2 * 8 * 66 * 4) == 0
+    assert n > 0
     call = lambda q, lens, o, ws, size: L.osdn_paged_decode(ctypes.byref(p), c, q, lens, None, o, None, ws, size, None)
     assert call(none, FAKE, r, FAKE, n) == NULL
     assert call(r, None, r, FAKE, n) == NULL
@@ -142,7 +142,7 @@ def test_decode_pointers_and_workspace():
     assert call(r, FAKE, r, FAKE, n - 1) == WORKSPACE
     assert call(r, FAKE, r, FAKE + 4, n) == WORKSPACE
     assert call(r, FAKE, ctypes.byref(rows(batch=0)), FAKE, n) == SHAPE
-    assert ob.osdn_paged_decode_workspace_bytes(ob.make_decode_params(2, 8, 4, 64, True, 128)) == 0          # one piece
+    assert ob.osdn_paged_decode_workspace_bytes(ob.make_decode_params(2, 8, 4, 64, True, 128)) == 0          # no second kernel
     assert ob.osdn_paged_decode_workspace_bytes(ob.make_decode_params(2, 8, 4, 64, True, 0)) == 0
 
 
