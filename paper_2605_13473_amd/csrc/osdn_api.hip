@@ -440,7 +440,7 @@ int osdn_qk_norm_fwd(const osdn_norm_params *p, const osdn_rows *q, const osdn_r
 
 size_t osdn_qk_norm_bwd_workspace_bytes(const osdn_norm_params *p) {
     if (check_norm(p) != OSDN_OK) return 0;
-    return (size_t)heads_bwd_workgroups((long long)p->B * p->T) * 2 * p->K * sizeof(float);
+    return (size_t)heads_plan((long long)p->B * p->T, p->Hq, p->Hk, p->K, p->io_dtype == OSDN_BF16, false, true).workgroups * 2 * p->K * sizeof(float);
 }
 
 int osdn_qk_norm_bwd(const osdn_norm_params *p, const osdn_rows *q, const osdn_rows *k, const float *weight_q, const float *weight_k,
@@ -499,7 +499,7 @@ static int check_decode(const osdn_decode_params *p, DecodeArgs &a, size_t &byte
     if (!std::isfinite(p->scale) || p->window < 0 || p->shares < -1 || p->shares > 65535) return OSDN_ERR_PARAM;
     a.head_tiles = (p->Hq / p->Hk + 15) / 16;
     a.part_heads = p->Hq / p->Hk < 16 ? p->Hq / p->Hk : 16;
-    const long long rows = (long long)p->B * p->Hk * a.head_tiles, units = decode_units(p->max_length, p->window);
+    const long long rows = (long long)p->B * p->Hk * a.head_tiles, units = decode_units(p->max_length, p->window, p->K, p->io_dtype == OSDN_BF16);
     if (rows * units > 0x7fffffffLL) return OSDN_ERR_SHAPE;            // (units are counted in 32 bits)
     a.shares = p->shares == -1 ? 0 : p->shares ? p->shares : decode_shares(rows, units, p->K, p->io_dtype == OSDN_BF16);
     bytes = !a.shares ? 0 : (size_t)a.shares * 2 * a.part_heads * (p->K + 2) * sizeof(float) + (size_t)rows * 2 * sizeof(int);

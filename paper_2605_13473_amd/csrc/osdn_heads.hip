@@ -246,7 +246,7 @@ __global__ __launch_bounds__(HEADS_T) void heads_fwd_kernel(HeadsArgs a) {
     }
 }
 
-// Backward: a wavefront walks tokens in steps of the grid, so that its sums over rows of dw stay in registers until the end; the
+// Backward: a wavefront walks (token, part) pairs in steps of the grid, so that its sums over rows of dw stay in registers until the end; the
 // partial sums of a workgroup go to a row of `partial` [gridDim.x][2][K], which heads_dw_kernel adds up in a fixed order.
 template <typename T, int K, bool VEC, int ROT>
 __global__ __launch_bounds__(HEADS_T) void heads_bwd_kernel(HeadsArgs a) {
@@ -266,14 +266,17 @@ __global__ __launch_bounds__(HEADS_T) void heads_bwd_kernel(HeadsArgs a) {
         }
     }
 
-    for (unsigned token = __builtin_amdgcn_readfirstlane(blockIdx.x * WAVES + wave); token < (unsigned)a.tokens; token += gridDim.x * WAVES) {
-        const int b = token / (unsigned)a.T, t = token % (unsigned)a.T;
+    const unsigned items = (unsigned)a.tokens * (unsigned)a.parts, stride = gridDim.x * WAVES;
+    for (unsigned item = __builtin_amdgcn_readfirstlane(blockIdx.x * WAVES + wave); item < items; item += stride) {
+        const unsigned token = item / (unsigned)a.parts;
+        const int part = item % (unsigned)a.parts, b = token / (unsigned)a.T, t = token % (unsigned)a.T;
+        const int blk_end = min(a.blocks, (part + 1) * a.per_part);
         const int pos = a.positions ? a.positions[token] : t;
         const bool none = pos < 0;
         const bool off_table = ROT && pos >= a.rotary_rows;
         float c[VE], s[VE];
         if constexpr (ROT != ROT_NONE) turn.load(a.rotary + (size_t)(none || off_table ? 0 : pos) * a.rotary_dim, a.rotary_dim, c, s);
-        for (int blk0 = 0; blk0 < a.blocks; blk0 += NB) {
+        for (int blk0 = part * a.per_part; blk0 < blk_end; blk0 += NB) {
             u32x4 rx[NB], rz[NB];
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
@@ -281,7 +284,7 @@ __global__ __launch_bounds__(HEADS_T) void heads_bwd_kernel(HeadsArgs a) {
                 const bool query = blk < a.q_blocks;
                 const int h = (query ? blk : blk - a.q_blocks) * ROWS + sub;
                 rx[i] = rz[i] = u32x4{0u, 0u, 0u, 0u};
-                if (h < (query ? a.Hq : a.Hk)) {
+                if (blk < blk_end && h < (query ? a.Hq : a.Hk)) {
                     rx[i] = load_row<T, VEC>(row_at<const T, VEC>(query ? a.q : a.k, b, t, h) + e0);
                     rz[i] = load_row<T, VEC>(row_at<const T, VEC>(query ? a.dq_out : a.dk_out, b, t, h) + e0);
                 }
@@ -291,7 +294,7 @@ __global__ __launch_bounds__(HEADS_T) void heads_bwd_kernel(HeadsArgs a) {
                 const int blk = blk0 + i;
                 const bool query = blk < a.q_blocks;
                 const int h = (query ? blk : blk - a.q_blocks) * ROWS + sub;
-                if (blk >= a.blocks) break;
+                if (blk >= blk_end) break;
                 const bool live = h < (query ? a.Hq : a.Hk);
                 float x[VE], dy[VE], g[VE];
                 unpack<T>(rx[i], x);
@@ -374,23 +377,18 @@ __global__ __launch_bounds__(DW_T) void heads_dw_kernel(const float *partial, in
 }
 
 namespace {
-template <typename T, int K> void count_blocks(HeadsArgs &a) {
-    constexpr int ROWS = HeadRow<T, K>::ROWS;
-    a.q_blocks = (a.Hq + ROWS - 1) / ROWS;
-    a.k_blocks = (a.Hk + ROWS - 1) / ROWS;
-    a.blocks = a.q_blocks + a.k_blocks * (a.append ? 2 : 1);
+template <typename T, int K> int cut(HeadsArgs &a, bool backward) {
+    const HeadsPlan h = heads_plan(a.tokens, a.Hq, a.Hk, K, sizeof(T) == 2, a.append, backward);
+    a.q_blocks = h.q_blocks; a.k_blocks = h.k_blocks; a.blocks = h.blocks; a.parts = h.parts; a.per_part = h.per_part;
+    return h.workgroups;
 }
 template <typename T, int K, bool VEC, int ROT> void fwd_of(HeadsArgs a, hipStream_t st) {
-    count_blocks<T, K>(a);
-    a.per_part = heads_blocks_per_wave(a.tokens, a.blocks);
-    a.parts = (a.blocks + a.per_part - 1) / a.per_part;
-    const dim3 g((unsigned)heads_fwd_workgroups((long long)a.tokens * a.parts)), t(HEADS_T);
+    const dim3 g((unsigned)cut<T, K>(a, false)), t(HEADS_T);
     if (a.append) hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, true>), g, t, 0, st, a);
     else hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, false>), g, t, 0, st, a);
 }
 template <typename T, int K, bool VEC, int ROT> void bwd_of(HeadsArgs a, hipStream_t st) {
-    count_blocks<T, K>(a);
-    const int n = heads_bwd_workgroups(a.tokens);
+    const int n = cut<T, K>(a, true);
     hipLaunchKernelGGL((heads_bwd_kernel<T, K, VEC, ROT>), dim3((unsigned)n), dim3(HEADS_T), 0, st, a);
     if (a.partial)
         hipLaunchKernelGGL(heads_dw_kernel, dim3(2 * K / DW_COLS), dim3(DW_T), 0, st, a.partial, n, K, a.dweight_q, a.dweight_k);

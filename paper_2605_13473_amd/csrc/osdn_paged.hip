@@ -37,7 +37,7 @@ __device__ __forceinline__ float max_xor32(float x) {
 
 template <typename T, int K> struct DecodeTile {
     static constexpr bool BF = sizeof(T) == 2;
-    static constexpr int TT = BF && K <= 128 ? 32 : 16; // tokens: the depth of the second product's matrix instruction (fp32: four of them; wide rows: half, for the registers)
+    static constexpr int TT = decode_tile(K, BF);       // tokens: the depth of the second product's matrix instruction (fp32: four of them)
     static constexpr int SETS = TT / 16;                // 16-token products that make the scores
     static constexpr int VE = 16 / sizeof(T);           // elements of a 16-byte vector
     static constexpr int STEPS = K / (4 * VE);          // vectors of a row, per lane (four lanes share a row)
@@ -86,21 +86,13 @@ __device__ __forceinline__ bool broken(const DecodeArgs &a, int length, int seq)
     return (unsigned)seq >= (unsigned)a.n_seqs || length > a.max_length || (length > 0 && (length - 1) >> a.page_shift >= a.max_pages);
 }
 __device__ __forceinline__ int first_seen(const DecodeArgs &a, int length) { return a.window > 0 && length > a.window ? length - a.window : 0; }
-// Units of DECODE_UNIT tokens, from a multiple of DECODE_TILE on, of each row of sequence b; one where there is nothing to see, so that its zeros
+// Units of UNIT tokens, from a multiple of DECODE_TILE on, of each row of sequence b; one where there is nothing to see, so that its zeros
 // (or NaN) are written
-__device__ __forceinline__ int units_of(const DecodeArgs &a, int b) {
+template <int UNIT> __device__ __forceinline__ int units_of(const DecodeArgs &a, int b) {
     const int length = a.lengths[b], seq = a.seq ? a.seq[b] : b;
     if (length <= 0 || broken(a, length, seq)) return 1;
-    return (length - (first_seen(a, length) & ~(DECODE_TILE - 1)) + DECODE_UNIT - 1) / DECODE_UNIT;
+    return (length - (first_seen(a, length) & ~(DECODE_TILE - 1)) + UNIT - 1) / UNIT;
 }
-
-// The even shares of n units among W workgroups: the first n % W have one more
-struct Shares {
-    int q, rem;
-    __device__ __forceinline__ Shares(int n, int W) : q(n / W), rem(n % W) {}
-    __device__ __forceinline__ int begin(int w) const { return w * q + min(w, rem); }
-    __device__ __forceinline__ int owner(int unit) const { return unit < rem * (q + 1) ? unit / (q + 1) : rem + (unit - rem * (q + 1)) / q; }
-};
 
 // SHARED: even shares; else a workgroup takes one row, whole (short rows, or many: no search and no second kernel)
 template <typename T, int K, bool SHARED>
@@ -118,17 +110,17 @@ __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kern
     if constexpr (!SHARED) {
         b = w / (unsigned)rows;
         base = 0;
-        const int u = units_of(a, b);
+        const int u = units_of<STRIDE>(a, b);
         at = (w - b * rows) * u;
         until = at + u;
     } else {
         if (a.B == 1) {
-            total = units_of(a, 0) * rows;
+            total = units_of<STRIDE>(a, 0) * rows;
             b = base = 0;
         } else {                        // where the share begins: a sum over the sequences before it, a run of them a thread
             const int run = (a.B + DEC_T - 1) / DEC_T, i0 = threadIdx.x * run, i1 = min(a.B, i0 + run);
             int mine = 0;
-            for (int i = i0; i < i1; ++i) mine += units_of(a, i);
+            for (int i = i0; i < i1; ++i) mine += units_of<STRIDE>(a, i);
             int upto = mine;
 #pragma unroll
             for (int x = 1; x < 64; x <<= 1) {
@@ -146,10 +138,10 @@ __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kern
             total = __builtin_amdgcn_readfirstlane(total) * rows;
             const int start = Shares(total, a.shares).begin(w);
             if (start >= before * rows && start < (before + mine) * rows) {
-                int i = i0, u = units_of(a, i);
+                int i = i0, u = units_of<STRIDE>(a, i);
                 while (start >= (before + u) * rows) {
                     before += u;
-                    u = units_of(a, ++i);
+                    u = units_of<STRIDE>(a, ++i);
                 }
                 found[0] = i;
                 found[1] = before * rows;
@@ -166,14 +158,14 @@ __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kern
     const int share_begin = at;
 
     do {
-        const int units = units_of(a, b), kt = (at - base) / units, u0 = at - base - kt * units, u1 = min(units, u0 + until - at);
+        const int units = units_of<STRIDE>(a, b), kt = (at - base) / units, u0 = at - base - kt * units, u1 = min(units, u0 + until - at);
         const int kv = a.head_tiles == 1 ? kt : kt / a.head_tiles, h0 = kv * a.group + 16 * (kt - kv * a.head_tiles);
         const int heads = min(16, (kv + 1) * a.group - h0);
         const int seq = a.seq ? a.seq[b] : b, length = a.lengths[b], lo = first_seen(a, length);
         const bool bad_call = broken(a, length, seq);
         const int *row = a.table + (bad_call ? 0 : seq * a.table_stride);
-        const int begin = (lo & ~(DECODE_TILE - 1)) + u0 * DECODE_UNIT;
-        const int end = bad_call ? 0 : u1 == units ? length : begin + (u1 - u0) * DECODE_UNIT;
+        const int begin = (lo & ~(DECODE_TILE - 1)) + u0 * STRIDE;
+        const int end = bad_call ? 0 : u1 == units ? length : begin + (u1 - u0) * STRIDE;
         TileLoads<T, K> x;
         x.ask(a, row, begin + wave * TT, lane);
         // queries: lane l holds head l % 16
@@ -333,7 +325,7 @@ __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kern
         if (wave == 0 && g == 0) { all[0][col] = M; all[1][col] = L; }
         __syncthreads();
         const bool alone = !SHARED || u1 - u0 == units;                     // (nothing to join)
-        const size_t slot = 2 * (size_t)w + (at == share_begin ? 0 : 1);    // a share has at most two rows that are not whole: its first and its last
+        const size_t slot = part_slot(w, at == share_begin);
         if (SHARED && u0 == 0 && threadIdx.x == 0) {
             const int last = alone ? w : Shares(total, a.shares).owner(at + units - 1);
             a.info[((size_t)b * rows + kt) * 2] = (int)slot;
@@ -397,7 +389,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
     const int *info = a.info + ((size_t)bh / a.Hq * a.Hk * a.head_tiles + kv * a.head_tiles + (in >> 4)) * 2;
     const int first_slot = info[0], n = info[1];
     if (n <= 1) return;                 // decode_kernel has written it
-    auto place = [&](int i) { return (size_t)(i == 0 ? first_slot : (first_slot & ~1) + 2 * i) * a.part_heads + hh; };
+    auto place = [&](int i) { return (size_t)part_of_row(first_slot, i) * a.part_heads + hh; };
     const float *ml = a.part_ml, *po = a.part_o + c0;
     // the first four of a lane's parts are on their way before the maximum is known
     constexpr int STEP = ROWS * WAVES, AHEAD = 4;

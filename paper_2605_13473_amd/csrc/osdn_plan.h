@@ -242,31 +242,70 @@ inline int heads_blocks_per_wave(long long tokens, int blocks) {
 // Workgroups (four wavefronts) for so many (token, part) pairs: 65536 tokens appended with up to 2048, 4096 and 16384 of them 190, 180 and 173 us
 inline int heads_fwd_workgroups(long long items) { return (int)(items < 4 * 16384 ? (items + 3) / 4 : 16384); }
 // ... of heads_bwd_kernel, each with a row of partial sums: 2 x 8192 x (32 + 8) heads with 1024 and 2048 178 and 179 us (both passes), 4 x 2048 x (16 + 4) of 64 33 and 36
-inline int heads_bwd_workgroups(long long tokens) { return (int)(tokens < 4 * 1024 ? (tokens + 3) / 4 : 1024); }
+constexpr int HEADS_BWD_WGS = 1024;
+inline int heads_bwd_workgroups(long long items) { return (int)(items < 4 * HEADS_BWD_WGS ? (items + 3) / 4 : HEADS_BWD_WGS); }
+// Blocks of a token for one of its wavefronts: all where the tokens give every wavefront one, else as few as that takes (fours, as its loads go, from
+// four on).  us, all and so: 27 tokens of 48 blocks 31.6 and 5.1, 502 of 20 19.7 and 10.8.
+inline int heads_bwd_blocks_per_wave(long long tokens, int blocks) {
+    const long long per = tokens * blocks / (4 * HEADS_BWD_WGS);
+    return (int)(per < 1 ? 1 : per > blocks ? blocks : per < 4 ? per : per / 4 * 4);
+}
+// How a call is cut: the blocks of rows of a token's queries, of all its rows (`values`: those of the keys count twice), for one wavefront, and
+// how many wavefronts that makes; the workgroups
+struct HeadsPlan { int q_blocks, k_blocks, blocks, per_part, parts, workgroups; };
+inline HeadsPlan heads_plan(long long tokens, int Hq, int Hk, int K, bool bf16, bool values, bool backward) {
+    const int rows = 1024 / (K * (bf16 ? 2 : 4));
+    HeadsPlan h{};
+    h.q_blocks = (Hq + rows - 1) / rows;
+    h.k_blocks = (Hk + rows - 1) / rows;
+    h.blocks = h.q_blocks + h.k_blocks * (values ? 2 : 1);
+    h.per_part = backward ? heads_bwd_blocks_per_wave(tokens, h.blocks) : heads_blocks_per_wave(tokens, h.blocks);
+    h.parts = (h.blocks + h.per_part - 1) / h.per_part;
+    h.workgroups = backward ? heads_bwd_workgroups(tokens * h.parts) : heads_fwd_workgroups(tokens * h.parts);
+    return h;
+}
 
 // Attention over a paged cache: tokens that a sequence of at most max_length may see, counted from a multiple of the tile of 32
-constexpr int DECODE_TILE = 32, DECODE_UNIT = 128, DEC_THREADS = 256;       // a unit: a tile for each of the workgroup's four wavefronts (K = 256 and fp32: two)
+constexpr int DECODE_TILE = 32, DEC_THREADS = 256;
+// Tokens of a wavefront's tile (wide rows: half, for the registers), and of a unit: a tile for each of a workgroup's four wavefronts
+constexpr int decode_tile(int K, bool bf16) { return bf16 && K <= 128 ? 32 : 16; }
+constexpr int decode_unit(int K, bool bf16) { return DEC_THREADS / 64 * decode_tile(K, bf16); }
 inline long long decode_span(int max_length, int window) {
     const long long seen = window > 0 && window < max_length ? (long long)window + DECODE_TILE - 1 : max_length;
     return seen < max_length ? seen : max_length;
 }
-inline long long decode_units(int max_length, int window) {
-    const long long units = (decode_span(max_length, window) + DECODE_UNIT - 1) / DECODE_UNIT;
+inline long long decode_units(int max_length, int window, int K, bool bf16) {
+    const long long units = (decode_span(max_length, window) + decode_unit(K, bf16) - 1) / decode_unit(K, bf16);
     return units < 1 ? 1 : units;
 }
 // ... and the shares that they are cut into for `rows` (sequence, group of query heads) pairs, 0: a row each and no second kernel.  us, four heads of the
 // cache of K = 128 in bf16 unless said; "uneven": lengths spread from 1 to the longest.
 //  - a row each for short rows, and for up to 1024 tokens where the rows fill the chip, against 512 shares: 1 x 300 tokens 9.3 and 10.3, 256 x 300
-//    35.7 and 39.7, uneven 512 x 300 41 and 56; 64 x 1000 32.2 and 33.3, uneven 512 x 1000 108 and 116; but 1 x 500 12.0 and 10.3, 16 x 500 14.0 and 12.8,
+//    35.7 and 39.7, uneven 512 x 300 41 and 56; 32 x 500 14.4 and 15.2; 64 x 1000 32.2 and 33.3, uneven 512 x 1000 108 and 116; but 1 x 500 12.0 and
+//    10.3, 16 x 500 14.0 and 12.8, 32 x 1000 22.8 and 20.3,
 //    uneven 256 x 2000 125 and 114, 512 x 4096 429 and 380.
 //  - two shares a CU, which start and end together whatever the lengths.  With 256, 512, 768 and 1024: 1 x 131072 x 8 heads 99.8, 99.5, 99.9, 101;
 //    uneven 512 x 4096 392, 379, 382, 383, 64 x 8192 x 8 199, 186, 187, 188; 16 x 4096 x 8, K = 256, 100, 104, 121, 106; fp32 115, 102, 119, 102.  With 384 and
 //    640, half a share a CU more or less, 434 and 414 for the first of the uneven ones.  K = 64, three: uneven 64 x 4096 x 8 72.5, 63.5, 57.8, 62.7; fp32
 //    and K = 256, whose registers hold one workgroup, one: 8 x 4096 63.5, 68.4, 74.0, 79.4.
 inline int decode_shares(long long rows, long long units, int K, bool bf16) {
-    if (units <= 3 || (rows >= NUM_CU && units <= 8)) return 0;
+    const long long tokens = units * decode_unit(K, bf16);
+    if (units <= 3 || (rows >= NUM_CU && tokens <= 1024) || (rows >= NUM_CU / 2 && tokens <= 512)) return 0;
     const long long most = NUM_CU * (K == 64 ? 3 : K == 256 && !bf16 ? 1 : 2);
     return (int)(rows * units < most ? rows * units : most);
 }
+
+// (constexpr: for the device too)
+// The even shares of n units among W workgroups: the first n % W have one more.  `owner`: the share that a unit falls to.
+struct Shares {
+    int q, rem;
+    constexpr Shares(int n, int W) : q(n / W), rem(n % W) {}
+    constexpr int begin(int w) const { return w * q + (w < rem ? w : rem); }
+    constexpr int owner(int unit) const { return unit < rem * (q + 1) ? unit / (q + 1) : rem + (unit - rem * (q + 1)) / q; }
+};
+// Where share w leaves its part of a row that it does not hold whole: a share has at most two of those, its first row and its last.  A row's
+// parts are those of its first share, which may be either, and of the ones behind it, which begin with it.
+constexpr int part_slot(int w, bool first_of_share) { return 2 * w + (first_of_share ? 0 : 1); }
+constexpr int part_of_row(int first_slot, int i) { return i == 0 ? first_slot : (first_slot & ~1) + 2 * i; }
 
 }  // namespace osdn

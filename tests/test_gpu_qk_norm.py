@@ -173,7 +173,10 @@ def test_one_of_the_two_and_repeatable():
         again = ob.qk_norm_backward(x["q"], x["k"], x["dq"], x["dk"], x["wq"], x["wk"], x["table"], None, x["hp"])
         assert all(torch.equal(first[n], again[n]) for n in first)
     only = ob.qk_norm_backward(None, x["k"], None, x["dk"], None, x["wk"], x["table"], None, x["hp"])
-    assert only["dq"] is None and torch.equal(only["dk"], first["dk"]) and torch.equal(only["dweight_k"], first["dweight_k"])
+    assert only["dq"] is None and torch.equal(only["dk"], first["dk"])
+    # (a call without queries is cut otherwise: the weights' sums in another order, each within the bound of the exact ones)
+    size = (1.5 * x["dk"].float().abs().amax(-1, keepdim=True) * ob.qk_norm(None, x["k"], hp=x["hp"])[1].float().abs()).sum((0, 1, 2))
+    assert ((only["dweight_k"] - first["dweight_k"]).abs() <= 2 * 2.0 ** -18 * size).all()
 
 
 def test_rows_of_zeros_and_positions_off_the_table():
