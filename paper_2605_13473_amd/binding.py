@@ -507,6 +507,19 @@ def alloc_paged_cache(n_pages: int, page_size: int, H: int, K: int, dtype=torch.
     return tuple(torch.empty(n_pages, H, page_size, K, dtype=dtype, device=device).transpose(1, 2) for _ in range(2))
 
 
+def _here(t, name):
+    """Launches go to the current device, which need not see the memory of another."""
+    if t.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"{name}: is on {t.device}, the current device is {torch._C._cuda_getDevice()}")
+
+
+def _array(t, dtype, shape, name):
+    p = _ptr(t, dtype, shape, name)
+    if t is not None:
+        _here(t, name)
+    return p
+
+
 def _rows(t, dtype, shape, name):
     """Rows of the last axis, wherever they stand: [B,T,H,K], or [B,H,K]."""
     if t is None:
@@ -517,8 +530,7 @@ def _rows(t, dtype, shape, name):
         raise TypeError(f"{name}: expected dtype {dtype}, got {t.dtype}")
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.device.index != torch._C._cuda_getDevice():
-        raise ValueError(f"{name}: is on {t.device}, the current device is {torch._C._cuda_getDevice()}")
+    _here(t, name)
     st = t.stride()
     if st[-1] != 1:
         raise ValueError(f"{name}: the elements of a row must be adjacent")
@@ -535,6 +547,7 @@ def _cache(k_cache, v_cache, page_table, dtype, H, K):
         raise TypeError("page_table: expected an int32 CUDA/HIP torch tensor")
     if page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
         raise ValueError("page_table: expected [n_seqs, max_pages] with adjacent entries of a row")
+    _here(page_table, "page_table")
     n_seqs, max_pages = page_table.shape
     k, v = k_cache.stride(), v_cache.stride()
     stride = page_table.stride(0) if n_seqs > 1 else max_pages
@@ -554,8 +567,8 @@ def _norm_rows(p, q, k, *more):
 
 def _norm_shared(p, weight_q, weight_k, rotary, positions):
     f32 = torch.float32
-    return (_ptr(weight_q, f32, (p.K,), "weight_q"), _ptr(weight_k, f32, (p.K,), "weight_k"),
-            _ptr(rotary, f32, (p.rotary_rows, p.rotary_dim), "rotary"), _ptr(positions, torch.int32, (p.B, p.T), "positions"))
+    return (_array(weight_q, f32, (p.K,), "weight_q"), _array(weight_k, f32, (p.K,), "weight_k"),
+            _array(rotary, f32, (p.rotary_rows, p.rotary_dim), "rotary"), _array(positions, torch.int32, (p.B, p.T), "positions"))
 
 
 def osdn_qk_norm_fwd(params, q, k, weight_q, weight_k, rotary, positions, q_out, k_out, stream=None):
@@ -574,7 +587,7 @@ def osdn_qk_norm_bwd(params, q, k, weight_q, weight_k, rotary, positions, dq_out
     r = _norm_rows(p, q, k, (dq_out, "dq_out"), (dk_out, "dk_out"), (dq, "dq"), (dk, "dk"))
     _check(lib().osdn_qk_norm_bwd(
         ctypes.byref(p), _ref(r[0]), _ref(r[1]), *_norm_shared(p, weight_q, weight_k, rotary, positions), *(_ref(x) for x in r[2:]),
-        _ptr(dweight_q, f32, (p.K,), "dweight_q"), _ptr(dweight_k, f32, (p.K,), "dweight_k"), _ptr(workspace, torch.uint8, None, "workspace"),
+        _array(dweight_q, f32, (p.K,), "dweight_q"), _array(dweight_k, f32, (p.K,), "dweight_k"), _array(workspace, torch.uint8, None, "workspace"),
         ctypes.c_size_t(0 if workspace is None else workspace.numel()), _stream_ptr(stream)))
 
 
@@ -584,7 +597,7 @@ def osdn_paged_append(params, q, k, v, k_cache, v_cache, page_table, weight_q, w
     cache = _cache(k_cache, v_cache, page_table, _io_torch_dtype(p), p.Hk, p.K)
     _check(lib().osdn_paged_append(
         ctypes.byref(p), ctypes.byref(cache), *(_ref(x) for x in r[:3]), *_norm_shared(p, weight_q, weight_k, rotary, positions),
-        _ptr(seq, torch.int32, (p.B, p.T), "seq"), _ref(r[3]), _stream_ptr(stream)))
+        _array(seq, torch.int32, (p.B, p.T), "seq"), _ref(r[3]), _stream_ptr(stream)))
 
 
 def osdn_paged_decode_workspace_bytes(params) -> int:
@@ -597,8 +610,8 @@ def osdn_paged_decode(params, q, k_cache, v_cache, page_table, lengths, seq, o, 
     qr, orows = _rows(q, io, rows, "q"), _rows(o, io, rows, "o")
     cache = _cache(k_cache, v_cache, page_table, io, p.Hk, p.K)
     _check(lib().osdn_paged_decode(
-        ctypes.byref(p), ctypes.byref(cache), _ref(qr), _ptr(lengths, i32, (p.B,), "lengths"), _ptr(seq, i32, (p.B,), "seq"), _ref(orows),
-        _ptr(lse, torch.float32, (p.B, p.Hq), "lse"), _ptr(workspace, torch.uint8, None, "workspace"),
+        ctypes.byref(p), ctypes.byref(cache), _ref(qr), _array(lengths, i32, (p.B,), "lengths"), _array(seq, i32, (p.B,), "seq"), _ref(orows),
+        _array(lse, torch.float32, (p.B, p.Hq), "lse"), _array(workspace, torch.uint8, None, "workspace"),
         ctypes.c_size_t(0 if workspace is None else workspace.numel()), _stream_ptr(stream)))
 
 

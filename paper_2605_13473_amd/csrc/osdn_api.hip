@@ -322,7 +322,7 @@ const char *osdn_strerror(int status) {
                                      "attention layer: K in {64,128,256}, rotary_dim a multiple of 16, page_size a power of two, rows of a cache on 16 bytes)";
         case OSDN_ERR_DTYPE: return "io_dtype must be OSDN_F32 or OSDN_BF16";
         case OSDN_ERR_WORKSPACE: return "workspace too small or not 256-byte aligned";
-        case OSDN_ERR_PARAM: return "invalid scalar parameter (eta < 0, eps <= 0 or non-finite)";
+        case OSDN_ERR_PARAM: return "invalid scalar parameter (eta < 0, eps <= 0, non-finite, or a flag or scheduling field out of range)";
         case OSDN_ERR_LAUNCH: return "HIP launch error";
         default: return "unknown status";
     }

@@ -62,6 +62,8 @@ DECODE = [
     dict(lengths=[5000, 4096, 4097, 1], Hq=4, Hk=1, K=128, page=64, shares=7),
     dict(lengths=[130] * 70, Hq=2, Hk=2, K=64, page=32),
     dict(lengths=[20000], Hq=2, Hk=1, K=128, page=64),
+    dict(lengths=[(37 * i) % 200 - 3 for i in range(600)], Hq=2, Hk=1, K=64, page=16, shares=50),
+    dict(lengths=[(91 * i) % 400 for i in range(300)], Hq=3, Hk=1, K=256, page=32, io="f32", window=150),
 ]
 
 
