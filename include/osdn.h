@@ -257,7 +257,8 @@ int osdn_bwd_packed(const osdn_params *p, const void *q, const void *k, const vo
 /*
  * Around the recurrence: the rows of queries, keys and values of a layer, each K adjacent elements of io_dtype (K in {64, 128, 256}),
  * wherever the caller has them (slices of one projection's output, views): element (b, t, h, i) stands
- * batch b + token t + head h + i elements behind data.  No two rows of an output may overlap.  Rows
+ * batch b + token t + head h + i elements behind data.  No two rows of an output may overlap (a step of less than K along an axis
+ * of more than one is refused).  Rows
  * need no more alignment than their elements; rows that start on 16 bytes are read and written in one piece.
  */
 typedef struct { void *data; int64_t batch, token, head; } osdn_rows;
@@ -328,8 +329,8 @@ typedef struct {
  *   positions         [B,T] int32: place of the token in its sequence, also what it is rotated by.  Negative: no token,
  *                     nothing is appended and its query is zero
  *   seq               [B,T] int32 or NULL (=> the batch entry): the sequence (row of the table) that the token belongs to
- * A token whose sequence or page is not there is not appended.  Two tokens of one call with the same place: one of them
- * is what the place holds.  Nothing else in the cache is touched.
+ * A token whose sequence or page is not there is not appended.  Two tokens of one call must not have the same place (what it
+ * then holds is undefined).  Nothing else in the cache is touched.
  */
 int osdn_paged_append(const osdn_norm_params *p, const osdn_cache *cache, const osdn_rows *q, const osdn_rows *k, const osdn_rows *v,
                       const float *weight_q, const float *weight_k, const float *rotary, const int32_t *positions,
@@ -355,7 +356,7 @@ typedef struct {
  *   seq               [B] int32 or NULL (=> b): row of the table.  Several queries may read one sequence, each
  *                     with its own length: drafted tokens, or a prompt token by token
  *   lse               [B,Hq] fp32 or NULL
- *   workspace         osdn_paged_decode_workspace_bytes(p) bytes, 256-byte aligned (may be NULL if that is 0)
+ *   workspace         osdn_paged_decode_workspace_bytes(p) bytes (0 also for invalid parameters), 256-byte aligned; may be NULL if that is 0
  * B Hq is below 2^21, and B Hk max_length / 64 (with more than 16 query heads a key head as many times that) below 2^31.
  * What a length hides is not looked at, whatever the cache holds there.  A length above max_length or above what a row of the
  * table holds, a sequence or a page that is not there: o and lse are NaN, and nothing outside the cache is read.

@@ -483,6 +483,8 @@ class NormHyper:
 def make_norm_params(B, T, Hq, Hk, K, bf16: bool, hp: NormHyper = NormHyper(), rotary=None) -> OsdnNormParams:
     if hp.norm not in NORMS:
         raise ValueError(f"norm: expected one of {sorted(NORMS)}, got {hp.norm!r}")
+    if rotary is not None and (not isinstance(rotary, torch.Tensor) or rotary.dim() != 2):
+        raise TypeError("rotary: expected a table [positions, rotary_dim]")
     rows, dim = (0, 0) if rotary is None else rotary.shape
     return OsdnNormParams(B, T, Hq, Hk, K, OSDN_BF16 if bf16 else OSDN_F32, NORMS[hp.norm], dim, rows, int(bool(hp.interleaved)),
                           hp.eps)
@@ -623,24 +625,16 @@ def _params_of(q, k, hp, rotary):
     return make_norm_params(B, T, 0 if q is None else q.shape[2], 0 if k is None else k.shape[2], K, x.dtype == torch.bfloat16, hp, rotary)
 
 
-def _native_call(name, like, *args):
-    """The call through the extension module: its results, or None for what it leaves to the code below."""
-    if _lib is None:
-        lib()
-    if _rows_native is None or not isinstance(like, torch.Tensor) or not like.is_cuda:
-        return None
-    dev = torch._C._cuda_getDevice()
-    r = getattr(_rows_native, name)(*args, dev, torch._C._cuda_getCurrentRawStream(dev))
-    if type(r) is int:
-        _check(r)
-    return r
-
-
+# A call of plain tensors on the current device goes through the extension module, once the library is loaded (_rows_native is then set);
+# for what that leaves alone it returns None, and a status for what the library refuses.
 def qk_norm(q, k, weight_q=None, weight_k=None, rotary=None, positions=None, hp: NormHyper = NormHyper()):
     """Allocate outputs and call osdn_qk_norm_fwd (either of q and k may be None).  Returns (q_out, k_out)."""
-    r = _native_call("qk_norm", k if q is None else q, q, k, weight_q, weight_k, rotary, positions, hp)
-    if r is not None:
-        return r
+    x = k if q is None else q
+    if _rows_native is not None and type(x) is torch.Tensor and x.is_cuda:
+        dev = torch._C._cuda_getDevice()
+        r = _rows_native.qk_norm(q, k, weight_q, weight_k, rotary, positions, hp, dev, torch._C._cuda_getCurrentRawStream(dev))
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
     p = _params_of(q, k, hp, rotary)
     out = [None if x is None else x.new_empty(x.shape) for x in (q, k)]
     osdn_qk_norm_fwd(p, q, k, weight_q, weight_k, rotary, positions, *out)
@@ -650,9 +644,15 @@ def qk_norm(q, k, weight_q=None, weight_k=None, rotary=None, positions=None, hp:
 def qk_norm_backward(q, k, dq_out, dk_out, weight_q=None, weight_k=None, rotary=None, positions=None, hp: NormHyper = NormHyper()):
     """Allocate gradients and call osdn_qk_norm_bwd on the inputs of ``qk_norm``.  Returns a dict of dq, dk and, where there are
     weights, dweight_q, dweight_k."""
-    r = _native_call("qk_norm_backward", k if q is None else q, q, k, dq_out, dk_out, weight_q, weight_k, rotary, positions, hp)
-    if r is not None:
-        return dict(zip(("dq", "dk", "dweight_q", "dweight_k"), r))
+    x = k if q is None else q
+    if _rows_native is not None and type(x) is torch.Tensor and x.is_cuda:
+        dev = torch._C._cuda_getDevice()
+        r = _rows_native.qk_norm_backward(q, k, dq_out, dk_out, weight_q, weight_k, rotary, positions, hp, dev,
+                                          torch._C._cuda_getCurrentRawStream(dev))
+        if type(r) is tuple:
+            return {"dq": r[0], "dk": r[1], "dweight_q": r[2], "dweight_k": r[3]}
+        if r is not None:
+            _check(r)
     p = _params_of(q, k, hp, rotary)
     g = {"dq": None if q is None else q.new_empty(q.shape), "dk": None if k is None else k.new_empty(k.shape),
          "dweight_q": None if weight_q is None else torch.empty_like(weight_q), "dweight_k": None if weight_k is None else torch.empty_like(weight_k)}
@@ -667,9 +667,12 @@ def paged_append(k, v, k_cache, v_cache, page_table, positions, seq=None, q=None
                  hp: NormHyper = NormHyper()):
     """Append keys (normed and rotated) and values [B,T,Hk,K] to a paged cache [n_pages, page_size, Hk, K]; with q [B,T,Hq,K],
     returns the queries normed and rotated alike, from the same launch."""
-    r = _native_call("paged_append", k, k, v, k_cache, v_cache, page_table, positions, seq, q, weight_q, weight_k, rotary, hp)
-    if r is not None:
-        return r[0]
+    if _rows_native is not None and type(k) is torch.Tensor and k.is_cuda:
+        dev = torch._C._cuda_getDevice()
+        r = _rows_native.paged_append(k, v, k_cache, v_cache, page_table, positions, seq, q, weight_q, weight_k, rotary, hp, dev,
+                                      torch._C._cuda_getCurrentRawStream(dev))
+        if r is not None:
+            return r[0] if type(r) is tuple else _check(r)
     p = _params_of(q, k, hp, rotary)
     q_out = None if q is None else q.new_empty(q.shape)
     osdn_paged_append(p, q, k, v, k_cache, v_cache, page_table, weight_q, weight_k, rotary, positions, seq, q_out)
@@ -680,9 +683,14 @@ def paged_decode(q, k_cache, v_cache, page_table, lengths, seq=None, scale=None,
                  workspace=None):
     """Attention of one new token per sequence, q [B,Hq,K], over a paged cache.  max_length: no length is above it (None: what a
     row of the table can hold).  Returns o, or (o, lse)."""
-    r = _native_call("paged_decode", q, q, k_cache, v_cache, page_table, lengths, seq, workspace, scale, window, max_length, want_lse)
-    if r is not None:
-        return r if want_lse else r[0]
+    if _rows_native is not None and type(q) is torch.Tensor and q.is_cuda:
+        dev = torch._C._cuda_getDevice()
+        r = _rows_native.paged_decode(q, k_cache, v_cache, page_table, lengths, seq, workspace, scale, window, max_length, want_lse, dev,
+                                      torch._C._cuda_getCurrentRawStream(dev))
+        if type(r) is tuple:
+            return r if want_lse else r[0]
+        if r is not None:
+            _check(r)
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
         raise TypeError("expected q [B,Hq,K] and a cache [n_pages, page_size, Hk, K] as CUDA/HIP torch tensors")
     B, Hq, K = q.shape

@@ -383,26 +383,29 @@ static int check_norm(const osdn_norm_params *p) {
     return OSDN_OK;
 }
 
-// A batch of rows of H heads: `on` tells whether it is there, `out` that it is written (no two rows at one place).  The rows' addresses
-// are those of their elements; clears `aligned` unless every row starts on 16 bytes.
-static int take_rows(const osdn_rows *r, long long B, long long T, long long H, size_t es, bool out, HeadRows &to, bool &aligned) {
+// whether steps along axes of n entries keep rows of K elements apart (as far as one axis can tell)
+static bool apart(long long n, long long step, int K) { return n <= 1 || step >= K || step <= -K; }
+
+// A batch of rows of H heads (none: not looked at).  `out`: they are written, so no two may stand at one place.  Clears `aligned` unless
+// every row starts on 16 bytes.
+static int take_rows(const osdn_rows *r, long long B, long long T, long long H, int K, size_t es, bool out, HeadRows &to, bool &aligned) {
     if (H == 0) return OSDN_OK;
     if (!r || !r->data) return OSDN_ERR_NULL;
     const uintptr_t at = reinterpret_cast<uintptr_t>(r->data);
     if (at % es != 0) return OSDN_ERR_SHAPE;
-    if (out && ((B > 1 && r->batch == 0) || (T > 1 && r->token == 0) || (H > 1 && r->head == 0))) return OSDN_ERR_SHAPE;
+    if (out && !(apart(B, r->batch, K) && apart(T, r->token, K) && apart(H, r->head, K))) return OSDN_ERR_SHAPE;
     const long long ve = 16 / (long long)es;
     if (at % 16 != 0 || (B > 1 && r->batch % ve != 0) || (T > 1 && r->token % ve != 0) || (H > 1 && r->head % ve != 0)) aligned = false;
     to = HeadRows{r->data, r->batch, r->token, r->head};
     return OSDN_OK;
 }
 
-static int check_cache(const osdn_cache *c, int H, size_t es, int &shift) {
+static int check_cache(const osdn_cache *c, int H, int K, size_t es, int &shift) {
     if (!c || !c->k || !c->v || !c->table) return OSDN_ERR_NULL;
     if (c->n_pages < 1 || c->n_seqs < 1 || c->max_pages < 1 || c->page_size < 1 || (c->page_size & (c->page_size - 1)) != 0) return OSDN_ERR_SHAPE;
     if (c->table_stride < 0 || (c->table_stride < c->max_pages && c->table_stride != 0)) return OSDN_ERR_SHAPE;
-    if ((c->n_pages > 1 && (c->k_page == 0 || c->v_page == 0)) || (c->page_size > 1 && (c->k_token == 0 || c->v_token == 0)) ||
-        (H > 1 && (c->k_head == 0 || c->v_head == 0)))
+    if (!(apart(c->n_pages, c->k_page, K) && apart(c->n_pages, c->v_page, K) && apart(c->page_size, c->k_token, K) && apart(c->page_size, c->v_token, K) &&
+          apart(H, c->k_head, K) && apart(H, c->v_head, K)))
         return OSDN_ERR_SHAPE;
     const long long ve = 16 / (long long)es;
     for (long long s : {c->k_page, c->k_token, c->k_head, c->v_page, c->v_token, c->v_head})
@@ -430,8 +433,8 @@ int osdn_qk_norm_fwd(const osdn_norm_params *p, const osdn_rows *q, const osdn_r
     if (p->rotary_dim && !rotary) return OSDN_ERR_NULL;
     HeadsArgs a = heads_args(p, weight_q, weight_k, rotary, positions);
     const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
-    if ((rc = take_rows(q, p->B, p->T, p->Hq, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(k, p->B, p->T, p->Hk, es, false, a.k, a.aligned)) != OSDN_OK ||
-        (rc = take_rows(q_out, p->B, p->T, p->Hq, es, true, a.q_out, a.aligned)) != OSDN_OK || (rc = take_rows(k_out, p->B, p->T, p->Hk, es, true, a.k_out, a.aligned)) != OSDN_OK)
+    if ((rc = take_rows(q, p->B, p->T, p->Hq, p->K, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(k, p->B, p->T, p->Hk, p->K, es, false, a.k, a.aligned)) != OSDN_OK ||
+        (rc = take_rows(q_out, p->B, p->T, p->Hq, p->K, es, true, a.q_out, a.aligned)) != OSDN_OK || (rc = take_rows(k_out, p->B, p->T, p->Hk, p->K, es, true, a.k_out, a.aligned)) != OSDN_OK)
         return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (timed(KID_QK_NORM, st, [&] { return launch_heads_fwd(a, p->io_dtype == OSDN_BF16, st); }) != 0) return OSDN_ERR_SHAPE;
@@ -451,10 +454,10 @@ int osdn_qk_norm_bwd(const osdn_norm_params *p, const osdn_rows *q, const osdn_r
     if (p->rotary_dim && !rotary) return OSDN_ERR_NULL;
     HeadsArgs a = heads_args(p, weight_q, weight_k, rotary, positions);
     const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
-    if ((rc = take_rows(q, p->B, p->T, p->Hq, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(k, p->B, p->T, p->Hk, es, false, a.k, a.aligned)) != OSDN_OK ||
-        (rc = take_rows(dq_out, p->B, p->T, p->Hq, es, false, a.dq_out, a.aligned)) != OSDN_OK ||
-        (rc = take_rows(dk_out, p->B, p->T, p->Hk, es, false, a.dk_out, a.aligned)) != OSDN_OK ||
-        (rc = take_rows(dq, p->B, p->T, p->Hq, es, true, a.dq, a.aligned)) != OSDN_OK || (rc = take_rows(dk, p->B, p->T, p->Hk, es, true, a.dk, a.aligned)) != OSDN_OK)
+    if ((rc = take_rows(q, p->B, p->T, p->Hq, p->K, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(k, p->B, p->T, p->Hk, p->K, es, false, a.k, a.aligned)) != OSDN_OK ||
+        (rc = take_rows(dq_out, p->B, p->T, p->Hq, p->K, es, false, a.dq_out, a.aligned)) != OSDN_OK ||
+        (rc = take_rows(dk_out, p->B, p->T, p->Hk, p->K, es, false, a.dk_out, a.aligned)) != OSDN_OK ||
+        (rc = take_rows(dq, p->B, p->T, p->Hq, p->K, es, true, a.dq, a.aligned)) != OSDN_OK || (rc = take_rows(dk, p->B, p->T, p->Hk, p->K, es, true, a.dk, a.aligned)) != OSDN_OK)
         return rc;
     if (dweight_q || dweight_k) {
         rc = check_ws(workspace, workspace_bytes, osdn_qk_norm_bwd_workspace_bytes(p));
@@ -475,10 +478,10 @@ int osdn_paged_append(const osdn_norm_params *p, const osdn_cache *cache, const 
     if (p->Hk < 1) return OSDN_ERR_SHAPE;
     if ((p->rotary_dim && !rotary) || !positions) return OSDN_ERR_NULL;
     const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
-    if ((rc = check_cache(cache, p->Hk, es, shift)) != OSDN_OK) return rc;
+    if ((rc = check_cache(cache, p->Hk, p->K, es, shift)) != OSDN_OK) return rc;
     HeadsArgs a = heads_args(p, weight_q, weight_k, rotary, positions);
-    if ((rc = take_rows(q, p->B, p->T, p->Hq, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(k, p->B, p->T, p->Hk, es, false, a.k, a.aligned)) != OSDN_OK ||
-        (rc = take_rows(v, p->B, p->T, p->Hk, es, false, a.v, a.aligned)) != OSDN_OK || (rc = take_rows(q_out, p->B, p->T, p->Hq, es, true, a.q_out, a.aligned)) != OSDN_OK)
+    if ((rc = take_rows(q, p->B, p->T, p->Hq, p->K, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(k, p->B, p->T, p->Hk, p->K, es, false, a.k, a.aligned)) != OSDN_OK ||
+        (rc = take_rows(v, p->B, p->T, p->Hk, p->K, es, false, a.v, a.aligned)) != OSDN_OK || (rc = take_rows(q_out, p->B, p->T, p->Hq, p->K, es, true, a.q_out, a.aligned)) != OSDN_OK)
         return rc;
     a.append = true;
     a.cache_k = HeadRows{cache->k, cache->k_page, cache->k_token, cache->k_head};
@@ -520,9 +523,9 @@ int osdn_paged_decode(const osdn_decode_params *p, const osdn_cache *cache, cons
     if (rc != OSDN_OK) return rc;
     if (!lengths) return OSDN_ERR_NULL;
     const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
-    if ((rc = check_cache(cache, p->Hk, es, a.page_shift)) != OSDN_OK) return rc;
+    if ((rc = check_cache(cache, p->Hk, p->K, es, a.page_shift)) != OSDN_OK) return rc;
     a.aligned = true;
-    if ((rc = take_rows(q, p->B, 1, p->Hq, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(o, p->B, 1, p->Hq, es, true, a.o, a.aligned)) != OSDN_OK) return rc;
+    if ((rc = take_rows(q, p->B, 1, p->Hq, p->K, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(o, p->B, 1, p->Hq, p->K, es, true, a.o, a.aligned)) != OSDN_OK) return rc;
     if (a.shares) {
         rc = check_ws(workspace, workspace_bytes, bytes);
         if (rc != OSDN_OK) return rc;

@@ -69,7 +69,8 @@ def test_rows():
         assert L.osdn_qk_norm_fwd(ctypes.byref(p), a[0], a[1], None, None, None, None, a[2], a[3], None) == NULL
     assert norm_fwd(p, q=rows(at=FAKE + 1)) == SHAPE                     # not on an element
     for axis in ("batch", "token", "head"):
-        assert norm_fwd(p, qo=rows(**{axis: 0})) == SHAPE                # rows written to one place
+        for step in (0, 63, -63):
+            assert norm_fwd(p, qo=rows(**{axis: step})) == SHAPE         # rows written over one another
     assert L.osdn_qk_norm_fwd(None, r, r, None, None, None, None, r, r, None) == NULL
 
 
@@ -87,7 +88,8 @@ def test_gradients_of_weights_need_a_workspace():
 BAD_CACHE = [
     (dict(k=None), NULL), (dict(v=None), NULL), (dict(table=None), NULL), (dict(n_pages=0), SHAPE), (dict(page_size=0), SHAPE), (dict(page_size=24), SHAPE),
     (dict(n_seqs=0), SHAPE), (dict(max_pages=0), SHAPE), (dict(table_stride=7), SHAPE), (dict(table_stride=-8), SHAPE), (dict(k=FAKE + 8), SHAPE),
-    (dict(v=FAKE + 2), SHAPE), (dict(table=FAKE + 2), SHAPE), (dict(k_token=257), SHAPE), (dict(v_head=-64), SHAPE), (dict(k_head=0), SHAPE), (dict(v_page=0), SHAPE), (dict(k_token=0), SHAPE),
+    (dict(v=FAKE + 2), SHAPE), (dict(table=FAKE + 2), SHAPE), (dict(k_token=257), SHAPE), (dict(v_head=-64), SHAPE), (dict(k_head=0), SHAPE), (dict(v_page=0), SHAPE), (dict(k_token=0), SHAPE), (dict(k_head=56), SHAPE),
+    (dict(v_token=56), SHAPE),
 ]
 
 
