@@ -8,7 +8,8 @@
 // rows (a row: a sequence and a group of up to 16 query heads of one key head) make one list that is cut into even shares, one a
 // workgroup, whatever the lengths; a share is a part of a row, or the end of one, whole ones and the beginning of the last.  The four wavefronts of
 // a workgroup take a row's tiles in turn, each with a running maximum and sum of its own, and join at its end; rows that a share does
-// not hold whole go to a second kernel, which joins their parts in their order.  2.1 GB of keys and values of 512 sequences of 1 to 4096
+// not hold whole go to a second kernel, which joins their parts in their order (4 us; the fence that a join inside this one would take after every part
+// costs more: the next figures 900 and 180 us).  2.1 GB of keys and values of 512 sequences of 1 to 4096
 // tokens: 380 us, 5.6 TB/s (cut into pieces of 1024 tokens, a workgroup each, 401); 0.54 GB of one sequence 99 us, 5.4 TB/s.
 //
 // A wavefront's tile is TT tokens.  Keys go from memory to registers as the matrix product wants them (lane l: token l % 16, 16 bytes);
@@ -51,7 +52,7 @@ template <typename T, int K> struct TileLoads {
     using D = DecodeTile<T, K>;
     int page[D::SETS];
     u32x4 k[D::SETS][D::STEPS], v[D::SETS][D::STEPS];
-    // pages of the tile at token tok, as far as the table goes (whatever the length: it need not be known yet)
+    // pages of the tile at token tok, as far as the table goes (whatever the length)
     __device__ __forceinline__ void ask(const DecodeArgs &a, const int *row, int tok, int lane) {
 #pragma unroll
         for (int i = 0; i < D::SETS; ++i) page[i] = row[min((tok + 16 * i + (lane & 15)) >> a.page_shift, a.max_pages - 1)];
@@ -228,7 +229,7 @@ __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kern
 #pragma unroll
                     for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) x.v[i][s][w] = seen ? x.v[i][s][w] : 0u;
+                        for (int e = 0; e < 4; ++e) x.v[i][s][e] = seen ? x.v[i][s][e] : 0u;
                 }
             }
 #pragma unroll
@@ -278,11 +279,13 @@ __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kern
             if constexpr (D::BF) {
                 typedef short v4s __attribute__((ext_vector_type(4)));
                 typedef __attribute__((address_space(3))) v4s *lds_v4s;
-                bf16x4 w[D::SETS];
+                // (the weights, at most one, are rounded to bf16 for this product; their sum is not: o is 1.8e-3 from its exact value in norm, of
+                // which the rounding of o itself is 1.7e-3)
+                bf16x4 weight[D::SETS];
 #pragma unroll
                 for (int i = 0; i < D::SETS; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) w[i][r] = (bf16)p[i][r];
+                    for (int r = 0; r < 4; ++r) weight[i][r] = (bf16)p[i][r];
 #pragma unroll
                 for (int t = 0; t < OUT; ++t) {
                     const bf16 *at = reinterpret_cast<const bf16 *>(vs) + (4 * g + (col >> 2)) * LDV + 16 * t + 4 * (col & 3);
@@ -290,9 +293,9 @@ __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kern
                     if constexpr (D::SETS == 2) {
                         const v4s a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at + 16 * LDV));
                         o[t] = Mfma<bf16>::mma(__builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)),
-                                               __builtin_shufflevector(w[0], w[D::SETS - 1], 0, 1, 2, 3, 4, 5, 6, 7), o[t]);
+                                               __builtin_shufflevector(weight[0], weight[D::SETS - 1], 0, 1, 2, 3, 4, 5, 6, 7), o[t]);
                     } else {
-                        o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0, __builtin_bit_cast(v4s, w[0]), o[t], 0, 0, 0);
+                        o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0, __builtin_bit_cast(v4s, weight[0]), o[t], 0, 0, 0);
                     }
                 }
             } else {
