@@ -342,7 +342,7 @@ typedef struct {
     int32_t window;                 /* > 0: only the last so many tokens are seen; 0: all */
     int32_t max_length;             /* no length is above it (the launch is sized by it) */
     int32_t shares;                 /* scheduling: > 0 (up to 65535): cut the tokens among so many workgroups; -1: a workgroup for each
-                                       sequence and group of query heads; 0: the library decides */
+                                       sequence, key head and 16 of its query heads; 0: the library decides */
     float scale;                    /* multiplies the scores (usually K^-1/2) */
 } osdn_decode_params;
 

@@ -493,7 +493,8 @@ int osdn_paged_append(const osdn_norm_params *p, const osdn_cache *cache, const 
     return launch_status();
 }
 
-static int check_decode(const osdn_decode_params *p, DecodeArgs &a, size_t &bytes) {
+// heads_together: the cache holds the heads of a token side by side
+static int check_decode(const osdn_decode_params *p, bool heads_together, DecodeArgs &a, size_t &bytes) {
     if (!p) return OSDN_ERR_NULL;
     if (p->io_dtype != OSDN_F32 && p->io_dtype != OSDN_BF16) return OSDN_ERR_DTYPE;
     if (p->B < 1 || p->B > 65535 || p->Hk < 1 || p->Hq < p->Hk || p->Hq % p->Hk != 0 || p->Hq > 65535 || (long long)p->B * p->Hq >= 1 << 21) return OSDN_ERR_SHAPE;
@@ -502,24 +503,32 @@ static int check_decode(const osdn_decode_params *p, DecodeArgs &a, size_t &byte
     if (!std::isfinite(p->scale) || p->window < 0 || p->shares < -1 || p->shares > 65535) return OSDN_ERR_PARAM;
     a.head_tiles = (p->Hq / p->Hk + 15) / 16;
     a.part_heads = p->Hq / p->Hk < 16 ? p->Hq / p->Hk : 16;
-    const long long rows = (long long)p->B * p->Hk * a.head_tiles, units = decode_units(p->max_length, p->window, p->K, p->io_dtype == OSDN_BF16);
-    if (rows * units > 0x7fffffffLL) return OSDN_ERR_SHAPE;            // (units are counted in 32 bits)
-    a.shares = p->shares == -1 ? 0 : p->shares ? p->shares : decode_shares(rows, units, p->K, p->io_dtype == OSDN_BF16);
-    bytes = !a.shares ? 0 : (size_t)a.shares * 2 * a.part_heads * (p->K + 2) * sizeof(float) + (size_t)rows * 2 * sizeof(int);
+    const int rows = p->Hk * a.head_tiles;
+    const DecodePlan plan = decode_plan(p->B, rows, p->max_length, p->window, p->K, p->io_dtype == OSDN_BF16, a.part_heads, heads_together || a.head_tiles > 1, p->shares);
+    const long long groups = (long long)p->B * rows / plan.row_group;
+    if (groups * plan.units > 0x7fffffffLL) return OSDN_ERR_SHAPE;     // (units are counted in 32 bits)
+    a.row_group = plan.row_group;
+    a.shares = plan.shares;
+    bytes = !a.shares ? 0 : (size_t)a.shares * 2 * a.row_group * a.part_heads * (p->K + 2) * sizeof(float) + (size_t)groups * 2 * sizeof(int);
     return OSDN_OK;
 }
 
-size_t osdn_paged_decode_workspace_bytes(const osdn_decode_params *p) {
-    DecodeArgs a{};
-    size_t bytes;
-    return check_decode(p, a, bytes) == OSDN_OK ? bytes : 0;
+size_t osdn_paged_decode_workspace_bytes(const osdn_decode_params *p) {         // (for a cache of either order)
+    size_t most = 0;
+    for (bool together : {false, true}) {
+        DecodeArgs a{};
+        size_t bytes = 0;
+        if (check_decode(p, together, a, bytes) != OSDN_OK) return 0;
+        most = std::max(most, bytes);
+    }
+    return most;
 }
 
 int osdn_paged_decode(const osdn_decode_params *p, const osdn_cache *cache, const osdn_rows *q, const int32_t *lengths, const int32_t *seq,
                       const osdn_rows *o, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
     DecodeArgs a{};
     size_t bytes = 0;
-    int rc = check_decode(p, a, bytes);
+    int rc = check_decode(p, cache && cache->k_head < cache->k_token, a, bytes);
     if (rc != OSDN_OK) return rc;
     if (!lengths) return OSDN_ERR_NULL;
     const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
@@ -529,7 +538,7 @@ int osdn_paged_decode(const osdn_decode_params *p, const osdn_cache *cache, cons
     if (a.shares) {
         rc = check_ws(workspace, workspace_bytes, bytes);
         if (rc != OSDN_OK) return rc;
-        const size_t parts = (size_t)a.shares * 2 * a.part_heads;
+        const size_t parts = (size_t)a.shares * 2 * a.row_group * a.part_heads;
         a.part_o = static_cast<float *>(workspace);
         a.part_ml = a.part_o + parts * p->K;
         a.info = reinterpret_cast<int *>(a.part_ml + parts * 2);

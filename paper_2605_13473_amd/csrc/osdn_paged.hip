@@ -4,13 +4,15 @@
 //   s_j = scale <q, k_j>,  m = max_j s_j,  l = sum_j e^(s_j - m),  o = sum_j e^(s_j - m) v_j / l,  lse = m + log l
 //
 // Bound by memory: every visible key and value is read once, for all query heads that share it (up to 16 side by side: the columns
-// of a 16 x 16 matrix product, so that one query head costs what 16 do, 3 % of the matrix cores' time).  The visible tokens of all
-// rows (a row: a sequence and a group of up to 16 query heads of one key head) make one list that is cut into even shares, one a
-// workgroup, whatever the lengths; a share is a part of a row, or the end of one, whole ones and the beginning of the last.  The four wavefronts of
-// a workgroup take a row's tiles in turn, each with a running maximum and sum of its own, and join at its end; rows that a share does
-// not hold whole go to a second kernel, which joins their parts in their order (4 us; the fence that a join inside this one would take after every part
-// costs more: the next figures 900 and 180 us).  2.1 GB of keys and values of 512 sequences of 1 to 4096
-// tokens: 380 us, 5.6 TB/s (cut into pieces of 1024 tokens, a workgroup each, 401); 0.54 GB of one sequence 99 us, 5.4 TB/s.
+// of a 16 x 16 matrix product, so that one query head costs what 16 do, 3 % of the matrix cores' time).  A row is a sequence and a group of up to
+// 16 query heads of one key head.  A workgroup takes R adjacent rows of a sequence over the same tokens, each by 4 / R of its
+// wavefronts, which take the row's tiles in turn, with a running maximum and sum of their own, and join at its end (R = 4: nothing to join).
+// The visible tokens of all groups of R rows make one list that is cut into even shares, one a workgroup, whatever the lengths; a share is
+// a part of a group, or the end of one, whole ones and the beginning of the last.  Rows that a share does not hold whole go to a second
+// kernel, which joins their parts in their order.
+// 2.1 GB of keys and values of 512 sequences of 1 to 4096 tokens: 380 us, 5.6 TB/s (cut into pieces of 1024 tokens, a workgroup each, 401); 0.54 GB of one
+// sequence 99 us, 5.4 TB/s.  The second kernel takes 4 us; the fence that a join inside the first would take after every part costs more
+// (900 and 180 us).
 //
 // A wavefront's tile is TT tokens.  Keys go from memory to registers as the matrix product wants them (lane l: token l % 16, 16 bytes);
 // scores come out transposed, lane l with four tokens of head l % 16, which is how the second product (values transposed,
@@ -95,28 +97,30 @@ template <int UNIT> __device__ __forceinline__ int units_of(const DecodeArgs &a,
     return (length - (first_seen(a, length) & ~(DECODE_TILE - 1)) + UNIT - 1) / UNIT;
 }
 
-// SHARED: even shares; else a workgroup takes one row, whole (short rows, or many: no search and no second kernel)
-template <typename T, int K, bool SHARED>
+// SHARED: even shares; else a workgroup takes one row, whole (short ones, or many: no search and no second kernel)
+template <typename T, int K, int R, bool SHARED>
 __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kernel(DecodeArgs a) {
     using D = DecodeTile<T, K>;
-    constexpr int TT = D::TT, VE = D::VE, STEPS = D::STEPS, LDV = D::LDV, OUT = D::OUT, LDO = K + 4, STRIDE = DEC_W * TT;
-    __shared__ __align__(16) char lds[DEC_W * (TT * LDV * sizeof(T) > 16 * LDO * 4 ? TT * LDV * sizeof(T) : 16 * LDO * 4)];
-    __shared__ float ml[DEC_W][2][16], all[2][16];
+    constexpr int TT = D::TT, VE = D::VE, STEPS = D::STEPS, LDV = D::LDV, OUT = D::OUT, LDO = K + 4, WPR = DEC_W / R, STRIDE = WPR * TT;
+    constexpr size_t VALUES = TT * LDV * sizeof(T), SUMS = R < 4 ? 16 * LDO * 4 : 0;
+    __shared__ __align__(16) char lds[DEC_W * (VALUES > SUMS ? VALUES : SUMS)];
+    __shared__ float ml[R < 4 ? DEC_W : 1][2][16];
     __shared__ int found[2], sums[DEC_W];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     ask_arguments(a);
-    const int rows = a.Hk * a.head_tiles, w = blockIdx.x;          // rows of a sequence
+    const int groups = a.Hk * a.head_tiles / R, w = blockIdx.x;     // groups of rows of a sequence
+    const int turn = wave % WPR;                                    // this wavefront's among those of its row
     // This workgroup's share: units [at, until), the first of them of sequence b, whose units start at `base`
     int b, base, at, until, total = 0;
     if constexpr (!SHARED) {
-        b = w / (unsigned)rows;
+        b = w / (unsigned)groups;
         base = 0;
         const int u = units_of<STRIDE>(a, b);
-        at = (w - b * rows) * u;
+        at = (w - b * groups) * u;
         until = at + u;
     } else {
         if (a.B == 1) {
-            total = units_of<STRIDE>(a, 0) * rows;
+            total = units_of<STRIDE>(a, 0) * groups;
             b = base = 0;
         } else {                        // where the share begins: a sum over the sequences before it, a run of them a thread
             const int run = (a.B + DEC_T - 1) / DEC_T, i0 = threadIdx.x * run, i1 = min(a.B, i0 + run);
@@ -136,16 +140,16 @@ __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kern
                 if (u < wave) before += sums[u];
                 total += sums[u];
             }
-            total = __builtin_amdgcn_readfirstlane(total) * rows;
+            total = __builtin_amdgcn_readfirstlane(total) * groups;
             const int start = Shares(total, a.shares).begin(w);
-            if (start >= before * rows && start < (before + mine) * rows) {
+            if (start >= before * groups && start < (before + mine) * groups) {
                 int i = i0, u = units_of<STRIDE>(a, i);
-                while (start >= (before + u) * rows) {
+                while (start >= (before + u) * groups) {
                     before += u;
                     u = units_of<STRIDE>(a, ++i);
                 }
                 found[0] = i;
-                found[1] = before * rows;
+                found[1] = before * groups;
             }
             __syncthreads();
             b = __builtin_amdgcn_readfirstlane(found[0]);
@@ -159,7 +163,8 @@ __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kern
     const int share_begin = at;
 
     do {
-        const int units = units_of<STRIDE>(a, b), kt = (at - base) / units, u0 = at - base - kt * units, u1 = min(units, u0 + until - at);
+        const int units = units_of<STRIDE>(a, b), group = (at - base) / units, u0 = at - base - group * units, u1 = min(units, u0 + until - at);
+        const int kt = group * R + wave / WPR;                      // this wavefront's row
         const int kv = a.head_tiles == 1 ? kt : kt / a.head_tiles, h0 = kv * a.group + 16 * (kt - kv * a.head_tiles);
         const int heads = min(16, (kv + 1) * a.group - h0);
         const int seq = a.seq ? a.seq[b] : b, length = a.lengths[b], lo = first_seen(a, length);
@@ -168,7 +173,7 @@ __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kern
         const int begin = (lo & ~(DECODE_TILE - 1)) + u0 * STRIDE;
         const int end = bad_call ? 0 : u1 == units ? length : begin + (u1 - u0) * STRIDE;
         TileLoads<T, K> x;
-        x.ask(a, row, begin + wave * TT, lane);
+        x.ask(a, row, begin + turn * TT, lane);
         // queries: lane l holds head l % 16
         u32x4 q[STEPS];
 #pragma unroll
@@ -198,7 +203,7 @@ __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kern
         bool bad_page = false;
 
         // The rows of the next tile are asked for when this one's are in the matrix products' registers and in LDS, its pages a tile earlier
-        int tok = begin + wave * TT;
+        int tok = begin + turn * TT;
         if (tok < end) {
             bad_page = x.load(a, kc, vc, tok, lo, end, lane);
             x.ask(a, row, tok + STRIDE, lane);
@@ -306,46 +311,19 @@ __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kern
             }
             tok = next;
         }
-        // the four wavefronts join
         l = add_xor32(add_xor16(l));
         if (bad_call || __any(bad_page)) l = __builtin_nanf("");
-        if (g == 0) { ml[wave][0][col] = m; ml[wave][1][col] = l; }
-        __syncthreads();
-        float M = ml[0][0][col], L = 0.f;
-#pragma unroll
-        for (int u = 1; u < DEC_W; ++u) M = fmaxf(M, ml[u][0][col]);
-#pragma unroll
-        for (int u = 0; u < DEC_W; ++u) L = __builtin_fmaf(ml[u][1][col], __builtin_amdgcn_exp2f(ml[u][0][col] - M), L);
-        const float f = __builtin_amdgcn_exp2f(m - M);
-        float *os = reinterpret_cast<float *>(lds) + wave * 16 * LDO;
-#pragma unroll
-        for (int t = 0; t < OUT; ++t) {
-            f32x4 x = o[t];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] *= f;
-            *reinterpret_cast<f32x4 *>(os + col * LDO + 16 * t + 4 * g) = x;
-        }
-        if (wave == 0 && g == 0) { all[0][col] = M; all[1][col] = L; }
-        __syncthreads();
         const bool alone = !SHARED || u1 - u0 == units;                     // (nothing to join)
-        const size_t slot = part_slot(w, at == share_begin);
+        const int slot = part_slot(w, at == share_begin);
         if (SHARED && u0 == 0 && threadIdx.x == 0) {
             const int last = alone ? w : Shares(total, a.shares).owner(at + units - 1);
-            a.info[((size_t)b * rows + kt) * 2] = (int)slot;
-            a.info[((size_t)b * rows + kt) * 2 + 1] = last - w + 1;
+            a.info[((size_t)b * groups + group) * 2] = slot;
+            a.info[((size_t)b * groups + group) * 2 + 1] = last - w + 1;
         }
-        for (int i = threadIdx.x; i < heads * (K / 4); i += DEC_T) {
-            const int h = i / (K / 4), d = i % (K / 4) * 4;
-            f32x4 x = load4(reinterpret_cast<const float *>(lds) + h * LDO + d);
-#pragma unroll
-            for (int u = 1; u < DEC_W; ++u) {
-                const f32x4 y = load4(reinterpret_cast<const float *>(lds) + (u * 16 + h) * LDO + d);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] += y[r];
-            }
-            const size_t bh = (size_t)b * a.Hq + h0 + h;
+        // four elements of head h of this wavefront's row from d on, whose maximum and sum are M and L
+        auto leave = [&](int h, int d, f32x4 x, float M, float L) {
             if (alone) {
-                const float sum = all[1][h], inv = sum == 0.f ? 0.f : 1.f / sum;
+                const float inv = L == 0.f ? 0.f : 1.f / L;
                 T *dst = static_cast<T *>(a.o.data) + b * a.o.batch + (h0 + h) * a.o.head + d;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) x[r] *= inv;
@@ -355,22 +333,60 @@ __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kern
 #pragma unroll
                     for (int r = 0; r < 4; ++r) dst[r] = from_f32<T>(x[r]);
                 }
-                if (a.lse && d == 0) a.lse[bh] = sum == 0.f ? -INFINITY : __builtin_fmaf(all[0][h], LN2, logf(sum));
+                if (a.lse && d == 0) a.lse[(size_t)b * a.Hq + h0 + h] = L == 0.f ? -INFINITY : __builtin_fmaf(M, LN2, logf(L));
             } else {
-                const size_t to = slot * a.part_heads + h;
+                const size_t to = ((size_t)slot * R + wave / WPR) * a.part_heads + h;
                 store4(a.part_o + to * K + d, x);
                 if (d == 0) {
-                    a.part_ml[to * 2] = all[0][h];
-                    a.part_ml[to * 2 + 1] = all[1][h];
+                    a.part_ml[to * 2] = M;
+                    a.part_ml[to * 2 + 1] = L;
                 }
+            }
+        };
+        if constexpr (R == 4) {
+            if (col < heads) {
+#pragma unroll
+                for (int t = 0; t < OUT; ++t) leave(col, 16 * t + 4 * g, o[t], m, l);
+            }
+        } else {                            // the wavefronts of a row join
+            const int first = wave - turn;
+            if (g == 0) { ml[wave][0][col] = m; ml[wave][1][col] = l; }
+            __syncthreads();
+            float M = ml[first][0][col];
+#pragma unroll
+            for (int u = 1; u < WPR; ++u) M = fmaxf(M, ml[first + u][0][col]);
+            const float f = __builtin_amdgcn_exp2f(m - M);
+            float *os = reinterpret_cast<float *>(lds) + wave * 16 * LDO;
+#pragma unroll
+            for (int t = 0; t < OUT; ++t) {
+                f32x4 x = o[t];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] *= f;
+                *reinterpret_cast<f32x4 *>(os + col * LDO + 16 * t + 4 * g) = x;
+            }
+            __syncthreads();
+            for (int i = turn * 64 + lane; i < heads * (K / 4); i += WPR * 64) {
+                const int h = i / (K / 4), d = i % (K / 4) * 4;
+                float top = ml[first][0][h], sum = 0.f;
+#pragma unroll
+                for (int u = 1; u < WPR; ++u) top = fmaxf(top, ml[first + u][0][h]);
+                f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int u = 0; u < WPR; ++u) {
+                    sum = __builtin_fmaf(ml[first + u][1][h], __builtin_amdgcn_exp2f(ml[first + u][0][h] - top), sum);
+                    const f32x4 y = load4(reinterpret_cast<const float *>(lds) + ((first + u) * 16 + h) * LDO + d);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[r] += y[r];
+                }
+                leave(h, d, x, top, sum);
             }
         }
         at += u1 - u0;
-        if (at == base + rows * units) {
+        if (at == base + groups * units) {
             base = at;
             ++b;
         }
-        if (SHARED && at < until) __syncthreads();         // (the next row's values take the place of these sums)
+        if (SHARED && R < 4 && at < until) __syncthreads();        // (the next row's values take the place of these sums)
     } while (SHARED && at < until);
 }
 
@@ -389,10 +405,11 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
     const int b = bh / (unsigned)a.Hq, h = bh % (unsigned)a.Hq;
     // its row, the slot of the first part and how many there are: the parts after the first are each the first of their share
     const int kv = h / (unsigned)a.group, in = h - kv * a.group, hh = in & 15;
-    const int *info = a.info + ((size_t)bh / a.Hq * a.Hk * a.head_tiles + kv * a.head_tiles + (in >> 4)) * 2;
+    const int kt = kv * a.head_tiles + (in >> 4), group = kt / (unsigned)a.row_group, r = kt - group * a.row_group;
+    const int *info = a.info + ((size_t)b * (a.Hk * a.head_tiles / (unsigned)a.row_group) + group) * 2;
     const int first_slot = info[0], n = info[1];
     if (n <= 1) return;                 // decode_kernel has written it
-    auto place = [&](int i) { return (size_t)part_of_row(first_slot, i) * a.part_heads + hh; };
+    auto place = [&](int i) { return ((size_t)part_of_row(first_slot, i) * a.row_group + r) * a.part_heads + hh; };
     const float *ml = a.part_ml, *po = a.part_o + c0;
     // the first four of a lane's parts are on their way before the maximum is known
     constexpr int STEP = ROWS * WAVES, AHEAD = 4;
@@ -411,7 +428,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
         const float f = __builtin_amdgcn_exp2f(ml[2 * place(i)] - M);
         L = __builtin_fmaf(ml[2 * place(i) + 1], f, L);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = __builtin_fmaf(y[r], f, x[r]);
+        for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(y[e], f, x[e]);
     };
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
@@ -454,14 +471,16 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
 
 namespace {
 template <typename T, int K> void decode_of(const DecodeArgs &a, hipStream_t st) {
-    const unsigned rows = (unsigned)a.B * a.Hk * a.head_tiles, heads = (unsigned)a.B * a.Hq;
-    if (!a.shares) {
-        hipLaunchKernelGGL((decode_kernel<T, K, false>), dim3(rows), dim3(DEC_T), 0, st, a);
+    const unsigned groups = (unsigned)a.B * a.Hk * a.head_tiles / a.row_group, heads = (unsigned)a.B * a.Hq, shares = (unsigned)a.shares;
+    if (!shares) {
+        hipLaunchKernelGGL((decode_kernel<T, K, 1, false>), dim3(groups), dim3(DEC_T), 0, st, a);
         return;
     }
-    hipLaunchKernelGGL((decode_kernel<T, K, true>), dim3(a.shares), dim3(DEC_T), 0, st, a);
+    if (a.row_group == 4) hipLaunchKernelGGL((decode_kernel<T, K, 4, true>), dim3(shares), dim3(DEC_T), 0, st, a);
+    else if (a.row_group == 2) hipLaunchKernelGGL((decode_kernel<T, K, 2, true>), dim3(shares), dim3(DEC_T), 0, st, a);
+    else hipLaunchKernelGGL((decode_kernel<T, K, 1, true>), dim3(shares), dim3(DEC_T), 0, st, a);
     // (many parts of few rows: a workgroup each, as the loads of a row are then what takes the time)
-    if ((unsigned)a.shares > 16 * rows) hipLaunchKernelGGL((decode_join_kernel<T, K, 32, true>), dim3(heads * (K / 32)), dim3(256), 0, st, a);
+    if (shares > 16 * groups) hipLaunchKernelGGL((decode_join_kernel<T, K, 16, true>), dim3(heads * (K / 16)), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((decode_join_kernel<T, K, 64, false>), dim3((heads * (K / 64) + 3) / 4), dim3(256), 0, st, a);
 }
 }  // namespace

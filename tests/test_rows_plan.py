@@ -16,7 +16,7 @@ MAIN = r"""
 #include <vector>
 using namespace osdn;
 // heads: tokens Hq Hk K bf16 values backward -> q_blocks k_blocks blocks per_part parts workgroups, 1 if the parts cover the blocks
-// decode: B groups max_length window K bf16 -> units shares unit
+// decode: B rows max_length window K bf16 part_heads heads_together asked -> row_group units shares unit
 // cut: W rows B u_0 .. u_(B-1) -> 1 if the shares cover the rows' units, every slot is written once, and a row's parts are found where they were left
 int main(int, char **argv) {
     if (!std::strcmp(argv[1], "heads")) {
@@ -32,10 +32,10 @@ int main(int, char **argv) {
             std::printf("%d %d %d %d %d %d %d\n", h.q_blocks, h.k_blocks, h.blocks, h.per_part, h.parts, h.workgroups, covered == h.blocks);
         }
     } else if (!std::strcmp(argv[1], "decode")) {
-        int B, rows, L, win, K, bf;
-        while (std::scanf("%d %d %d %d %d %d", &B, &rows, &L, &win, &K, &bf) == 6) {
-            const long long u = decode_units(L, win, K, bf);
-            std::printf("%lld %d %d\n", u, decode_shares((long long)B * rows, u, K, bf), decode_unit(K, bf));
+        int B, rows, L, win, K, bf, ph, tog, ask;
+        while (std::scanf("%d %d %d %d %d %d %d %d %d", &B, &rows, &L, &win, &K, &bf, &ph, &tog, &ask) == 9) {
+            const DecodePlan p = decode_plan(B, rows, L, win, K, bf, ph, tog, ask);
+            std::printf("%d %lld %d %d\n", p.row_group, p.units, p.shares, decode_unit(K, bf, p.row_group));
         }
     } else {
         int W, rows, B;
@@ -105,16 +105,18 @@ def test_every_block_of_rows_falls_to_one_wavefront(plan):
 
 
 def test_decode_plans(plan):
-    asked = [(B, r, L, win, K, bf) for B in (1, 8, 64, 512, 65535) for r in (1, 4, 16) for L in (0, 1, 127, 128, 129, 1000, 4096, 131072) for win in (0, 1, 33, 1000)
-             for K in (64, 128, 256) for bf in (0, 1)]
-    for (B, r, L, win, K, bf), (units, shares, unit) in zip(asked, plan("decode", asked)):
+    asked = [(B, r, L, win, K, bf, ph, tog, ask) for B in (1, 8, 64, 512, 65535) for r in (1, 2, 3, 4, 6, 16) for L in (0, 1, 127, 128, 129, 1000, 4096, 131072) for win in (0, 33, 1000)
+             for K in (64, 128, 256) for bf in (0, 1) for ph in (1, 16) for tog in (0, 1) for ask in (0, -1, 7)]
+    for (B, r, L, win, K, bf, ph, tog, ask), (together, units, shares, unit) in zip(asked, plan("decode", asked)):
         seen = min(L, win + 31) if win else L
-        assert unit == (128 if bf and K <= 128 else 64) and units == max(1, -(-seen // unit))
-        assert 0 <= shares <= min(B * r * units, 768)
-        assert shares > 0 or units <= 3 or B * r >= 128
-    # what measurements put on one course: short rows and full launches one row a workgroup, long ones even shares
-    assert plan("decode", [(1, 4, 1531, 0, 128, 1), (1, 8, 131072, 0, 128, 1), (512, 4, 4096, 0, 128, 1), (1, 4, 300, 0, 128, 1), (256, 4, 1000, 0, 128, 1), (64, 8, 4096, 0, 64, 1),
-                           (16, 8, 4096, 0, 256, 0)]) == [[12, 48, 128], [1024, 512, 128], [32, 512, 128], [3, 0, 128], [8, 0, 128], [32, 768, 128], [64, 256, 64]]
+        assert together in (1, 2, 4) and r % together == 0
+        assert unit == (128 if bf and K <= 128 else 64) // together and units == max(1, -(-seen // unit))
+        if ask:
+            assert shares == max(ask, 0) and (ask > 0 or together == 1)
+        else:
+            assert 0 <= shares <= min(B * r // together * units, 768)
+            assert (shares > 0 or together == 1) and (shares > 0 or seen <= 384 or B * r >= 128)
+        assert tog or (K == 64 and bf) or together == 1
 
 
 def test_shares_cover_and_are_joined(plan):
