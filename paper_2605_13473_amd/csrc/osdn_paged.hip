@@ -97,7 +97,7 @@ template <int UNIT> __device__ __forceinline__ int units_of(const DecodeArgs &a,
     return (length - (first_seen(a, length) & ~(DECODE_TILE - 1)) + UNIT - 1) / UNIT;
 }
 
-// SHARED: even shares; else a workgroup takes one row, whole (short ones, or many: no search and no second kernel)
+// SHARED: even shares; else a workgroup takes one group of rows, whole (short ones, or many: no search and no second kernel)
 template <typename T, int K, int R, bool SHARED>
 __global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kernel(DecodeArgs a) {
     using D = DecodeTile<T, K>;
@@ -470,15 +470,15 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
 }
 
 namespace {
+template <typename T, int K, bool SHARED> void decode_rows(const DecodeArgs &a, unsigned workgroups, hipStream_t st) {
+    if (a.row_group == 4) hipLaunchKernelGGL((decode_kernel<T, K, 4, SHARED>), dim3(workgroups), dim3(DEC_T), 0, st, a);
+    else if (a.row_group == 2) hipLaunchKernelGGL((decode_kernel<T, K, 2, SHARED>), dim3(workgroups), dim3(DEC_T), 0, st, a);
+    else hipLaunchKernelGGL((decode_kernel<T, K, 1, SHARED>), dim3(workgroups), dim3(DEC_T), 0, st, a);
+}
 template <typename T, int K> void decode_of(const DecodeArgs &a, hipStream_t st) {
     const unsigned groups = (unsigned)a.B * a.Hk * a.head_tiles / a.row_group, heads = (unsigned)a.B * a.Hq, shares = (unsigned)a.shares;
-    if (!shares) {
-        hipLaunchKernelGGL((decode_kernel<T, K, 1, false>), dim3(groups), dim3(DEC_T), 0, st, a);
-        return;
-    }
-    if (a.row_group == 4) hipLaunchKernelGGL((decode_kernel<T, K, 4, true>), dim3(shares), dim3(DEC_T), 0, st, a);
-    else if (a.row_group == 2) hipLaunchKernelGGL((decode_kernel<T, K, 2, true>), dim3(shares), dim3(DEC_T), 0, st, a);
-    else hipLaunchKernelGGL((decode_kernel<T, K, 1, true>), dim3(shares), dim3(DEC_T), 0, st, a);
+    if (!shares) return decode_rows<T, K, false>(a, groups, st);
+    decode_rows<T, K, true>(a, shares, st);
     // (many parts of few rows: a workgroup each, as the loads of a row are then what takes the time)
     if (shares > 16 * groups) hipLaunchKernelGGL((decode_join_kernel<T, K, 16, true>), dim3(heads * (K / 16)), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((decode_join_kernel<T, K, 64, false>), dim3((heads * (K / 64) + 3) / 4), dim3(256), 0, st, a);

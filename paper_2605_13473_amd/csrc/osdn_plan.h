@@ -280,26 +280,32 @@ inline long long decode_span(int max_length, int window) {
 //  - a row each for short rows, and for up to 1024 tokens where the rows fill the chip, against 512 shares: 1 x 300 tokens 9.3 and 10.3, 256 x 300
 //    35.7 and 39.7, uneven 512 x 300 41 and 56; 32 x 500 14.4 and 15.2; 64 x 1000 32.2 and 33.3, uneven 512 x 1000 108 and 116; but 1 x 500 12.0 and
 //    10.3, 16 x 500 14.0 and 12.8, 32 x 1000 22.8 and 20.3, uneven 256 x 2000 125 and 114, 512 x 4096 429 and 380.
-//  - four rows (or two) together where the cache holds the heads of a token side by side, so that what is asked for at a time is not each fourth or
-//    eighth 256 bytes of it, or where rows share their key head; one by one and so: uneven 64 x 8192 x 8 204 and 185, 512 x 4096 388 and 374, 1 x 131072 x 8 113 and
-//    100, 16 x 4096 x 16 106 and 99, K = 64, uneven 64 x 4096 x 8 65 and 56.  Head after head, rows one by one do as well with fewer parts to join
-//    (185 and 186, 378 and 384, 99 and 105), but for rows of 128 bytes (64 x 4096 x 8 57.5 and 54.5).
-//  - two shares a CU, which start and end together whatever the lengths.  Rows one by one with 256, 512, 768 and 1024: 1 x 131072 x 8 99.8, 99.5, 99.9, 101;
-//    uneven 512 x 4096 392, 379, 382, 383, 64 x 8192 x 8 199, 186, 187, 188; 16 x 4096 x 8, K = 256, 100, 104, 121, 106; fp32 115, 102, 119, 102.  With 384 and
-//    640, half a share a CU more or less, 434 and 414 for the first of the uneven ones.  K = 64 in fp32, three; fp32 and K = 256, whose registers hold one
-//    workgroup, one: 8 x 4096 63.5, 68.4, 74.0, 79.4.  Four rows of K = 128 in bf16 together, one: 256 and 512, 1 x 131072 x 8 99.8 and 102.8, 512 x 4096 374
-//    and 378.  And not so many that the parts (an fp32 row of each query head) outweigh what a share reads: 8 x 8000 x 2 with 32 query heads each, 256
-//    and 512 shares 31.6 and 35.3.
+//  - of the former, four rows (or two) together, a wavefront each, where a wavefront has no more than a tile, or four of them and rows enough:
+//    one by one and so, 370 x 5 tokens x 8, K = 256, 31.3 and 18.5; but 256 x 300 35.7 and 36.4, uneven 512 x 300 41 and 48.
+//  - of the latter, four rows (or two) together where the cache holds the heads of a token side by side, so that what is asked for at a time is not
+//    each fourth or eighth 256 bytes of it, or where rows share their key head: one by one and so, uneven 64 x 8192 x 8 204 and 185, 512 x 4096 388 and
+//    374, 1 x 131072 x 8 113 and 100, 16 x 4096 x 16 106 and 99, K = 64, uneven 64 x 4096 x 8 65 and 56.  Head after head, rows one by one do as well
+//    with fewer parts to join (185 and 186, 378 and 384, 99 and 105), but for rows of 128 bytes (64 x 4096 x 8 57.5 and 54.5).
+//  - two shares a CU, which start and end together whatever the lengths.  Rows one by one with 256, 512, 768 and 1024: uneven 512 x 4096 392, 379, 382,
+//    383, 64 x 8192 x 8 199, 186, 187, 188; 16 x 4096 x 8, K = 256, 100, 104, 121, 106; fp32 115, 102, 119, 102; with 384 and 640, half a share a CU more
+//    or less, 434 and 414 for the first.  Three for rows of 64 elements one by one (fp32, or bf16 alone: 64 x 4096 x 8 72.5, 63.5, 57.8, 62.7).
+//    One for fp32 and K = 256, whose registers hold one workgroup (8 x 4096 63.5, 68.4, 74.0, 79.4), for four rows of K = 128 in bf16 together (1 x 131072 x 8
+//    99.8 and 102.8, 512 x 4096 374 and 378), and for few rows, of which each share is a part to join (with 192, 256, 512 and 768, fp32 K = 64, 1 x 84732 x 1
+//    18.7, 18.3, 20.3, 21.8, bf16 2 x 58831 x 2 16.2, 16.1, 18.8, 20.9, K = 128, 4 x 32768 x 1 25.5, 22.1, 22.8, 24.4; but 8 x 4096 x 4 18.4, 19.4, 18.2, 17.5).
+//  - and not so many that the parts (an fp32 row of each query head) outweigh what a share reads: 8 x 8000 x 2 with 32 query heads each, 256 and 512
+//    shares 31.6 and 35.3.
 struct DecodePlan { int row_group, shares; long long units; };
 inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K, bool bf16, int part_heads, bool heads_together, int asked) {
     const long long span = decode_span(max_length, window), all = (long long)B * rows;
     const bool each = asked < 0 || (asked == 0 && (span <= 3 * decode_unit(K, bf16, 1) || (all >= NUM_CU && span <= 1024) || (all >= NUM_CU / 2 && span <= 512)));
-    const bool together = !each && (heads_together || (K == 64 && bf16));
+    const int tile = decode_tile(K, bf16);
+    const bool together = each ? span <= tile || (all >= 4 * NUM_CU && span <= 4 * tile) : heads_together || (K == 64 && bf16);
     DecodePlan p{};
     p.row_group = together && rows % 4 == 0 ? 4 : together && rows % 2 == 0 ? 2 : 1;
     const int unit = decode_unit(K, bf16, p.row_group);
     p.units = span < 1 ? 1 : (span + unit - 1) / unit;
-    const long long groups = all / p.row_group, per_cu = K == 64 && p.row_group < 4 ? 3 : (K == 256 && !bf16) || (K == 128 && bf16 && p.row_group == 4) ? 1 : 2;
+    const long long groups = all / p.row_group;
+    const int per_cu = all <= 16 || (K == 256 && !bf16) || (K == 128 && bf16 && p.row_group == 4) ? 1 : K == 64 && p.row_group < 4 ? 3 : 2;
     const long long worth = groups * span / (16 * part_heads), most = per_cu * NUM_CU < worth ? per_cu * NUM_CU : worth > NUM_CU ? worth : NUM_CU;
     p.shares = each ? 0 : asked > 0 ? asked : (int)(groups * p.units < most ? groups * p.units : most);
     return p;

@@ -112,11 +112,11 @@ def test_decode_plans(plan):
         assert together in (1, 2, 4) and r % together == 0
         assert unit == (128 if bf and K <= 128 else 64) // together and units == max(1, -(-seen // unit))
         if ask:
-            assert shares == max(ask, 0) and (ask > 0 or together == 1)
+            assert shares == max(ask, 0)
         else:
             assert 0 <= shares <= min(B * r // together * units, 768)
-            assert (shares > 0 or together == 1) and (shares > 0 or seen <= 384 or B * r >= 128)
-        assert tog or (K == 64 and bf) or together == 1
+            assert shares > 0 or seen <= 384 or B * r >= 128
+        assert tog or (K == 64 and bf) or together == 1 or (shares == 0 and seen <= 128)
 
 
 def test_shares_cover_and_are_joined(plan):
