@@ -504,8 +504,8 @@ def rotary_table(rows: int, dim: int, theta: float = 10000.0, device="cuda") -> 
 
 
 def alloc_paged_cache(n_pages: int, page_size: int, H: int, K: int, dtype=torch.bfloat16, device="cuda"):
-    """(k_cache, v_cache), [n_pages, page_size, H, K]: a page holds its tokens head after head, which is the order that
-    paged_decode reads (any order of pages, tokens and heads is taken)."""
+    """(k_cache, v_cache), [n_pages, page_size, H, K]: a page holds its tokens head after head (any order of pages,
+    tokens and heads is taken, the other one as fast)."""
     return tuple(torch.empty(n_pages, H, page_size, K, dtype=dtype, device=device).transpose(1, 2) for _ in range(2))
 
 
