@@ -315,3 +315,15 @@ def test_serving_loop_in_a_graph():
         pos += 1
         length += 1
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("K", [64, 128, 256])
+def test_fp32_scores_are_summed_in_parts(K):
+    """fp32, scores of a spread of 4.  Rounding a sum of n products of variance s^2 one by one is off by less than 2^-24 s sqrt(n (n + 1) / 2) in the mean
+    square; in sums of at most 32 products, K / 32 of them (four at least), and those two by two, K = 256 comes to 2^-24 s sqrt(8 x 528 + 3 x 256) = 71
+    2^-24 s, as one sum to 181 2^-24 s; s = 4 and the scale 1 / 16 make 1.05e-6 and 2.7e-6 of a score, a weight, and so of o in norm.  The score's
+    scaling and the maximum's subtraction, each off by 2^-25 of about 4 sqrt(log2 e), and e^x with its 2^-23, add 0.4e-6: 1.15e-6 in all."""
+    x = make_decode([861, 1500], 8, 4, K, 16, io="f32", seed=11, spread=4.0)
+    o, _ = call(x)
+    want, _, _ = ref.decode(ref.f64(x["q"]), ref.f64(x["kc"]), ref.f64(x["vc"]), x["table"].cpu(), x["lengths"].cpu(), torch.arange(2), K ** -0.5, 0)
+    assert float((o.double().cpu() - want).norm() / want.norm()) < 1.15e-6
