@@ -46,7 +46,6 @@ template <typename T, int K> struct DecodeTile {
     static constexpr int STEPS = K / (4 * VE);          // vectors of a row, per lane (four lanes share a row)
     static constexpr int LDV = K + VE;                  // row of the values in LDS: 16 rows of one column start on 16 different quads of banks
     static constexpr int OUT = K / 16;                  // 16-row tiles of the transposed result
-    static constexpr int PER_CU = K == 64 ? 4 : K == 128 ? (BF ? 3 : 2) : BF ? 2 : 1;      // workgroups that a CU's registers hold
 };
 
 // The rows of a tile that a lane loads, token 16 i + l % 16 of the tile, on their way: first their pages, then the rows.  In place of a token outside
@@ -102,7 +101,7 @@ template <int UNIT> __device__ __forceinline__ int units_of(const DecodeArgs &a,
 
 // SHARED: even shares; else a workgroup takes one group of rows, whole (short ones, or many: no search and no second kernel)
 template <typename T, int K, int R, bool SHARED>
-__global__ __launch_bounds__(DEC_T, (DecodeTile<T, K>::PER_CU)) void decode_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(DEC_T, (decode_per_cu(K, sizeof(T) == 2))) void decode_kernel(DecodeArgs a) {
     using D = DecodeTile<T, K>;
     constexpr int TT = D::TT, VE = D::VE, STEPS = D::STEPS, LDV = D::LDV, OUT = D::OUT, LDO = K + 4, WPR = DEC_W / R, STRIDE = WPR * TT;
     constexpr size_t VALUES = TT * LDV * sizeof(T), SUMS = R < 4 ? 16 * LDO * 4 : 0;

@@ -269,6 +269,8 @@ inline HeadsPlan heads_plan(long long tokens, int Hq, int Hk, int K, bool bf16, 
 constexpr int DECODE_TILE = 32, DEC_THREADS = 256;
 // Tokens of a wavefront's tile (wide rows: half, for the registers), and of a unit: a tile for each wavefront of a row, where a workgroup's four take R rows
 constexpr int decode_tile(int K, bool bf16) { return bf16 && K <= 128 ? 32 : 16; }
+// Workgroups that the registers of a CU hold
+constexpr int decode_per_cu(int K, bool bf16) { return K == 64 ? 4 : K == 128 ? (bf16 ? 3 : 2) : bf16 ? 2 : 1; }
 constexpr int decode_unit(int K, bool bf16, int R) { return DEC_THREADS / 64 / R * decode_tile(K, bf16); }
 inline long long decode_span(int max_length, int window) {
     const long long seen = window > 0 && window < max_length ? (long long)window + DECODE_TILE - 1 : max_length;
@@ -277,11 +279,14 @@ inline long long decode_span(int max_length, int window) {
 // How a call is cut, for B sequences of `rows` rows (groups of up to 16 query heads of a key head) each: the rows that a workgroup takes together, the
 // units of a sequence of max_length, and the shares (0: a row each, and no second kernel).  asked: > 0 shares, -1 a row each, 0 by these rules.
 // us; "even": all lengths the same, "uneven": spread from 1 to the longest; four heads of the cache of K = 128 in bf16, head after head, unless said.
-//  - a row each for short rows, and for up to 1024 tokens where the rows fill the chip, against 512 shares: 1 x 300 tokens 9.3 and 10.3, 256 x 300
-//    35.7 and 39.7, uneven 512 x 300 41 and 56; 32 x 500 14.4 and 15.2; 64 x 1000 32.2 and 33.3, uneven 512 x 1000 108 and 116; but 1 x 500 12.0 and
-//    10.3, 16 x 500 14.0 and 12.8, 32 x 1000 22.8 and 20.3, uneven 256 x 2000 125 and 114, 512 x 4096 429 and 380.
-//  - of the former, four rows (or two) together, a wavefront each, where a wavefront has no more than a tile, or four of them and rows enough:
-//    one by one and so, 370 x 5 tokens x 8, K = 256, 31.3 and 18.5; but 256 x 300 35.7 and 36.4, uneven 512 x 300 41 and 48.
+//  - a row each, against 512 shares, for rows of a few units, the more so for many rows: 1 x 300 tokens 9.3 and 10.3, 256 x 300 34.2 and 39.7, uneven
+//    40 x 400 11.9 and 14.0, 512 x 450 54.5 and 57.9; but 1 x 500 12.0 and 10.3, 16 x 500 14.0 and 12.8, fp32 1 x 200 x 8 13.3 and 10.5.
+//  - and for up to 1024 tokens where the rows fill the chip: uneven 200 x 700 38.8 and 42.8, fp32, K = 64, 512 x 1000 x 8 186 and 221; but not so many
+//    where a token's heads stand side by side (uneven 200 x 1000 59 and 49, K = 64, 512 x 900 x 8 213 and 171) or in rows of 256 (uneven 200 x 700 x 2
+//    48.7 and 40.3), and none where one workgroup is all that a CU holds (fp32, K = 256, uneven 300 x 500 x 2 95 and 81).
+//  - of the former, four rows (or two) together, a wavefront each, where a row is no more than a tile and one by one they are more workgroups than
+//    the chip holds, or four tiles and half as many again: one by one and so, times 8 heads: uneven 500 x 1 22.0 and 11.1, fp32, K = 256, 94 and 31;
+//    300 x 20 17.5 and 11.7; 300 x 70 24.0 and 21.6; but 300 x 128 36.1 and 36.5, K = 256 100 x 250 46.8 and 48.6; 80 x 70 11 % more so, 50 x 16 6 %.
 //  - of the latter, four rows (or two) together where the cache holds the heads of a token side by side, so that what is asked for at a time is not
 //    each fourth or eighth 256 bytes of it, or where rows share their key head: one by one and so, uneven 64 x 8192 x 8 204 and 185, 512 x 4096 388 and
 //    374, 1 x 131072 x 8 113 and 100, 16 x 4096 x 16 106 and 99, K = 64, uneven 64 x 4096 x 8 65 and 56.  Head after head, rows one by one do as well
@@ -289,23 +294,26 @@ inline long long decode_span(int max_length, int window) {
 //  - two shares a CU, which start and end together whatever the lengths.  Rows one by one with 256, 512, 768 and 1024: uneven 512 x 4096 392, 379, 382,
 //    383, 64 x 8192 x 8 199, 186, 187, 188; 16 x 4096 x 8, K = 256, 100, 104, 121, 106; fp32 115, 102, 119, 102; with 384 and 640, half a share a CU more
 //    or less, 434 and 414 for the first.  Three for rows of 64 elements one by one (fp32, or bf16 alone: 64 x 4096 x 8 72.5, 63.5, 57.8, 62.7).
-//    One for fp32 and K = 256, whose registers hold one workgroup (8 x 4096 63.5, 68.4, 74.0, 79.4), for four rows of K = 128 in bf16 together (1 x 131072 x 8
-//    99.8 and 102.8, 512 x 4096 374 and 378), and for few rows, of which each share is a part to join (with 192, 256, 512 and 768, fp32 K = 64, 1 x 84732 x 1
+//    One for fp32 and K = 256, whose registers hold one workgroup (8 x 4096 63.5, 68.4, 74.0, 79.4), for four long rows of K = 128 in bf16 together (1 x 131072
+//    x 8 99.8 and 102.8, 512 x 4096 374 and 378; but uneven 150 x 700 32.6 and 30.3, 512 x 1000 107 and 106), and for few rows, of which each share is a part to join (with 192, 256, 512 and 768, fp32 K = 64, 1 x 84732 x 1
 //    18.7, 18.3, 20.3, 21.8, bf16 2 x 58831 x 2 16.2, 16.1, 18.8, 20.9, K = 128, 4 x 32768 x 1 25.5, 22.1, 22.8, 24.4; but 8 x 4096 x 4 18.4, 19.4, 18.2, 17.5).
 //  - and not so many that the parts (an fp32 row of each query head) outweigh what a share reads: 8 x 8000 x 2 with 32 query heads each, 256 and 512
 //    shares 31.6 and 35.3.
 struct DecodePlan { int row_group, shares; long long units; };
 inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K, bool bf16, int part_heads, bool heads_together, int asked) {
     const long long span = decode_span(max_length, window), all = (long long)B * rows;
-    const bool each = asked < 0 || (asked == 0 && (span <= 3 * decode_unit(K, bf16, 1) || (all >= NUM_CU && span <= 1024) || (all >= NUM_CU / 2 && span <= 512)));
-    const int tile = decode_tile(K, bf16);
-    const bool together = each ? span <= tile || (all >= 4 * NUM_CU && span <= 4 * tile) : heads_together || (K == 64 && bf16);
+    const int tile = decode_tile(K, bf16), alone = decode_unit(K, bf16, 1), held = decode_per_cu(K, bf16) * NUM_CU;
+    const bool beside = heads_together && rows % 2 == 0;
+    const bool few_units = span <= (K == 64 ? 4 : bf16 ? 3 : 2) * alone || (span <= 4 * alone && all >= NUM_CU / 2);
+    const bool full = all >= held && held > NUM_CU && span <= (beside || K == 256 ? 512 : 1024);
+    const bool each = asked < 0 || (asked == 0 && (few_units || full));
+    const bool together = each ? (span <= tile && all > held) || (span <= 4 * tile && 2 * all > 3 * held) : beside || (K == 64 && bf16);
     DecodePlan p{};
     p.row_group = together && rows % 4 == 0 ? 4 : together && rows % 2 == 0 ? 2 : 1;
     const int unit = decode_unit(K, bf16, p.row_group);
     p.units = span < 1 ? 1 : (span + unit - 1) / unit;
     const long long groups = all / p.row_group;
-    const int per_cu = all <= 16 || (K == 256 && !bf16) || (K == 128 && bf16 && p.row_group == 4) ? 1 : K == 64 && p.row_group < 4 ? 3 : 2;
+    const int per_cu = all <= 16 || (K == 256 && !bf16) || (K == 128 && bf16 && p.row_group == 4 && span > 1024) ? 1 : K == 64 && p.row_group < 4 ? 3 : 2;
     const long long worth = groups * span / (16 * part_heads), most = per_cu * NUM_CU < worth ? per_cu * NUM_CU : worth > NUM_CU ? worth : NUM_CU;
     p.shares = each ? 0 : asked > 0 ? asked : (int)(groups * p.units < most ? groups * p.units : most);
     return p;
