@@ -11,7 +11,7 @@
 // A wavefront works on one token, so that the angles of its position are loaded once for its rows; 16 bytes per lane, K elements
 // in K * sizeof(T) / 16 lanes, 64 lanes in as many rows as that makes (a block of rows).  bf16, K = 128: 4 x 4096 tokens of 16 + 16 rows, unit length,
 // forward 44 us (6.1 TB/s, a part still in the last level cache), backward 78 us (5.2 TB/s: what a device copy reaches); 2 x 8192 of 32 + 8 with weights
-// and rotation 60 and 110 us; 65536 tokens of 16 + 4 + 4 appended 173 us (4.9 TB/s).
+// and rotation 60 and 110 us; 65536 tokens of 16 + 4 + 4 appended 164 us (5.1 TB/s).
 #include "osdn_kernels.h"
 
 namespace osdn {
@@ -158,8 +158,9 @@ template <bool APPEND> __device__ __forceinline__ void ask_arguments(const Heads
 }
 
 // A wavefront walks (token, part of its blocks of rows) pairs in steps of the grid; it has the loads of NB blocks in flight at a time.
-// APPEND: keys go to the cache, values follow them unchanged.
-template <typename T, int K, bool VEC, int ROT, bool APPEND>
+// APPEND: keys go to the cache, values follow them unchanged.  AHEAD: the next blocks are asked for before these are written, as a wait for loads is one
+// for the writes before them too (rule and figures: heads_ahead).
+template <typename T, int K, bool VEC, int ROT, bool APPEND, bool AHEAD>
 __global__ __launch_bounds__(HEADS_T) void heads_fwd_kernel(HeadsArgs a) {
     using HR = HeadRow<T, K>;
     constexpr int VE = HR::VE, ROWS = HR::ROWS, NB = 2;
@@ -191,16 +192,24 @@ __global__ __launch_bounds__(HEADS_T) void heads_fwd_kernel(HeadsArgs a) {
                 }
             }
         }
-        for (int blk0 = part * a.per_part; blk0 < blk_end; blk0 += NB) {
+        const int first = part * a.per_part;
+        u32x4 ahead[NB] = {};
+        for (int blk0 = AHEAD ? first - NB : first; blk0 < blk_end; blk0 += NB) {
             u32x4 raw[NB];
+            if constexpr (AHEAD) {
+#pragma unroll
+                for (int i = 0; i < NB; ++i) raw[i] = ahead[i];
+            }
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
-                const int blk = blk0 + i, kind = blk < a.q_blocks ? 0 : blk < a.q_blocks + a.k_blocks ? 1 : 2;
+                const int blk = blk0 + (AHEAD ? NB : 0) + i, kind = blk < a.q_blocks ? 0 : blk < a.q_blocks + a.k_blocks ? 1 : 2;
                 const int h = (blk - (kind == 0 ? 0 : kind == 1 ? a.q_blocks : a.q_blocks + a.k_blocks)) * ROWS + sub;
                 const HeadRows &src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
-                raw[i] = u32x4{0u, 0u, 0u, 0u};
-                if (blk < blk_end && h < (kind == 0 ? a.Hq : a.Hk)) raw[i] = load_row<T, VEC>(row_at<const T, VEC>(src, b, t, h) + e0);
+                u32x4 &to = AHEAD ? ahead[i] : raw[i];
+                to = u32x4{0u, 0u, 0u, 0u};
+                if (blk < blk_end && h < (kind == 0 ? a.Hq : a.Hk)) to = load_row<T, VEC>(row_at<const T, VEC>(src, b, t, h) + e0);
             }
+            if (AHEAD && blk0 < first) continue;
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
                 const int blk = blk0 + i, kind = blk < a.q_blocks ? 0 : blk < a.q_blocks + a.k_blocks ? 1 : 2;
@@ -386,8 +395,9 @@ template <typename T, int K> int cut(HeadsArgs &a, bool backward) {
 }
 template <typename T, int K, bool VEC, int ROT> void fwd_of(HeadsArgs a, hipStream_t st) {
     const dim3 g((unsigned)cut<T, K>(a, false)), t(HEADS_T);
-    if (a.append) hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, true>), g, t, 0, st, a);
-    else hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, false>), g, t, 0, st, a);
+    if (!a.append) hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, false, false>), g, t, 0, st, a);
+    else if (VEC && heads_ahead(a.tokens, a.blocks)) hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, true, VEC>), g, t, 0, st, a);
+    else hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, true, false>), g, t, 0, st, a);
 }
 template <typename T, int K, bool VEC, int ROT> void bwd_of(HeadsArgs a, hipStream_t st) {
     const int n = cut<T, K>(a, true);
