@@ -243,7 +243,7 @@ inline int heads_blocks_per_wave(long long tokens, int blocks) {
 // other and so: 65536 tokens of 6 blocks 176 and 164, 30000 86 and 81, fp32 3120 of 32 51.4 and 50.5; but 3158 of 10 18.8 and 19.4, 858 of 7 7.6 and 7.9.
 // (Without the cache's rows it does not pay: 20000 of 2 17.8 and 18.6, 16384 of 10 69 and 70.)
 inline bool heads_ahead(long long tokens, int blocks) { return tokens * blocks >= 256 * NUM_CU; }
-// Workgroups (four wavefronts) for so many (token, part) pairs: 65536 tokens appended with up to 2048, 4096 and 16384 of them 190, 180 and 173 us
+// Workgroups (four wavefronts) for so many (token, part) pairs: 65536 tokens appended with up to 2048, 4096 and 16384 of them 175, 168 and 163 us
 inline int heads_fwd_workgroups(long long items) { return (int)(items < 4 * 16384 ? (items + 3) / 4 : 16384); }
 // ... of heads_bwd_kernel, each with a row of partial sums: 2 x 8192 x (32 + 8) heads with 1024 and 2048 178 and 179 us (both passes), 4 x 2048 x (16 + 4) of 64 33 and 36
 constexpr int HEADS_BWD_WGS = 1024;
