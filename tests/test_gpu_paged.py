@@ -327,3 +327,33 @@ def test_fp32_scores_are_summed_in_parts(K):
     o, _ = call(x)
     want, _, _ = ref.decode(ref.f64(x["q"]), ref.f64(x["kc"]), ref.f64(x["vc"]), x["table"].cpu(), x["lengths"].cpu(), torch.arange(2), K ** -0.5, 0)
     assert float((o.double().cpu() - want).norm() / want.norm()) < 1.15e-6
+
+
+# More rows than the chip holds workgroups: four (two) short ones together, a wavefront each; and rows whose heads stand side by side
+MANY = [
+    dict(lengths=[(7 * i) % 34 - 2 for i in range(400)], Hq=8, Hk=4, K=64, page=16),
+    dict(lengths=[(7 * i) % 125 for i in range(300)], Hq=4, Hk=4, K=128, page=8, order="token"),
+    dict(lengths=[(5 * i) % 17 for i in range(400)], Hq=6, Hk=2, K=256, page=16, window=9),
+    dict(lengths=[(11 * i) % 65 - 1 for i in range(200)], Hq=4, Hk=4, K=256, page=32, io="f32"),
+    dict(lengths=[(3 * i) % 60 for i in range(450)], Hq=8, Hk=4, K=64, page=2, io="f32", order="page_inside"),
+    dict(lengths=[(13 * i) % 50 for i in range(500)], Hq=40, Hk=1, K=64, page=64),
+    dict(lengths=[(131 * i) % 700 for i in range(90)], Hq=8, Hk=4, K=128, page=16, order="token"),
+    dict(lengths=[(131 * i) % 700 for i in range(90)], Hq=6, Hk=6, K=64, page=16, order="token", io="f32"),
+]
+
+
+@pytest.mark.parametrize("case", MANY, ids=lambda c: "-".join(str(v) for k, v in c.items() if k != "lengths"))
+def test_decode_many_rows(case):
+    test_decode(case)
+
+
+APPEND_MANY = [
+    dict(B=1, T=23000, Hq=2, Hk=2, K=128, page=32, rotary=128, packed=True),
+    dict(B=1, T=13000, Hq=9, Hk=9, K=64, page=64, rotary=32, packed=True, order="token"),
+    dict(B=2, T=1100, Hq=15, Hk=9, K=256, page=16, io="f32", norm="l2", rotary=64, interleaved=True, order="page_inside"),
+]
+
+
+@pytest.mark.parametrize("case", APPEND_MANY, ids=lambda c: "-".join(str(v) for v in c.values()))
+def test_append_many_tokens(case):
+    test_append(case)
