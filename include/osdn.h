@@ -350,7 +350,7 @@ typedef struct {
  * Attention of one new token per sequence over a paged cache that holds it already.  Query head h reads head h Hk / Hq of the cache:
  *     s_j = scale <q, k_j> for max(0, length - window) <= j < length,  m = max_j s_j,
  *     lse = m + log sum_j e^(s_j - m),  o = sum_j e^(s_j - lse) v_j
- * in fp32, but that with bf16 I/O the weights e^(s_j - m) are rounded to bf16 for the product with the values.
+ * in fp32; with bf16 I/O the weights e^(s_j - m) go into the product with the values as the sum of two bf16 numbers (2^-16 off at most).
  *   q, o              [B,Hq,K] (rows; token is not used); o may be q
  *   lengths           [B] int32, tokens of the sequence in the cache; 0 (or less): none, o is zero and lse minus infinity
  *   seq               [B] int32 or NULL (=> b): row of the table.  Several queries may read one sequence, each

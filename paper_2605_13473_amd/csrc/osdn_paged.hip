@@ -38,6 +38,20 @@ __device__ __forceinline__ float max_xor32(float x) {
     return fmaxf(x, y);
 }
 
+// Weights of the second product with bf16 values: each as the sum of two bf16 numbers, at most 2^-16 of it off.  The first is the bits of the float
+// below it, cut off, so that neither is negative, and the second not zero where the weight is not: a value that is infinite makes the sum that.
+// (From the exact value in norm, with two numbers and with one: 33 tokens, K = 128, 1.654e-3, which is the rounding of o alone, and 1.741e-3, 1531
+// tokens 1.545e-3 and 1.589e-3.  us: 1531 tokens 10.25 and 10.14, uneven 64 x 8192 x 8 186.5 and 186.5, 512 x 4096 390.3 and 390.8.)
+__device__ __forceinline__ void two_parts(const f32x4 &p, bf16x4 &high, bf16x4 &low) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float x = p[r];           // (a bit cast of p[r] itself takes element 0)
+        const uint32_t top = __builtin_elementwise_sub_sat(__builtin_bit_cast(uint32_t, x), 1u) & 0xffff0000u;
+        high[r] = __builtin_bit_cast(bf16, (uint16_t)(top >> 16));
+        low[r] = (bf16)(x - __builtin_bit_cast(float, top));
+    }
+}
+
 template <typename T, int K> struct DecodeTile {
     static constexpr bool BF = sizeof(T) == 2;
     static constexpr int TT = decode_tile(K, BF);       // tokens: the depth of the second product's matrix instruction (fp32: four of them)
@@ -299,23 +313,21 @@ __global__ __launch_bounds__(DEC_T, (decode_per_cu(K, sizeof(T) == 2))) void dec
             if constexpr (D::BF) {
                 typedef short v4s __attribute__((ext_vector_type(4)));
                 typedef __attribute__((address_space(3))) v4s *lds_v4s;
-                // (the weights, at most one, are rounded to bf16 for this product; their sum is not: o is 1.8e-3 from its exact value in norm, of
-                // which the rounding of o itself is 1.7e-3)
-                bf16x4 weight[D::SETS];
+                bf16x4 high[D::SETS], low[D::SETS];
 #pragma unroll
-                for (int i = 0; i < D::SETS; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) weight[i][r] = (bf16)p[i][r];
+                for (int i = 0; i < D::SETS; ++i) two_parts(p[i], high[i], low[i]);
 #pragma unroll
                 for (int t = 0; t < OUT; ++t) {
                     const bf16 *at = reinterpret_cast<const bf16 *>(vs) + (4 * g + (col >> 2)) * LDV + 16 * t + 4 * (col & 3);
                     const v4s a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at));
                     if constexpr (D::SETS == 2) {
                         const v4s a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at + 16 * LDV));
-                        o[t] = Mfma<bf16>::mma(__builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7)),
-                                               __builtin_shufflevector(weight[0], weight[D::SETS - 1], 0, 1, 2, 3, 4, 5, 6, 7), o[t]);
+                        const bf16x8 values = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+                        o[t] = Mfma<bf16>::mma(values, __builtin_shufflevector(low[0], low[D::SETS - 1], 0, 1, 2, 3, 4, 5, 6, 7), o[t]);
+                        o[t] = Mfma<bf16>::mma(values, __builtin_shufflevector(high[0], high[D::SETS - 1], 0, 1, 2, 3, 4, 5, 6, 7), o[t]);
                     } else {
-                        o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0, __builtin_bit_cast(v4s, weight[0]), o[t], 0, 0, 0);
+                        o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0, __builtin_bit_cast(v4s, low[0]), o[t], 0, 0, 0);
+                        o[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a0, __builtin_bit_cast(v4s, high[0]), o[t], 0, 0, 0);
                     }
                 }
             } else {
