@@ -100,17 +100,12 @@ __device__ __forceinline__ void ask_arguments(const DecodeArgs &a) {
     asm volatile("" ::"s"(a.B), "s"(a.q.token), "s"(a.cache_k.data), "s"(a.cache_v.token), "s"(a.table_stride), "s"(a.part_ml));
 }
 
-// What the caller promised and did not keep makes the result NaN: nothing outside the cache is read
-__device__ __forceinline__ bool broken(const DecodeArgs &a, int length, int seq) {
-    return (unsigned)seq >= (unsigned)a.n_seqs || length > a.max_length || (length > 0 && (length - 1) >> a.page_shift >= a.max_pages);
+__device__ __forceinline__ Seen seen_of(const DecodeArgs &a, int length, int seq) {
+    return seen_tokens(length, seq, a.n_seqs, a.max_length, a.window, a.page_shift, a.max_pages);
 }
-__device__ __forceinline__ int first_seen(const DecodeArgs &a, int length) { return a.window > 0 && length > a.window ? length - a.window : 0; }
-// Units of UNIT tokens, from a multiple of DECODE_TILE on, of each row of sequence b; one where there is nothing to see, so that its zeros
-// (or NaN) are written
+// Units of UNIT tokens of each row of sequence b
 template <int UNIT> __device__ __forceinline__ int units_of(const DecodeArgs &a, int b) {
-    const int length = a.lengths[b], seq = a.seq ? a.seq[b] : b;
-    if (length <= 0 || broken(a, length, seq)) return 1;
-    return (length - (first_seen(a, length) & ~(DECODE_TILE - 1)) + UNIT - 1) / UNIT;
+    return seen_units(seen_of(a, a.lengths[b], a.seq ? a.seq[b] : b), UNIT);
 }
 
 // SHARED: even shares; else a workgroup takes one group of rows, whole (short ones, or many: no search and no second kernel)
@@ -183,11 +178,10 @@ __global__ __launch_bounds__(DEC_T, (decode_per_cu(K, sizeof(T) == 2))) void dec
         const int kt = group * R + wave / WPR;                      // this wavefront's row
         const int kv = a.head_tiles == 1 ? kt : kt / a.head_tiles, h0 = kv * a.group + 16 * (kt - kv * a.head_tiles);
         const int heads = min(16, (kv + 1) * a.group - h0);
-        const int seq = a.seq ? a.seq[b] : b, length = a.lengths[b], lo = first_seen(a, length);
-        const bool bad_call = broken(a, length, seq);
-        const int *row = a.table + (bad_call ? 0 : seq * a.table_stride);
-        const int begin = (lo & ~(DECODE_TILE - 1)) + u0 * STRIDE;
-        const int end = bad_call ? 0 : u1 == units ? length : begin + (u1 - u0) * STRIDE;
+        const int seq = a.seq ? a.seq[b] : b;
+        const Seen see = seen_of(a, a.lengths[b], seq);
+        const int *row = a.table + (see.end > 0 ? seq * a.table_stride : 0);
+        const int lo = see.lo, begin = seen_begin(see) + u0 * STRIDE, end = u1 == units ? see.end : begin + (u1 - u0) * STRIDE;
         TileLoads<T, K> x;
         x.ask(a, row, begin + turn * TT, lo, end, lane);
         // queries: lane l holds head l % 16
@@ -339,7 +333,7 @@ __global__ __launch_bounds__(DEC_T, (decode_per_cu(K, sizeof(T) == 2))) void dec
             tok = next;
         }
         l = add_xor32(add_xor16(l));
-        if (bad_call || __any(bad_page)) l = __builtin_nanf("");
+        if (see.broken || __any(bad_page)) l = __builtin_nanf("");
         const bool alone = !SHARED || u1 - u0 == units;                     // (nothing to join)
         const int slot = part_slot(w, at == share_begin);
         if (SHARED && u0 == 0 && threadIdx.x == 0) {

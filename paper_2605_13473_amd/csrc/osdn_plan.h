@@ -323,7 +323,20 @@ inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K
     return p;
 }
 
-// (constexpr: for the device too)
+// (constexpr, as what follows: for the device too)
+// The tokens [lo, end) that a query of a sequence sees; none where `broken`: what the caller promised and did not keep makes the result NaN, and nothing
+// outside the cache is read.  Both lie in [0, max_length] whatever stands for the length, so that counting on from them by tiles stays in 32 bits.
+struct Seen { int lo, end; bool broken; };
+constexpr Seen seen_tokens(int length, int seq, int n_seqs, int max_length, int window, int page_shift, int max_pages) {
+    const int last = length > 0 ? length - 1 : 0;
+    const bool broken = ((unsigned)seq >= (unsigned)n_seqs) | (length > max_length) | (last >> page_shift >= max_pages);
+    const int end = broken | (length <= 0) ? 0 : length;
+    return Seen{(window > 0) & (end > window) ? end - window : 0, end, broken};
+}
+// Where the first unit of a row begins, and how many of `unit` tokens it has; one where there is nothing to see, so that its zeros (or NaN) are written
+constexpr int seen_begin(const Seen &s) { return s.lo & ~(DECODE_TILE - 1); }
+constexpr int seen_units(const Seen &s, int unit) { return s.end > 0 ? (s.end - seen_begin(s) + unit - 1) / unit : 1; }
+
 // The even shares of n units among W workgroups: the first n % W have one more.  `owner`: the share that a unit falls to.
 struct Shares {
     int q, rem;
