@@ -352,7 +352,8 @@ typedef struct {
  *     lse = m + log sum_j e^(s_j - m),  o = sum_j e^(s_j - lse) v_j
  * in fp32; with bf16 I/O the weights e^(s_j - m) go into the product with the values as the sum of two bf16 numbers (2^-16 off at most).
  *   q, o              [B,Hq,K] (rows; token is not used); o may be q
- *   lengths           [B] int32, tokens of the sequence in the cache; 0 (or less): none, o is zero and lse minus infinity
+ *   lengths           [B] int32, tokens of the sequence in the cache; 0 (or less): none, o is zero and lse minus infinity, whatever
+ *                     stands for the sequence (a slot that nobody uses)
  *   seq               [B] int32 or NULL (=> b): row of the table.  Several queries may read one sequence, each
  *                     with its own length: drafted tokens, or a prompt token by token
  *   lse               [B,Hq] fp32 or NULL

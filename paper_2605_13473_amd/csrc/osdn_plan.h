@@ -325,12 +325,13 @@ inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K
 
 // (constexpr, as what follows: for the device too)
 // The tokens [lo, end) that a query of a sequence sees; none where `broken`: what the caller promised and did not keep makes the result NaN, and nothing
-// outside the cache is read.  Both lie in [0, max_length] whatever stands for the length, so that counting on from them by tiles stays in 32 bits.
+// outside the cache is read.  Without a token nothing is looked up, so the sequence is not asked for either.  Both lie in [0, max_length] whatever
+// stands for the length, so that counting on from them by tiles stays in 32 bits.
 struct Seen { int lo, end; bool broken; };
 constexpr Seen seen_tokens(int length, int seq, int n_seqs, int max_length, int window, int page_shift, int max_pages) {
-    const int last = length > 0 ? length - 1 : 0;
-    const bool broken = ((unsigned)seq >= (unsigned)n_seqs) | (length > max_length) | (last >> page_shift >= max_pages);
-    const int end = broken | (length <= 0) ? 0 : length;
+    const bool any = length > 0;
+    const bool broken = any & (((unsigned)seq >= (unsigned)n_seqs) | (length > max_length) | ((length - any) >> page_shift >= max_pages));
+    const int end = any & !broken ? length : 0;
     return Seen{(window > 0) & (end > window) ? end - window : 0, end, broken};
 }
 // Where the first unit of a row begins, and how many of `unit` tokens it has; one where there is nothing to see, so that its zeros (or NaN) are written

@@ -53,3 +53,9 @@ def test_tokens_that_are_seen(seen):
 def test_sequences_that_are_not_there(seen):
     for seq, n, broken in ((0, 1, 0), (1, 1, 1), (-1, 5, 1), (4, 5, 0), (5, 5, 1), (TOP, TOP, 1), (-TOP - 1, TOP, 1)):
         assert seen([(40, seq, n, 100, 0, 4, 10, 128)])[0][:3] == ([0, 0, 1] if broken else [0, 40, 0])
+
+
+def test_without_a_token_the_sequence_is_not_asked_for(seen):
+    for length in (0, -1, -TOP - 1):
+        for seq in (0, -1, 5, TOP, -TOP - 1):
+            assert seen([(length, seq, 5, 100, 7, 4, 10, 128)]) == [[0, 0, 0, 0, 1]]
