@@ -238,8 +238,9 @@ __global__ __launch_bounds__(HEADS_T) void heads_fwd_kernel(HeadsArgs a) {
                     turn.partners(raw[i], y);
 #pragma unroll
                     for (int e = 0; e < VE; ++e) {
-                        const float own = x[e] * (kind == 0 ? w.own[0][e] : w.own[1][e]), other = y[e] * (kind == 0 ? w.partner[0][e] : w.partner[1][e]);
-                        z[e] = r * __builtin_fmaf(own, c[e], other * s[e]);
+                        // (r first: where the sum of squares passes fp32 it is 0, and what it multiplies must not be infinite by then)
+                        const float own = x[e] * (r * (kind == 0 ? w.own[0][e] : w.own[1][e])), other = y[e] * (r * (kind == 0 ? w.partner[0][e] : w.partner[1][e]));
+                        z[e] = __builtin_fmaf(own, c[e], other * s[e]);
                     }
                 }
                 if (!live) continue;
