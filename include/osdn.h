@@ -279,8 +279,9 @@ typedef struct {
  * Norm of queries and keys for each head, with the position rotation in the same pass.  A row x becomes
  *     z = R(p) (w . x r),
  * R(p): pair i of the first rotary_dim elements turned by the angle whose cosine and sine are rotary[p][i] and
- * rotary[p][rotary_dim / 2 + i].  Computed in fp32, rounded once; a row whose sum of squares passes what fp32 holds
- * becomes zeros.  (norm = L2 without weights or rotation is what osdn_fwd expects of its caller's queries and keys.)
+ * rotary[p][rotary_dim / 2 + i].  Computed in fp32, rounded once; a row of finite elements whose sum of squares passes what
+ * fp32 holds becomes zeros, and so does its gradient.  (norm = L2 without weights or rotation is what osdn_fwd expects of its
+ * caller's queries and keys.)
  *   q, k              [B,T,Hq,K], [B,T,Hk,K]; Hq or Hk may be 0, then its arguments are not looked at
  *   weight_q, weight_k [K] fp32 or NULL (=> ones)
  *   rotary            [rotary_rows, rotary_dim] fp32, NULL iff rotary_dim == 0

@@ -327,6 +327,7 @@ __global__ __launch_bounds__(HEADS_T) void heads_bwd_kernel(HeadsArgs a) {
                 if (a.norm != 0) {
                     r = rsqrtf(__builtin_fmaf(row_sum<HR::LANES>(ss), a.mean, a.eps));
                     gx = row_sum<HR::LANES>(gx) * (r * r * a.mean);
+                    if (r == 0.f) gx = 0.f;             // (the sum of squares passes fp32, and so may this one: the row is zeros, and so is its gradient)
                 } else {
                     gx = 0.f;
                 }

@@ -57,3 +57,14 @@ def test_large_weights_on_large_rows(kind, io):
         rows, w = ref.f64(x[n]), ref.f64(x["w" + n])
         want, y = (ref.norm_rows(rows, w, t, pos, hp.norm, hp.eps, hp.interleaved) for t in (table, None))
         check(got, want, y.abs().amax(-1, keepdim=True), io == "bf16", n)
+
+
+@pytest.mark.parametrize("norm", ["l2", "rms"])
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", KINDS, ids=str)
+def test_gradients_of_rows_whose_squares_pass_fp32(kind, io, norm):
+    """They are zero, and the gradients of the weights are what they are without those rows."""
+    x, y = _with_large_rows(kind, io, norm)
+    g, want = (ob.qk_norm_backward(i["q"], i["k"], i["dq"], i["dk"], i["wq"], i["wk"], i["table"], None, i["hp"]) for i in (x, y))
+    for n in g:
+        assert (g[n] is None and want[n] is None) or torch.equal(g[n], want[n]), n
