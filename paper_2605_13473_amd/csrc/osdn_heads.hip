@@ -328,8 +328,6 @@ __global__ __launch_bounds__(HEADS_T) void heads_bwd_kernel(HeadsArgs a) {
                     r = rsqrtf(__builtin_fmaf(row_sum<HR::LANES>(ss), a.mean, a.eps));
                     gx = row_sum<HR::LANES>(gx) * (r * r * a.mean);
                     if (r == 0.f) gx = 0.f;             // (the sum of squares passes fp32, and so may this one: the row is zeros, and so is its gradient)
-                } else {
-                    gx = 0.f;
                 }
                 if (off_table) r = __builtin_nanf("");
                 if (none || !live) {
@@ -340,7 +338,7 @@ __global__ __launch_bounds__(HEADS_T) void heads_bwd_kernel(HeadsArgs a) {
                 float dx[VE];
 #pragma unroll
                 for (int e = 0; e < VE; ++e) {
-                    dx[e] = r * __builtin_fmaf(-gx, x[e], g[e]);
+                    dx[e] = r * (a.norm != 0 ? __builtin_fmaf(-gx, x[e], g[e]) : g[e]);       // (without a norm x has no part in it, infinite or NaN)
                     const float term = dy[e] * r;
                     if (query) dw[0][e] = __builtin_fmaf(term, x[e], dw[0][e]);
                     else dw[1][e] = __builtin_fmaf(term, x[e], dw[1][e]);

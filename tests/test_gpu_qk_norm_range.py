@@ -1,4 +1,6 @@
-"""Norm and rotation at the ends of the range of fp32: rows whose sum of squares passes it, products with weights that do."""
+"""Norm and rotation at the ends of the range of fp32: rows whose sum of squares passes it, products with weights that do, rows that are not looked at."""
+import math
+
 import pytest
 import torch
 
@@ -68,3 +70,16 @@ def test_gradients_of_rows_whose_squares_pass_fp32(kind, io, norm):
     g, want = (ob.qk_norm_backward(i["q"], i["k"], i["dq"], i["dk"], i["wq"], i["wk"], i["table"], None, i["hp"]) for i in (x, y))
     for n in g:
         assert (g[n] is None and want[n] is None) or torch.equal(g[n], want[n]), n
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", KINDS, ids=str)
+def test_without_a_norm_gradients_of_rows_do_not_see_them(kind, io):
+    """dx = w . R(-p) dz: what a row holds has no part in it, infinite or not a number."""
+    x = make(B=2, T=5, Hq=3, Hk=2, K=64, io=io, norm="none", seed=6, **kind)
+    args = (x["wq"], x["wk"], x["table"], None, x["hp"])
+    want = ob.qk_norm_backward(x["q"], x["k"], x["dq"], x["dk"], *args)
+    for n in "qk":
+        x[n][0, 2, 1, 7], x[n][1, 1, 0, 3], x[n][1, 4, 1] = math.inf, math.nan, -math.inf
+    got = ob.qk_norm_backward(x["q"], x["k"], x["dq"], x["dk"], *args)
+    assert torch.equal(got["dq"], want["dq"]) and torch.equal(got["dk"], want["dk"]) and bool(got["dq"].isfinite().all())
