@@ -257,9 +257,10 @@ int osdn_bwd_packed(const osdn_params *p, const void *q, const void *k, const vo
 /*
  * Around the recurrence: the rows of queries, keys and values of a layer, each K adjacent elements of io_dtype (K in {64, 128, 256}),
  * wherever the caller has them (slices of one projection's output, views): element (b, t, h, i) stands
- * batch b + token t + head h + i elements behind data.  No two rows of an output may overlap (a step of less than K along an axis
- * of more than one is refused).  Rows
- * need no more alignment than their elements; rows that start on 16 bytes are read and written in one piece.
+ * batch b + token t + head h + i elements behind data.  Rows need no more alignment than their elements; rows that start on 16
+ * bytes are read and written in one piece.  No two rows that a call writes may overlap.  Within one output, or a cache that is appended
+ * to, that is looked at, and the call refused unless the axes of more than one entry nest: taken from the smallest step on,
+ * each step is at least the extent of those before it (so in every slice or reordering of an array).
  */
 typedef struct { void *data; int64_t batch, token, head; } osdn_rows;
 

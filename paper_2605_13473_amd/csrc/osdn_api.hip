@@ -383,7 +383,7 @@ static int check_norm(const osdn_norm_params *p) {
     return OSDN_OK;
 }
 
-// whether steps along axes of n entries keep rows of K elements apart (as far as one axis can tell)
+// whether steps along an axis of n entries keep rows of K elements apart, as far as it alone can tell
 static bool apart(long long n, long long step, int K) { return n <= 1 || step >= K || step <= -K; }
 
 // A batch of rows of H heads (none: not looked at).  `out`: they are written, so no two may stand at one place.  Clears `aligned` unless
@@ -393,19 +393,23 @@ static int take_rows(const osdn_rows *r, long long B, long long T, long long H, 
     if (!r || !r->data) return OSDN_ERR_NULL;
     const uintptr_t at = reinterpret_cast<uintptr_t>(r->data);
     if (at % es != 0) return OSDN_ERR_SHAPE;
-    if (out && !(apart(B, r->batch, K) && apart(T, r->token, K) && apart(H, r->head, K))) return OSDN_ERR_SHAPE;
+    if (out && !rows_apart({B, T, H}, {r->batch, r->token, r->head}, K)) return OSDN_ERR_SHAPE;
     const long long ve = 16 / (long long)es;
     if (at % 16 != 0 || (B > 1 && r->batch % ve != 0) || (T > 1 && r->token % ve != 0) || (H > 1 && r->head % ve != 0)) aligned = false;
     to = HeadRows{r->data, r->batch, r->token, r->head};
     return OSDN_OK;
 }
 
-static int check_cache(const osdn_cache *c, int H, int K, size_t es, int &shift) {
+// `out`: rows are written
+static int check_cache(const osdn_cache *c, int H, int K, size_t es, bool out, int &shift) {
     if (!c || !c->k || !c->v || !c->table) return OSDN_ERR_NULL;
     if (c->n_pages < 1 || c->n_seqs < 1 || c->max_pages < 1 || c->page_size < 1 || (c->page_size & (c->page_size - 1)) != 0) return OSDN_ERR_SHAPE;
     if (c->table_stride < 0 || (c->table_stride < c->max_pages && c->table_stride != 0)) return OSDN_ERR_SHAPE;
     if (!(apart(c->n_pages, c->k_page, K) && apart(c->n_pages, c->v_page, K) && apart(c->page_size, c->k_token, K) && apart(c->page_size, c->v_token, K) &&
           apart(H, c->k_head, K) && apart(H, c->v_head, K)))
+        return OSDN_ERR_SHAPE;
+    if (out && !(rows_apart({c->n_pages, c->page_size, H}, {c->k_page, c->k_token, c->k_head}, K) &&
+                 rows_apart({c->n_pages, c->page_size, H}, {c->v_page, c->v_token, c->v_head}, K)))
         return OSDN_ERR_SHAPE;
     const long long ve = 16 / (long long)es;
     for (long long s : {c->k_page, c->k_token, c->k_head, c->v_page, c->v_token, c->v_head})
@@ -478,7 +482,7 @@ int osdn_paged_append(const osdn_norm_params *p, const osdn_cache *cache, const 
     if (p->Hk < 1) return OSDN_ERR_SHAPE;
     if ((p->rotary_dim && !rotary) || !positions) return OSDN_ERR_NULL;
     const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
-    if ((rc = check_cache(cache, p->Hk, p->K, es, shift)) != OSDN_OK) return rc;
+    if ((rc = check_cache(cache, p->Hk, p->K, es, true, shift)) != OSDN_OK) return rc;
     HeadsArgs a = heads_args(p, weight_q, weight_k, rotary, positions);
     if ((rc = take_rows(q, p->B, p->T, p->Hq, p->K, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(k, p->B, p->T, p->Hk, p->K, es, false, a.k, a.aligned)) != OSDN_OK ||
         (rc = take_rows(v, p->B, p->T, p->Hk, p->K, es, false, a.v, a.aligned)) != OSDN_OK || (rc = take_rows(q_out, p->B, p->T, p->Hq, p->K, es, true, a.q_out, a.aligned)) != OSDN_OK)
@@ -532,7 +536,7 @@ int osdn_paged_decode(const osdn_decode_params *p, const osdn_cache *cache, cons
     if (rc != OSDN_OK) return rc;
     if (!lengths) return OSDN_ERR_NULL;
     const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
-    if ((rc = check_cache(cache, p->Hk, p->K, es, a.page_shift)) != OSDN_OK) return rc;
+    if ((rc = check_cache(cache, p->Hk, p->K, es, false, a.page_shift)) != OSDN_OK) return rc;
     a.aligned = true;
     if ((rc = take_rows(q, p->B, 1, p->Hq, p->K, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(o, p->B, 1, p->Hq, p->K, es, true, a.o, a.aligned)) != OSDN_OK) return rc;
     if (a.shares) {

@@ -231,6 +231,26 @@ inline bool solved_plan(const osdn_params *p, long long chains, int longest, boo
     return p->p1_solved > 0 || (p->p1_solved == 0 && chains * (quarter ? 4 : 8) <= NUM_CU);
 }
 
+// Whether no two rows of K elements of a batch [n[0], n[1], n[2]] stand in one another, by its steps: taken from the smallest on, each is at least
+// the extent of what is inside it.  That holds for every slice, reordering and part of an array whose rows are apart; steps that only mesh
+// (2 K and 3 K, twice each) are not told from those that meet.
+inline bool rows_apart(const long long (&n)[3], const long long (&step)[3], int K) {
+    unsigned __int128 extent = (unsigned)K, size[3];
+    int axis[3], axes = 0;
+    for (int i = 0; i < 3; ++i) {
+        size[i] = step[i] < 0 ? -(__int128)step[i] : (__int128)step[i];
+        if (n[i] <= 1) continue;
+        int at = axes++;
+        for (; at > 0 && size[axis[at - 1]] > size[i]; --at) axis[at] = axis[at - 1];
+        axis[at] = i;
+    }
+    for (int i = 0; i < axes; ++i) {
+        if (size[axis[i]] < extent) return false;
+        extent += size[axis[i]] * (unsigned long long)(n[axis[i]] - 1);
+    }
+    return true;
+}
+
 // Blocks of rows (64 lanes of 16 bytes) of a token that one wavefront of heads_fwd_kernel takes: all of them where every CU then has sixteen wavefronts,
 // else as many pairs as leave it sixteen (its loads go in pairs), and one by one below eight.  us, from eight wavefronts with any number and from
 // sixteen: 1531 tokens of 8 blocks 8.5 and 7.5, 800 of 12 9.7 and 9.0, fp32 1500 of 8 8.6 and 7.7; 4000 of 2 one by one 8.4, as a pair 7.3.
