@@ -360,7 +360,8 @@ typedef struct {
  *                     with its own length: drafted tokens, or a prompt token by token
  *   lse               [B,Hq] fp32 or NULL
  *   workspace         osdn_paged_decode_workspace_bytes(p) bytes (0 also for invalid parameters), 256-byte aligned; may be NULL if that is 0
- * B Hq is below 2^21, and B Hk max_length / 64 (with more than 16 query heads a key head as many times that) below 2^31.
+ * B is at most 65535, B Hq below 2^21, and B Hk max_length / 64 (with more than 16 query heads a key head as many times that) below
+ * 2^31.
  * What a length hides is not looked at, whatever the cache holds there.  A length above max_length or above what a row of the
  * table holds, a sequence or a page that is not there: o and lse are NaN, and nothing outside the cache is read.
  */

@@ -26,6 +26,7 @@ _step_native = None        # _native.step, once the library is loaded (None: no 
 _rows_native = None        # _native, for the operators around the recurrence
 
 OSDN_F32, OSDN_BF16 = 0, 1
+OSDN_ERR_SHAPE = -2
 
 
 class OsdnParams(ctypes.Structure):
@@ -682,25 +683,37 @@ def paged_append(k, v, k_cache, v_cache, page_table, positions, seq=None, q=None
 def paged_decode(q, k_cache, v_cache, page_table, lengths, seq=None, scale=None, window: int = 0, max_length=None, want_lse: bool = False,
                  workspace=None):
     """Attention of one new token per sequence, q [B,Hq,K], over a paged cache.  max_length: no length is above it (None: what a
-    row of the table can hold).  Returns o, or (o, lse)."""
+    row of the table can hold).  More queries than a call of osdn_paged_decode takes go in several.  Returns o, or (o, lse)."""
     if _rows_native is not None and type(q) is torch.Tensor and q.is_cuda:
         dev = torch._C._cuda_getDevice()
         r = _rows_native.paged_decode(q, k_cache, v_cache, page_table, lengths, seq, workspace, scale, window, max_length, want_lse, dev,
                                       torch._C._cuda_getCurrentRawStream(dev))
         if type(r) is tuple:
             return r if want_lse else r[0]
-        if r is not None:
+        if r is not None and r != OSDN_ERR_SHAPE:           # (too many queries are that, too)
             _check(r)
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
         raise TypeError("expected q [B,Hq,K] and a cache [n_pages, page_size, Hk, K] as CUDA/HIP torch tensors")
     B, Hq, K = q.shape
     if max_length is None:
         max_length = min(page_table.shape[1] * k_cache.shape[1], 0x7fffff00)
-    p = make_decode_params(B, Hq, k_cache.shape[2], K, q.dtype == torch.bfloat16, max_length, scale, window)
+    most = min(65535, ((1 << 21) - 1) // max(Hq, 1)) or 1
+    if B > most:
+        if not q.is_cuda:
+            raise TypeError("q: expected a CUDA/HIP torch tensor")
+        _array(lengths, torch.int32, (B,), "lengths")
+        _array(seq, torch.int32, (B,), "seq")
+        if seq is None:
+            seq = torch.arange(B, dtype=torch.int32, device=q.device)
+        most = -(-B // -(-B // most))                       # (as many in each)
     o = q.new_empty(q.shape)
     lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device) if want_lse else None
-    if workspace is None:
-        n = osdn_paged_decode_workspace_bytes(p)
-        workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-    osdn_paged_decode(p, q, k_cache, v_cache, page_table, lengths, seq, o, lse, workspace)
+    of = (lambda t, i: t) if B <= most else (lambda t, i: None if t is None else t[i:i + most])
+    for i in range(0, max(B, 1), most):
+        p = make_decode_params(min(most, B - i), Hq, k_cache.shape[2], K, q.dtype == torch.bfloat16, max_length, scale, window)
+        ws = workspace
+        if ws is None:
+            n = osdn_paged_decode_workspace_bytes(p)
+            ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+        osdn_paged_decode(p, of(q, i), k_cache, v_cache, page_table, of(lengths, i), of(seq, i), of(o, i), of(lse, i), ws)
     return (o, lse) if want_lse else o
