@@ -493,7 +493,9 @@ def make_norm_params(B, T, Hq, Hk, K, bf16: bool, hp: NormHyper = NormHyper(), r
 
 def make_decode_params(B, Hq, Hk, K, bf16: bool, max_length: int, scale: float | None = None, window: int = 0,
                        shares: int = 0) -> OsdnDecodeParams:
-    return OsdnDecodeParams(B, Hq, Hk, K, OSDN_BF16 if bf16 else OSDN_F32, int(window or 0), int(max_length), int(shares),
+    # (a number past its field's end is the end: a window still shows all, the others are refused)
+    end = lambda x: max(-2**31, min(2**31 - 1, int(x)))
+    return OsdnDecodeParams(B, Hq, Hk, K, OSDN_BF16 if bf16 else OSDN_F32, end(window or 0), end(max_length), end(shares),
                             float(K) ** -0.5 if scale is None else float(scale))
 
 
