@@ -343,8 +343,9 @@ typedef struct {
     int32_t io_dtype;               /* osdn_dtype of q, o and the cache */
     int32_t window;                 /* > 0: only the last so many tokens are seen; 0: all */
     int32_t max_length;             /* no length is above it (the launch is sized by it) */
-    int32_t shares;                 /* scheduling: > 0 (up to 65535): cut the tokens among so many workgroups; -1: a workgroup for each
-                                       sequence, key head and 16 of its query heads; 0: the library decides */
+    int32_t shares;                 /* scheduling: > 0 (up to 65535): cut the tokens among so many workgroups; -1: no row is cut (a row: a
+                                       sequence, a key head and up to 16 of its query heads), a workgroup takes one, two or
+                                       four adjacent ones, as the library decides; 0: the library decides all of it */
     float scale;                    /* multiplies the scores (usually K^-1/2) */
 } osdn_decode_params;
 

@@ -11,7 +11,8 @@
 // A wavefront works on one token, so that the angles of its position are loaded once for its rows; 16 bytes per lane, K elements
 // in K * sizeof(T) / 16 lanes, 64 lanes in as many rows as that makes (a block of rows).  bf16, K = 128: 4 x 4096 tokens of 16 + 16 rows, unit length,
 // forward 44 us (6.1 TB/s, a part still in the last level cache), backward 78 us (5.2 TB/s: what a device copy reaches); 2 x 8192 of 32 + 8 with weights
-// and rotation 60 and 110 us; 65536 tokens of 16 + 4 + 4 appended 164 us (5.1 TB/s).
+// and rotation 61 and 110 us (4.6 of them the sum of dw); 65536 tokens of 16 + 4 + 4 appended 159 us (5.1 TB/s).  (Kernel times of a trace, medians,
+// three sets of inputs in turn.)
 #include "osdn_kernels.h"
 
 namespace osdn {

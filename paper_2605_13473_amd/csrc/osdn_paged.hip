@@ -4,15 +4,15 @@
 //   s_j = scale <q, k_j>,  m = max_j s_j,  l = sum_j e^(s_j - m),  o = sum_j e^(s_j - m) v_j / l,  lse = m + log l
 //
 // Bound by memory: every visible key and value is read once, for all query heads that share it (up to 16 side by side: the columns
-// of a 16 x 16 matrix product, so that one query head costs what 16 do, 3 % of the matrix cores' time).  A row is a sequence and a group of up to
+// of a 16 x 16 matrix product, so that one query head costs what 16 do, 6 % of the matrix cores' time).  A row is a sequence and a group of up to
 // 16 query heads of one key head.  A workgroup takes R adjacent rows of a sequence over the same tokens, each by 4 / R of its
 // wavefronts, which take the row's tiles in turn, with a running maximum and sum of their own, and join at its end (R = 4: nothing to join).
 // The visible tokens of all groups of R rows make one list that is cut into even shares, one a workgroup, whatever the lengths; a share is
 // a part of a group, or the end of one, whole ones and the beginning of the last.  Rows that a share does not hold whole go to a second
 // kernel, which joins their parts in their order.
-// 2.1 GB of keys and values of 512 sequences of 1 to 4096 tokens: 378 us, 5.7 TB/s (cut into pieces of 1024 tokens, a workgroup each, 401); 0.54 GB of one
-// sequence 99 us, 5.4 TB/s.  The second kernel takes 4 us; the fence that a join inside the first would take after every part costs more
-// (900 and 180 us).
+// 2.1 GB of keys and values of 512 sequences of 1 to 4096 tokens: 371 us, 5.8 TB/s (cut into pieces of 1024 tokens, a workgroup each, 22 more); 0.54 GB of
+// one sequence 97 us, 5.5 TB/s; reading alone reaches 5.9.  (Calls among others.)  The second kernel takes 3 to 6 us; the fence that a join inside the
+// first would take after every part costs more (900 and 180 us).
 //
 // A wavefront's tile is TT tokens.  Keys go from memory to registers as the matrix product wants them (lane l: token l % 16, 16 bytes);
 // scores come out transposed, lane l with four tokens of head l % 16, which is how the second product (values transposed,
