@@ -372,6 +372,149 @@ int osdn_paged_decode(const osdn_decode_params *p, const osdn_cache *cache, cons
                       void *stream);
 
 /*
+ * The pages of a cache from the lengths of requests, on the device: nothing of it has to be known to the host, and it may be
+ * captured into a graph.  A list holds the pages that are not in use: entries [0, n_free) of free_list, taken from its end.
+ */
+typedef struct {
+    int32_t *table;                 /* [n_seqs, max_pages], rows table_stride entries apart; NULL where a call only reads lengths */
+    int64_t table_stride;
+    int32_t *free_list;             /* [free_capacity] page numbers */
+    int32_t free_capacity;
+    int32_t n_pages, page_size, n_seqs, max_pages;          /* as those of osdn_cache */
+} osdn_pages;
+
+/*
+ * Places for the new tokens of B requests.  Request b brings fresh[b] tokens to sequence seq[b], which has cached[b]: it needs
+ * ceil((cached + fresh) / page_size) - ceil(cached / page_size) more pages.  Requests are looked at in their order: one is served if it
+ * needs no page or the needs up to it are no more than the list holds, and if it brings no token or those up to it are no more
+ * than `tokens`.  The i-th page that is granted is the i-th from the end of the list.
+ *   cached, fresh     [B] int32
+ *   seq               [B] int32 or NULL (=> b)
+ *   n_free            [1] int32: how many pages the list holds;  n_free_out [1] int32 out: and how many it holds then (may be n_free)
+ *   lengths           [B] int32 out: cached + fresh, or cached of a request that is not served (may be cached)
+ *   starts            [B + 1] int32 out: where the request's tokens begin on the token axis, and their number last
+ *   positions, rows   [tokens] int32 out: position and sequence of every token (-1 and -1 behind the last), as osdn_paged_append takes them
+ *   slots             [tokens] int64 out or NULL: page * page_size + place in the page; -1 behind the last, and where the page is not there
+ * Not served either, and without a part in the sums: a request whose sequence is not in the table, whose cached or fresh is negative or whose
+ * tokens its row of the table does not hold; and those that bring tokens to a sequence that another one brings some too.
+ * (lengths: 0 where the sequence is not in the table or cached is negative.)  B is at most 65535, tokens at least 1;
+ * with seq, n_seqs is at most 131072.
+ */
+int osdn_paged_plan(const osdn_pages *pages, int32_t B, int32_t tokens, const int32_t *cached, const int32_t *fresh, const int32_t *seq,
+                    const int32_t *n_free, int32_t *n_free_out, int32_t *lengths, int32_t *starts, int32_t *positions, int32_t *rows,
+                    int64_t *slots, void *stream);
+
+/*
+ * The pages of B sequences that end go back onto the list, and their entries of the table become -1: the first
+ * ceil(lengths[b] / page_size) of row seq[b], those that are there.  They lie so that the next requests take them in the order that they
+ * had.  A sequence that is named twice keeps its pages.  What the list has no room for is dropped.  Limits as for osdn_paged_plan.
+ */
+int osdn_paged_release(const osdn_pages *pages, int32_t B, const int32_t *lengths, const int32_t *seq, const int32_t *n_free,
+                       int32_t *n_free_out, void *stream);
+
+/*
+ * A paged cache in 4 bits (the microscaling format with 4-bit floats): blocks of 32 adjacent elements of a row share a scale 2^e, kept
+ * as the byte e + 127, and every element is a code of four bits: a sign (8) and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6.  The byte 255 makes all of a
+ * block NaN.  A row is K / 2 bytes of codes, two to a byte (the first in the lower bits), and K / 32 bytes of scales, which stand
+ * apart.  Steps are in bytes; rows of codes start on 16 bytes, rows of scales, for K = 256, on 2.  The page table is as
+ * in osdn_cache.
+ */
+typedef struct {
+    void *k, *v;                                    /* codes */
+    uint8_t *k_scale, *v_scale;
+    int64_t k_page, k_token, k_head, v_page, v_token, v_head;
+    int64_t k_scale_page, k_scale_token, k_scale_head, v_scale_page, v_scale_token, v_scale_head;
+    const int32_t *table;
+    int64_t table_stride;
+    int32_t n_pages, page_size, n_seqs, max_pages;
+} osdn_cache_mx;
+
+/*
+ * osdn_paged_append for a cache in 4 bits.  e is the least, from -120 to 125, with the largest element of the block no more than 7 * 2^e
+ * (a block without an element that is not zero: -120), the codes are the nearest values, ties to the even code; a block with an
+ * infinity or a NaN is kept as NaN.  Keys are normed and rotated in 64 bits and not rounded before, so that a code does not hang on the order of a sum.
+ * Queries are those of osdn_paged_append.
+ */
+int osdn_paged_append_mx(const osdn_norm_params *p, const osdn_cache_mx *cache, const osdn_rows *q, const osdn_rows *k, const osdn_rows *v,
+                         const float *weight_q, const float *weight_k, const float *rotary, const int32_t *positions,
+                         const int32_t *seq, const osdn_rows *q_out, void *stream);
+
+/*
+ * The rows that tokens have in a cache in 4 bits, as the values that they stand for (exact in both types of rows).
+ *   p                 B, T, Hk, K and io_dtype are looked at
+ *   positions, seq    as for osdn_paged_append; rows of a token that does not exist are zero, those of a sequence or page that is not there NaN
+ *   k_out, v_out      [B,T,Hk,K] out
+ */
+int osdn_paged_read_mx(const osdn_norm_params *p, const osdn_cache_mx *cache, const int32_t *positions, const int32_t *seq,
+                       const osdn_rows *k_out, const osdn_rows *v_out, void *stream);
+
+/*
+ * osdn_paged_decode over a cache in 4 bits: the same with the values that the codes stand for (io_dtype: of q and o).  Products are of bf16
+ * numbers with fp32 sums: the cache's values are exact in bf16; with bf16 I/O weights are the sum of two such numbers, with fp32 I/O
+ * queries and weights that of three, which hold all digits of a float.
+ */
+size_t osdn_paged_decode_mx_workspace_bytes(const osdn_decode_params *p);
+int osdn_paged_decode_mx(const osdn_decode_params *p, const osdn_cache_mx *cache, const osdn_rows *q, const int32_t *lengths,
+                         const int32_t *seq, const osdn_rows *o, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Attention over a few pages of a long cache, selected for each query and key head by a bound of their scores.
+ */
+typedef struct {
+    int32_t B, Hq, Hk, K;           /* queries (bounds: sequences), their heads (bounds: not looked at), heads of the cache, width */
+    int32_t io_dtype;               /* osdn_dtype of q, of the bounds, and of the cache unless that is in 4 bits */
+    int32_t max_length;             /* select: no length is above it */
+    int32_t max_new;                /* bounds: no sequence gets more new tokens (those beyond it are left out) */
+    int32_t pages;                  /* select: pages for each key head, at most; at least first + last */
+    int32_t first, last;            /* select: so many pages from the front (>= 0) and from the end (>= 1) are always among them */
+} osdn_select_params;
+
+/*
+ * The smallest and the largest key of every page, for each head and element, kept up with what is appended: those of the pages that the
+ * tokens cached[b] <= i < lengths[b] of sequence seq[b] stand in.  A page that had tokens before keeps their bounds, one that begins
+ * with these tokens gets new ones.  NaN among the keys makes the element's bounds NaN.
+ *   cache             the keys alone are looked at (v may be NULL)
+ *   cached, lengths   [B] int32 (as osdn_paged_plan leaves them); nothing to do where cached >= lengths
+ *   seq               [B] int32 or NULL (=> b).  No sequence twice
+ *   bounds            [n_pages, Hk, 2, K] io_dtype, in and out, 16-byte aligned: the smallest, then the largest
+ */
+int osdn_page_bounds(const osdn_select_params *p, const osdn_cache *cache, const int32_t *cached, const int32_t *lengths,
+                     const int32_t *seq, void *bounds, void *stream);
+int osdn_page_bounds_mx(const osdn_select_params *p, const osdn_cache_mx *cache, const int32_t *cached, const int32_t *lengths,
+                        const int32_t *seq, void *bounds, void *stream);
+
+/*
+ * The pages that a query reads.  For key head h and page g the score is sum over its query heads and the elements of
+ *     max(q_i lo_i, q_i hi_i),
+ * which no key of the page passes (computed in 64 bits).  Of the pages that the sequence has, the first `first`, the last `last` and
+ * those of the largest scores are chosen, p->pages in all or as many as there are; equal scores: the earlier page.  A page that is not
+ * there, and one whose score is NaN, come before all others.
+ *   q                 [B,Hq,K] rows (token is not used)
+ *   lengths, seq      as for osdn_paged_decode
+ *   chosen            [B,Hk,pages] int32 out: page numbers in the order of their tokens, -1 behind the last (and for one that is not there)
+ *   tokens            [B,Hk] int32 out: the tokens that they hold; 2^31 - 1 where osdn_paged_decode's results would be NaN
+ *                     for the length or the sequence
+ *   workspace         osdn_page_select_workspace_bytes(p) bytes, 256-byte aligned; may be NULL if that is 0
+ */
+size_t osdn_page_select_workspace_bytes(const osdn_select_params *p, int32_t page_size);
+int osdn_page_select(const osdn_select_params *p, const osdn_pages *pages, const osdn_rows *q, const void *bounds, const int32_t *lengths,
+                     const int32_t *seq, int32_t *chosen, int32_t *tokens, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * osdn_paged_decode over chosen pages: query head group h of entry b sees the first tokens[b][h] tokens of the pages chosen[b][h][...].
+ *   p                 as for osdn_paged_decode; max_length: no entry of tokens is above it; window is 0; B Hk at most 65535
+ *   cache             its table is not looked at
+ *   chosen            [B,Hk,n_chosen] int32
+ *   workspace         osdn_paged_decode_pages_workspace_bytes(p) (.._mx: of the cache in 4 bits) bytes
+ */
+size_t osdn_paged_decode_pages_workspace_bytes(const osdn_decode_params *p);
+size_t osdn_paged_decode_pages_mx_workspace_bytes(const osdn_decode_params *p);
+int osdn_paged_decode_pages(const osdn_decode_params *p, const osdn_cache *cache, const osdn_rows *q, const int32_t *chosen, int32_t n_chosen,
+                            const int32_t *tokens, const osdn_rows *o, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+int osdn_paged_decode_pages_mx(const osdn_decode_params *p, const osdn_cache_mx *cache, const osdn_rows *q, const int32_t *chosen, int32_t n_chosen,
+                               const int32_t *tokens, const osdn_rows *o, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Diagnostic query for tests: the decisions of the projection's derivative (Section 4.5,
  * reverse sweep through the projected affine recurrence) that osdn_bwd took, as it left them
  * in the workspace.  Returns the byte offset, inside a workspace of a plain (not packed) batch

@@ -64,6 +64,22 @@ class OsdnDecodeParams(ctypes.Structure):
         ("scale", ctypes.c_float)]
 
 
+class OsdnPages(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("free_list", ctypes.c_void_p)] + [
+        (n, ctypes.c_int32) for n in ("free_capacity", "n_pages", "page_size", "n_seqs", "max_pages")]
+
+
+class OsdnCacheMx(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+                + [(f"{t}_{n}", ctypes.c_int64) for t in ("k", "v", "k_scale", "v_scale") for n in ("page", "token", "head")]
+                + [("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64)]
+                + [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "n_seqs", "max_pages")])
+
+
+class OsdnSelectParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hk", "K", "io_dtype", "max_length", "max_new", "pages", "first", "last")]
+
+
 class OsdnError(RuntimeError):
     def __init__(self, status: int):
         self.status = status
@@ -119,6 +135,21 @@ def lib():
         L.osdn_paged_decode_workspace_bytes.argtypes = [dp]
         L.osdn_paged_decode.restype = ctypes.c_int
         L.osdn_paged_decode.argtypes = [dp, cp, rp, vp, vp, rp, fp, vp, ctypes.c_size_t, vp]
+        mp, gp, sp = ctypes.POINTER(OsdnCacheMx), ctypes.POINTER(OsdnPages), ctypes.POINTER(OsdnSelectParams)
+        i32, size = ctypes.c_int32, ctypes.c_size_t
+        for name, of in (("osdn_paged_plan", [gp, i32, i32] + [vp] * 11), ("osdn_paged_release", [gp, i32] + [vp] * 5),
+                         ("osdn_paged_append_mx", [np_, mp, rp, rp, rp, fp, fp, fp, vp, vp, rp, vp]), ("osdn_paged_read_mx", [np_, mp, vp, vp, rp, rp, vp]),
+                         ("osdn_paged_decode_mx", [dp, mp, rp, vp, vp, rp, fp, vp, size, vp]),
+                         ("osdn_paged_decode_pages", [dp, cp, rp, vp, i32, vp, rp, fp, vp, size, vp]),
+                         ("osdn_paged_decode_pages_mx", [dp, mp, rp, vp, i32, vp, rp, fp, vp, size, vp]),
+                         ("osdn_page_bounds", [sp, cp, vp, vp, vp, vp, vp]), ("osdn_page_bounds_mx", [sp, mp, vp, vp, vp, vp, vp]),
+                         ("osdn_page_select", [sp, gp, rp, vp, vp, vp, vp, vp, vp, size, vp])):
+            getattr(L, name).restype = ctypes.c_int
+            getattr(L, name).argtypes = of
+        for name, of in (("osdn_paged_decode_mx_workspace_bytes", [dp]), ("osdn_paged_decode_pages_workspace_bytes", [dp]),
+                         ("osdn_paged_decode_pages_mx_workspace_bytes", [dp]), ("osdn_page_select_workspace_bytes", [sp, i32])):
+            getattr(L, name).restype = size
+            getattr(L, name).argtypes = of
         L.osdn_profile_enable.restype = None
         L.osdn_profile_enable.argtypes = [ctypes.c_int]
         L.osdn_profile_kernel_count.restype = ctypes.c_int
@@ -133,6 +164,10 @@ def lib():
             _native.bind_rows(*(ctypes.cast(f, vp).value for f in (
                 L.osdn_qk_norm_fwd, L.osdn_qk_norm_bwd, L.osdn_qk_norm_bwd_workspace_bytes, L.osdn_paged_append, L.osdn_paged_decode,
                 L.osdn_paged_decode_workspace_bytes)), *(ctypes.sizeof(c) for c in (OsdnRows, OsdnNormParams, OsdnCache, OsdnDecodeParams)))
+            _native.bind_pages(tuple(ctypes.cast(getattr(L, "osdn_" + f), vp).value for f in (
+                "paged_plan", "paged_release", "paged_append_mx", "paged_read_mx", "paged_decode_mx", "paged_decode_mx_workspace_bytes", "page_bounds",
+                "page_bounds_mx", "page_select", "page_select_workspace_bytes", "paged_decode_pages", "paged_decode_pages_workspace_bytes",
+                "paged_decode_pages_mx", "paged_decode_pages_mx_workspace_bytes")), *(ctypes.sizeof(c) for c in (OsdnPages, OsdnCacheMx, OsdnSelectParams)))
             _step_native, _rows_native = _native.step, _native
         except (ImportError, TypeError, AttributeError) as e:       # (TypeError, AttributeError: one of an earlier interface)
             warnings.warn(f"no extension module ({e}): step goes through Python, at twice the time of a small call; "
@@ -719,3 +754,389 @@ def paged_decode(q, k_cache, v_cache, page_table, lengths, seq=None, scale=None,
             ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
         osdn_paged_decode(p, of(q, i), k_cache, v_cache, page_table, of(lengths, i), of(seq, i), of(o, i), of(lse, i), ws)
     return (o, lse) if want_lse else o
+
+
+# ----------------------------------------------------------------- the pages of a cache ----
+def _table_of(page_table):
+    """(n_seqs, max_pages, stride) of a page table."""
+    if not isinstance(page_table, torch.Tensor) or not page_table.is_cuda or page_table.dtype != torch.int32:
+        raise TypeError("page_table: expected an int32 CUDA/HIP torch tensor")
+    if page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table: expected [n_seqs, max_pages] with adjacent entries of a row")
+    _here(page_table, "page_table")
+    n_seqs, max_pages = page_table.shape
+    return n_seqs, max_pages, page_table.stride(0) if n_seqs > 1 else max_pages
+
+
+def _pages(page_table, page_size, n_pages, free_pages=None):
+    n_seqs, max_pages, stride = _table_of(page_table)
+    free = _array(free_pages, torch.int32, None, "free_pages")
+    capacity = 0 if free_pages is None else free_pages.numel()
+    end = lambda x: max(-1, min(2**31 - 1, int(x)))
+    return OsdnPages(page_table.data_ptr(), stride, free, end(capacity), end(n_pages), end(page_size), n_seqs, max_pages)
+
+
+def _requests(t, name):
+    if not isinstance(t, torch.Tensor) or t.dim() != 1:
+        raise TypeError(f"{name}: expected an int32 CUDA/HIP torch tensor [B]")
+    return t.shape[0]
+
+
+def osdn_paged_plan(pages, B, tokens, cached, fresh, seq, n_free, n_free_out, lengths, starts, positions, rows, slots=None, stream=None):
+    i32 = torch.int32
+    of = lambda t, n, name: _array(t, i32, (n,), name)
+    _check(lib().osdn_paged_plan(
+        ctypes.byref(pages), B, tokens, of(cached, B, "cached"), of(fresh, B, "fresh"), of(seq, B, "seq"), of(n_free, 1, "n_free"), of(n_free_out, 1, "n_free_out"),
+        of(lengths, B, "lengths"), of(starts, B + 1, "starts"), _array(positions, i32, None, "positions"), _array(rows, i32, None, "rows"),
+        _array(slots, torch.int64, (tokens,), "slots"), _stream_ptr(stream)))
+
+
+def osdn_paged_release(pages, B, lengths, seq, n_free, n_free_out, stream=None):
+    of = lambda t, n, name: _array(t, torch.int32, (n,), name)
+    _check(lib().osdn_paged_release(ctypes.byref(pages), B, of(lengths, B, "lengths"), of(seq, B, "seq"), of(n_free, 1, "n_free"),
+                                    of(n_free_out, 1, "n_free_out"), _stream_ptr(stream)))
+
+
+def paged_plan(page_table, cached, fresh, free_pages, n_free, page_size: int, tokens: int, seq=None, n_pages=None, want_slots: bool = False):
+    """Places for the new tokens of a batch of requests: request b brings fresh[b] tokens to sequence seq[b] (None: b), which has cached[b].  The pages that it
+    needs come off the end of free_pages, of which n_free [1] are in the list, into page_table; both are written in place.  tokens: the length of
+    the token axis, at least the sum of fresh.  n_pages: of the cache (None: as many as the list has room for).  Returns a dict: lengths [B], starts [B + 1],
+    positions and seq [1, tokens] as ``paged_append`` takes them, n_free [1] (for the next call) and, if wanted, slots [tokens] int64.  A request that
+    finds no pages is not served: its length stays, its tokens have no places, and starts[b + 1] == starts[b]."""
+    if _rows_native is not None and type(page_table) is torch.Tensor and page_table.is_cuda:
+        dev = torch._C._cuda_getDevice()
+        r = _rows_native.paged_plan(page_table, cached, fresh, free_pages, n_free, seq, page_size, tokens, n_pages, want_slots, dev,
+                                    torch._C._cuda_getCurrentRawStream(dev))
+        if type(r) is tuple:
+            return {"lengths": r[0], "starts": r[1], "positions": r[2], "seq": r[3], "n_free": r[4], "slots": r[5]}
+        if r is not None:
+            _check(r)
+    B, N = _requests(cached, "cached"), int(tokens)
+    g = _pages(page_table, page_size, free_pages.numel() if n_pages is None and isinstance(free_pages, torch.Tensor) else n_pages or 0, free_pages)
+    new = lambda *shape, dtype=torch.int32: torch.empty(*shape, dtype=dtype, device=page_table.device)
+    if N < 0 or N > 2**31 - 1:
+        raise OsdnError(OSDN_ERR_SHAPE)
+    r = {"lengths": new(B), "starts": new(B + 1), "positions": new(1, N), "seq": new(1, N), "n_free": new(1),
+         "slots": new(N, dtype=torch.int64) if want_slots else None}
+    osdn_paged_plan(g, B, N, cached, fresh, seq, n_free, r["n_free"], r["lengths"], r["starts"], r["positions"], r["seq"], r["slots"])
+    return r
+
+
+def paged_release(page_table, lengths, free_pages, n_free, page_size: int, seq=None, n_pages=None):
+    """The pages of sequences that end (rows seq of the table, None: the first ones, of these lengths) go back onto the list; in place.  Returns how many
+    the list holds then, [1]."""
+    if _rows_native is not None and type(page_table) is torch.Tensor and page_table.is_cuda:
+        dev = torch._C._cuda_getDevice()
+        r = _rows_native.paged_release(page_table, lengths, free_pages, n_free, seq, page_size, n_pages, dev, torch._C._cuda_getCurrentRawStream(dev))
+        if r is not None:
+            return r[0] if type(r) is tuple else _check(r)
+    B = _requests(lengths, "lengths")
+    g = _pages(page_table, page_size, free_pages.numel() if n_pages is None and isinstance(free_pages, torch.Tensor) else n_pages or 0, free_pages)
+    out = torch.empty(1, dtype=torch.int32, device=page_table.device)
+    osdn_paged_release(g, B, lengths, seq, n_free, out)
+    return out
+
+
+# ------------------------------------------------------------------- a cache in 4 bits ----
+def alloc_paged_cache_mx(n_pages: int, page_size: int, H: int, K: int, device="cuda"):
+    """(k, v, k_scale, v_scale) of a cache in 4 bits: codes [n_pages, page_size, H, K / 2] and scales [n_pages, page_size, H, K / 32], uint8; a page
+    holds its tokens head after head (any order of pages, tokens and heads is taken)."""
+    new = lambda n: torch.empty(n_pages, H, page_size, n, dtype=torch.uint8, device=device).transpose(1, 2)
+    return new(K // 2), new(K // 2), new(K // 32), new(K // 32)
+
+
+def _cache_mx(cache, page_table, H, K, keys_alone=False):
+    """page_table None: one that is not looked at."""
+    n = 2 if keys_alone else 4
+    if not isinstance(cache, (tuple, list)) or len(cache) != n or not isinstance(cache[0], torch.Tensor) or cache[0].dim() != 4:
+        raise TypeError("cache: expected (k, k_scale), codes and scales" if keys_alone else "cache: expected (k, v, k_scale, v_scale), codes [n_pages, page_size, H, K / 2] and "
+                        "scales [n_pages, page_size, H, K / 32]")
+    n_pages, page_size = cache[0].shape[:2]
+    r = [_rows(t, torch.uint8, (n_pages, page_size, H, K // (2 if i < n // 2 else 32)), name)
+         for i, (t, name) in enumerate(zip(cache, ("k", "k_scale") if keys_alone else ("k", "v", "k_scale", "v_scale")))]
+    if any(x is None for x in r):
+        raise TypeError("cache: expected CUDA/HIP torch tensors")
+    k, v, ks, vs = (r[0], r[0], r[1], r[1]) if keys_alone else r
+    n_seqs, max_pages, stride = (1, 1, 1) if page_table is None else _table_of(page_table)
+    steps = [x for y in (k, v, ks, vs) for x in (y.batch, y.token, y.head)]
+    return OsdnCacheMx(k.data, v.data, ks.data, vs.data, *steps, None if page_table is None else page_table.data_ptr(), stride, n_pages, page_size, n_seqs, max_pages)
+
+
+def osdn_paged_append_mx(params, q, k, v, cache, page_table, weight_q, weight_k, rotary, positions, seq, q_out, stream=None):
+    p = params
+    r = _norm_rows(p, q, k, (v, "v"), (q_out, "q_out"))
+    c = _cache_mx(cache, page_table, p.Hk, p.K)
+    _check(lib().osdn_paged_append_mx(
+        ctypes.byref(p), ctypes.byref(c), *(_ref(x) for x in r[:3]), *_norm_shared(p, weight_q, weight_k, rotary, positions),
+        _array(seq, torch.int32, (p.B, p.T), "seq"), _ref(r[3]), _stream_ptr(stream)))
+
+
+def osdn_paged_read_mx(params, cache, page_table, positions, seq, k_out, v_out, stream=None):
+    p, i32 = params, torch.int32
+    r = [_rows(t, _io_torch_dtype(p), (p.B, p.T, p.Hk, p.K), name) for t, name in ((k_out, "k_out"), (v_out, "v_out"))]
+    c = _cache_mx(cache, page_table, p.Hk, p.K)
+    _check(lib().osdn_paged_read_mx(ctypes.byref(p), ctypes.byref(c), _array(positions, i32, (p.B, p.T), "positions"), _array(seq, i32, (p.B, p.T), "seq"),
+                                    _ref(r[0]), _ref(r[1]), _stream_ptr(stream)))
+
+
+def osdn_paged_decode_mx_workspace_bytes(params) -> int:
+    return int(lib().osdn_paged_decode_mx_workspace_bytes(ctypes.byref(params)))
+
+
+def _decode_outputs(p, q, o, lse, workspace):
+    io, rows = _io_torch_dtype(p), (p.B, p.Hq, p.K)
+    return (_ref(_rows(q, io, rows, "q")), _ref(_rows(o, io, rows, "o")), _array(lse, torch.float32, (p.B, p.Hq), "lse"),
+            _array(workspace, torch.uint8, None, "workspace"), ctypes.c_size_t(0 if workspace is None else workspace.numel()))
+
+
+def osdn_paged_decode_mx(params, q, cache, page_table, lengths, seq, o, lse, workspace=None, stream=None):
+    p, i32 = params, torch.int32
+    c = _cache_mx(cache, page_table, p.Hk, p.K)
+    qr, orows, lp, ws, n = _decode_outputs(p, q, o, lse, workspace)
+    _check(lib().osdn_paged_decode_mx(ctypes.byref(p), ctypes.byref(c), qr, _array(lengths, i32, (p.B,), "lengths"), _array(seq, i32, (p.B,), "seq"), orows, lp,
+                                      ws, n, _stream_ptr(stream)))
+
+
+def paged_append_mx(k, v, cache, page_table, positions, seq=None, q=None, weight_q=None, weight_k=None, rotary=None, hp: NormHyper = NormHyper()):
+    """``paged_append`` to a cache in 4 bits (``alloc_paged_cache_mx``)."""
+    if _rows_native is not None and type(k) is torch.Tensor and k.is_cuda and type(cache) is tuple and len(cache) == 4:
+        dev = torch._C._cuda_getDevice()
+        r = _rows_native.paged_append_mx(k, v, *cache, page_table, positions, seq, q, weight_q, weight_k, rotary, hp, dev,
+                                         torch._C._cuda_getCurrentRawStream(dev))
+        if r is not None:
+            return r[0] if type(r) is tuple else _check(r)
+    p = _params_of(q, k, hp, rotary)
+    q_out = None if q is None else q.new_empty(q.shape)
+    osdn_paged_append_mx(p, q, k, v, cache, page_table, weight_q, weight_k, rotary, positions, seq, q_out)
+    return q_out
+
+
+def paged_read_mx(cache, page_table, positions, seq=None, dtype=torch.bfloat16):
+    """The rows that the tokens at positions [B,T] of their sequences have in a cache in 4 bits, as values: (k, v) [B,T,H,K]."""
+    if _rows_native is not None and type(positions) is torch.Tensor and positions.is_cuda and type(cache) is tuple and len(cache) == 4:
+        dev = torch._C._cuda_getDevice()
+        r = _rows_native.paged_read_mx(*cache, page_table, positions, seq, dtype is torch.bfloat16, dtype is torch.float32, dev,
+                                       torch._C._cuda_getCurrentRawStream(dev))
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("dtype: expected torch.bfloat16 or torch.float32")
+    if not isinstance(positions, torch.Tensor) or positions.dim() != 2:
+        raise TypeError("positions: expected an int32 CUDA/HIP torch tensor [B,T]")
+    if not isinstance(cache, (tuple, list)) or len(cache) != 4 or not isinstance(cache[0], torch.Tensor) or cache[0].dim() != 4:
+        raise TypeError("cache: expected (k, v, k_scale, v_scale), codes [n_pages, page_size, H, K / 2] and scales [n_pages, page_size, H, K / 32]")
+    (B, T), (H, K) = positions.shape, (cache[0].shape[2], 2 * cache[0].shape[3])
+    p = OsdnNormParams(B, T, 0, H, K, OSDN_BF16 if dtype == torch.bfloat16 else OSDN_F32, 0, 0, 0, 0, 0.0)
+    out = [torch.empty(B, T, H, K, dtype=dtype, device=positions.device) for _ in range(2)]
+    osdn_paged_read_mx(p, cache, page_table, positions, seq, *out)
+    return tuple(out)
+
+
+def _decode_in_parts(q, most, lengths, bytes_of, call, per_head, workspace, want_lse):
+    """Calls of at most `most` queries each; per_head: what goes with a query."""
+    B, Hq, _ = q.shape
+    most = most if B <= most else -(-B // -(-B // most))
+    o = q.new_empty(q.shape)
+    lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device) if want_lse else None
+    of = (lambda t, i: t) if B <= most else (lambda t, i: None if t is None else t[i:i + most])
+    for i in range(0, max(B, 1), most):
+        n = min(most, B - i)
+        ws = workspace
+        if ws is None:
+            size = bytes_of(n)
+            ws = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
+        call(n, of(q, i), *(of(t, i) for t in per_head), of(o, i), of(lse, i), ws)
+    return (o, lse) if want_lse else o
+
+
+def paged_decode_mx(q, cache, page_table, lengths, seq=None, scale=None, window: int = 0, max_length=None, want_lse: bool = False, workspace=None):
+    """``paged_decode`` over a cache in 4 bits."""
+    if _rows_native is not None and type(q) is torch.Tensor and q.is_cuda and type(cache) is tuple and len(cache) == 4:
+        dev = torch._C._cuda_getDevice()
+        r = _rows_native.paged_decode_mx(q, *cache, page_table, lengths, seq, workspace, scale, window, max_length, want_lse, dev,
+                                         torch._C._cuda_getCurrentRawStream(dev))
+        if type(r) is tuple:
+            return r if want_lse else r[0]
+        if r is not None and r != OSDN_ERR_SHAPE:           # (too many queries are that, too)
+            _check(r)
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(cache, (tuple, list)) or len(cache) != 4 or not isinstance(cache[0], torch.Tensor) or cache[0].dim() != 4:
+        raise TypeError("expected q [B,Hq,K] and a cache (k, v, k_scale, v_scale) as CUDA/HIP torch tensors")
+    B, Hq, K = q.shape
+    Hk = cache[0].shape[2]
+    if max_length is None:
+        max_length = min(page_table.shape[1] * cache[0].shape[1], 0x7fffff00)
+    most = min(65535, ((1 << 21) - 1) // max(Hq, 1)) or 1
+    if B > most:
+        if not q.is_cuda:
+            raise TypeError("q: expected a CUDA/HIP torch tensor")
+        _array(lengths, torch.int32, (B,), "lengths")
+        _array(seq, torch.int32, (B,), "seq")
+        if seq is None:
+            seq = torch.arange(B, dtype=torch.int32, device=q.device)
+    params = lambda n: make_decode_params(n, Hq, Hk, K, q.dtype == torch.bfloat16, max_length, scale, window)
+    return _decode_in_parts(q, most, lengths, lambda n: osdn_paged_decode_mx_workspace_bytes(params(n)),
+                            lambda n, q, lengths, seq, o, lse, ws: osdn_paged_decode_mx(params(n), q, cache, page_table, lengths, seq, o, lse, ws), (lengths, seq), workspace, want_lse)
+
+
+# ------------------------------------------------------- attention over selected pages ----
+def alloc_page_bounds(n_pages: int, H: int, K: int, dtype=torch.bfloat16, device="cuda"):
+    """Bounds of the keys of every page, [n_pages, H, 2, K]: the smallest, the largest."""
+    return torch.empty(n_pages, H, 2, K, dtype=dtype, device=device)
+
+
+def make_select_params(B, Hq, Hk, K, bf16: bool, max_length: int = 0, max_new: int = 1, pages: int = 2, first: int = 1, last: int = 1) -> OsdnSelectParams:
+    end = lambda x: max(-2**31, min(2**31 - 1, int(x)))
+    return OsdnSelectParams(B, Hq, Hk, K, OSDN_BF16 if bf16 else OSDN_F32, *(end(x) for x in (max_length, max_new, pages, first, last)))
+
+
+def osdn_page_bounds(params, keys, page_table, cached, lengths, seq, bounds, stream=None):
+    """keys: those of a cache [n_pages, page_size, Hk, K], or (codes, scales) of one in 4 bits (osdn_page_bounds_mx)."""
+    p, i32 = params, torch.int32
+    more = [_array(t, i32, (p.B,), name) for t, name in ((cached, "cached"), (lengths, "lengths"), (seq, "seq"))]
+    if isinstance(keys, (tuple, list)):
+        c, call = _cache_mx(keys, page_table, p.Hk, p.K, keys_alone=True), lib().osdn_page_bounds_mx
+    else:
+        c, call = _cache(keys, keys, page_table, _io_torch_dtype(p), p.Hk, p.K), lib().osdn_page_bounds
+    _check(call(ctypes.byref(p), ctypes.byref(c), *more, _array(bounds, _io_torch_dtype(p), (c.n_pages, p.Hk, 2, p.K), "bounds"), _stream_ptr(stream)))
+
+
+def osdn_page_select_workspace_bytes(params, page_size: int) -> int:
+    return int(lib().osdn_page_select_workspace_bytes(ctypes.byref(params), int(page_size)))
+
+
+def osdn_page_select(params, pages, q, bounds, lengths, seq, chosen, tokens, workspace=None, stream=None):
+    p, i32 = params, torch.int32
+    io = _io_torch_dtype(p)
+    _check(lib().osdn_page_select(
+        ctypes.byref(p), ctypes.byref(pages), _ref(_rows(q, io, (p.B, p.Hq, p.K), "q")), _array(bounds, io, (pages.n_pages, p.Hk, 2, p.K), "bounds"),
+        _array(lengths, i32, (p.B,), "lengths"), _array(seq, i32, (p.B,), "seq"), _array(chosen, i32, (p.B, p.Hk, p.pages), "chosen"),
+        _array(tokens, i32, (p.B, p.Hk), "tokens"), _array(workspace, torch.uint8, None, "workspace"),
+        ctypes.c_size_t(0 if workspace is None else workspace.numel()), _stream_ptr(stream)))
+
+
+def _pages_bytes(params, mx) -> int:
+    return int((lib().osdn_paged_decode_pages_mx_workspace_bytes if mx else lib().osdn_paged_decode_pages_workspace_bytes)(ctypes.byref(params)))
+
+
+def osdn_paged_decode_pages_workspace_bytes(params) -> int:
+    return _pages_bytes(params, False)
+
+
+def osdn_paged_decode_pages_mx_workspace_bytes(params) -> int:
+    return _pages_bytes(params, True)
+
+
+def _chosen(p, chosen, tokens):
+    if not isinstance(chosen, torch.Tensor) or chosen.dim() != 3:
+        raise TypeError("chosen: expected an int32 CUDA/HIP torch tensor [B,Hk,pages]")
+    n = chosen.shape[2]
+    return _array(chosen, torch.int32, (p.B, p.Hk, n), "chosen"), n, _array(tokens, torch.int32, (p.B, p.Hk), "tokens")
+
+
+def osdn_paged_decode_pages(params, q, k_cache, v_cache, chosen, tokens, o, lse, workspace=None, stream=None):
+    p = params
+    at, n, toks = _chosen(p, chosen, tokens)
+    c = _cache(k_cache, v_cache, chosen.flatten(0, 1), _io_torch_dtype(p), p.Hk, p.K)
+    qr, orows, lp, ws, size = _decode_outputs(p, q, o, lse, workspace)
+    _check(lib().osdn_paged_decode_pages(ctypes.byref(p), ctypes.byref(c), qr, at, n, toks, orows, lp, ws, size, _stream_ptr(stream)))
+
+
+def osdn_paged_decode_pages_mx(params, q, cache, chosen, tokens, o, lse, workspace=None, stream=None):
+    p = params
+    at, n, toks = _chosen(p, chosen, tokens)
+    c = _cache_mx(cache, None, p.Hk, p.K)
+    qr, orows, lp, ws, size = _decode_outputs(p, q, o, lse, workspace)
+    _check(lib().osdn_paged_decode_pages_mx(ctypes.byref(p), ctypes.byref(c), qr, at, n, toks, orows, lp, ws, size, _stream_ptr(stream)))
+
+
+def page_bounds(keys, page_table, cached, lengths, bounds, seq=None, max_new=None):
+    """Keep the bounds of the pages up with what was appended: the tokens cached[b] <= i < lengths[b] of sequence seq[b] (None: b).  keys: those of
+    a cache [n_pages, page_size, Hk, K], or (codes, scales) of one in 4 bits.  bounds [n_pages, Hk, 2, K] are written in place.
+    max_new: no sequence gets more new tokens (None: what a row of the table can hold)."""
+    mx = isinstance(keys, (tuple, list))
+    k = keys[0] if mx and len(keys) == 2 else keys
+    if _rows_native is not None and type(bounds) is torch.Tensor and bounds.is_cuda and (not mx or len(keys) == 2):
+        dev = torch._C._cuda_getDevice()
+        r = _rows_native.page_bounds(k, keys[1] if mx else None, page_table, cached, lengths, seq, bounds, max_new, dev, torch._C._cuda_getCurrentRawStream(dev))
+        if r is not None:
+            return None if type(r) is tuple else _check(r)
+    if not isinstance(k, torch.Tensor) or k.dim() != 4 or not isinstance(bounds, torch.Tensor) or bounds.dim() != 4:
+        raise TypeError("expected keys [n_pages, page_size, Hk, K] and bounds [n_pages, Hk, 2, K] as CUDA/HIP torch tensors")
+    if max_new is None:
+        max_new = page_table.shape[1] * k.shape[1]
+    p = make_select_params(_requests(cached, "cached"), 0, k.shape[2], bounds.shape[3], bounds.dtype == torch.bfloat16, max_new=max_new)
+    osdn_page_bounds(p, keys, page_table, cached, lengths, seq, bounds)
+
+
+def page_select(q, bounds, page_table, lengths, page_size: int, pages: int, seq=None, first: int = 1, last: int = 1, max_length=None, workspace=None):
+    """The pages that queries [B,Hq,K] read: of every key head the first, the last and those of the largest bounds of a score, at most `pages`.
+    Returns (chosen [B,Hk,pages], tokens [B,Hk]) for ``paged_decode_pages``."""
+    if _rows_native is not None and type(q) is torch.Tensor and q.is_cuda:
+        dev = torch._C._cuda_getDevice()
+        r = _rows_native.page_select(q, bounds, page_table, lengths, seq, workspace, page_size, pages, first, last, max_length, dev,
+                                     torch._C._cuda_getCurrentRawStream(dev))
+        if r is not None:
+            return r if type(r) is tuple else _check(r)
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(bounds, torch.Tensor) or bounds.dim() != 4:
+        raise TypeError("expected q [B,Hq,K] and bounds [n_pages, Hk, 2, K] as CUDA/HIP torch tensors")
+    B, Hq, K = q.shape
+    n_pages, Hk = bounds.shape[:2]
+    g = _pages(page_table, page_size, n_pages)
+    if max_length is None:
+        max_length = min(g.max_pages * max(int(page_size), 0), 0x7fffff00)
+    p = make_select_params(B, Hq, Hk, K, q.dtype == torch.bfloat16, max_length, pages=pages, first=first, last=last)
+    if p.pages < 1:
+        raise OsdnError(-5)
+    new = lambda *shape: torch.empty(*shape, dtype=torch.int32, device=q.device)
+    chosen, tokens = new(B, Hk, p.pages), new(B, Hk)
+    if workspace is None:
+        n = osdn_page_select_workspace_bytes(p, page_size)
+        workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    osdn_page_select(p, g, q, bounds, lengths, seq, chosen, tokens, workspace)
+    return chosen, tokens
+
+
+def _decode_pages(q, cache, Hk, page_size, chosen, tokens, scale, max_length, want_lse, workspace, mx):
+    B, Hq, K = q.shape
+    if not isinstance(chosen, torch.Tensor) or chosen.dim() != 3:
+        raise TypeError("chosen: expected an int32 CUDA/HIP torch tensor [B,Hk,pages]")
+    if max_length is None:
+        max_length = min(chosen.shape[2] * page_size, 0x7fffff00)
+    most = min(65535 // max(Hk, 1), ((1 << 21) - 1) // max(Hq, 1)) or 1
+    if B > most:
+        _array(chosen, torch.int32, (B, Hk, chosen.shape[2]), "chosen")
+        _array(tokens, torch.int32, (B, Hk), "tokens")
+    params = lambda n: make_decode_params(n, Hq, Hk, K, q.dtype == torch.bfloat16, max_length, scale)
+    call = osdn_paged_decode_pages_mx if mx else osdn_paged_decode_pages
+    return _decode_in_parts(q, most, tokens, lambda n: _pages_bytes(params(n), mx),
+                            lambda n, q, chosen, tokens, o, lse, ws: call(params(n), q, *cache, chosen, tokens, o, lse, ws), (chosen, tokens), workspace, want_lse)
+
+
+def paged_decode_pages(q, k_cache, v_cache, chosen, tokens, scale=None, max_length=None, want_lse: bool = False, workspace=None):
+    """Attention of q [B,Hq,K] over chosen pages: those of each key head, chosen [B,Hk,pages], of which the first tokens [B,Hk] tokens are seen
+    (``page_select``).  max_length: no entry of tokens is above it (None: what the pages hold).  Returns o, or (o, lse)."""
+    if _rows_native is not None and type(q) is torch.Tensor and q.is_cuda:
+        dev = torch._C._cuda_getDevice()
+        r = _rows_native.paged_decode_pages(q, k_cache, v_cache, None, None, chosen, tokens, workspace, scale, max_length, want_lse, dev,
+                                            torch._C._cuda_getCurrentRawStream(dev))
+        if type(r) is tuple:
+            return r if want_lse else r[0]
+        if r is not None and r != OSDN_ERR_SHAPE:
+            _check(r)
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise TypeError("expected q [B,Hq,K] and a cache [n_pages, page_size, Hk, K] as CUDA/HIP torch tensors")
+    return _decode_pages(q, (k_cache, v_cache), k_cache.shape[2], k_cache.shape[1], chosen, tokens, scale, max_length, want_lse, workspace, False)
+
+
+def paged_decode_pages_mx(q, cache, chosen, tokens, scale=None, max_length=None, want_lse: bool = False, workspace=None):
+    """``paged_decode_pages`` over a cache in 4 bits."""
+    if _rows_native is not None and type(q) is torch.Tensor and q.is_cuda and type(cache) is tuple and len(cache) == 4:
+        dev = torch._C._cuda_getDevice()
+        r = _rows_native.paged_decode_pages(q, *cache, chosen, tokens, workspace, scale, max_length, want_lse, dev, torch._C._cuda_getCurrentRawStream(dev))
+        if type(r) is tuple:
+            return r if want_lse else r[0]
+        if r is not None and r != OSDN_ERR_SHAPE:
+            _check(r)
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(cache, (tuple, list)) or len(cache) != 4 or not isinstance(cache[0], torch.Tensor) or cache[0].dim() != 4:
+        raise TypeError("expected q [B,Hq,K] and a cache (k, v, k_scale, v_scale) as CUDA/HIP torch tensors")
+    return _decode_pages(q, (cache,), cache[0].shape[2], cache[0].shape[1], chosen, tokens, scale, max_length, want_lse, workspace, True)

@@ -18,11 +18,12 @@ using namespace osdn;
 // only process-wide state the library has).  Not thread-safe; meant for benchmarks.
 enum { KID_PRECOND_FWD, KID_CHUNK_PREP, KID_STATE_FWD, KID_OUTPUT_FWD, KID_BWD_CHAIN,
        KID_BWD_POST, KID_PRECOND_MASK, KID_PRECOND_CHAIN, KID_PRECOND_POST, KID_STEP, KID_TABLES, KID_UNFOLD, KID_PRECOND_LIN,
-       KID_QK_NORM, KID_QK_NORM_BWD, KID_PAGED_APPEND, KID_PAGED_DECODE, KID_COUNT };
+       KID_QK_NORM, KID_QK_NORM_BWD, KID_PAGED_APPEND, KID_PAGED_DECODE, KID_PAGED_PLAN, KID_PAGED_RELEASE, KID_PAGED_READ, KID_PAGE_BOUNDS, KID_PAGE_SELECT, KID_COUNT };
 const char *const kKernelNames[KID_COUNT] = {"precond_fwd", "chunk_prep", "state_fwd", "output_fwd",
                                              "bwd_chain", "bwd_post", "precond_mask",
                                              "precond_chain", "precond_post", "step", "tables", "unfold", "precond_lin",
-                                             "qk_norm", "qk_norm_bwd", "paged_append", "paged_decode"};
+                                             "qk_norm", "qk_norm_bwd", "paged_append", "paged_decode", "paged_plan", "paged_release", "paged_read",
+                                             "page_bounds", "page_select"};
 struct Timed { int id; hipEvent_t e0, e1; };
 bool g_prof_on = false;
 std::vector<Timed> g_prof;
@@ -400,11 +401,20 @@ static int take_rows(const osdn_rows *r, long long B, long long T, long long H, 
     return OSDN_OK;
 }
 
+// The table of a cache, or its sizes alone
+static int check_table(const int32_t *table, long long stride, int n_pages, int page_size, int n_seqs, int max_pages, int &shift) {
+    if (n_pages < 1 || n_seqs < 1 || max_pages < 1 || page_size < 1 || (page_size & (page_size - 1)) != 0) return OSDN_ERR_SHAPE;
+    if (stride < 0 || (stride < max_pages && stride != 0) || reinterpret_cast<uintptr_t>(table) % 4 != 0) return OSDN_ERR_SHAPE;
+    shift = 0;
+    while ((1 << shift) < page_size) ++shift;
+    return OSDN_OK;
+}
+
 // `out`: rows are written
 static int check_cache(const osdn_cache *c, int H, int K, size_t es, bool out, int &shift) {
     if (!c || !c->k || !c->v || !c->table) return OSDN_ERR_NULL;
-    if (c->n_pages < 1 || c->n_seqs < 1 || c->max_pages < 1 || c->page_size < 1 || (c->page_size & (c->page_size - 1)) != 0) return OSDN_ERR_SHAPE;
-    if (c->table_stride < 0 || (c->table_stride < c->max_pages && c->table_stride != 0)) return OSDN_ERR_SHAPE;
+    const int rc = check_table(c->table, c->table_stride, c->n_pages, c->page_size, c->n_seqs, c->max_pages, shift);
+    if (rc != OSDN_OK) return rc;
     if (!(apart(c->n_pages, c->k_page, K) && apart(c->n_pages, c->v_page, K) && apart(c->page_size, c->k_token, K) && apart(c->page_size, c->v_token, K) &&
           apart(H, c->k_head, K) && apart(H, c->v_head, K)))
         return OSDN_ERR_SHAPE;
@@ -414,9 +424,7 @@ static int check_cache(const osdn_cache *c, int H, int K, size_t es, bool out, i
     const long long ve = 16 / (long long)es;
     for (long long s : {c->k_page, c->k_token, c->k_head, c->v_page, c->v_token, c->v_head})
         if (s < 0 || s % ve != 0) return OSDN_ERR_SHAPE;
-    if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) % 16 != 0 || reinterpret_cast<uintptr_t>(c->table) % 4 != 0) return OSDN_ERR_SHAPE;
-    shift = 0;
-    while ((1 << shift) < c->page_size) ++shift;
+    if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) % 16 != 0) return OSDN_ERR_SHAPE;
     return OSDN_OK;
 }
 
@@ -474,9 +482,40 @@ int osdn_qk_norm_bwd(const osdn_norm_params *p, const osdn_rows *q, const osdn_r
     return launch_status();
 }
 
-int osdn_paged_append(const osdn_norm_params *p, const osdn_cache *cache, const osdn_rows *q, const osdn_rows *k, const osdn_rows *v,
-                      const float *weight_q, const float *weight_k, const float *rotary, const int32_t *positions, const int32_t *seq,
-                      const osdn_rows *q_out, void *stream) {
+static void take_cache(const osdn_cache *c, HeadRows &k, HeadRows &v, HeadRows &, HeadRows &) {
+    k = HeadRows{c->k, c->k_page, c->k_token, c->k_head};
+    v = HeadRows{c->v, c->v_page, c->v_token, c->v_head};
+}
+static void take_cache(const osdn_cache_mx *c, HeadRows &k, HeadRows &v, HeadRows &ks, HeadRows &vs) {
+    k = HeadRows{c->k, c->k_page, c->k_token, c->k_head};
+    v = HeadRows{c->v, c->v_page, c->v_token, c->v_head};
+    ks = HeadRows{c->k_scale, c->k_scale_page, c->k_scale_token, c->k_scale_head};
+    vs = HeadRows{c->v_scale, c->v_scale_page, c->v_scale_token, c->v_scale_head};
+}
+// (es: not used; values: the values are looked at too)
+static int check_cache(const osdn_cache_mx *c, int H, int K, size_t, bool out, int &shift, bool values = true) {
+    if (!c || !c->k || !c->k_scale || (values && (!c->v || !c->v_scale)) || !c->table) return OSDN_ERR_NULL;
+    const int rc = check_table(c->table, c->table_stride, c->n_pages, c->page_size, c->n_seqs, c->max_pages, shift);
+    if (rc != OSDN_OK) return rc;
+    struct { const void *at; long long page, token, head; int bytes, align; } rows[4] = {
+        {c->k, c->k_page, c->k_token, c->k_head, K / 2, 16}, {c->k_scale, c->k_scale_page, c->k_scale_token, c->k_scale_head, K / 32, K == 256 ? 2 : 1},
+        {c->v, c->v_page, c->v_token, c->v_head, K / 2, 16}, {c->v_scale, c->v_scale_page, c->v_scale_token, c->v_scale_head, K / 32, K == 256 ? 2 : 1}};
+    for (int i = 0; i < (values ? 4 : 2); ++i) {
+        const auto &r = rows[i];
+        if (reinterpret_cast<uintptr_t>(r.at) % r.align != 0) return OSDN_ERR_SHAPE;
+        for (long long step : {r.page, r.token, r.head})
+            if (step < 0 || step % r.align != 0) return OSDN_ERR_SHAPE;
+        if (!(apart(c->n_pages, r.page, r.bytes) && apart(c->page_size, r.token, r.bytes) && apart(H, r.head, r.bytes))) return OSDN_ERR_SHAPE;
+        if (out && !rows_apart({c->n_pages, c->page_size, H}, {r.page, r.token, r.head}, r.bytes)) return OSDN_ERR_SHAPE;
+    }
+    return OSDN_OK;
+}
+
+extern "C++" {
+template <typename Cache>
+static int append_impl(const osdn_norm_params *p, const Cache *cache, const osdn_rows *q, const osdn_rows *k, const osdn_rows *v,
+                       const float *weight_q, const float *weight_k, const float *rotary, const int32_t *positions, const int32_t *seq,
+                       const osdn_rows *q_out, void *stream) {
     int rc = check_norm(p), shift = 0;
     if (rc != OSDN_OK) return rc;
     if (p->Hk < 1) return OSDN_ERR_SHAPE;
@@ -488,28 +527,67 @@ int osdn_paged_append(const osdn_norm_params *p, const osdn_cache *cache, const 
         (rc = take_rows(v, p->B, p->T, p->Hk, p->K, es, false, a.v, a.aligned)) != OSDN_OK || (rc = take_rows(q_out, p->B, p->T, p->Hq, p->K, es, true, a.q_out, a.aligned)) != OSDN_OK)
         return rc;
     a.append = true;
-    a.cache_k = HeadRows{cache->k, cache->k_page, cache->k_token, cache->k_head};
-    a.cache_v = HeadRows{cache->v, cache->v_page, cache->v_token, cache->v_head};
+    a.mx = std::is_same<Cache, osdn_cache_mx>::value;
+    take_cache(cache, a.cache_k, a.cache_v, a.scale_k, a.scale_v);
     a.table = cache->table; a.table_stride = cache->table_stride; a.seq = seq;
     a.n_pages = cache->n_pages; a.page_shift = shift; a.n_seqs = cache->n_seqs; a.max_pages = cache->max_pages;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (timed(KID_PAGED_APPEND, st, [&] { return launch_heads_fwd(a, p->io_dtype == OSDN_BF16, st); }) != 0) return OSDN_ERR_SHAPE;
     return launch_status();
 }
+}
 
-// heads_together: the cache holds the heads of a token side by side
-static int check_decode(const osdn_decode_params *p, bool heads_together, DecodeArgs &a, size_t &bytes) {
+int osdn_paged_append(const osdn_norm_params *p, const osdn_cache *cache, const osdn_rows *q, const osdn_rows *k, const osdn_rows *v,
+                      const float *weight_q, const float *weight_k, const float *rotary, const int32_t *positions, const int32_t *seq,
+                      const osdn_rows *q_out, void *stream) {
+    return append_impl(p, cache, q, k, v, weight_q, weight_k, rotary, positions, seq, q_out, stream);
+}
+
+int osdn_paged_append_mx(const osdn_norm_params *p, const osdn_cache_mx *cache, const osdn_rows *q, const osdn_rows *k, const osdn_rows *v,
+                         const float *weight_q, const float *weight_k, const float *rotary, const int32_t *positions, const int32_t *seq,
+                         const osdn_rows *q_out, void *stream) {
+    return append_impl(p, cache, q, k, v, weight_q, weight_k, rotary, positions, seq, q_out, stream);
+}
+
+int osdn_paged_read_mx(const osdn_norm_params *p, const osdn_cache_mx *cache, const int32_t *positions, const int32_t *seq,
+                       const osdn_rows *k_out, const osdn_rows *v_out, void *stream) {
+    if (!p) return OSDN_ERR_NULL;
+    osdn_norm_params rows{p->B, p->T, 0, p->Hk, p->K, p->io_dtype, OSDN_NORM_NONE, 0, 0, 0, 0.f};
+    int rc = check_norm(&rows), shift = 0;
+    if (rc != OSDN_OK) return rc;
+    if (!positions) return OSDN_ERR_NULL;
+    const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
+    if ((rc = check_cache(cache, p->Hk, p->K, es, false, shift)) != OSDN_OK) return rc;
+    HeadsArgs a = heads_args(&rows, nullptr, nullptr, nullptr, positions);
+    if ((rc = take_rows(k_out, p->B, p->T, p->Hk, p->K, es, true, a.k_out, a.aligned)) != OSDN_OK || (rc = take_rows(v_out, p->B, p->T, p->Hk, p->K, es, true, a.v, a.aligned)) != OSDN_OK)
+        return rc;
+    take_cache(cache, a.cache_k, a.cache_v, a.scale_k, a.scale_v);
+    a.table = cache->table; a.table_stride = cache->table_stride; a.seq = seq;
+    a.n_pages = cache->n_pages; a.page_shift = shift; a.n_seqs = cache->n_seqs; a.max_pages = cache->max_pages;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (timed(KID_PAGED_READ, st, [&] { return launch_read_mx(a, p->io_dtype == OSDN_BF16, st); }) != 0) return OSDN_ERR_SHAPE;
+    return launch_status();
+}
+
+// What a call of attention over a cache is cut into.  mx: a cache in 4 bits; heads_together: the cache holds the heads of a token side by side; pages: a table for
+// each key head, whose rows are then a sequence's each
+static int check_decode(const osdn_decode_params *p, bool mx, bool heads_together, bool pages, DecodeArgs &a, size_t &bytes) {
     if (!p) return OSDN_ERR_NULL;
     if (p->io_dtype != OSDN_F32 && p->io_dtype != OSDN_BF16) return OSDN_ERR_DTYPE;
     if (p->B < 1 || p->B > 65535 || p->Hk < 1 || p->Hq < p->Hk || p->Hq % p->Hk != 0 || p->Hq > 65535 || (long long)p->B * p->Hq >= 1 << 21) return OSDN_ERR_SHAPE;
+    if (pages && (long long)p->B * p->Hk > 65535) return OSDN_ERR_SHAPE;
     if (p->K != 64 && p->K != 128 && p->K != 256) return OSDN_ERR_SHAPE;
     if (p->max_length < 0 || p->max_length > 0x7fffff00) return OSDN_ERR_SHAPE;
-    if (!std::isfinite(p->scale) || p->window < 0 || p->shares < -1 || p->shares > 65535) return OSDN_ERR_PARAM;
-    a.head_tiles = (p->Hq / p->Hk + 15) / 16;
-    a.part_heads = p->Hq / p->Hk < 16 ? p->Hq / p->Hk : 16;
-    const int rows = p->Hk * a.head_tiles;
-    const DecodePlan plan = decode_plan(p->B, rows, p->max_length, p->window, p->K, p->io_dtype == OSDN_BF16, a.part_heads, heads_together || a.head_tiles > 1, p->shares);
-    const long long groups = (long long)p->B * rows / plan.row_group;
+    if (!std::isfinite(p->scale) || p->window < 0 || (pages && p->window != 0) || p->shares < -1 || p->shares > 65535) return OSDN_ERR_PARAM;
+    a.group = p->Hq / p->Hk;
+    a.table_heads = pages ? p->Hk : 1;
+    a.B = p->B * a.table_heads; a.Hk = p->Hk / a.table_heads; a.Hq = a.Hk * a.group; a.K = p->K;
+    a.scale = p->scale; a.window = p->window; a.max_length = p->max_length;
+    a.head_tiles = (a.group + 15) / 16;
+    a.part_heads = a.group < 16 ? a.group : 16;
+    const int rows = a.Hk * a.head_tiles;
+    const DecodePlan plan = decode_plan(a.B, rows, p->max_length, p->window, p->K, p->io_dtype == OSDN_BF16, a.part_heads, (heads_together && !pages) || a.head_tiles > 1, p->shares, mx);
+    const long long groups = (long long)a.B * rows / plan.row_group;
     if (groups * plan.units > 0x7fffffffLL) return OSDN_ERR_SHAPE;     // (units are counted in 32 bits)
     a.row_group = plan.row_group;
     a.shares = plan.shares;
@@ -517,26 +595,41 @@ static int check_decode(const osdn_decode_params *p, bool heads_together, Decode
     return OSDN_OK;
 }
 
-size_t osdn_paged_decode_workspace_bytes(const osdn_decode_params *p) {         // (for a cache of either order)
+static size_t decode_bytes(const osdn_decode_params *p, bool mx, bool pages) {         // (for a cache of either order)
     size_t most = 0;
     for (bool together : {false, true}) {
         DecodeArgs a{};
         size_t bytes = 0;
-        if (check_decode(p, together, a, bytes) != OSDN_OK) return 0;
+        if (check_decode(p, mx, together, pages, a, bytes) != OSDN_OK) return 0;
         most = std::max(most, bytes);
     }
     return most;
 }
+size_t osdn_paged_decode_workspace_bytes(const osdn_decode_params *p) { return decode_bytes(p, false, false); }
+size_t osdn_paged_decode_mx_workspace_bytes(const osdn_decode_params *p) { return decode_bytes(p, true, false); }
+size_t osdn_paged_decode_pages_workspace_bytes(const osdn_decode_params *p) { return decode_bytes(p, false, true); }
+size_t osdn_paged_decode_pages_mx_workspace_bytes(const osdn_decode_params *p) { return decode_bytes(p, true, true); }
 
-int osdn_paged_decode(const osdn_decode_params *p, const osdn_cache *cache, const osdn_rows *q, const int32_t *lengths, const int32_t *seq,
-                      const osdn_rows *o, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+// chosen (with tokens in the place of lengths): the pages of each key head, n_chosen of them, in place of the cache's table
+extern "C++" {
+template <typename Cache>
+static int decode_impl(const osdn_decode_params *p, const Cache *cache, const osdn_rows *q, const int32_t *lengths, const int32_t *seq, bool pages,
+                       const int32_t *chosen, int n_chosen, const osdn_rows *o, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    constexpr bool mx = std::is_same<Cache, osdn_cache_mx>::value;
     DecodeArgs a{};
     size_t bytes = 0;
-    int rc = check_decode(p, cache && cache->k_head < cache->k_token, a, bytes);
+    int rc = check_decode(p, mx, cache && cache->k_head < cache->k_token, pages, a, bytes);
     if (rc != OSDN_OK) return rc;
     if (!lengths) return OSDN_ERR_NULL;
+    Cache c{};
+    if (cache) c = *cache;
+    if (pages) {
+        if (!chosen) return OSDN_ERR_NULL;
+        if (n_chosen < 1) return OSDN_ERR_SHAPE;
+        c.table = chosen; c.table_stride = n_chosen; c.n_seqs = a.B; c.max_pages = n_chosen;
+    }
     const size_t es = p->io_dtype == OSDN_BF16 ? 2 : 4;
-    if ((rc = check_cache(cache, p->Hk, p->K, es, false, a.page_shift)) != OSDN_OK) return rc;
+    if ((rc = check_cache(cache ? &c : nullptr, p->Hk, p->K, es, false, a.page_shift)) != OSDN_OK) return rc;
     a.aligned = true;
     if ((rc = take_rows(q, p->B, 1, p->Hq, p->K, es, false, a.q, a.aligned)) != OSDN_OK || (rc = take_rows(o, p->B, 1, p->Hq, p->K, es, true, a.o, a.aligned)) != OSDN_OK) return rc;
     if (a.shares) {
@@ -547,14 +640,165 @@ int osdn_paged_decode(const osdn_decode_params *p, const osdn_cache *cache, cons
         a.part_ml = a.part_o + parts * p->K;
         a.info = reinterpret_cast<int *>(a.part_ml + parts * 2);
     }
-    a.B = p->B; a.Hq = p->Hq; a.Hk = p->Hk; a.K = p->K; a.group = p->Hq / p->Hk;
-    a.scale = p->scale; a.window = p->window; a.max_length = p->max_length;
-    a.cache_k = HeadRows{cache->k, cache->k_page, cache->k_token, cache->k_head};
-    a.cache_v = HeadRows{cache->v, cache->v_page, cache->v_token, cache->v_head};
-    a.table = cache->table; a.table_stride = cache->table_stride; a.lengths = lengths; a.seq = seq; a.lse = lse;
-    a.n_pages = cache->n_pages; a.n_seqs = cache->n_seqs; a.max_pages = cache->max_pages;
+    take_cache(&c, a.cache_k, a.cache_v, a.scale_k, a.scale_v);
+    a.table = c.table; a.table_stride = c.table_stride; a.lengths = lengths; a.seq = seq; a.lse = lse;
+    a.n_pages = c.n_pages; a.n_seqs = c.n_seqs; a.max_pages = c.max_pages;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (timed(KID_PAGED_DECODE, st, [&] { return launch_paged_decode(a, p->io_dtype == OSDN_BF16, st); }) != 0) return OSDN_ERR_SHAPE;
+    const bool bf = p->io_dtype == OSDN_BF16;
+    if (timed(KID_PAGED_DECODE, st, [&] { return mx ? launch_paged_decode_mx(a, bf, st) : launch_paged_decode(a, bf, st); }) != 0) return OSDN_ERR_SHAPE;
+    return launch_status();
+}
+}
+
+int osdn_paged_decode(const osdn_decode_params *p, const osdn_cache *cache, const osdn_rows *q, const int32_t *lengths, const int32_t *seq,
+                      const osdn_rows *o, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    return decode_impl(p, cache, q, lengths, seq, false, nullptr, 0, o, lse, workspace, workspace_bytes, stream);
+}
+int osdn_paged_decode_mx(const osdn_decode_params *p, const osdn_cache_mx *cache, const osdn_rows *q, const int32_t *lengths, const int32_t *seq,
+                         const osdn_rows *o, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    return decode_impl(p, cache, q, lengths, seq, false, nullptr, 0, o, lse, workspace, workspace_bytes, stream);
+}
+int osdn_paged_decode_pages(const osdn_decode_params *p, const osdn_cache *cache, const osdn_rows *q, const int32_t *chosen, int32_t n_chosen,
+                            const int32_t *tokens, const osdn_rows *o, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    return decode_impl(p, cache, q, tokens, nullptr, true, chosen, n_chosen, o, lse, workspace, workspace_bytes, stream);
+}
+int osdn_paged_decode_pages_mx(const osdn_decode_params *p, const osdn_cache_mx *cache, const osdn_rows *q, const int32_t *chosen, int32_t n_chosen,
+                               const int32_t *tokens, const osdn_rows *o, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    return decode_impl(p, cache, q, tokens, nullptr, true, chosen, n_chosen, o, lse, workspace, workspace_bytes, stream);
+}
+
+// ---- the pages of a cache ------------------------------------------------------------------
+// `list`: the free pages are looked at too
+static int check_pages(const osdn_pages *g, bool list, bool index, int &shift) {
+    if (!g || !g->table || (list && !g->free_list)) return OSDN_ERR_NULL;
+    if (list && (g->free_capacity < 1 || reinterpret_cast<uintptr_t>(g->free_list) % 4 != 0)) return OSDN_ERR_SHAPE;
+    if (list && g->n_seqs > 1 && g->table_stride == 0) return OSDN_ERR_SHAPE;          // (rows that are written)
+    if (list && index && g->n_seqs > PLAN_MAX_ROWS) return OSDN_ERR_SHAPE;
+    return check_table(g->table, g->table_stride, g->n_pages, g->page_size, g->n_seqs, g->max_pages, shift);
+}
+static PlanArgs plan_args(const osdn_pages *g, int B, int shift) {
+    PlanArgs a{};
+    a.B = B;
+    a.table = g->table; a.table_stride = g->table_stride; a.free_list = g->free_list; a.free_capacity = g->free_capacity;
+    a.n_pages = g->n_pages; a.page_shift = shift; a.n_seqs = g->n_seqs; a.max_pages = g->max_pages;
+    return a;
+}
+
+int osdn_paged_plan(const osdn_pages *pages, int32_t B, int32_t tokens, const int32_t *cached, const int32_t *fresh, const int32_t *seq,
+                    const int32_t *n_free, int32_t *n_free_out, int32_t *lengths, int32_t *starts, int32_t *positions, int32_t *rows,
+                    int64_t *slots, void *stream) {
+    int shift = 0;
+    const int rc = check_pages(pages, true, seq != nullptr, shift);
+    if (rc != OSDN_OK) return rc;
+    if (B < 1 || B > 65535 || tokens < 1) return OSDN_ERR_SHAPE;
+    if (!cached || !fresh || !n_free || !n_free_out || !lengths || !starts || !positions || !rows) return OSDN_ERR_NULL;
+    PlanArgs a = plan_args(pages, B, shift);
+    a.N = tokens; a.cached = cached; a.fresh = fresh; a.seq = seq; a.n_free = n_free; a.n_free_out = n_free_out;
+    a.lengths = lengths; a.starts = starts; a.positions = positions; a.rows = rows; a.slots = reinterpret_cast<long long *>(slots);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (timed(KID_PAGED_PLAN, st, [&] { return launch_plan(a, st); }) != 0) return OSDN_ERR_SHAPE;
+    return launch_status();
+}
+
+int osdn_paged_release(const osdn_pages *pages, int32_t B, const int32_t *lengths, const int32_t *seq, const int32_t *n_free,
+                       int32_t *n_free_out, void *stream) {
+    int shift = 0;
+    const int rc = check_pages(pages, true, seq != nullptr, shift);
+    if (rc != OSDN_OK) return rc;
+    if (B < 1 || B > 65535) return OSDN_ERR_SHAPE;
+    if (!lengths || !n_free || !n_free_out) return OSDN_ERR_NULL;
+    PlanArgs a = plan_args(pages, B, shift);
+    a.cached = lengths; a.seq = seq; a.n_free = n_free; a.n_free_out = n_free_out;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (timed(KID_PAGED_RELEASE, st, [&] { return launch_release(a, st); }) != 0) return OSDN_ERR_SHAPE;
+    return launch_status();
+}
+
+static int check_select(const osdn_select_params *p) {
+    if (!p) return OSDN_ERR_NULL;
+    if (p->io_dtype != OSDN_F32 && p->io_dtype != OSDN_BF16) return OSDN_ERR_DTYPE;
+    if (p->B < 1 || p->B > 65535 || p->Hk < 1 || p->Hk > 65535 || (long long)p->B * p->Hk > 1 << 21) return OSDN_ERR_SHAPE;
+    return p->K == 64 || p->K == 128 || p->K == 256 ? OSDN_OK : OSDN_ERR_SHAPE;
+}
+
+// the keys alone: the values' arguments become the keys' for the checks
+static int check_keys(const osdn_cache *c, int H, int K, size_t es, int &shift, BoundsArgs &a) {
+    if (!c) return OSDN_ERR_NULL;
+    osdn_cache keys = *c;
+    keys.v = keys.k; keys.v_page = keys.k_page; keys.v_token = keys.k_token; keys.v_head = keys.k_head;
+    a.keys = HeadRows{c->k, c->k_page, c->k_token, c->k_head};
+    return check_cache(&keys, H, K, es, false, shift);
+}
+static int check_keys(const osdn_cache_mx *c, int H, int K, size_t es, int &shift, BoundsArgs &a) {
+    if (!c) return OSDN_ERR_NULL;
+    a.keys = HeadRows{c->k, c->k_page, c->k_token, c->k_head};
+    a.scales = HeadRows{c->k_scale, c->k_scale_page, c->k_scale_token, c->k_scale_head};
+    return check_cache(c, H, K, es, false, shift, false);
+}
+extern "C++" {
+template <typename Cache>
+static int bounds_impl(const osdn_select_params *p, const Cache *cache, const int32_t *cached, const int32_t *lengths, const int32_t *seq, void *bounds, void *stream) {
+    int rc = check_select(p), shift = 0;
+    if (rc != OSDN_OK) return rc;
+    if (p->max_new < 1) return OSDN_ERR_SHAPE;
+    if (!cached || !lengths || !bounds) return OSDN_ERR_NULL;
+    BoundsArgs a{};
+    if ((rc = check_keys(cache, p->Hk, p->K, p->io_dtype == OSDN_BF16 ? 2 : 4, shift, a)) != OSDN_OK) return rc;
+    if (reinterpret_cast<uintptr_t>(bounds) % 16 != 0) return OSDN_ERR_SHAPE;
+    a.B = p->B; a.Hk = p->Hk; a.K = p->K;
+    a.touched = (int)std::min<long long>(cache->max_pages, ((long long)p->max_new + cache->page_size - 2) / cache->page_size + 1);
+    if ((long long)a.B * a.touched * a.Hk > 0x7fffffffLL) return OSDN_ERR_SHAPE;
+    a.max_new = p->max_new;
+    a.table = cache->table; a.table_stride = cache->table_stride; a.seq = seq; a.cached = cached; a.lengths = lengths; a.bounds = bounds;
+    a.n_pages = cache->n_pages; a.page_shift = shift; a.n_seqs = cache->n_seqs; a.max_pages = cache->max_pages;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    constexpr bool mx = std::is_same<Cache, osdn_cache_mx>::value;
+    if (timed(KID_PAGE_BOUNDS, st, [&] { return launch_bounds(a, p->io_dtype == OSDN_BF16, mx, st); }) != 0) return OSDN_ERR_SHAPE;
+    return launch_status();
+}
+}
+int osdn_page_bounds(const osdn_select_params *p, const osdn_cache *cache, const int32_t *cached, const int32_t *lengths, const int32_t *seq, void *bounds, void *stream) {
+    return bounds_impl(p, cache, cached, lengths, seq, bounds, stream);
+}
+int osdn_page_bounds_mx(const osdn_select_params *p, const osdn_cache_mx *cache, const int32_t *cached, const int32_t *lengths, const int32_t *seq, void *bounds, void *stream) {
+    return bounds_impl(p, cache, cached, lengths, seq, bounds, stream);
+}
+
+static int check_choice(const osdn_select_params *p, int page_size, long long &seen) {
+    const int rc = check_select(p);
+    if (rc != OSDN_OK) return rc;
+    if (p->Hq < p->Hk || p->Hq % p->Hk != 0 || p->Hq > 65535 || p->max_length < 0 || p->max_length > 0x7fffff00 || page_size < 1) return OSDN_ERR_SHAPE;
+    if (p->first < 0 || p->last < 1 || p->pages < 1 || (long long)p->first + p->last > p->pages || (long long)p->pages * page_size > 0x7fffff00) return OSDN_ERR_PARAM;
+    seen = ((long long)p->max_length + page_size - 1) / page_size;
+    return (long long)p->B * p->Hk * seen > 0x7fffffffLL || (long long)p->B * p->Hk * p->pages > 0x7fffffffLL ? OSDN_ERR_SHAPE : OSDN_OK;
+}
+size_t osdn_page_select_workspace_bytes(const osdn_select_params *p, int32_t page_size) {
+    long long seen = 0;
+    return check_choice(p, page_size, seen) != OSDN_OK || seen <= p->pages ? 0 : (size_t)p->B * p->Hk * seen * sizeof(unsigned long long);
+}
+int osdn_page_select(const osdn_select_params *p, const osdn_pages *pages, const osdn_rows *q, const void *bounds, const int32_t *lengths,
+                     const int32_t *seq, int32_t *chosen, int32_t *tokens, void *workspace, size_t workspace_bytes, void *stream) {
+    SelectArgs a{};
+    int rc = check_pages(pages, false, false, a.page_shift);
+    if (rc != OSDN_OK) return rc;
+    long long seen = 0;
+    if ((rc = check_choice(p, pages->page_size, seen)) != OSDN_OK) return rc;
+    if (!bounds || !lengths || !chosen || !tokens) return OSDN_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(bounds) % 16 != 0) return OSDN_ERR_SHAPE;
+    bool aligned = true;
+    if ((rc = take_rows(q, p->B, 1, p->Hq, p->K, p->io_dtype == OSDN_BF16 ? 2 : 4, false, a.q, aligned)) != OSDN_OK) return rc;
+    const size_t bytes = osdn_page_select_workspace_bytes(p, pages->page_size);
+    if (bytes) {
+        if ((rc = check_ws(workspace, workspace_bytes, bytes)) != OSDN_OK) return rc;
+        a.keys = static_cast<unsigned long long *>(workspace);
+    }
+    a.B = p->B; a.Hk = p->Hk; a.K = p->K; a.group = p->Hq / p->Hk; a.max_length = p->max_length;
+    a.pages = p->pages; a.first = p->first; a.last = p->last; a.max_pages_seen = (int)seen;
+    a.bounds = bounds; a.table = pages->table; a.table_stride = pages->table_stride; a.seq = seq; a.lengths = lengths;
+    a.n_pages = pages->n_pages; a.n_seqs = pages->n_seqs; a.max_pages = pages->max_pages;
+    a.chosen = chosen; a.tokens = tokens;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (timed(KID_PAGE_SELECT, st, [&] { return launch_select(a, p->io_dtype == OSDN_BF16, st); }) != 0) return OSDN_ERR_SHAPE;
     return launch_status();
 }
 

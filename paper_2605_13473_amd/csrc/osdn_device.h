@@ -38,6 +38,21 @@ template <typename T> __device__ __forceinline__ T from_f32(float x);
 template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
 template <> __device__ __forceinline__ bf16 from_f32<bf16>(float x) { return (bf16)x; }  // RNE
 
+// Rows in 4 bits: eight codes of a word (a sign and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6; the lowest bits first) times their block's scale 2^(byte - 127).  The
+// conversion is one instruction a pair and exact in bf16; the byte 255 makes NaN of all.
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float fp4_scale(unsigned byte) { return __builtin_bit_cast(float, byte << 23); }
+__device__ __forceinline__ bf16x8 fp4_values(uint32_t codes, float scale) {
+    const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+    const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ __forceinline__ void fp4_values(uint32_t codes, float scale, float (&x)[8]) {
+    const bf16x8 v = fp4_values(codes, scale);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = to_f32(v[e]);
+}
+
 // ------------------------------------------------------------------ MFMA ----
 // Operand conventions: an operand tile is addressed as X(row, k) where `row` is the
 // M index (A operand) or the N index (B operand) and k the contraction index.

@@ -254,8 +254,8 @@ struct HeadsArgs {
     const float *rotary;                  // [rotary_rows, rotary_dim] or null
     const int *positions;                 // [tokens] or null (a token's place in its batch entry)
     // append
-    bool append;
-    HeadRows cache_k, cache_v;
+    bool append, mx;                      // mx: a cache in 4 bits, its steps in bytes
+    HeadRows cache_k, cache_v, scale_k, scale_v;
     const int *table, *seq;               // [n_seqs, max_pages], [tokens] or null (the batch entry)
     long long table_stride;
     int n_pages, page_shift, n_seqs, max_pages;
@@ -266,15 +266,18 @@ struct HeadsArgs {
 };
 int launch_heads_fwd(const HeadsArgs &a, bool bf16_io, hipStream_t st);
 int launch_heads_bwd(const HeadsArgs &a, bool bf16_io, hipStream_t st);
+int launch_read_mx(const HeadsArgs &a, bool bf16_io, hipStream_t st);      // rows of a 4-bit cache to k_out and v
 
 // Attention of one token per sequence over a paged cache (osdn_paged.hip)
 struct DecodeArgs {
     int B, Hq, Hk, K, group, head_tiles;  // group: query heads of a key head; head_tiles: rows (of up to 16 query heads) that they make
     float scale;
     int window, max_length;
+    int table_heads;                      // 1, or key heads of q and o: the table has a row for each, B is sequences x heads and Hq, Hk those of one
     int row_group;                        // adjacent rows of a sequence that a workgroup takes: 1, 2 or 4
     int shares, part_heads;               // shares: workgroups that the tokens are cut among, 0: one for each group of rows; part_heads: heads of a row, at most
     HeadRows q, o, cache_k, cache_v;      // q, o: token unused
+    HeadRows scale_k, scale_v;            // a cache in 4 bits, its steps in bytes
     bool aligned;                         // every row of q and o starts on 16 bytes
     const int *table, *seq, *lengths;     // [n_seqs, max_pages], [B] or null (the batch entry), [B]
     long long table_stride;
@@ -285,5 +288,42 @@ struct DecodeArgs {
     int *info;
 };
 int launch_paged_decode(const DecodeArgs &a, bool bf16_io, hipStream_t st);
+int launch_paged_decode_mx(const DecodeArgs &a, bool bf16_io, hipStream_t st);
+
+// The pages of a cache (osdn_pages.hip)
+struct PlanArgs {
+    int B, N;                             // requests, tokens of all of them, at most
+    int *table, *free_list;
+    long long table_stride;
+    int n_pages, page_shift, n_seqs, max_pages, free_capacity;
+    const int *cached, *fresh, *seq;      // release: cached is the lengths
+    const int *n_free;
+    int *n_free_out, *lengths, *starts, *positions, *rows;
+    long long *slots;                     // or null
+};
+int launch_plan(const PlanArgs &a, hipStream_t st);
+int launch_release(const PlanArgs &a, hipStream_t st);
+
+struct BoundsArgs {
+    int B, Hk, K, touched, max_new;       // touched: pages of a sequence that get tokens, at most
+    HeadRows keys, scales;                // of the cache (scales: 4-bit rows, steps in bytes)
+    const int *table, *seq, *cached, *lengths;
+    long long table_stride;
+    int n_pages, page_shift, n_seqs, max_pages;
+    void *bounds;                         // [n_pages, Hk, 2, K] io
+};
+int launch_bounds(const BoundsArgs &a, bool bf16_io, bool mx, hipStream_t st);
+
+struct SelectArgs {
+    int B, Hk, K, group, max_length, pages, first, last, max_pages_seen;
+    HeadRows q;
+    const void *bounds;                   // [n_pages, Hk, 2, K] io
+    const int *table, *seq, *lengths;
+    long long table_stride;
+    int n_pages, page_shift, n_seqs, max_pages;
+    unsigned long long *keys;             // [B, Hk, max_pages_seen]
+    int *chosen, *tokens;                 // [B, Hk, pages], [B, Hk]
+};
+int launch_select(const SelectArgs &a, bool bf16_io, hipStream_t st);
 
 }  // namespace osdn

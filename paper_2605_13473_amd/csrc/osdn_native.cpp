@@ -6,6 +6,7 @@
 // to the Python code, which says what is wrong with it: then this returns None and has done nothing.
 #include <Python.h>
 
+#include <algorithm>
 #include <cfloat>
 #include <climits>
 #include <cmath>
@@ -397,6 +398,410 @@ PyObject *paged_decode(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- the pages of a cache, the cache in 4 bits, attention over selected pages ----------------
+struct {
+    decltype(&osdn_paged_plan) plan;
+    decltype(&osdn_paged_release) release;
+    decltype(&osdn_paged_append_mx) append;
+    decltype(&osdn_paged_read_mx) read;
+    decltype(&osdn_paged_decode_mx) decode;
+    decltype(&osdn_paged_decode_mx_workspace_bytes) decode_bytes;
+    decltype(&osdn_page_bounds) bounds;
+    decltype(&osdn_page_bounds_mx) bounds_mx;
+    decltype(&osdn_page_select) select;
+    decltype(&osdn_page_select_workspace_bytes) select_bytes;
+    decltype(&osdn_paged_decode_pages) decode_pages;
+    decltype(&osdn_paged_decode_pages_workspace_bytes) decode_pages_bytes;
+    decltype(&osdn_paged_decode_pages_mx) decode_pages_mx;
+    decltype(&osdn_paged_decode_pages_mx_workspace_bytes) decode_pages_mx_bytes;
+} g_pages{};
+constexpr int PAGES_ENTRIES = 14;
+bool ordinary() { return g_pages.plan && at::impl::PythonTorchFunctionTLS::stack_len() == 0; }
+
+// an int that its field holds
+bool int_of(PyObject *o, int32_t &out) {
+    if (!PyLong_CheckExact(o)) return false;
+    int over = 0;
+    const long x = PyLong_AsLongAndOverflow(o, &over);
+    if (over || x < INT_MIN || x > INT_MAX) return false;
+    out = (int32_t)x;
+    return true;
+}
+// ... or None, for which another value stands
+bool int_or(PyObject *o, int64_t other, int32_t &out) {
+    if (o != Py_None) return int_of(o, out);
+    if (other > INT_MAX) return false;
+    out = (int32_t)other;
+    return true;
+}
+bool table_of(const at::Tensor *t, int64_t dev, int64_t &seqs, int64_t &most, int64_t &stride) {
+    if (!t || t->dim() != 2 || !strided(*t, at::kInt, dev) || (t->size(1) > 1 && t->stride(1) != 1)) return false;
+    seqs = t->size(0);
+    most = t->size(1);
+    stride = seqs > 1 ? t->stride(0) : most;
+    return seqs <= INT_MAX && most <= INT_MAX;
+}
+bool int_array(const at::Tensor *t, int64_t dev, at::IntArrayRef shape, const int32_t **p, bool needed = true) {
+    const void *at = nullptr;
+    if ((needed && !t) || !array(t, at::kInt, dev, shape, &at)) return false;
+    *p = static_cast<const int32_t *>(at);
+    return true;
+}
+int32_t *ints(const at::Tensor &t) { return static_cast<int32_t *>(t.data_ptr()); }
+PyObject *tuple_of(std::initializer_list<at::Tensor> ts) {
+    PyObject *out = PyTuple_New((Py_ssize_t)ts.size());
+    if (!out) return nullptr;
+    Py_ssize_t i = 0;
+    for (const at::Tensor &t : ts) PyTuple_SET_ITEM(out, i++, wrapped(t));
+    return out;
+}
+bool pages_of(const at::Tensor *table, const at::Tensor *free_pages, PyObject *page_size, PyObject *n_pages, int64_t dev, osdn_pages &g) {
+    int64_t seqs, most, stride;
+    const int32_t *list;
+    if (!table_of(table, dev, seqs, most, stride) || !free_pages || free_pages->dim() != 1 || !int_array(free_pages, dev, free_pages->sizes(), &list)) return false;
+    g = osdn_pages{static_cast<int32_t *>(table->data_ptr()), stride, const_cast<int32_t *>(list), 0, 0, 0, (int32_t)seqs, (int32_t)most};
+    if (free_pages->numel() > INT_MAX) return false;
+    g.free_capacity = (int32_t)free_pages->numel();
+    return int_of(page_size, g.page_size) && int_or(n_pages, free_pages->numel(), g.n_pages);
+}
+
+// paged_plan(page_table, cached, fresh, free_pages, n_free, seq, page_size, tokens, n_pages, want_slots, device, stream): (lengths, starts, positions, rows, n_free,
+// slots or None), a status, or None
+PyObject *paged_plan(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const at::Tensor *t[6];
+    long dev;
+    void *stream;
+    osdn_pages g;
+    int32_t tokens;
+    const int32_t *cached, *fresh, *seq, *n_free;
+    if (n != 12 || !ordinary() || !tensors(a, 6, t) || !device_and_stream(a[10], a[11], dev, stream) || !t[1] || t[1]->dim() != 1 || !PyBool_Check(a[9]) ||
+        !int_of(a[7], tokens) || tokens < 1 || !pages_of(t[0], t[3], a[6], a[8], dev, g))
+        Py_RETURN_NONE;
+    const int64_t B = t[1]->size(0), one = 1;
+    const at::IntArrayRef b(&B, 1);
+    if (B < 1 || B > 65535 || !int_array(t[1], dev, b, &cached) || !int_array(t[2], dev, b, &fresh) || !int_array(t[5], dev, b, &seq, false) ||
+        !int_array(t[4], dev, at::IntArrayRef(&one, 1), &n_free))
+        Py_RETURN_NONE;
+    const at::TensorOptions i32 = t[0]->options();
+    at::Tensor lengths = at::empty({B}, i32), starts = at::empty({B + 1}, i32), pos = at::empty({1, tokens}, i32), rows = at::empty({1, tokens}, i32), left = at::empty({1}, i32), slots;
+    if (a[9] == Py_True) slots = at::empty({tokens}, i32.dtype(at::kLong));
+    int32_t *l = ints(lengths), *s = ints(starts), *p = ints(pos), *r = ints(rows), *f = ints(left);
+    int64_t *sl = slots.defined() ? static_cast<int64_t *>(slots.data_ptr()) : nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_pages.plan(&g, (int32_t)B, tokens, cached, fresh, seq, n_free, f, l, s, p, r, sl, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != OSDN_OK) return PyLong_FromLong(rc);
+    return tuple_of({lengths, starts, pos, rows, left, slots});
+    END_HANDLE_TH_ERRORS
+}
+
+// paged_release(page_table, lengths, free_pages, n_free, seq, page_size, n_pages, device, stream): (n_free,), a status, or None
+PyObject *paged_release(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const at::Tensor *t[5];
+    long dev;
+    void *stream;
+    osdn_pages g;
+    const int32_t *lengths, *seq, *n_free;
+    if (n != 9 || !ordinary() || !tensors(a, 5, t) || !device_and_stream(a[7], a[8], dev, stream) || !t[1] || t[1]->dim() != 1 || !pages_of(t[0], t[2], a[5], a[6], dev, g))
+        Py_RETURN_NONE;
+    const int64_t B = t[1]->size(0), one = 1;
+    const at::IntArrayRef b(&B, 1);
+    if (B < 1 || B > 65535 || !int_array(t[1], dev, b, &lengths) || !int_array(t[4], dev, b, &seq, false) || !int_array(t[3], dev, at::IntArrayRef(&one, 1), &n_free)) Py_RETURN_NONE;
+    at::Tensor left = at::empty({1}, t[0]->options());
+    int32_t *f = ints(left);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_pages.release(&g, (int32_t)B, lengths, seq, n_free, f, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != OSDN_OK) return PyLong_FromLong(rc);
+    return tuple_of({left});
+    END_HANDLE_TH_ERRORS
+}
+
+// a cache in 4 bits: codes [pages, page, H, K / 2] and scales [.., K / 32] of keys and values (values null: the keys alone; table null: one that is not looked at)
+bool cache_mx_of(const at::Tensor *k, const at::Tensor *v, const at::Tensor *ks, const at::Tensor *vs, const at::Tensor *table, int64_t dev, int64_t H, int64_t K, osdn_cache_mx &c) {
+    if (!k || k->dim() != 4) return false;
+    osdn_rows r[4];
+    const int64_t pages = k->size(0), page = k->size(1);
+    const at::Tensor *t[4] = {k, v, ks, vs};
+    if (!ks || pages > INT_MAX || page > INT_MAX || H < 1) return false;
+    for (int i = 0; i < 4; ++i)
+        if (t[i] && !rows_of(t[i], at::kByte, dev, pages, page, H, i < 2 ? K / 2 : K / 32, r[i])) return false;
+    if (!v || !vs) {
+        if (v || vs) return false;
+        r[1] = r[0];
+        r[3] = r[2];
+    }
+    int64_t seqs = 1, most = 1, stride = 1;
+    if (table && !table_of(table, dev, seqs, most, stride)) return false;
+    c = osdn_cache_mx{r[0].data, r[1].data, static_cast<uint8_t *>(r[2].data), static_cast<uint8_t *>(r[3].data), r[0].batch, r[0].token, r[0].head, r[1].batch, r[1].token, r[1].head,
+                      r[2].batch, r[2].token, r[2].head, r[3].batch, r[3].token, r[3].head, table ? static_cast<const int32_t *>(table->data_ptr()) : nullptr, stride,
+                      (int32_t)pages, (int32_t)page, (int32_t)seqs, (int32_t)most};
+    return true;
+}
+
+// paged_append_mx(k, v, codes of k, of v, scales of k, of v, page_table, positions, seq, q, weight_q, weight_k, rotary, hp, device, stream): (q_out,), a status, or None
+PyObject *paged_append_mx(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const at::Tensor *t[13];
+    long dev;
+    void *stream;
+    NormCall c;
+    osdn_cache_mx cache;
+    osdn_rows q{}, k{}, v{}, qo{};
+    const int32_t *seq;
+    if (n != 16 || !ordinary() || !tensors(a, 13, t) || !device_and_stream(a[14], a[15], dev, stream) || !t[0] || !c.take(t[9], t[0], t[10], t[11], t[12], t[7], a[13], dev) ||
+        !rows_of(t[9], c.io, dev, c.p.B, c.p.T, c.p.Hq, c.p.K, q) || !rows_of(t[0], c.io, dev, c.p.B, c.p.T, c.p.Hk, c.p.K, k) ||
+        !rows_of(t[1], c.io, dev, c.p.B, c.p.T, c.p.Hk, c.p.K, v) || !t[3] || !t[5] || !t[6] || !cache_mx_of(t[2], t[3], t[4], t[5], t[6], dev, c.p.Hk, c.p.K, cache))
+        Py_RETURN_NONE;
+    const int64_t bt[] = {c.p.B, c.p.T};
+    if (!int_array(t[8], dev, at::IntArrayRef(bt, 2), &seq, false)) Py_RETURN_NONE;
+    at::Tensor out;
+    if (t[9]) {
+        out = at::empty(t[9]->sizes(), t[9]->options());
+        qo = dense(out);
+    }
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_pages.append(&c.p, &cache, &q, &k, &v, c.fwq(), c.fwk(), c.table(), c.pos(), seq, &qo, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != OSDN_OK) return PyLong_FromLong(rc);
+    return tuple_of({out});
+    END_HANDLE_TH_ERRORS
+}
+
+// paged_read_mx(codes of k, of v, scales of k, of v, page_table, positions, seq, bf16, f32, device, stream): (k, v), a status, or None
+PyObject *paged_read_mx(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const at::Tensor *t[7];
+    long dev;
+    void *stream;
+    osdn_cache_mx cache;
+    const int32_t *pos, *seq;
+    if (n != 11 || !ordinary() || !tensors(a, 7, t) || !device_and_stream(a[9], a[10], dev, stream) || !t[0] || t[0]->dim() != 4 || !t[1] || !t[3] || !t[4] || !t[5] || t[5]->dim() != 2 ||
+        (a[7] != Py_True && a[8] != Py_True))
+        Py_RETURN_NONE;
+    const int64_t B = t[5]->size(0), T = t[5]->size(1), H = t[0]->size(2), K = 2 * t[0]->size(3);
+    for (int64_t x : {B, T, H, K})
+        if (x > INT_MAX) Py_RETURN_NONE;
+    if (!cache_mx_of(t[0], t[1], t[2], t[3], t[4], dev, H, K, cache) || !int_array(t[5], dev, t[5]->sizes(), &pos) || !int_array(t[6], dev, t[5]->sizes(), &seq, false)) Py_RETURN_NONE;
+    osdn_norm_params p{(int32_t)B, (int32_t)T, 0, (int32_t)H, (int32_t)K, a[7] == Py_True ? OSDN_BF16 : OSDN_F32, 0, 0, 0, 0, 0.f};
+    const at::TensorOptions io = t[0]->options().dtype(a[7] == Py_True ? at::kBFloat16 : at::kFloat);
+    at::Tensor k = at::empty({B, T, H, K}, io), v = at::empty({B, T, H, K}, io);
+    osdn_rows ko = dense(k), vo = dense(v);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_pages.read(&p, &cache, pos, seq, &ko, &vo, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != OSDN_OK) return PyLong_FromLong(rc);
+    return tuple_of({k, v});
+    END_HANDLE_TH_ERRORS
+}
+
+// What the calls of attention share: sizes, scale, window (null: none) and the outputs
+struct DecodeCall {
+    osdn_decode_params p;
+    osdn_rows q, o;
+    at::Tensor out, lse, ws;
+    void *scratch = nullptr;
+    bool take(const at::Tensor *query, int64_t Hk, PyObject *scale, PyObject *window, PyObject *longest, int64_t capacity, PyObject *want_lse, int64_t dev) {
+        if (!query || query->dim() != 3 || !PyBool_Check(want_lse) || (scale != Py_None && !PyFloat_CheckExact(scale))) return false;
+        const int64_t B = query->size(0), Hq = query->size(1), K = query->size(2);
+        for (int64_t x : {B, Hq, Hk, K})
+            if (x > INT_MAX) return false;
+        const at::ScalarType io = query->scalar_type() == at::kBFloat16 ? at::kBFloat16 : at::kFloat;
+        const double s = scale == Py_None ? std::pow((double)K, -0.5) : PyFloat_AS_DOUBLE(scale);
+        p = osdn_decode_params{(int32_t)B, (int32_t)Hq, (int32_t)Hk, (int32_t)K, io == at::kBFloat16 ? OSDN_BF16 : OSDN_F32, 0, 0, 0, (float)s};
+        return !(std::fabs(s) > FLT_MAX) && (!window || int_of(window, p.window)) && int_or(longest, capacity < 0x7fffff00 ? capacity : 0x7fffff00, p.max_length) &&
+               rows_of(query, io, dev, B, -1, Hq, K, q);
+    }
+    bool outputs(const at::Tensor &query, const at::Tensor *workspace, size_t &bytes, bool want_lse, int64_t dev) {
+        if (workspace) {
+            if (!plain(*workspace, at::kByte, dev, workspace->sizes())) return false;
+            bytes = (size_t)workspace->numel();
+            scratch = workspace->data_ptr();
+        } else if (bytes) {
+            ws = at::empty({(int64_t)bytes}, query.options().dtype(at::kByte));
+            scratch = ws.data_ptr();
+        }
+        out = at::empty(query.sizes(), query.options());
+        if (want_lse) lse = at::empty({p.B, p.Hq}, query.options().dtype(at::kFloat));
+        o = osdn_rows{out.data_ptr(), out.stride(0), 0, out.stride(1)};
+        return true;
+    }
+    float *l() const { return lse.defined() ? static_cast<float *>(lse.data_ptr()) : nullptr; }
+};
+
+// paged_decode_mx(q, codes of k, of v, scales of k, of v, page_table, lengths, seq, workspace, scale, window, max_length, want_lse, device, stream): (o, lse or None),
+// a status, or None
+PyObject *paged_decode_mx(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const at::Tensor *t[9];
+    long dev;
+    void *stream;
+    osdn_cache_mx cache;
+    DecodeCall d;
+    const int32_t *lengths, *seq;
+    if (n != 15 || !ordinary() || !tensors(a, 9, t) || !device_and_stream(a[13], a[14], dev, stream) || !t[0] || t[0]->dim() != 3 || !t[1] || t[1]->dim() != 4 || !t[2] || !t[4] || !t[5])
+        Py_RETURN_NONE;
+    const int64_t B = t[0]->size(0), Hk = t[1]->size(2);
+    if (!cache_mx_of(t[1], t[2], t[3], t[4], t[5], dev, Hk, t[0]->size(2), cache) ||
+        !d.take(t[0], Hk, a[9], a[10], a[11], (int64_t)cache.max_pages * cache.page_size, a[12], dev) || !int_array(t[6], dev, at::IntArrayRef(&B, 1), &lengths) ||
+        !int_array(t[7], dev, at::IntArrayRef(&B, 1), &seq, false))
+        Py_RETURN_NONE;
+    size_t bytes = g_pages.decode_bytes(&d.p);
+    if (!d.outputs(*t[0], t[8], bytes, a[12] == Py_True, dev)) Py_RETURN_NONE;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_pages.decode(&d.p, &cache, &d.q, lengths, seq, &d.o, d.l(), d.scratch, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != OSDN_OK) return PyLong_FromLong(rc);
+    return tuple_of({d.out, d.lse});
+    END_HANDLE_TH_ERRORS
+}
+
+// paged_decode_pages(q, k, v, scales of k, of v (both None: rows of q's type), chosen, tokens, workspace, scale, max_length, want_lse, device, stream): (o, lse or
+// None), a status, or None
+PyObject *paged_decode_pages(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const at::Tensor *t[8];
+    long dev;
+    void *stream;
+    DecodeCall d;
+    if (n != 13 || !ordinary() || !tensors(a, 8, t) || !device_and_stream(a[11], a[12], dev, stream) || !t[0] || t[0]->dim() != 3 || !t[1] || t[1]->dim() != 4 || !t[2] || !t[5] ||
+        t[5]->dim() != 3)
+        Py_RETURN_NONE;
+    const bool mx = t[3] && t[4];
+    const int64_t B = t[0]->size(0), Hk = t[1]->size(2), N = t[5]->size(2), bhn[] = {B, Hk, N};
+    const int32_t *chosen, *tokens;
+    if ((!mx && (t[3] || t[4])) || N > INT_MAX || !int_array(t[5], dev, at::IntArrayRef(bhn, 3), &chosen) || !int_array(t[6], dev, at::IntArrayRef(bhn, 2), &tokens) ||
+        !d.take(t[0], Hk, a[8], nullptr, a[9], N * t[1]->size(1), a[10], dev))
+        Py_RETURN_NONE;
+    osdn_cache cache;
+    osdn_cache_mx cache_mx;
+    if (mx) {
+        if (!cache_mx_of(t[1], t[2], t[3], t[4], nullptr, dev, Hk, d.p.K, cache_mx)) Py_RETURN_NONE;
+    } else {
+        const at::ScalarType io = d.p.io_dtype == OSDN_BF16 ? at::kBFloat16 : at::kFloat;
+        const int64_t pages = t[1]->size(0), page = t[1]->size(1);
+        osdn_rows k, v;
+        if (pages > INT_MAX || page > INT_MAX || !rows_of(t[1], io, dev, pages, page, Hk, d.p.K, k) || !rows_of(t[2], io, dev, pages, page, Hk, d.p.K, v)) Py_RETURN_NONE;
+        cache = osdn_cache{k.data, v.data, k.batch, k.token, k.head, v.batch, v.token, v.head, chosen, N, (int32_t)pages, (int32_t)page, 1, (int32_t)N};
+    }
+    size_t bytes = mx ? g_pages.decode_pages_mx_bytes(&d.p) : g_pages.decode_pages_bytes(&d.p);
+    if (!d.outputs(*t[0], t[7], bytes, a[10] == Py_True, dev)) Py_RETURN_NONE;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = mx ? g_pages.decode_pages_mx(&d.p, &cache_mx, &d.q, chosen, (int32_t)N, tokens, &d.o, d.l(), d.scratch, bytes, stream)
+            : g_pages.decode_pages(&d.p, &cache, &d.q, chosen, (int32_t)N, tokens, &d.o, d.l(), d.scratch, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != OSDN_OK) return PyLong_FromLong(rc);
+    return tuple_of({d.out, d.lse});
+    END_HANDLE_TH_ERRORS
+}
+
+// page_bounds(keys, their scales or None, page_table, cached, lengths, seq, bounds, max_new, device, stream): (), a status, or None
+PyObject *page_bounds(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const at::Tensor *t[7];
+    long dev;
+    void *stream;
+    const int32_t *cached, *lengths, *seq;
+    const void *bounds;
+    if (n != 10 || !ordinary() || !tensors(a, 7, t) || !device_and_stream(a[8], a[9], dev, stream) || !t[0] || t[0]->dim() != 4 || !t[2] || !t[3] || t[3]->dim() != 1 || !t[6] ||
+        t[6]->dim() != 4)
+        Py_RETURN_NONE;
+    const int64_t B = t[3]->size(0), Hk = t[0]->size(2), K = t[6]->size(3), shape[] = {t[0]->size(0), Hk, 2, K};
+    const at::ScalarType io = t[6]->scalar_type() == at::kBFloat16 ? at::kBFloat16 : at::kFloat;
+    osdn_cache cache;
+    osdn_cache_mx cache_mx;
+    osdn_select_params p{};
+    if (B > INT_MAX || Hk > INT_MAX || K > INT_MAX || !array(t[6], io, dev, at::IntArrayRef(shape, 4), &bounds) || !int_array(t[3], dev, at::IntArrayRef(&B, 1), &cached) ||
+        !int_array(t[4], dev, at::IntArrayRef(&B, 1), &lengths) || !int_array(t[5], dev, at::IntArrayRef(&B, 1), &seq, false))
+        Py_RETURN_NONE;
+    if (t[1] ? !cache_mx_of(t[0], nullptr, t[1], nullptr, t[2], dev, Hk, K, cache_mx) : !cache_of(t[0], t[0], t[2], io, dev, Hk, K, cache)) Py_RETURN_NONE;
+    p.B = (int32_t)B; p.Hk = (int32_t)Hk; p.K = (int32_t)K; p.io_dtype = io == at::kBFloat16 ? OSDN_BF16 : OSDN_F32;
+    if (!int_or(a[7], t[2]->size(1) * t[0]->size(1), p.max_new)) Py_RETURN_NONE;
+    void *to = const_cast<void *>(bounds);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = t[1] ? g_pages.bounds_mx(&p, &cache_mx, cached, lengths, seq, to, stream) : g_pages.bounds(&p, &cache, cached, lengths, seq, to, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != OSDN_OK) return PyLong_FromLong(rc);
+    return PyTuple_New(0);
+    END_HANDLE_TH_ERRORS
+}
+
+// page_select(q, bounds, page_table, lengths, seq, workspace, page_size, pages, first, last, max_length, device, stream): (chosen, tokens), a status, or None
+PyObject *page_select(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const at::Tensor *t[6];
+    long dev;
+    void *stream;
+    const int32_t *lengths, *seq;
+    const void *bounds;
+    osdn_rows q;
+    osdn_pages g{};
+    osdn_select_params p{};
+    int64_t seqs, most, stride;
+    if (n != 13 || !ordinary() || !tensors(a, 6, t) || !device_and_stream(a[11], a[12], dev, stream) || !t[0] || t[0]->dim() != 3 || !t[1] || t[1]->dim() != 4 ||
+        !table_of(t[2], dev, seqs, most, stride) || !int_of(a[6], g.page_size) || !int_of(a[7], p.pages) || !int_of(a[8], p.first) || !int_of(a[9], p.last) ||
+        !int_or(a[10], std::min<int64_t>(most * std::max(g.page_size, 0), 0x7fffff00), p.max_length))
+        Py_RETURN_NONE;
+    const int64_t B = t[0]->size(0), Hq = t[0]->size(1), K = t[0]->size(2), pages = t[1]->size(0), Hk = t[1]->size(1), shape[] = {pages, Hk, 2, K};
+    const at::ScalarType io = t[0]->scalar_type() == at::kBFloat16 ? at::kBFloat16 : at::kFloat;
+    for (int64_t x : {B, Hq, Hk, K, pages})
+        if (x > INT_MAX) Py_RETURN_NONE;
+    if (p.pages < 1 || !rows_of(t[0], io, dev, B, -1, Hq, K, q) || !array(t[1], io, dev, at::IntArrayRef(shape, 4), &bounds) || !int_array(t[3], dev, at::IntArrayRef(&B, 1), &lengths) ||
+        !int_array(t[4], dev, at::IntArrayRef(&B, 1), &seq, false))
+        Py_RETURN_NONE;
+    g.table = static_cast<int32_t *>(t[2]->data_ptr()); g.table_stride = stride; g.n_pages = (int32_t)pages; g.n_seqs = (int32_t)seqs; g.max_pages = (int32_t)most;
+    p.B = (int32_t)B; p.Hq = (int32_t)Hq; p.Hk = (int32_t)Hk; p.K = (int32_t)K; p.io_dtype = io == at::kBFloat16 ? OSDN_BF16 : OSDN_F32;
+    size_t bytes = g_pages.select_bytes(&p, g.page_size);
+    at::Tensor ws;
+    void *scratch = nullptr;
+    if (t[5]) {
+        if (!plain(*t[5], at::kByte, dev, t[5]->sizes())) Py_RETURN_NONE;
+        bytes = (size_t)t[5]->numel();
+        scratch = t[5]->data_ptr();
+    } else if (bytes) {
+        ws = at::empty({(int64_t)bytes}, t[0]->options().dtype(at::kByte));
+        scratch = ws.data_ptr();
+    }
+    if (B * Hk > (1 << 21) || B * Hk * p.pages > INT_MAX) Py_RETURN_NONE;
+    at::Tensor chosen = at::empty({B, Hk, p.pages}, t[2]->options()), tokens = at::empty({B, Hk}, t[2]->options());
+    int32_t *c = ints(chosen), *k = ints(tokens);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = g_pages.select(&p, &g, &q, bounds, lengths, seq, c, k, scratch, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != OSDN_OK) return PyLong_FromLong(rc);
+    return tuple_of({chosen, tokens});
+    END_HANDLE_TH_ERRORS
+}
+
+// bind_pages(the addresses in the order of g_pages, as a tuple, sizes of the three structs): refused where the structs are not those this was built for
+PyObject *bind_pages(PyObject *, PyObject *args) {
+    PyObject *at;
+    Py_ssize_t size[3];
+    if (!PyArg_ParseTuple(args, "O!nnn", &PyTuple_Type, &at, &size[0], &size[1], &size[2])) return nullptr;
+    const size_t want[] = {sizeof(osdn_pages), sizeof(osdn_cache_mx), sizeof(osdn_select_params)};
+    for (int i = 0; i < 3; ++i)
+        if ((size_t)size[i] != want[i]) return PyErr_Format(PyExc_ImportError, "built for a struct of %zd bytes, not %zd", (Py_ssize_t)want[i], size[i]);
+    if (PyTuple_GET_SIZE(at) != PAGES_ENTRIES) return PyErr_Format(PyExc_TypeError, "expected %d addresses", PAGES_ENTRIES);
+    void *p[PAGES_ENTRIES];
+    for (int i = 0; i < PAGES_ENTRIES; ++i) {
+        p[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(at, i));
+        if (PyErr_Occurred()) return nullptr;
+    }
+    static_assert(sizeof(g_pages) == sizeof(p), "one address for each");
+    std::memcpy(&g_pages, p, sizeof(p));
+    Py_RETURN_NONE;
+}
+
 // bind_rows(the six addresses in the order of g_rows, sizes of their four structs): refused where the structs are not those this was built for
 PyObject *bind_rows(PyObject *, PyObject *args) {
     PyObject *at[6];
@@ -437,6 +842,15 @@ PyMethodDef kMethods[] = {
     {"qk_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(qk_norm_backward)), METH_FASTCALL, "osdn_qk_norm_bwd on tensors, or None"},
     {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append)), METH_FASTCALL, "osdn_paged_append on tensors, or None"},
     {"paged_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_decode)), METH_FASTCALL, "osdn_paged_decode on tensors, or None"},
+    {"paged_plan", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_plan)), METH_FASTCALL, "osdn_paged_plan on tensors, or None"},
+    {"paged_release", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_release)), METH_FASTCALL, "osdn_paged_release on tensors, or None"},
+    {"paged_append_mx", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append_mx)), METH_FASTCALL, "osdn_paged_append_mx on tensors, or None"},
+    {"paged_read_mx", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_read_mx)), METH_FASTCALL, "osdn_paged_read_mx on tensors, or None"},
+    {"paged_decode_mx", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_decode_mx)), METH_FASTCALL, "osdn_paged_decode_mx on tensors, or None"},
+    {"paged_decode_pages", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_decode_pages)), METH_FASTCALL, "osdn_paged_decode_pages(_mx) on tensors, or None"},
+    {"page_bounds", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(page_bounds)), METH_FASTCALL, "osdn_page_bounds(_mx) on tensors, or None"},
+    {"page_select", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(page_select)), METH_FASTCALL, "osdn_page_select on tensors, or None"},
+    {"bind_pages", bind_pages, METH_VARARGS, "addresses of the entry points of pages and the cache in 4 bits, sizes of their structs"},
     {"bind_rows", bind_rows, METH_VARARGS, "addresses of the entry points around the recurrence, sizes of their structs"},
     {"bind", bind, METH_VARARGS, "address of osdn_step, size of osdn_params, version of the tensor library"},
     {nullptr, nullptr, 0, nullptr}};

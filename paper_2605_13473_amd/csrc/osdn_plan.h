@@ -296,6 +296,10 @@ constexpr int decode_tile(int K, bool bf16) { return bf16 && K <= 128 ? 32 : 16;
 // Workgroups that the registers of a CU hold
 constexpr int decode_per_cu(int K, bool bf16) { return K == 64 ? 4 : K == 128 ? (bf16 ? 3 : 2) : bf16 ? 2 : 1; }
 constexpr int decode_unit(int K, bool bf16, int R) { return DEC_THREADS / 64 / R * decode_tile(K, bf16); }
+// ... over a cache in 4 bits
+constexpr int DECODE_MX_TILE = 32;
+constexpr int decode_mx_per_cu(int K, bool bf16) { return K == 256 ? (bf16 ? 2 : 1) : bf16 ? (K == 64 ? 4 : 3) : 2; }
+constexpr int decode_mx_unit(int R) { return DEC_THREADS / 64 / R * DECODE_MX_TILE; }
 inline long long decode_span(int max_length, int window) {
     const long long seen = window > 0 && window < max_length ? (long long)window + DECODE_TILE - 1 : max_length;
     return seen < max_length ? seen : max_length;
@@ -324,9 +328,9 @@ inline long long decode_span(int max_length, int window) {
 //  - and not so many that the parts (an fp32 row of each query head) outweigh what a share reads: 8 x 8000 x 2 with 32 query heads each, 256 and 512
 //    shares 31.6 and 35.3.
 struct DecodePlan { int row_group, shares; long long units; };
-inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K, bool bf16, int part_heads, bool heads_together, int asked) {
+inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K, bool bf16, int part_heads, bool heads_together, int asked, bool mx = false) {
     const long long span = decode_span(max_length, window), all = (long long)B * rows;
-    const int tile = decode_tile(K, bf16), alone = decode_unit(K, bf16, 1), held = decode_per_cu(K, bf16) * NUM_CU;
+    const int tile = mx ? DECODE_MX_TILE : decode_tile(K, bf16), alone = mx ? decode_mx_unit(1) : decode_unit(K, bf16, 1), held = (mx ? decode_mx_per_cu(K, bf16) : decode_per_cu(K, bf16)) * NUM_CU;
     const bool beside = heads_together && rows % 2 == 0;
     const bool few_units = span <= (K == 64 ? 4 : bf16 ? 3 : 2) * alone || (span <= 4 * alone && all >= NUM_CU / 2);
     const bool full = all >= held && held > NUM_CU && span <= (beside || K == 256 ? 512 : 1024);
@@ -334,13 +338,23 @@ inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K
     const bool together = each ? (span <= tile && all > held) || (span <= 4 * tile && 2 * all > 3 * held) : beside || (K == 64 && bf16);
     DecodePlan p{};
     p.row_group = together && rows % 4 == 0 ? 4 : together && rows % 2 == 0 ? 2 : 1;
-    const int unit = decode_unit(K, bf16, p.row_group);
+    const int unit = mx ? decode_mx_unit(p.row_group) : decode_unit(K, bf16, p.row_group);
     p.units = span < 1 ? 1 : (span + unit - 1) / unit;
     const long long groups = all / p.row_group;
     const int per_cu = all <= 16 || (K == 256 && !bf16) || (K == 128 && bf16 && p.row_group == 4 && span > 1024) ? 1 : K == 64 && p.row_group < 4 ? 3 : 2;
     const long long worth = groups * span / (16 * part_heads), most = per_cu * NUM_CU < worth ? per_cu * NUM_CU : worth > NUM_CU ? worth : NUM_CU;
     p.shares = each ? 0 : asked > 0 ? asked : (int)(groups * p.units < most ? groups * p.units : most);
     return p;
+}
+
+// Tokens of a batch of requests whose places one workgroup writes, beside the running sums; more go in a launch of their own
+constexpr int PLAN_TOKENS_HERE = 2048;
+// Rows of a page table that a call with an index of them may have (two bits each in LDS)
+constexpr int PLAN_MAX_ROWS = 1 << 17;
+// Workgroups (four wavefronts, a page each at a time) for the scores of a sequence's pages of one group of key heads
+inline unsigned select_chunks(int B, int Hk, int heads, int pages) {
+    const long long others = (long long)B * ((Hk + heads - 1) / heads), want = (8 * NUM_CU + others - 1) / others, most = (pages + 3) / 4;
+    return (unsigned)(want < most ? want : most);
 }
 
 // (constexpr, as what follows: for the device too)
