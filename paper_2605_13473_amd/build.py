@@ -18,7 +18,7 @@ NATIVE = os.path.join(HERE, "_native" + sysconfig.get_config_var("EXT_SUFFIX")) 
 NATIVE_SOURCE = os.path.join(CSRC, "osdn_native.cpp")
 SOURCES = ["osdn_api.hip", "osdn_precond.hip", "osdn_precond_bwd.hip", "osdn_precond_gen.hip", "osdn_step.hip", "osdn_tables.hip",
            "osdn_chunk_fwd.hip", "osdn_chunk_bwd.hip", "osdn_heads.hip", "osdn_paged.hip", "osdn_paged_mx.hip",
-           "osdn_pages.hip"]
+           "osdn_chosen.hip", "osdn_chosen_mx.hip", "osdn_pages.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -26,7 +26,7 @@ FLAGS = [
 ]
 # decode_kernel scales its sums between products: kept in the registers that ordinary instructions read (fp32, K = 256: 388 -> 336 of them, 310 moves
 # less; narrower rows come out the same)
-FLAGS_OF = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("osdn_paged.hip", "osdn_paged_mx.hip")}
+FLAGS_OF = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("osdn_paged.hip", "osdn_paged_mx.hip", "osdn_chosen.hip", "osdn_chosen_mx.hip")}
 
 
 def build(verbose: bool = False, only=None) -> str:

@@ -610,6 +610,15 @@ size_t osdn_paged_decode_mx_workspace_bytes(const osdn_decode_params *p) { retur
 size_t osdn_paged_decode_pages_workspace_bytes(const osdn_decode_params *p) { return decode_bytes(p, false, true); }
 size_t osdn_paged_decode_pages_mx_workspace_bytes(const osdn_decode_params *p) { return decode_bytes(p, true, true); }
 
+// Whether the rows of a 4-bit cache are laid out alike, as alloc's are: values as keys, scales with a sixteenth of the steps of the codes, and steps
+// that 32 bits hold (24 from slot to slot).  (Uneven 512 x 4096 tokens, four heads: with an offset for each array, whose 64-bit products take
+// a quarter of the kernel's vector time, 152 us, so 128.)
+static bool fp4_regular(const DecodeArgs &a) {
+    const HeadRows &k = a.cache_k, &v = a.cache_v, &ks = a.scale_k, &vs = a.scale_v;
+    return k.batch == v.batch && k.token == v.token && k.batch == 16 * ks.batch && k.token == 16 * ks.token && k.batch == 16 * vs.batch && k.token == 16 * vs.token &&
+           k.batch < 1LL << 32 && k.token < 1LL << 24 && a.page_shift < 24 && k.token * (1LL << a.page_shift) < 1LL << 32;
+}
+
 // chosen (with tokens in the place of lengths): the pages of each key head, n_chosen of them, in place of the cache's table
 extern "C++" {
 template <typename Cache>
@@ -641,11 +650,14 @@ static int decode_impl(const osdn_decode_params *p, const Cache *cache, const os
         a.info = reinterpret_cast<int *>(a.part_ml + parts * 2);
     }
     take_cache(&c, a.cache_k, a.cache_v, a.scale_k, a.scale_v);
+    if constexpr (mx) a.regular = fp4_regular(a);
     a.table = c.table; a.table_stride = c.table_stride; a.lengths = lengths; a.seq = seq; a.lse = lse;
     a.n_pages = c.n_pages; a.n_seqs = c.n_seqs; a.max_pages = c.max_pages;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool bf = p->io_dtype == OSDN_BF16;
-    if (timed(KID_PAGED_DECODE, st, [&] { return mx ? launch_paged_decode_mx(a, bf, st) : launch_paged_decode(a, bf, st); }) != 0) return OSDN_ERR_SHAPE;
+    if (timed(KID_PAGED_DECODE, st, [&] { 
+        return pages ? (mx ? launch_chosen_decode_mx(a, bf, st) : launch_chosen_decode(a, bf, st)) : mx ? launch_paged_decode_mx(a, bf, st) : launch_paged_decode(a, bf, st);
+    }) != 0) return OSDN_ERR_SHAPE;
     return launch_status();
 }
 }

@@ -1,0 +1,15 @@
+// Attention over chosen pages of a cache in 4 bits.
+#include "osdn_decode_tiles.h"
+
+namespace osdn {
+
+template <int K> using Fp4Bf16 = Fp4Tile<bf16, K, true, true>;
+template <int K> using Fp4F32 = Fp4Tile<float, K, true, true>;
+template <int K> using Fp4Bf16Any = Fp4Tile<bf16, K, false, true>;
+template <int K> using Fp4F32Any = Fp4Tile<float, K, false, true>;
+int launch_chosen_decode_mx(const DecodeArgs &a, bool bf16_io, hipStream_t st) {
+    if (a.regular) return bf16_io ? decode_by_width<Fp4Bf16>(a, st) : decode_by_width<Fp4F32>(a, st);
+    return bf16_io ? decode_by_width<Fp4Bf16Any>(a, st) : decode_by_width<Fp4F32Any>(a, st);
+}
+
+}  // namespace osdn

@@ -107,10 +107,10 @@ template <int UNIT> __device__ __forceinline__ int units_of(const DecodeArgs &a,
     return seen_units(seen_of(a, a.lengths[b], a.seq ? a.seq[b] : b), UNIT);
 }
 
-// Entry b of the batch is a sequence, or (table_heads > 1: a table for each key head) one key head of a sequence: which one of q and o, and that head
+// Entry b of the batch is a sequence, or (CHOSEN: a table for each key head) one key head of a sequence: which one of q and o, and that head
 struct Entry { int b, head; };
-__device__ __forceinline__ Entry entry_of(const DecodeArgs &a, int b) {
-    if (a.table_heads == 1) return {b, 0};
+template <bool CHOSEN> __device__ __forceinline__ Entry entry_of(const DecodeArgs &a, int b) {
+    if constexpr (!CHOSEN) return {b, 0};
     const int i = b / (unsigned)a.table_heads;
     return {i, b - i * a.table_heads};
 }
@@ -127,6 +127,7 @@ __global__ __launch_bounds__(DEC_T, D::PER_CU) void decode_kernel(DecodeArgs a) 
     __shared__ int found[2], sums[DEC_W];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     ask_arguments(a);
+    D::ask_arguments(a);
     const int groups = a.Hk * a.head_tiles / R, w = blockIdx.x;     // groups of rows of a sequence
     const int turn = wave % WPR;                                    // this wavefront's among those of its row
     // This workgroup's share: units [at, until), the first of them of sequence b, whose units start at `base`
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(DEC_T, D::PER_CU) void decode_kernel(DecodeArgs a) 
         const int kt = group * R + wave / WPR;                      // this wavefront's row
         const int kv = a.head_tiles == 1 ? kt : kt / a.head_tiles, h0 = kv * a.group + 16 * (kt - kv * a.head_tiles);
         const int heads = min(16, (kv + 1) * a.group - h0);
-        const Entry from = entry_of(a, b);
+        const Entry from = entry_of<D::CHOSEN>(a, b);
         const int seq = a.seq ? a.seq[b] : b;
         const Seen see = seen_of(a, a.lengths[b], seq);
         const int *row = a.table + (see.end > 0 ? seq * a.table_stride : 0);
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(DEC_T, D::PER_CU) void decode_kernel(DecodeArgs a) 
         D x;                                                        // this lane's part of a tile, on its way
         x.begin(a, kv + from.head, lane);
         x.ask(a, row, begin + turn * TT, lo, end, lane);
-        const T *qrow = static_cast<const T *>(a.q.data) + from.b * a.q.batch + (from.head * a.group + h0 + col) * a.q.head;
+        const T *qrow = static_cast<const T *>(a.q.data) + from.b * a.q.batch + (D::CHOSEN ? from.head * a.group + h0 + col : h0 + col) * a.q.head;
         typename D::Query q;                                        // lane l holds head l % 16
         q.load(qrow, col < heads, a.aligned, lane);
         V *vs = reinterpret_cast<V *>(lds) + wave * TT * LDV;
@@ -218,9 +219,7 @@ __global__ __launch_bounds__(DEC_T, D::PER_CU) void decode_kernel(DecodeArgs a) 
             float top = m;
             const bool whole = tok >= lo && tok + TT <= end;
 #pragma unroll
-            for (int i = 0; i < D::SETS; ++i) {
-                p[i] = x.scores(i, q);
-            }
+            for (int i = 0; i < D::SETS; ++i) p[i] = x.scores(i, q);
             if (!whole) {               // what is not seen has no weight, and must not be infinite or NaN either
 #pragma unroll
                 for (int i = 0; i < D::SETS; ++i) {
@@ -286,10 +285,10 @@ __global__ __launch_bounds__(DEC_T, D::PER_CU) void decode_kernel(DecodeArgs a) 
         auto leave = [&](int h, int d, f32x4 x, float M, float L) {
             if (alone) {
                 const float inv = L == 0.f ? 0.f : 1.f / L;
-                int again = b;              // (found once more: kept from the start it would cost registers that the loop wants)
-                asm volatile("" : "+s"(again));
-                const Entry of = entry_of(a, again);
-                T *dst = static_cast<T *>(a.o.data) + of.b * a.o.batch + (of.head * a.group + h0 + h) * a.o.head + d;
+                int again = b;
+                asm volatile("" : "+s"(again));     // (found once more: kept from the start it would cost registers that the loop wants)
+                const Entry of = entry_of<D::CHOSEN>(a, again);
+                T *dst = static_cast<T *>(a.o.data) + of.b * a.o.batch + (D::CHOSEN ? of.head * a.group + h0 + h : h0 + h) * a.o.head + d;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) x[r] *= inv;
                 if (a.aligned) {
@@ -357,7 +356,7 @@ __global__ __launch_bounds__(DEC_T, D::PER_CU) void decode_kernel(DecodeArgs a) 
 
 // The parts of the query heads, joined in their order.  A wavefront (WG: a workgroup, its four wavefronts a quarter of the parts each) joins JC columns
 // of one head: a lane four columns of every (64 / (JC / 4))-th part.
-template <typename T, int K, int JC, bool WG>
+template <typename T, int K, bool CHOSEN, int JC, bool WG>
 __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
     constexpr int QUADS = JC / 4, ROWS = 64 / QUADS, WAVES = WG ? 4 : 1;
     __shared__ float red[4][JC], sums[4];
@@ -422,8 +421,8 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a) {
     }
     if (lane >= QUADS) return;
     const float inv = L == 0.f ? 0.f : 1.f / L;
-    const Entry of = entry_of(a, b);
-    T *dst = static_cast<T *>(a.o.data) + of.b * a.o.batch + (of.head * a.group + h) * a.o.head + c0;
+    const Entry of = entry_of<CHOSEN>(a, b);
+    T *dst = static_cast<T *>(a.o.data) + of.b * a.o.batch + (CHOSEN ? of.head * a.group + h : h) * a.o.head + c0;
 #pragma unroll
     for (int r = 0; r < 4; ++r) x[r] *= inv;
     if (a.aligned) {
@@ -448,8 +447,8 @@ template <typename D> void decode_of(const DecodeArgs &a, hipStream_t st) {
     if (!shares) return decode_rows<D, false>(a, groups, st);
     decode_rows<D, true>(a, shares, st);
     // (many parts of few rows: a workgroup each, as the loads of a row are then what takes the time)
-    if (shares > 16 * groups) hipLaunchKernelGGL((decode_join_kernel<T, K, 16, true>), dim3(heads * (K / 16)), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((decode_join_kernel<T, K, 64, false>), dim3((heads * (K / 64) + 3) / 4), dim3(256), 0, st, a);
+    if (shares > 16 * groups) hipLaunchKernelGGL((decode_join_kernel<T, K, D::CHOSEN, 16, true>), dim3(heads * (K / 16)), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((decode_join_kernel<T, K, D::CHOSEN, 64, false>), dim3((heads * (K / 64) + 3) / 4), dim3(256), 0, st, a);
 }
 template <template <int> class Tile> int decode_by_width(const DecodeArgs &a, hipStream_t st) {
     switch (a.K) {

@@ -273,22 +273,26 @@ struct DecodeArgs {
     int B, Hq, Hk, K, group, head_tiles;  // group: query heads of a key head; head_tiles: rows (of up to 16 query heads) that they make
     float scale;
     int window, max_length;
-    int table_heads;                      // 1, or key heads of q and o: the table has a row for each, B is sequences x heads and Hq, Hk those of one
     int row_group;                        // adjacent rows of a sequence that a workgroup takes: 1, 2 or 4
     int shares, part_heads;               // shares: workgroups that the tokens are cut among, 0: one for each group of rows; part_heads: heads of a row, at most
     HeadRows q, o, cache_k, cache_v;      // q, o: token unused
-    HeadRows scale_k, scale_v;            // a cache in 4 bits, its steps in bytes
     bool aligned;                         // every row of q and o starts on 16 bytes
     const int *table, *seq, *lengths;     // [n_seqs, max_pages], [B] or null (the batch entry), [B]
     long long table_stride;
     int n_pages, page_shift, n_seqs, max_pages;
+    int table_heads;                      // 1, or key heads of q and o: the table has a row for each, B is sequences x heads and Hq, Hk those of one
     float *lse;                           // [B, Hq] or null
     // shares > 0: two parts of each, [shares, 2, row_group, part_heads, K] and (maximum, sum) [..., 2]; the first part and how many, of each group of rows
     float *part_o, *part_ml;
     int *info;
+    // a cache in 4 bits, its steps in bytes (last: a cache of whole rows does not ask for them); regular: see fp4_regular
+    HeadRows scale_k, scale_v;
+    bool regular;
 };
 int launch_paged_decode(const DecodeArgs &a, bool bf16_io, hipStream_t st);
 int launch_paged_decode_mx(const DecodeArgs &a, bool bf16_io, hipStream_t st);
+int launch_chosen_decode(const DecodeArgs &a, bool bf16_io, hipStream_t st);
+int launch_chosen_decode_mx(const DecodeArgs &a, bool bf16_io, hipStream_t st);
 
 // The pages of a cache (osdn_pages.hip)
 struct PlanArgs {

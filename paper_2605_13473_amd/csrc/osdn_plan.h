@@ -298,7 +298,7 @@ constexpr int decode_per_cu(int K, bool bf16) { return K == 64 ? 4 : K == 128 ? 
 constexpr int decode_unit(int K, bool bf16, int R) { return DEC_THREADS / 64 / R * decode_tile(K, bf16); }
 // ... over a cache in 4 bits
 constexpr int DECODE_MX_TILE = 32;
-constexpr int decode_mx_per_cu(int K, bool bf16) { return K == 256 ? (bf16 ? 2 : 1) : bf16 ? (K == 64 ? 4 : 3) : 2; }
+constexpr int decode_mx_per_cu(int K, bool bf16) { return bf16 ? (K == 64 ? 4 : K == 128 ? 4 : 2) : K == 64 ? 4 : K == 128 ? 2 : 1; }
 constexpr int decode_mx_unit(int R) { return DEC_THREADS / 64 / R * DECODE_MX_TILE; }
 inline long long decode_span(int max_length, int window) {
     const long long seen = window > 0 && window < max_length ? (long long)window + DECODE_TILE - 1 : max_length;
@@ -327,6 +327,18 @@ inline long long decode_span(int max_length, int window) {
 //    18.7, 18.3, 20.3, 21.8, bf16 2 x 58831 x 2 16.2, 16.1, 18.8, 20.9, K = 128, 4 x 32768 x 1 25.5, 22.1, 22.8, 24.4; but 8 x 4096 x 4 18.4, 19.4, 18.2, 17.5).
 //  - and not so many that the parts (an fp32 row of each query head) outweigh what a share reads: 8 x 8000 x 2 with 32 query heads each, 256 and 512
 //    shares 31.6 and 35.3.
+// Over a cache in 4 bits, whose rows are a quarter as long, what is the same for every row and every call weighs more, and so does the join (us, as above, four heads of K = 128 in
+// bf16 unless said):
+//  - a row each up to 768 tokens (K = 256: 384), where the second kernel costs more than what it makes shorter: 1 x 500 x 8 7.1 and 8.7, 16 x 800 9.7 and 11.0, 4 x 300, K = 256, 8.8 and
+//    11.9; but 1 x 1200 x 8 11.9 and 8.7, 4 x 700, K = 256, 12.7 and 12.5; up to 2048 where every CU has a row (32 x 2000 x 8 18.7 and 21.8, uneven 17.9 and 25.5; 32 x 3000 x 8 uneven 24.1
+//    and 22.4), and to 3000 where it has two (64 x 3000 x 8 42.6 and 51.5, uneven 31.5 and 37.4; 512 x 3000 151 and 160; but uneven 64 x 8192 x 8 75.3 and 65.8).
+//  - four rows together from two rows a CU on: a share then begins fewer rows (uneven 512 x 4096, one by one 145, so 128; 64 x 8192 x 8 76.5 and 65.8; but 1 x 131072 x 8, whose rows all
+//    shares cut, 34.8 and 37.1).
+//  - two shares a CU, four for rows of 64 elements and where there is about a row for each (uneven 64 x 4096 x 8, K = 64, 256, 512, 768 and 1024 34.4, 27.4, 26.7, 25.5; 40 x 4000 x 8,
+//    K = 256, 84.3, 65.1, 58.8, 55.9; but 1 x 131072 x 8 44.6, 34.8, 37.8, 37.1; 16 x 8192 x 8 42.1, 34.7, 38.1, 37.5).
+inline bool decode_mx_each(long long span, long long all, int K) {
+    return span <= (all >= 2 * NUM_CU ? 3000 : all >= NUM_CU ? 2048 : K == 256 ? 384 : 768);
+}
 struct DecodePlan { int row_group, shares; long long units; };
 inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K, bool bf16, int part_heads, bool heads_together, int asked, bool mx = false) {
     const long long span = decode_span(max_length, window), all = (long long)B * rows;
@@ -334,14 +346,14 @@ inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K
     const bool beside = heads_together && rows % 2 == 0;
     const bool few_units = span <= (K == 64 ? 4 : bf16 ? 3 : 2) * alone || (span <= 4 * alone && all >= NUM_CU / 2);
     const bool full = all >= held && held > NUM_CU && span <= (beside || K == 256 ? 512 : 1024);
-    const bool each = asked < 0 || (asked == 0 && (few_units || full));
-    const bool together = each ? (span <= tile && all > held) || (span <= 4 * tile && 2 * all > 3 * held) : beside || (K == 64 && bf16);
+    const bool each = asked < 0 || (asked == 0 && (mx ? decode_mx_each(span, all, K) : few_units || full));
+    const bool together = each ? (span <= tile && all > held) || (span <= 4 * tile && 2 * all > 3 * held) : mx ? all >= 2 * NUM_CU : beside || (K == 64 && bf16);
     DecodePlan p{};
     p.row_group = together && rows % 4 == 0 ? 4 : together && rows % 2 == 0 ? 2 : 1;
     const int unit = mx ? decode_mx_unit(p.row_group) : decode_unit(K, bf16, p.row_group);
     p.units = span < 1 ? 1 : (span + unit - 1) / unit;
     const long long groups = all / p.row_group;
-    const int per_cu = all <= 16 || (K == 256 && !bf16) || (K == 128 && bf16 && p.row_group == 4 && span > 1024) ? 1 : K == 64 && p.row_group < 4 ? 3 : 2;
+    const int per_cu = mx ? (K == 64 || (all >= NUM_CU && all < 2 * NUM_CU) ? 4 : 2) : all <= 16 || (K == 256 && !bf16) || (K == 128 && bf16 && p.row_group == 4 && span > 1024) ? 1 : K == 64 && p.row_group < 4 ? 3 : 2;
     const long long worth = groups * span / (16 * part_heads), most = per_cu * NUM_CU < worth ? per_cu * NUM_CU : worth > NUM_CU ? worth : NUM_CU;
     p.shares = each ? 0 : asked > 0 ? asked : (int)(groups * p.units < most ? groups * p.units : most);
     return p;
