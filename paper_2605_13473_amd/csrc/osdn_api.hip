@@ -527,12 +527,13 @@ static int append_impl(const osdn_norm_params *p, const Cache *cache, const osdn
         (rc = take_rows(v, p->B, p->T, p->Hk, p->K, es, false, a.v, a.aligned)) != OSDN_OK || (rc = take_rows(q_out, p->B, p->T, p->Hq, p->K, es, true, a.q_out, a.aligned)) != OSDN_OK)
         return rc;
     a.append = true;
-    a.mx = std::is_same<Cache, osdn_cache_mx>::value;
     take_cache(cache, a.cache_k, a.cache_v, a.scale_k, a.scale_v);
     a.table = cache->table; a.table_stride = cache->table_stride; a.seq = seq;
     a.n_pages = cache->n_pages; a.page_shift = shift; a.n_seqs = cache->n_seqs; a.max_pages = cache->max_pages;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (timed(KID_PAGED_APPEND, st, [&] { return launch_heads_fwd(a, p->io_dtype == OSDN_BF16, st); }) != 0) return OSDN_ERR_SHAPE;
+    constexpr bool mx = std::is_same<Cache, osdn_cache_mx>::value;
+    const bool bf = p->io_dtype == OSDN_BF16;
+    if (timed(KID_PAGED_APPEND, st, [&] { return mx ? launch_append_mx(a, bf, st) : launch_heads_fwd(a, bf, st); }) != 0) return OSDN_ERR_SHAPE;
     return launch_status();
 }
 }

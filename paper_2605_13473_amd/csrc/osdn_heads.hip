@@ -13,236 +13,9 @@
 // forward 44 us (6.1 TB/s, a part still in the last level cache), backward 78 us (5.2 TB/s: what a device copy reaches); 2 x 8192 of 32 + 8 with weights
 // and rotation 61 and 110 us (4.6 of them the sum of dw); 65536 tokens of 16 + 4 + 4 appended 159 us (5.1 TB/s).  (Kernel times of a trace, medians,
 // three sets of inputs in turn.)
-#include "osdn_kernels.h"
+#include "osdn_heads.h"
 
 namespace osdn {
-
-constexpr int HEADS_T = 256;
-
-template <typename T, int K> struct HeadRow {
-    static constexpr int VE = 16 / sizeof(T);       // elements of a lane
-    static constexpr int LANES = K / VE;            // lanes of a row
-    static constexpr int ROWS = 64 / LANES;         // rows of a block
-};
-
-// 16 bytes of a row; VEC: at an address that is a multiple of 16, else element by element
-template <typename T, bool VEC> __device__ __forceinline__ u32x4 load_row(const T *p) {
-    if constexpr (VEC) {
-        return *reinterpret_cast<const u32x4 *>(p);
-    } else {
-        T v[16 / sizeof(T)];
-#pragma unroll
-        for (int e = 0; e < (int)(16 / sizeof(T)); ++e) v[e] = p[e];
-        return __builtin_bit_cast(u32x4, v);
-    }
-}
-template <typename T, bool VEC, int VE> __device__ __forceinline__ void store_row(T *p, const float (&v)[VE]) {
-    if constexpr (VEC) {
-        store_vec_t(p, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < VE; ++e) p[e] = from_f32<T>(v[e]);
-    }
-}
-template <typename T, int VE> __device__ __forceinline__ void unpack(const u32x4 &raw, float (&x)[VE]) {
-#pragma unroll
-    for (int e = 0; e < VE; ++e) x[e] = vec_get<T>(raw, e);
-}
-// sum over the LANES lanes of a row, every lane with the result
-template <int LANES> __device__ __forceinline__ float row_sum(float x) {
-    x += dpp_f32<0xB1>(x);         // quad_perm [1,0,3,2]
-    x += dpp_f32<0x4E>(x);         // quad_perm [2,3,0,1]
-    x += dpp_f32<0x141>(x);        // row_half_mirror
-    if (LANES > 8) x += dpp_f32<0x140>(x);      // row_mirror
-    if (LANES > 16) x = add_xor16(x);
-    if (LANES > 32) x = add_xor32(x);
-    return x;
-}
-
-// The caller's fp32 arrays are aligned as floats are
-struct __attribute__((packed, aligned(4))) FloatQuad { float v[4]; };
-template <int N> __device__ __forceinline__ void load_floats(float (&x)[N], const float *p) {
-    static_assert(N % 2 == 0, "");
-    if constexpr (N % 4 == 0) {
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i) {
-            const FloatQuad q = reinterpret_cast<const FloatQuad *>(p)[i];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * i + e] = q.v[e];
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = p[e];
-    }
-}
-
-// The pairs that turn: none, (i, i + R / 2) or (2i, 2i + 1)
-enum { ROT_NONE = 0, ROT_HALF = 1, ROT_PAIRS = 2 };
-
-// The rotation of a lane's elements: z = y c + partner s (transposed: y c - partner s).  Elements that do not turn: c = 1, partner = 0.
-template <typename T, int K, int ROT> struct Turn {
-    static constexpr int VE = HeadRow<T, K>::VE, LANES = HeadRow<T, K>::LANES;
-    bool on;                        // the lane's elements turn
-    int from;                       // the lane that holds their partners
-    int i0;                         // the first one's pair
-    float sign;
-    __device__ __forceinline__ Turn(int R, int lane) {
-        const int e0 = (lane & (LANES - 1)) * VE, half = R / 2;
-        const bool low = e0 < half;
-        on = e0 < R;
-        from = ROT == ROT_PAIRS || !on ? lane : low ? lane + half / VE : lane - half / VE;
-        i0 = !on ? 0 : ROT == ROT_PAIRS ? e0 / 2 : low ? e0 : e0 - half;
-        sign = low ? -1.f : 1.f;
-    }
-    __device__ __forceinline__ void load(const float *row, int R, float (&c)[VE], float (&s)[VE]) const {
-        constexpr int N = ROT == ROT_PAIRS ? VE / 2 : VE;
-        float cs[N], sn[N];
-        load_floats(cs, row + i0);
-        load_floats(sn, row + R / 2 + i0);
-#pragma unroll
-        for (int e = 0; e < VE; ++e) {
-            c[e] = on ? cs[ROT == ROT_PAIRS ? e / 2 : e] : 1.f;
-            s[e] = ROT == ROT_PAIRS ? ((e & 1) ? sn[e / 2] : -sn[e / 2]) : sn[e] * sign;
-        }
-    }
-    // the partners of a lane's elements (every lane of the wavefront calls it)
-    __device__ __forceinline__ void partners(const u32x4 &raw, float (&x)[VE]) const {
-        u32x4 o;
-        if constexpr (ROT == ROT_PAIRS) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) o[w] = sizeof(T) == 2 ? (raw[w] >> 16) | (raw[w] << 16) : raw[w ^ 1];
-        } else {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) o[w] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * from, (int)raw[w]);
-        }
-#pragma unroll
-        for (int w = 0; w < 4; ++w) o[w] = on ? o[w] : 0u;
-        unpack<T>(o, x);
-    }
-    // what stands at the partners' places of a row that all lanes of a row hold (weights)
-    __device__ __forceinline__ int partner_element(int lane, int e) const { return ROT == ROT_PAIRS ? (lane & (LANES - 1)) * VE + (e ^ 1) : (from & (LANES - 1)) * VE + e; }
-};
-
-// The weights of a lane's elements and of their partners, for queries (0) and keys (1); loaded once per wavefront
-template <typename T, int K, int ROT> struct Weights {
-    static constexpr int VE = HeadRow<T, K>::VE;
-    float own[2][VE], partner[2][VE];
-    __device__ __forceinline__ void load(const HeadsArgs &a, const Turn<T, K, ROT> &turn, int lane) {
-#pragma unroll
-        for (int kind = 0; kind < 2; ++kind) {
-            const float *w = kind == 0 ? a.weight_q : a.weight_k;
-            if (w) load_floats(own[kind], w + (lane & (HeadRow<T, K>::LANES - 1)) * VE);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                if (!w) own[kind][e] = 1.f;
-                if constexpr (ROT == ROT_PAIRS) partner[kind][e ^ 1] = own[kind][e];
-            }
-            if constexpr (ROT == ROT_HALF) {
-                if (w) load_floats(partner[kind], w + turn.partner_element(lane, 0));
-                else {
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) partner[kind][e] = 1.f;
-                }
-            }
-        }
-    }
-};
-
-template <typename T, bool VEC> __device__ __forceinline__ T *row_at(const HeadRows &r, int b, int t, int h) {
-    return static_cast<T *>(r.data) + b * r.batch + t * r.token + h * r.head;
-}
-
-// ---- rows in 4 bits ----
-// A block of 32 elements, VE of them a lane, becomes codes and a scale 2^e, e the least (from -120 to 125) with the largest element no more than 7 * 2^e: what lies
-// between 6 and 7 is off by no more than what lies between 4 and 6 may be.  The codes are the nearest values, ties to the even code.
-// Which code that is must not hang on a rounding before: values come as they are, keys in 64 bits.  There the lower word only says whether there is more
-// than the upper one shows (its last bit, set if so), as no border of two codes has that many digits.
-__device__ __forceinline__ int max_block(int x, int lanes) {
-    auto with = [&](int y) { x = max(x, y); };
-    with(__builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, true));         // quad_perm [1,0,3,2]
-    with(__builtin_amdgcn_update_dpp(0, x, 0x4E, 0xf, 0xf, true));         // quad_perm [2,3,0,1]
-    if (lanes > 4) with(__builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, true));     // row_half_mirror
-    return x;
-}
-template <int VE> struct Fp4Block {
-    uint32_t codes;
-    int byte;
-    __device__ __forceinline__ void scale_of(int exponent, bool beyond, bool finite) { byte = finite ? max(-120, min(125, exponent - 2 + beyond)) + 127 : 255; }
-    __device__ __forceinline__ void encode(const float (&y)[VE]) {
-        codes = 0;
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[0], y[1], 1.f, 0);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[2], y[3], 1.f, 1);
-        if constexpr (VE == 8) {
-            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[4], y[5], 1.f, 2);
-            codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[6], y[7], 1.f, 3);
-        }
-        if (byte == 255) codes = 0;
-    }
-    __device__ __forceinline__ explicit Fp4Block(const float (&x)[VE]) {
-        int top = 0;
-#pragma unroll
-        for (int e = 0; e < VE; ++e) top = max(top, __builtin_bit_cast(int, x[e]) & 0x7fffffff);
-        top = max_block(top, 32 / VE);
-        scale_of((top >> 23) - 127, (top & 0x7fffff) > 0x600000, top < 0x7f800000);
-        float y[VE];
-#pragma unroll
-        for (int e = 0; e < VE; ++e) y[e] = __builtin_ldexpf(x[e], 127 - byte);
-        encode(y);
-    }
-    __device__ __forceinline__ explicit Fp4Block(const double (&x)[VE]) {
-        int top = 0, upper[VE];
-#pragma unroll
-        for (int e = 0; e < VE; ++e) {
-            const uint64_t bits = __builtin_bit_cast(uint64_t, x[e]);
-            upper[e] = (int)(bits >> 32) | ((uint32_t)bits != 0);
-            top = max(top, upper[e] & 0x7fffffff);
-        }
-        top = max_block(top, 32 / VE);
-        scale_of((top >> 20) - 1023, (top & 0xfffff) > 0xc0000, top < 0x7ff00000);
-        float y[VE];
-#pragma unroll
-        for (int e = 0; e < VE; ++e) y[e] = (float)__builtin_ldexp(__builtin_bit_cast(double, (uint64_t)(uint32_t)upper[e] << 32), 127 - byte);
-        encode(y);
-    }
-    // e0: the lane's first element
-    __device__ __forceinline__ void store(char *row, unsigned char *scale, int e0) const {
-        if constexpr (VE == 8) *reinterpret_cast<uint32_t *>(row) = codes;
-        else *reinterpret_cast<uint16_t *>(row) = (uint16_t)codes;
-        if (e0 % 32 == 0) *scale = (unsigned char)byte;
-    }
-};
-template <int LANES> __device__ __forceinline__ double row_sum(double x) {
-#pragma unroll
-    for (int d = 1; d < LANES; d <<= 1) x += __shfl_xor(x, d, 64);
-    return x;
-}
-// A key's elements, normed, weighted and turned, in 64 bits
-template <typename T, int K, int ROT>
-__device__ __forceinline__ void key64(const HeadsArgs &a, const Turn<T, K, ROT> &turn, const Weights<T, K, ROT> &w, const u32x4 &raw,
-                                      const float (&x)[HeadRow<T, K>::VE], const float (&c)[HeadRow<T, K>::VE], const float (&s)[HeadRow<T, K>::VE], bool off_table,
-                                      double (&z)[HeadRow<T, K>::VE]) {
-    constexpr int VE = HeadRow<T, K>::VE;
-    double r = 1.0;
-    if (a.norm != 0) {
-        double ss = 0.0;
-#pragma unroll
-        for (int e = 0; e < VE; ++e) ss = __builtin_fma((double)x[e], (double)x[e], ss);
-        const double d = __builtin_fma(row_sum<HeadRow<T, K>::LANES>(ss), (double)a.mean, (double)a.eps);
-        r = __builtin_amdgcn_rsq(d);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) r = __builtin_fma(r * 0.5, __builtin_fma(-d * r, r, 1.0), r);
-        if (d == __builtin_inf()) r = 0.0;
-    }
-    if (off_table) r = __builtin_nan("");
-#pragma unroll
-    for (int e = 0; e < VE; ++e) z[e] = (double)x[e] * (r * (double)w.own[1][e]);
-    if constexpr (ROT != ROT_NONE) {
-        float y[VE];
-        turn.partners(raw, y);
-#pragma unroll
-        for (int e = 0; e < VE; ++e) z[e] = __builtin_fma(z[e], (double)c[e], (double)y[e] * (r * (double)w.partner[1][e]) * (double)s[e]);
-    }
-}
 
 // One use of each 64 bytes of the arguments, so that their loads are on their way at once (a token appended 3.79 us, so 3.58; 512 6.16, so 5.83)
 template <bool APPEND> __device__ __forceinline__ void ask_arguments(const HeadsArgs &a) {
@@ -251,9 +24,9 @@ template <bool APPEND> __device__ __forceinline__ void ask_arguments(const Heads
 }
 
 // A wavefront walks (token, part of its blocks of rows) pairs in steps of the grid; it has the loads of NB blocks in flight at a time.
-// APPEND: keys go to the cache, values follow them unchanged; MX: a cache in 4 bits, for which keys are computed in 64 bits (below).  AHEAD: the next blocks are asked for before these are written, as a wait for loads is one
+// APPEND: keys go to the cache, values follow them unchanged.  AHEAD: the next blocks are asked for before these are written, as a wait for loads is one
 // for the writes before them too (rule and figures: heads_ahead).
-template <typename T, int K, bool VEC, int ROT, bool APPEND, bool AHEAD, bool MX = false>
+template <typename T, int K, bool VEC, int ROT, bool APPEND, bool AHEAD>
 __global__ __launch_bounds__(HEADS_T) void heads_fwd_kernel(HeadsArgs a) {
     using HR = HeadRow<T, K>;
     constexpr int VE = HR::VE, ROWS = HR::ROWS, NB = 2;
@@ -273,21 +46,15 @@ __global__ __launch_bounds__(HEADS_T) void heads_fwd_kernel(HeadsArgs a) {
         const bool off_table = ROT && pos >= a.rotary_rows;
         float c[VE], s[VE];
         if constexpr (ROT != ROT_NONE) turn.load(a.rotary + (size_t)(none || off_table ? 0 : pos) * a.rotary_dim, a.rotary_dim, c, s);
-        using At = std::conditional_t<MX, char, T>;             // (rows in 4 bits: steps in bytes)
-        At *page_k = nullptr, *page_v = nullptr;
-        unsigned char *scale_k = nullptr, *scale_v = nullptr;
+        T *page_k = nullptr, *page_v = nullptr;
         if constexpr (APPEND) {
             const int seq = a.seq ? a.seq[token] : b, col = pos >> a.page_shift;
             if (!none && (unsigned)seq < (unsigned)a.n_seqs && col < a.max_pages) {
                 const int page = a.table[seq * a.table_stride + col];
                 const int slot = pos & ((1 << a.page_shift) - 1);
                 if ((unsigned)page < (unsigned)a.n_pages) {
-                    page_k = static_cast<At *>(a.cache_k.data) + page * a.cache_k.batch + slot * a.cache_k.token;
-                    page_v = static_cast<At *>(a.cache_v.data) + page * a.cache_v.batch + slot * a.cache_v.token;
-                    if constexpr (MX) {
-                        scale_k = static_cast<unsigned char *>(a.scale_k.data) + page * a.scale_k.batch + slot * a.scale_k.token + e0 / 32;
-                        scale_v = static_cast<unsigned char *>(a.scale_v.data) + page * a.scale_v.batch + slot * a.scale_v.token + e0 / 32;
-                    }
+                    page_k = static_cast<T *>(a.cache_k.data) + page * a.cache_k.batch + slot * a.cache_k.token;
+                    page_v = static_cast<T *>(a.cache_v.data) + page * a.cache_v.batch + slot * a.cache_v.token;
                 }
             }
         }
@@ -315,28 +82,12 @@ __global__ __launch_bounds__(HEADS_T) void heads_fwd_kernel(HeadsArgs a) {
                 const int h = (blk - (kind == 0 ? 0 : kind == 1 ? a.q_blocks : a.q_blocks + a.k_blocks)) * ROWS + sub;
                 if (blk >= blk_end) break;
                 const bool live = h < (kind == 0 ? a.Hq : a.Hk);
-                if constexpr (APPEND && !MX) {
-                    if (kind == 2) {
-                        if (live && page_v) *reinterpret_cast<u32x4 *>(page_v + h * a.cache_v.head + e0) = raw[i];
-                        continue;
-                    }
+                if (APPEND && kind == 2) {
+                    if (live && page_v) *reinterpret_cast<u32x4 *>(page_v + h * a.cache_v.head + e0) = raw[i];
+                    continue;
                 }
                 float x[VE], z[VE];
                 unpack<T>(raw[i], x);
-                if constexpr (MX) {                     // (every lane of a block takes part)
-                    if (kind == 2) {
-                        const Fp4Block<VE> v(x);
-                        if (live && page_v) v.store(page_v + h * a.cache_v.head + e0 / 2, scale_v + h * a.scale_v.head, e0);
-                        continue;
-                    }
-                    if (kind == 1) {
-                        double y[VE];
-                        key64<T, K, ROT>(a, turn, w, raw[i], x, c, s, off_table, y);
-                        const Fp4Block<VE> k(y);
-                        if (live && page_k) k.store(page_k + h * a.cache_k.head + e0 / 2, scale_k + h * a.scale_k.head, e0);
-                        continue;
-                    }
-                }
                 float r = 1.f;
                 if (a.norm != 0) {
                     float ss = 0.f;
@@ -363,13 +114,11 @@ __global__ __launch_bounds__(HEADS_T) void heads_fwd_kernel(HeadsArgs a) {
 #pragma unroll
                     for (int e = 0; e < VE; ++e) z[e] = 0.f;
                 }
-                if constexpr (APPEND && !MX) {
-                    if (kind == 1) {
-                        if (page_k) store_vec_t(page_k + h * a.cache_k.head + e0, z);
-                        continue;
-                    }
+                if (APPEND && kind == 1) {
+                    if (page_k) store_vec_t(page_k + h * a.cache_k.head + e0, z);
+                } else {
+                    store_row<T, VEC, VE>(row_at<T, VEC>(kind == 0 ? a.q_out : a.k_out, b, t, h) + e0, z);
                 }
-                store_row<T, VEC, VE>(row_at<T, VEC>(kind == 0 ? a.q_out : a.k_out, b, t, h) + e0, z);
             }
         }
     }
@@ -504,43 +253,6 @@ __global__ __launch_bounds__(DW_T) void heads_dw_kernel(const float *partial, in
     if (lane < DW_COLS && dst) dst[c < K ? c : c - K] = v;
 }
 
-// Rows of a 4-bit cache as values: a wavefront takes blocks of rows (64 lanes of 8 elements) of a token
-template <typename T, int K, bool VEC> __global__ __launch_bounds__(HEADS_T) void read_mx_kernel(HeadsArgs a) {
-    constexpr int VE = 8, LANES = K / VE, ROWS = 64 / LANES, PER = 16 / sizeof(T);
-    const int lane = threadIdx.x & 63, sub = lane / LANES, e0 = lane % LANES * VE;
-    const unsigned items = (unsigned)a.tokens * (unsigned)a.parts, stride = gridDim.x * (HEADS_T / 64);
-    for (unsigned item = __builtin_amdgcn_readfirstlane(blockIdx.x * (HEADS_T / 64) + (threadIdx.x >> 6)); item < items; item += stride) {
-        const unsigned token = item / (unsigned)a.parts;
-        const int part = item % (unsigned)a.parts, b = token / (unsigned)a.T, t = token % (unsigned)a.T;
-        const int pos = a.positions[token], seq = a.seq ? a.seq[token] : b, col = max(pos, 0) >> a.page_shift, slot = pos & ((1 << a.page_shift) - 1);
-        int page = -1;
-        if (pos >= 0 && (unsigned)seq < (unsigned)a.n_seqs && col < a.max_pages) page = a.table[seq * a.table_stride + col];
-        const bool there = (unsigned)page < (unsigned)a.n_pages;
-        for (int blk = part * a.per_part; blk < min(a.blocks, (part + 1) * a.per_part); ++blk) {
-            const bool value = blk >= a.k_blocks;
-            const int h = (value ? blk - a.k_blocks : blk) * ROWS + sub;
-            if (h >= a.Hk) continue;
-            const HeadRows &row = value ? a.cache_v : a.cache_k, &scale = value ? a.scale_v : a.scale_k, &out = value ? a.v : a.k_out;
-            float x[VE];
-            if (there) {
-                const uint32_t codes = *reinterpret_cast<const uint32_t *>(static_cast<const char *>(row.data) + page * row.batch + slot * row.token + h * row.head + e0 / 2);
-                fp4_values(codes, fp4_scale(*(static_cast<const unsigned char *>(scale.data) + page * scale.batch + slot * scale.token + h * scale.head + e0 / 32)), x);
-            } else {
-#pragma unroll
-                for (int e = 0; e < VE; ++e) x[e] = pos < 0 ? 0.f : __builtin_nanf("");
-            }
-            T *to = row_at<T, VEC>(out, b, t, h) + e0;
-#pragma unroll
-            for (int v = 0; v < VE / PER; ++v) {
-                float y[PER];
-#pragma unroll
-                for (int e = 0; e < PER; ++e) y[e] = x[v * PER + e];
-                store_row<T, VEC, PER>(to + v * PER, y);
-            }
-        }
-    }
-}
-
 namespace {
 template <typename T, int K> int cut(HeadsArgs &a, bool backward) {
     const HeadsPlan h = heads_plan(a.tokens, a.Hq, a.Hk, K, sizeof(T) == 2, a.append, backward);
@@ -550,7 +262,6 @@ template <typename T, int K> int cut(HeadsArgs &a, bool backward) {
 template <typename T, int K, bool VEC, int ROT> void fwd_of(HeadsArgs a, hipStream_t st) {
     const dim3 g((unsigned)cut<T, K>(a, false)), t(HEADS_T);
     if (!a.append) hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, false, false>), g, t, 0, st, a);
-    else if (a.mx) hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, true, false, true>), g, t, 0, st, a);
     else if (VEC && heads_ahead(a.tokens, a.blocks)) hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, true, VEC>), g, t, 0, st, a);
     else hipLaunchKernelGGL((heads_fwd_kernel<T, K, VEC, ROT, true, false>), g, t, 0, st, a);
 }
@@ -579,29 +290,6 @@ template <typename T> int by_width(const HeadsArgs &a, bool backward, hipStream_
 }
 }  // namespace
 
-namespace {
-template <typename T> int read_of(HeadsArgs a, hipStream_t st) {
-    const int rows = 64 * 8 / a.K;
-    a.k_blocks = (a.Hk + rows - 1) / rows;
-    a.blocks = 2 * a.k_blocks;
-    a.per_part = heads_blocks_per_wave(a.tokens, a.blocks);
-    a.parts = (a.blocks + a.per_part - 1) / a.per_part;
-    const dim3 g((unsigned)heads_fwd_workgroups((long long)a.tokens * a.parts)), t(HEADS_T);
-    auto go = [&](auto k) {
-        if (a.aligned) hipLaunchKernelGGL((read_mx_kernel<T, decltype(k)::value, true>), g, t, 0, st, a);
-        else hipLaunchKernelGGL((read_mx_kernel<T, decltype(k)::value, false>), g, t, 0, st, a);
-        return 0;
-    };
-    switch (a.K) {
-        case 64: return go(std::integral_constant<int, 64>{});
-        case 128: return go(std::integral_constant<int, 128>{});
-        case 256: return go(std::integral_constant<int, 256>{});
-        default: return -1;
-    }
-}
-}  // namespace
-
-int launch_read_mx(const HeadsArgs &a, bool bf16_io, hipStream_t st) { return bf16_io ? read_of<bf16>(a, st) : read_of<float>(a, st); }
 int launch_heads_fwd(const HeadsArgs &a, bool bf16_io, hipStream_t st) { return bf16_io ? by_width<bf16>(a, false, st) : by_width<float>(a, false, st); }
 int launch_heads_bwd(const HeadsArgs &a, bool bf16_io, hipStream_t st) { return bf16_io ? by_width<bf16>(a, true, st) : by_width<float>(a, true, st); }
 

@@ -254,8 +254,8 @@ struct HeadsArgs {
     const float *rotary;                  // [rotary_rows, rotary_dim] or null
     const int *positions;                 // [tokens] or null (a token's place in its batch entry)
     // append
-    bool append, mx;                      // mx: a cache in 4 bits, its steps in bytes
-    HeadRows cache_k, cache_v, scale_k, scale_v;
+    bool append;
+    HeadRows cache_k, cache_v;
     const int *table, *seq;               // [n_seqs, max_pages], [tokens] or null (the batch entry)
     long long table_stride;
     int n_pages, page_shift, n_seqs, max_pages;
@@ -263,10 +263,13 @@ struct HeadsArgs {
     HeadRows dq_out, dk_out, dq, dk;
     float *dweight_q, *dweight_k;         // [K] or null
     float *partial;                       // [workgroups][2][K], null without weights
+    HeadRows scale_k, scale_v;            // a cache in 4 bits, its steps in bytes
 };
 int launch_heads_fwd(const HeadsArgs &a, bool bf16_io, hipStream_t st);
 int launch_heads_bwd(const HeadsArgs &a, bool bf16_io, hipStream_t st);
-int launch_read_mx(const HeadsArgs &a, bool bf16_io, hipStream_t st);      // rows of a 4-bit cache to k_out and v
+// ... to a cache in 4 bits, and its rows to k_out and v (osdn_heads_mx.hip)
+int launch_append_mx(const HeadsArgs &a, bool bf16_io, hipStream_t st);
+int launch_read_mx(const HeadsArgs &a, bool bf16_io, hipStream_t st);
 
 // Attention of one token per sequence over a paged cache (osdn_paged.hip)
 struct DecodeArgs {

@@ -265,6 +265,11 @@ inline int heads_blocks_per_wave(long long tokens, int blocks) {
 inline bool heads_ahead(long long tokens, int blocks) { return tokens * blocks >= 256 * NUM_CU; }
 // Workgroups (four wavefronts) for so many (token, part) pairs: 65536 tokens appended with up to 2048, 4096 and 16384 of them 175, 168 and 163 us
 inline int heads_fwd_workgroups(long long items) { return (int)(items < 4 * 16384 ? (items + 3) / 4 : 16384); }
+// Heads that a wavefront of append_mx_kernel (read_mx_kernel) takes of its tokens, of which there are `groups`: all where every CU then has sixteen wavefronts
+inline int heads_mx_per_wave(long long groups, int heads) {
+    const long long per = groups * heads / (16 * NUM_CU);
+    return (int)(per < 1 ? 1 : per > heads ? heads : per);
+}
 // ... of heads_bwd_kernel, each with a row of partial sums: 2 x 8192 x (32 + 8) heads with 1024 and 2048 178 and 179 us (both passes), 4 x 2048 x (16 + 4) of 64 33 and 36
 constexpr int HEADS_BWD_WGS = 1024;
 inline int heads_bwd_workgroups(long long items) { return (int)(items < 4 * HEADS_BWD_WGS ? (items + 3) / 4 : HEADS_BWD_WGS); }
