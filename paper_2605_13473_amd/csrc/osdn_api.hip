@@ -787,7 +787,8 @@ static int check_choice(const osdn_select_params *p, int page_size, long long &s
 }
 size_t osdn_page_select_workspace_bytes(const osdn_select_params *p, int32_t page_size) {
     long long seen = 0;
-    return check_choice(p, page_size, seen) != OSDN_OK || seen <= p->pages ? 0 : (size_t)p->B * p->Hk * seen * sizeof(unsigned long long);
+    if (check_choice(p, page_size, seen) != OSDN_OK || seen <= p->pages || select_scores_itself((long long)p->B * p->Hk, (int)seen, 2 * p->K * (p->io_dtype == OSDN_BF16 ? 2 : 4))) return 0;
+    return (size_t)p->B * p->Hk * seen * sizeof(unsigned long long);
 }
 int osdn_page_select(const osdn_select_params *p, const osdn_pages *pages, const osdn_rows *q, const void *bounds, const int32_t *lengths,
                      const int32_t *seq, int32_t *chosen, int32_t *tokens, void *workspace, size_t workspace_bytes, void *stream) {
@@ -798,8 +799,8 @@ int osdn_page_select(const osdn_select_params *p, const osdn_pages *pages, const
     if ((rc = check_choice(p, pages->page_size, seen)) != OSDN_OK) return rc;
     if (!bounds || !lengths || !chosen || !tokens) return OSDN_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(bounds) % 16 != 0) return OSDN_ERR_SHAPE;
-    bool aligned = true;
-    if ((rc = take_rows(q, p->B, 1, p->Hq, p->K, p->io_dtype == OSDN_BF16 ? 2 : 4, false, a.q, aligned)) != OSDN_OK) return rc;
+    a.aligned = true;
+    if ((rc = take_rows(q, p->B, 1, p->Hq, p->K, p->io_dtype == OSDN_BF16 ? 2 : 4, false, a.q, a.aligned)) != OSDN_OK) return rc;
     const size_t bytes = osdn_page_select_workspace_bytes(p, pages->page_size);
     if (bytes) {
         if ((rc = check_ws(workspace, workspace_bytes, bytes)) != OSDN_OK) return rc;

@@ -2,7 +2,8 @@
 //
 // A wavefront takes 64 / LANES tokens next to each other, the lanes of a row one of them each, and walks the heads of their queries, keys and values: what does not depend on the head
 // (position, page, angles, the rows' addresses) is found once for all of them, and the codes of adjacent tokens, which a cache that holds a page head
-// after head has side by side, leave together.
+// after head has side by side, leave together.  Bound by memory: 65536 tokens of 16 + 4 + 4 heads of 128 in bf16 appended 154 us, 4.6 TB/s (a token a wavefront 205: 80 MB more are written,
+// as rows of 64 and 4 bytes leave one by one), and read back 29 us, 5.9 TB/s (43).
 #include "osdn_heads.h"
 
 namespace osdn {
@@ -10,8 +11,8 @@ namespace osdn {
 // A block of 32 elements, VE of them a lane, becomes codes and a scale 2^e, e the least (from -120 to 125) with the largest element no more than 7 * 2^e: what lies
 // between 6 and 7 is off by no more than what lies between 4 and 6 may be.  The codes are the nearest values, ties to the even code.
 // Which code that is must not hang on a rounding before.  Values come as they are.  Keys are computed in fp32 with a bound of their error, and where an element with
-// its error either way could get another code or its block another scale, which one block of rows in hundreds has, once more in 64 bits.  (All of them in 64 bits: 65536 tokens
-// of 16 + 4 + 4 heads of 128 in bf16 293 us, so TODO.)
+// its error either way could get another code or its block another scale, which one block of rows in hundreds has, once more in 64 bits.  (All of them in 64 bits,
+// a wavefront a token: 65536 tokens of 16 + 4 + 4 heads of 128 in bf16 293 us, so 201.)
 __device__ __forceinline__ int max_block(int x, int lanes) {
     auto with = [&](int y) { x = max(x, y); };
     with(__builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, true));         // quad_perm [1,0,3,2]
@@ -155,7 +156,7 @@ __device__ __forceinline__ bool row_ready(const HeadsArgs &a, const Turn<T, K, R
 
 template <typename T, int K, bool VEC, int ROT> __global__ __launch_bounds__(HEADS_T) void append_mx_kernel(HeadsArgs a) {
     using HR = HeadRow<T, K>;
-    constexpr int VE = HR::VE, ROWS = HR::ROWS, NB = 2;
+    constexpr int VE = HR::VE, ROWS = HR::ROWS, NB = sizeof(T) == 2 ? 4 : 2;
     const int lane = threadIdx.x & 63, sub = lane / HR::LANES, e0 = (lane % HR::LANES) * VE;
     const Turn<T, K, ROT> turn(a.rotary_dim, lane);
     const unsigned groups = ((unsigned)a.tokens + ROWS - 1) / ROWS, items = groups * (unsigned)a.parts, stride = gridDim.x * (HEADS_T / 64);
@@ -166,7 +167,8 @@ template <typename T, int K, bool VEC, int ROT> __global__ __launch_bounds__(HEA
         const unsigned token = live ? group * ROWS + sub : (unsigned)a.tokens - 1, b = token / (unsigned)a.T, t = token - b * (unsigned)a.T;
         const int pos = a.positions[token], seq = a.seq ? a.seq[token] : (int)b;
         const bool none = pos < 0, off_table = ROT && pos >= a.rotary_rows;
-        // the rows of heads [h0, h1) of this lane's token, two at a time, the next two asked for before these are made ready
+        // the rows of heads [h0, h1) of this lane's token, NB at a time, the next ones asked for before these are made ready (65536 tokens of 16 + 4 + 4, NB = 1, 2 and 4 164, 161 and
+        // 154 us; fp32, 8192 of 16 + 8 + 8, 45, 47, 51)
         auto rows = [&](const HeadRows &src, int h0, int h1, auto &&each) {
             if (h0 >= h1) return;
             const T *from = row_at<const T, VEC>(src, b, t, 0) + e0;

@@ -324,6 +324,7 @@ int launch_bounds(const BoundsArgs &a, bool bf16_io, bool mx, hipStream_t st);
 struct SelectArgs {
     int B, Hk, K, group, max_length, pages, first, last, max_pages_seen;
     HeadRows q;
+    bool aligned;                         // every row of q starts on 16 bytes
     const void *bounds;                   // [n_pages, Hk, 2, K] io
     const int *table, *seq, *lengths;
     long long table_stride;

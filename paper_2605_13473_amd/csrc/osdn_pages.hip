@@ -277,7 +277,7 @@ __device__ __forceinline__ float greatest(float x, float y) { return __builtin_e
 // A wavefront takes one page that got new tokens, for one head: its new rows, 64 / LANES at a time, and, where it had tokens before, its bounds.
 template <typename T, int K, bool MX> __global__ __launch_bounds__(256) void bounds_kernel(BoundsArgs a) {
     using R = KeyRow<T, K, MX>;
-    constexpr int VE = R::VE, ROWS = 64 / R::LANES;
+    constexpr int VE = R::VE, ROWS = 64 / R::LANES, PER = 16 / sizeof(T);
     const int lane = threadIdx.x & 63, sub = lane / R::LANES, e0 = lane % R::LANES * VE;
     const long long item = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = (int)(item % a.Hk);
@@ -297,8 +297,16 @@ template <typename T, int K, bool MX> __global__ __launch_bounds__(256) void bou
 #pragma unroll
     for (int e = 0; e < VE; ++e) { lo[e] = INFINITY; hi[e] = -INFINITY; }
     if (s0 > 0) {                       // (tokens from before)
+        auto old = [&](const T *at, float (&x)[VE]) {
 #pragma unroll
-        for (int e = 0; e < VE; ++e) { lo[e] = to_f32(out[e]); hi[e] = to_f32(out[K + e]); }
+            for (int v = 0; v < VE / PER; ++v) {
+                const u32x4 raw = *reinterpret_cast<const u32x4 *>(at + v * PER);
+#pragma unroll
+                for (int e = 0; e < PER; ++e) x[v * PER + e] = vec_get<T>(raw, e);
+            }
+        };
+        old(out, lo);
+        old(out + K, hi);
     }
     for (int s = s0 + sub; s < s1; s += ROWS) {
         float x[VE];
@@ -311,8 +319,17 @@ template <typename T, int K, bool MX> __global__ __launch_bounds__(256) void bou
 #pragma unroll
         for (int e = 0; e < VE; ++e) { lo[e] = least(lo[e], __shfl_xor(lo[e], d, 64)); hi[e] = greatest(hi[e], __shfl_xor(hi[e], d, 64)); }
     if (sub == 0) {
+        auto leave = [&](T *at, const float (&x)[VE]) {
 #pragma unroll
-        for (int e = 0; e < VE; ++e) { out[e] = from_f32<T>(lo[e]); out[K + e] = from_f32<T>(hi[e]); }
+            for (int v = 0; v < VE / PER; ++v) {
+                float y[PER];
+#pragma unroll
+                for (int e = 0; e < PER; ++e) y[e] = x[v * PER + e];
+                store_vec_t(at + v * PER, y);
+            }
+        };
+        leave(out, lo);
+        leave(out + K, hi);
     }
 }
 
@@ -325,80 +342,283 @@ __device__ __forceinline__ unsigned long long score_key(double s) {
     return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-// The first lanes of a row of 2 K bounds hold the smallest, the rest the largest; a lane holds VPL vectors of VE.  A wavefront takes `HEADS` key heads next to
-// each other and walks pages in steps.
-template <typename T, int K> struct ScoreRow {
-    static constexpr int VE = 16 / sizeof(T), ALL = 2 * K / VE, LANES = ALL < 64 ? ALL : 64, VPL = ALL / LANES, HEADS = 64 / LANES;
-};
-__device__ __forceinline__ double lane_sum(double x, int lanes) {
-    for (int d = 1; d < lanes; d <<= 1) x += __shfl_xor(x, d, 64);
+template <int CTRL> __device__ __forceinline__ int moved(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, true); }
+template <int CTRL> __device__ __forceinline__ double moved(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, (uint64_t)(uint32_t)moved<CTRL>((int)(u >> 32)) << 32 | (uint32_t)moved<CTRL>((int)(uint32_t)u));
+}
+// x and that of the lane 16 (32) away, added
+template <int AWAY> __device__ __forceinline__ double with_lanes_away(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    uint32_t a = (uint32_t)u, b = (uint32_t)(u >> 32), c = a, d = b;
+    if constexpr (AWAY == 16) asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1\n\tv_permlane16_swap_b32 %2, %3" : "+v"(a), "+v"(c), "+v"(b), "+v"(d));
+    else asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\tv_permlane32_swap_b32 %2, %3" : "+v"(a), "+v"(c), "+v"(b), "+v"(d));
+    return __builtin_bit_cast(double, (uint64_t)b << 32 | a) + __builtin_bit_cast(double, (uint64_t)d << 32 | c);
+}
+// Sums over the lanes up to this one; the largest of all lanes (in lane 63)
+__device__ __forceinline__ unsigned sum_upto(unsigned x) {
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true);       // row_shr:1, 2, 4, 8
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true);
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true);
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true);
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);      // row_bcast:15 into rows 1 and 3
+    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);      // row_bcast:31 into rows 2 and 3
     return x;
 }
+__device__ __forceinline__ unsigned largest_upto(unsigned x) {
+    auto with = [&](int y) { x = max(x, (unsigned)y); };
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));
+    return x;
+}
+
+// The bounds of a page and head are a row of 2 K elements, the smallest first: 16 bytes a lane, VPL of them, in LANES lanes; a wavefront has ROWS of them side by side.
+template <typename T, int K> struct ScoreRow {
+    static constexpr int VE = 16 / sizeof(T), ALL = 2 * K / VE, LANES = ALL < 64 ? ALL : 64, VPL = ALL / LANES, ROWS = 64 / LANES;
+    double w[VPL][VE];          // what a lane's elements are multiplied by: sums of the negative (smallest) or positive (largest) parts of the queries
+    __device__ __forceinline__ void weights(const SelectArgs &a, int b, int h, int lane) {
+#pragma unroll
+        for (int v = 0; v < VPL; ++v)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) w[v][e] = 0.0;
+        for (int i0 = 0; i0 < a.group; i0 += 4) {               // (four heads on their way together)
+            u32x4 raw[4][VPL];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const T *q = static_cast<const T *>(a.q.data) + b * a.q.batch + (long long)(h * a.group + min(i0 + i, a.group - 1)) * a.q.head;
+#pragma unroll
+                for (int v = 0; v < VPL; ++v) {
+                    const T *at = q + (lane % LANES + v * LANES) * VE % K;
+                    if (a.aligned) {
+                        raw[i][v] = *reinterpret_cast<const u32x4 *>(at);
+                    } else {
+                        T x[VE];
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) x[e] = at[e];
+                        raw[i][v] = __builtin_bit_cast(u32x4, x);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i0 + i < a.group) {
+#pragma unroll
+                    for (int v = 0; v < VPL; ++v) {
+                        const bool low = (lane % LANES + v * LANES) * VE < K;
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) {
+                            const float x = vec_get<T>(raw[i][v], e);
+                            w[v][e] += (double)(low ? least(x, 0.f) : greatest(x, 0.f));
+                        }
+                    }
+                }
+        }
+    }
+    static __device__ __forceinline__ void ask(const SelectArgs &a, long long page, int h, int lane, u32x4 (&raw)[VPL]) {
+        const T *from = static_cast<const T *>(a.bounds) + (page * a.Hk + h) * 2 * K + lane % LANES * VE;
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) raw[v] = *reinterpret_cast<const u32x4 *>(from + v * LANES * VE);
+    }
+    // the score, in every lane of the row
+    __device__ __forceinline__ double score(const u32x4 (&raw)[VPL]) const {
+        double s = 0.0;
+#pragma unroll
+        for (int v = 0; v < VPL; ++v)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) s = __builtin_fma(w[v][e], (double)vec_get<T>(raw[v], e), s);
+        s += moved<0xB1>(s);                    // quad_perm [1,0,3,2]
+        s += moved<0x4E>(s);                    // quad_perm [2,3,0,1]
+        s += moved<0x141>(s);                   // row_half_mirror
+        s += moved<0x140>(s);                   // row_mirror (a row has 16 lanes at least)
+        if constexpr (LANES > 16) s = with_lanes_away<16>(s);
+        if constexpr (LANES > 32) s = with_lanes_away<32>(s);
+        return s;
+    }
+};
 __device__ __forceinline__ Seen pages_seen(const SelectArgs &a, int b) {
     return seen_tokens(a.lengths[b], a.seq ? a.seq[b] : b, a.n_seqs, a.max_length, 0, a.page_shift, a.max_pages);
 }
+__device__ __forceinline__ int pages_of(const SelectArgs &a, const Seen &see) { return (see.end + (1 << a.page_shift) - 1) >> a.page_shift; }
 
-template <typename T, int K> __global__ __launch_bounds__(256) void score_kernel(SelectArgs a) {
+// Keys of the pages p0 + l (l < 4 ROWS or, HEADS: 4) + stride i of a table's row, below p1, for one head (lanes of a wavefront: ROWS pages next to each other) or, HEADS, for ROWS heads next
+// to each other.  The numbers of the pages of 16 steps (64 / (4 ROWS) if that is less) are on their way at once, the bounds of a step while those of the one before are summed.
+template <typename T, int K, bool HEADS> struct PageSteps {
+    static constexpr int SIDE = HEADS ? 1 : ScoreRow<T, K>::ROWS, STEP = 4 * SIDE, STEPS = 64 / STEP;
+    // the lane STEP i + l: page l of step i from p on (what stands behind the last page is looked at, and left out in the end)
+    static __device__ __forceinline__ int ask(const SelectArgs &a, const int *table, int p, int stride, int lane) {
+        return table[min((long long)p + (long long)(lane / STEP) * stride + lane % STEP, (long long)a.max_pages - 1)];
+    }
+};
+template <typename T, int K, bool HEADS, typename F>
+__device__ __forceinline__ void score_pages(const SelectArgs &a, const ScoreRow<T, K> &r, const int *table, int h, int own, int p0, int p1, int stride, int lane, F &&leave) {
     using R = ScoreRow<T, K>;
-    constexpr int VE = R::VE, VPL = R::VPL;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int b = blockIdx.y, h0 = (int)blockIdx.z * R::HEADS, h = h0 + lane / R::LANES;
-    const Seen see = pages_seen(a, b);
-    const int have = (see.end + (1 << a.page_shift) - 1) >> a.page_shift;
-    if (have <= a.pages) return;                        // (all of them are taken)
-    const int row = a.seq ? a.seq[b] : b, end = have - a.last;
-    const int stride = gridDim.x * 4, hh = min(h, a.Hk - 1);
-    // the weights of a lane's elements: sums of the negative (smallest) or positive (largest) parts of the queries
-    double w[VPL][VE];
+    using P = PageSteps<T, K, HEADS>;
+    constexpr int SIDE = P::SIDE, STEP = P::STEP, STEPS = P::STEPS;
+    const int sub = HEADS ? 0 : lane / R::LANES;
+    for (int p = p0; p < p1; p += STEPS * stride) {
+        if (p > p0) own = P::ask(a, table, p, stride, lane);
+        int page[4];
+        u32x4 raw[4][R::VPL];
+        auto ask = [&](int i) {
 #pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-        const int at = (lane % R::LANES + v * R::LANES) * VE;
-        const bool low = at < K;
+            for (int u = 0; u < 4; ++u) {
+                page[u] = __shfl(own, STEP * i + u * SIDE + sub, 64);
+                R::ask(a, (unsigned)page[u] < (unsigned)a.n_pages ? page[u] : 0, h, lane, raw[u]);
+            }
+        };
+        ask(0);
+        for (int i = 0; i < STEPS && p + i * stride < p1; ++i) {
+            u32x4 now[4][R::VPL];
+            bool there[4];
 #pragma unroll
-        for (int e = 0; e < VE; ++e) w[v][e] = 0.0;
-        for (int i = 0; i < a.group; ++i) {
-            const T *q = static_cast<const T *>(a.q.data) + b * a.q.batch + (long long)(hh * a.group + i) * a.q.head + at % K;
+            for (int u = 0; u < 4; ++u) {
+                there[u] = (unsigned)page[u] < (unsigned)a.n_pages;
 #pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                const float x = to_f32(q[e]);
-                w[v][e] += (double)(low ? __builtin_elementwise_minimum(x, 0.f) : __builtin_elementwise_maximum(x, 0.f));
+                for (int v = 0; v < R::VPL; ++v) now[u][v] = raw[u][v];
+            }
+            if (i + 1 < STEPS && p + (i + 1) * stride < p1) ask(i + 1);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const double s = r.score(now[u]);
+                const int at = p + i * stride + u * SIDE + sub;
+                if (at < p1) leave(at, there[u] ? score_key(s) : ~0ull);
             }
         }
     }
+}
+
+// Few rows of many pages: the keys by a launch of their own
+template <typename T, int K> __global__ __launch_bounds__(256) void score_kernel(SelectArgs a) {
+    using R = ScoreRow<T, K>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int b = blockIdx.y, h = (int)blockIdx.z * R::ROWS + lane / R::LANES, hh = min(h, a.Hk - 1), first = a.first + (int)(blockIdx.x * 4 + wave) * 4, stride = (int)gridDim.x * 16;
+    // (what does not hang on the length is asked for beside it)
+    const int row = a.seq ? a.seq[b] : b;
+    const int *table = a.table + ((unsigned)row < (unsigned)a.n_seqs ? (long long)row * a.table_stride : 0);
+    const int own = PageSteps<T, K, true>::ask(a, table, first, stride, lane);
+    R r;
+    r.weights(a, b, hh, lane);
+    const int have = pages_of(a, pages_seen(a, b));
+    if (have <= a.pages || first >= have - a.last) return;              // (all of them are taken)
     unsigned long long *keys = a.keys + ((long long)b * a.Hk + hh) * a.max_pages_seen;
-    const int *table = a.table + (long long)row * a.table_stride;
-    for (int p = a.first + blockIdx.x * 4 + wave; p < end; p += stride) {
-        const int page = table[p];
-        const bool there = (unsigned)page < (unsigned)a.n_pages;
-        const T *from = static_cast<const T *>(a.bounds) + ((long long)(there ? page : 0) * a.Hk + hh) * 2 * K + lane % R::LANES * VE;
-        double s = 0.0;
+    score_pages<T, K, true>(a, r, table, hh, own, first, have - a.last, stride, lane, [&](int p, unsigned long long key) {
+        if (lane % R::LANES == 0 && h < a.Hk) keys[p] = key;
+    });
+}
+
+constexpr int SEL_T = 512, SEL_W = SEL_T / 64, SEL_BINS = 2048, SEL_RUN = SEL_BINS / SEL_T, SEL_LIST = 64;
+// The n-th largest of a workgroup's keys, `need` of count: after it, taken are the keys above hi and the first `need` of those in [lo, hi].  The keys between the bounds known so far are
+// counted in 2048 even bins, the bin that holds it gives the next bounds, until all of a bin is taken, it is one key wide, or few enough are in it to be compared
+// with each other.  `each` calls its argument with every key of the thread.
+struct Cut { unsigned long long lo, hi; unsigned need; };
+struct CutSpace {
+    unsigned bins[SEL_BINS], part[SEL_W], found[3], listed;
+    unsigned edge[SEL_W][2];
+    unsigned long long list[SEL_LIST];
+};
+template <typename F> __device__ __forceinline__ Cut cut_keys(CutSpace &c, unsigned need, int lane, int wave, F &&each) {
+    unsigned least = 0, most = 0;               // of the upper words: the range starts at the least of them (kept as its complement) and ends with the largest
+    each([&](unsigned long long k) {
+        least = max(least, ~(unsigned)(k >> 32));
+        most = max(most, (unsigned)(k >> 32));
+    });
+    least = largest_upto(least);
+    most = largest_upto(most);
+    if (lane == 63) { c.edge[wave][0] = least; c.edge[wave][1] = most; }
+    for (int i = threadIdx.x; i < SEL_BINS; i += SEL_T) c.bins[i] = 0;
+    __syncthreads();
 #pragma unroll
-        for (int v = 0; v < VPL; ++v) {
-            const u32x4 raw = *reinterpret_cast<const u32x4 *>(from + v * R::LANES * VE);
+    for (int w = 0; w < SEL_W; ++w) {
+        least = max(least, c.edge[w][0]);
+        most = max(most, c.edge[w][1]);
+    }
+    least = __builtin_amdgcn_readfirstlane(least);
+    most = __builtin_amdgcn_readfirstlane(most);
+    unsigned long long lo = (unsigned long long)~least << 32, hi = (unsigned long long)most << 32 | 0xffffffffu;
+    for (;;) {
+        const unsigned long long width = hi - lo;
+        const int top = width ? 63 - __builtin_clzll(width) : 0, shift = top > 10 ? top - 10 : 0;
+        each([&](unsigned long long k) {
+            if (k >= lo && k <= hi) atomicAdd(&c.bins[(k - lo) >> shift], 1u);
+        });
+        if (threadIdx.x == 0) c.listed = 0;
+        __syncthreads();
+        // bins from the top, a run of them a thread
+        unsigned here[SEL_RUN], all = 0;
 #pragma unroll
-            for (int e = 0; e < VE; ++e) s = __builtin_fma(w[v][e], (double)vec_get<T>(raw, e), s);
+        for (int i = 0; i < SEL_RUN; ++i) {
+            here[i] = c.bins[SEL_BINS - 1 - (SEL_RUN * threadIdx.x + i)];
+            c.bins[SEL_BINS - 1 - (SEL_RUN * threadIdx.x + i)] = 0;
+            all += here[i];
         }
-        s = lane_sum(s, R::LANES);
-        if (lane % R::LANES == 0 && h < a.Hk) keys[p] = there ? score_key(s) : ~0ull;
+        const unsigned upto = sum_upto(all);
+        if (lane == 63) c.part[wave] = upto;
+        __syncthreads();
+        unsigned above = upto - all;
+#pragma unroll
+        for (int w = 0; w < SEL_W; ++w) above += w < wave ? c.part[w] : 0u;
+#pragma unroll
+        for (int i = 0; i < SEL_RUN; ++i) {
+            if (above < need && above + here[i] >= need) {
+                c.found[0] = SEL_BINS - 1 - (SEL_RUN * threadIdx.x + i); c.found[1] = need - above; c.found[2] = here[i];
+            }
+            above += here[i];
+        }
+        __syncthreads();
+        need = c.found[1];
+        const unsigned inside = c.found[2];
+        lo += (unsigned long long)c.found[0] << shift;
+        const unsigned long long far = lo + ((1ull << shift) - 1);
+        hi = far < hi && far >= lo ? far : hi;
+        if (inside == need || shift == 0) return {lo, hi, need};
+        if (inside <= SEL_LIST) {
+            each([&](unsigned long long k) {
+                if (k >= lo && k <= hi) c.list[atomicAdd(&c.listed, 1u)] = k;
+            });
+            __syncthreads();
+            // (every wavefront does the same with all of them)
+            const unsigned long long mine = lane < (int)inside ? c.list[lane] : 0;
+            unsigned more = 0, alike = 0;
+            for (unsigned i = 0; i < inside; ++i) {
+                const unsigned long long k = c.list[i];
+                more += k > mine;
+                alike += k == mine;
+            }
+            const unsigned long long who = __ballot(lane < (int)inside && more < need && need <= more + alike);
+            const int src = __builtin_ctzll(who);
+            const unsigned long long key = __shfl(mine, src, 64);
+            return {key, key, need - __shfl(more, src, 64)};
+        }
+        __syncthreads();
     }
 }
 
-// A workgroup takes the pages of one sequence and key head.  The n-th largest key: the keys between the bounds known so far are counted in
-// 2048 even bins, the bin that holds it gives the next bounds, until all of a bin is taken or it is one key wide.
-constexpr int SEL_T = 1024, SEL_W = SEL_T / 64, SEL_BINS = 2048;
-__global__ __launch_bounds__(SEL_T) void select_kernel(SelectArgs a) {
-    __shared__ unsigned bins[SEL_BINS], part[SEL_W];
-    __shared__ unsigned long long edge[SEL_W][2];
-    __shared__ unsigned found[3];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.x / (unsigned)a.Hk, h = blockIdx.x % (unsigned)a.Hk;
+// A workgroup takes one key head of a sequence: a run of EACH keys a thread (more pages than that: read again for every pass).  SCORE: it makes the keys itself, else score_kernel has.
+template <typename T, int K, int EACH, bool SCORE> __global__ __launch_bounds__(SEL_T) void select_kernel(SelectArgs a) {
+    __shared__ CutSpace space;
+    __shared__ unsigned long long made[SCORE ? EACH * SEL_T : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = blockIdx.x / (unsigned)a.Hk, h = blockIdx.x % (unsigned)a.Hk;
+    const int row = a.seq ? a.seq[b] : b;
+    const int *table = a.table + ((unsigned)row < (unsigned)a.n_seqs ? (long long)row * a.table_stride : 0);
+    using R = ScoreRow<T, K>;
+    using P = PageSteps<T, K, false>;
+    constexpr int STRIDE = SEL_W * P::STEP;
+    [[maybe_unused]] int own = 0;
+    [[maybe_unused]] R r;
+    if constexpr (SCORE) {              // (what does not hang on the length is asked for beside it)
+        own = P::ask(a, table, a.first + wave * P::STEP, STRIDE, lane);
+        r.weights(a, b, h, lane);
+    }
     const Seen see = pages_seen(a, b);
-    const int have = (see.end + (1 << a.page_shift) - 1) >> a.page_shift, row = a.seq ? a.seq[b] : b;
+    const int have = pages_of(a, see), n = min(have, a.pages);
     int *out = a.chosen + (long long)blockIdx.x * a.pages;
-    const int n = min(have, a.pages);
     if (threadIdx.x == 0) a.tokens[blockIdx.x] = see.broken ? 0x7fffffff : have ? ((n - 1) << a.page_shift) + ((see.end - 1) & ((1 << a.page_shift) - 1)) + 1 : 0;
     for (int i = n + threadIdx.x; i < a.pages; i += SEL_T) out[i] = -1;
     if (have == 0) return;
-    const int *table = a.table + (long long)row * a.table_stride;
     auto leave = [&](int place, int p) {
         const int page = table[p];
         out[place] = (unsigned)page < (unsigned)a.n_pages ? page : -1;
@@ -409,92 +629,59 @@ __global__ __launch_bounds__(SEL_T) void select_kernel(SelectArgs a) {
     }
     for (int i = threadIdx.x; i < a.first; i += SEL_T) leave(i, i);
     for (int i = threadIdx.x; i < a.last; i += SEL_T) leave(a.pages - a.last + i, have - a.last + i);
-    const unsigned long long *keys = a.keys + (long long)blockIdx.x * a.max_pages_seen;
-    const int begin = a.first, end = have - a.last;
-    unsigned need = a.pages - a.first - a.last;         // of the keys in [begin, end), which are more
+    const unsigned need = a.pages - a.first - a.last;   // of the pages [begin, end), which are more
     if (need == 0) return;
-    unsigned long long lo = ~0ull, hi = 0;
-    for (int i = begin + threadIdx.x; i < end; i += SEL_T) {
-        const unsigned long long k = keys[i];
-        lo = k < lo ? k : lo;
-        hi = k > hi ? k : hi;
+    const int begin = a.first, end = have - a.last, count = end - begin;
+    const unsigned long long *keys = a.keys + (long long)blockIdx.x * a.max_pages_seen + begin;
+    if constexpr (SCORE) {
+        score_pages<T, K, false>(a, r, table, h, own, begin + wave * P::STEP, end, STRIDE, lane, [&](int p, unsigned long long key) {
+            if (lane % R::LANES == 0) made[p - begin] = key;
+        });
+        __syncthreads();
+        keys = made;
     }
+    const int run = (count + SEL_T - 1) / SEL_T, at = min((int)threadIdx.x * run, count), mine = min(run, count - at);
+    unsigned long long k[EACH];
+    const bool held = SCORE || run <= EACH;
+    if (held) {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const unsigned long long x = __shfl_xor(lo, d, 64), y = __shfl_xor(hi, d, 64);
-        lo = x < lo ? x : lo;
-        hi = y > hi ? y : hi;
+        for (int i = 0; i < EACH; ++i) k[i] = i < mine ? keys[at + i] : 0;
     }
-    if (lane == 0) { edge[wave][0] = lo; edge[wave][1] = hi; }
+    auto each = [&](auto &&f) {
+        if (held) {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i)
+                if (i < mine) f(k[i]);
+        } else {
+            for (int i = 0; i < mine; ++i) f(keys[at + i]);
+        }
+    };
+    const Cut cut = cut_keys(space, need, lane, wave, each);
+    // of the pages before this thread's so many are above the cut and so many in it: as many of the first, and of the others up to cut.need, are taken
+    unsigned above = 0, in = 0;
+    each([&](unsigned long long x) {
+        above += x > cut.hi;
+        in += x >= cut.lo && x <= cut.hi;
+    });
+    unsigned a0 = sum_upto(above), i0 = sum_upto(in);
     __syncthreads();
-    for (int w = 0; w < SEL_W; ++w) {
-        lo = edge[w][0] < lo ? edge[w][0] : lo;
-        hi = edge[w][1] > hi ? edge[w][1] : hi;
-    }
-    // keys of [lo, hi]; all above are taken; `need` of these are still to be taken
-    for (;;) {
-        const unsigned long long width = hi - lo;
-        const int top = width ? 63 - __builtin_clzll(width) : 0, shift = top > 10 ? top - 10 : 0;
-        for (int i = threadIdx.x; i < SEL_BINS; i += SEL_T) bins[i] = 0;
-        __syncthreads();
-        for (int i = begin + threadIdx.x; i < end; i += SEL_T) {
-            const unsigned long long k = keys[i];
-            if (k >= lo && k <= hi) atomicAdd(&bins[(k - lo) >> shift], 1u);
-        }
-        __syncthreads();
-        // bins from the top: thread t holds bins 2047 - 2t and 2046 - 2t
-        const unsigned c0 = bins[SEL_BINS - 1 - 2 * threadIdx.x], c1 = bins[SEL_BINS - 2 - 2 * threadIdx.x];
-        unsigned upto = c0 + c1;
+    if (lane == 63) { space.part[wave] = a0; space.bins[wave] = i0; }
+    __syncthreads();
+    a0 -= above;
+    i0 -= in;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const unsigned y = __shfl_up(upto, d, 64);
-            if (lane >= d) upto += y;
-        }
-        if (lane == 63) part[wave] = upto;
-        __syncthreads();
-        for (int w = 0; w < wave; ++w) upto += part[w];
-        const unsigned above = upto - c0 - c1;
-        if (above < need && above + c0 >= need) {
-            found[0] = SEL_BINS - 1 - 2 * threadIdx.x; found[1] = need - above; found[2] = c0;
-        } else if (above + c0 < need && upto >= need) {
-            found[0] = SEL_BINS - 2 - 2 * threadIdx.x; found[1] = need - above - c0; found[2] = c1;
-        }
-        __syncthreads();
-        need = found[1];
-        const unsigned inside = found[2];
-        lo += (unsigned long long)found[0] << shift;
-        const unsigned long long far = lo + ((1ull << shift) - 1);
-        hi = far < hi && far >= lo ? far : hi;
-        if (inside == need || shift == 0) break;
-        __syncthreads();
+    for (int w = 0; w < SEL_W; ++w) {
+        a0 += w < wave ? space.part[w] : 0u;
+        i0 += w < wave ? space.bins[w] : 0u;
     }
-    // taken: keys above hi, and the first `need` of [lo, hi] (all of them unless they are equal)
-    unsigned placed = a.first, equal = 0;
-    for (int i0 = begin; i0 < end; i0 += SEL_T) {
-        const int i = i0 + threadIdx.x;
-        const unsigned long long k = i < end ? keys[i] : 0;
-        const bool above = i < end && k > hi, in = i < end && k >= lo && k <= hi;
-        const unsigned long long ins = __ballot(in), below = (1ull << lane) - 1;
-        __syncthreads();
-        if (lane == 0) part[wave] = __builtin_popcountll(ins);
-        __syncthreads();
-        unsigned rank = equal + __builtin_popcountll(ins & below);
-        for (int w = 0; w < SEL_W; ++w) {
-            if (w < wave) rank += part[w];
-            equal += part[w];
-        }
-        const bool take = above || (in && rank < need);
-        const unsigned long long takes = __ballot(take);
-        __syncthreads();
-        if (lane == 0) part[wave] = __builtin_popcountll(takes);
-        __syncthreads();
-        unsigned place = placed + __builtin_popcountll(takes & below);
-        for (int w = 0; w < SEL_W; ++w) {
-            if (w < wave) place += part[w];
-            placed += part[w];
-        }
-        if (take) leave(place, i);
-    }
+    int p = begin + at;
+    each([&](unsigned long long x) {
+        const bool up = x > cut.hi, inside = x >= cut.lo && x <= cut.hi;
+        if (up || (inside && i0 < cut.need)) leave(a.first + a0 + min(i0, cut.need), p);
+        a0 += up;
+        i0 += inside;
+        ++p;
+    });
 }
 
 namespace {
@@ -515,14 +702,20 @@ template <typename T> int bounds_of(const BoundsArgs &a, bool mx, hipStream_t st
     });
 }
 template <typename T> int select_of(const SelectArgs &a, hipStream_t st) {
-    int rc = 0;
-    if (a.max_pages_seen > a.pages)
-        rc = by_width(a.K, [&](auto k) {
-            using R = ScoreRow<T, decltype(k)::value>;
-            hipLaunchKernelGGL((score_kernel<T, decltype(k)::value>), dim3(select_chunks(a.B, a.Hk, R::HEADS, a.max_pages_seen), a.B, (a.Hk + R::HEADS - 1) / R::HEADS), dim3(256), 0, st, a);
-        });
-    if (rc == 0) hipLaunchKernelGGL(select_kernel, dim3((unsigned)a.B * a.Hk), dim3(SEL_T), 0, st, a);
-    return rc;
+    return by_width(a.K, [&](auto k) {
+        constexpr int K = decltype(k)::value;
+        using R = ScoreRow<T, K>;
+        const dim3 rows((unsigned)a.B * a.Hk), t(SEL_T);
+        if (select_scores_itself(a.B * (long long)a.Hk, a.max_pages_seen, 2 * K * (int)sizeof(T))) {
+            if (a.max_pages_seen <= 1024) hipLaunchKernelGGL((select_kernel<T, K, 1024 / SEL_T, true>), rows, t, 0, st, a);
+            else hipLaunchKernelGGL((select_kernel<T, K, 4096 / SEL_T, true>), rows, t, 0, st, a);
+            return;
+        }
+        if (a.max_pages_seen > a.pages)
+            hipLaunchKernelGGL((score_kernel<T, K>), dim3(select_chunks(a.B, a.Hk, R::ROWS, a.max_pages_seen), a.B, (a.Hk + R::ROWS - 1) / R::ROWS), dim3(256), 0, st, a);
+        if (a.max_pages_seen <= 4096) hipLaunchKernelGGL((select_kernel<T, 64, 4096 / SEL_T, false>), rows, t, 0, st, a);
+        else hipLaunchKernelGGL((select_kernel<T, 64, 16384 / SEL_T, false>), rows, t, 0, st, a);
+    });
 }
 }  // namespace
 

@@ -368,9 +368,11 @@ inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K
 constexpr int PLAN_TOKENS_HERE = 2048;
 // Rows of a page table that a call with an index of them may have (two bits each in LDS)
 constexpr int PLAN_MAX_ROWS = 1 << 17;
-// Workgroups (four wavefronts, a page each at a time) for the scores of a sequence's pages of one group of key heads
+// Selection of pages: whether a row's workgroup makes the scores itself, which saves a launch, or a launch of many workgroups does.  bytes: of a page's bounds
+inline bool select_scores_itself(long long rows, int pages, int bytes) { return pages <= 4096 && (rows >= NUM_CU / 2 || (long long)pages * bytes <= 1 << 18); }
+// Workgroups (four wavefronts, four pages each at a time) for the scores of a sequence's pages of one group of key heads
 inline unsigned select_chunks(int B, int Hk, int heads, int pages) {
-    const long long others = (long long)B * ((Hk + heads - 1) / heads), want = (8 * NUM_CU + others - 1) / others, most = (pages + 3) / 4;
+    const long long others = (long long)B * ((Hk + heads - 1) / heads), want = (4 * NUM_CU + others - 1) / others, most = (pages + 15) / 16;
     return (unsigned)(want < most ? want : most);
 }
 
