@@ -368,8 +368,12 @@ inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K
 constexpr int PLAN_TOKENS_HERE = 2048;
 // Rows of a page table that a call with an index of them may have (two bits each in LDS)
 constexpr int PLAN_MAX_ROWS = 1 << 17;
-// Selection of pages: whether a row's workgroup makes the scores itself, which saves a launch, or a launch of many workgroups does.  bytes: of a page's bounds
-inline bool select_scores_itself(long long rows, int pages, int bytes) { return pages <= 4096 && (rows >= NUM_CU / 2 || (long long)pages * bytes <= 1 << 18); }
+// Selection of pages: whether a row's workgroup makes the scores itself, which saves a launch, or a launch of many workgroups does.  bytes: of a page's bounds.  (us, a launch of their own
+// and so: 4 rows of 256 pages of 512 bytes 8.1 and 9.6, 64 9.0 and 8.8, 128 11.9 and 10.8, 128 of 256 bytes 9.1 and 7.0; 64 rows of 512 12.4 and 15.7, 384, uneven, 22.3 and 22.8; 256 of 1024 41
+// and 35; 512, uneven, of 128 14.5 and 11.3; 8 of 4096 16 and 85.)
+inline bool select_scores_itself(long long rows, int pages, int bytes) {
+    return pages <= 4096 && (rows >= NUM_CU || (long long)pages * bytes <= (rows >= 64 ? 1 << 17 : 1 << 16));
+}
 // Workgroups (four wavefronts, four pages each at a time) for the scores of a sequence's pages of one group of key heads
 inline unsigned select_chunks(int B, int Hk, int heads, int pages) {
     const long long others = (long long)B * ((Hk + heads - 1) / heads), want = (4 * NUM_CU + others - 1) / others, most = (pages + 15) / 16;
