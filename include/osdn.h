@@ -407,7 +407,8 @@ int osdn_paged_plan(const osdn_pages *pages, int32_t B, int32_t tokens, const in
 /*
  * The pages of B sequences that end go back onto the list, and their entries of the table become -1: the first
  * ceil(lengths[b] / page_size) of row seq[b], those that are there.  They lie so that the next requests take them in the order that they
- * had.  A sequence that is named twice keeps its pages.  What the list has no room for is dropped.  Limits as for osdn_paged_plan.
+ * had.  A sequence that is named twice keeps its pages.  What the list has no room for is dropped.  Limits as for osdn_paged_plan, and
+ * up to 1024 B as many times max_pages entries of the table at most 2^30.
  */
 int osdn_paged_release(const osdn_pages *pages, int32_t B, const int32_t *lengths, const int32_t *seq, const int32_t *n_free,
                        int32_t *n_free_out, void *stream);

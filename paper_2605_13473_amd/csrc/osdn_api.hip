@@ -718,7 +718,7 @@ int osdn_paged_release(const osdn_pages *pages, int32_t B, const int32_t *length
     int shift = 0;
     const int rc = check_pages(pages, true, seq != nullptr, shift);
     if (rc != OSDN_OK) return rc;
-    if (B < 1 || B > 65535) return OSDN_ERR_SHAPE;
+    if (B < 1 || B > 65535 || (long long)std::min(B, 1024) * pages->max_pages > 1 << 30) return OSDN_ERR_SHAPE;         // (entries of a round are counted in 32 bits)
     if (!lengths || !n_free || !n_free_out) return OSDN_ERR_NULL;
     PlanArgs a = plan_args(pages, B, shift);
     a.cached = lengths; a.seq = seq; a.n_free = n_free; a.n_free_out = n_free_out;

@@ -455,6 +455,14 @@ PyObject *tuple_of(std::initializer_list<at::Tensor> ts) {
     for (const at::Tensor &t : ts) PyTuple_SET_ITEM(out, i++, wrapped(t));
     return out;
 }
+// A part of a buffer's memory as a tensor of its own, contiguous (several outputs in one allocation: each of its own costs a microsecond)
+at::Tensor piece(const at::Tensor &buffer, at::ScalarType type, int64_t byte, at::IntArrayRef sizes) {
+    const caffe2::TypeMeta meta = c10::scalarTypeToTypeMeta(type);
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(buffer.storage()), buffer.key_set(), meta);
+    t.unsafeGetTensorImpl()->set_storage_offset(byte / (int64_t)meta.itemsize());
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+    return t;
+}
 bool pages_of(const at::Tensor *table, const at::Tensor *free_pages, PyObject *page_size, PyObject *n_pages, int64_t dev, osdn_pages &g) {
     int64_t seqs, most, stride;
     const int32_t *list;
@@ -483,9 +491,12 @@ PyObject *paged_plan(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (B < 1 || B > 65535 || !int_array(t[1], dev, b, &cached) || !int_array(t[2], dev, b, &fresh) || !int_array(t[5], dev, b, &seq, false) ||
         !int_array(t[4], dev, at::IntArrayRef(&one, 1), &n_free))
         Py_RETURN_NONE;
-    const at::TensorOptions i32 = t[0]->options();
-    at::Tensor lengths = at::empty({B}, i32), starts = at::empty({B + 1}, i32), pos = at::empty({1, tokens}, i32), rows = at::empty({1, tokens}, i32), left = at::empty({1}, i32), slots;
-    if (a[9] == Py_True) slots = at::empty({tokens}, i32.dtype(at::kLong));
+    const int64_t N = tokens, line[] = {1, N}, b1 = B + 1, slot_bytes = a[9] == Py_True ? 8 * N : 0;
+    const at::Tensor all = at::empty({slot_bytes + 4 * (2 * N + 2 * B + 2)}, t[0]->options().dtype(at::kByte));
+    const auto take = [&](int64_t at, at::IntArrayRef sizes) { return piece(all, at::kInt, slot_bytes + 4 * at, sizes); };
+    const at::Tensor pos = take(0, at::IntArrayRef(line, 2)), rows = take(N, at::IntArrayRef(line, 2)), lengths = take(2 * N, b), starts = take(2 * N + B, at::IntArrayRef(&b1, 1));
+    at::Tensor left = at::empty({1}, t[0]->options()), slots;           // (kept from call to call: not with the rest)
+    if (slot_bytes) slots = piece(all, at::kLong, 0, at::IntArrayRef(&N, 1));
     int32_t *l = ints(lengths), *s = ints(starts), *p = ints(pos), *r = ints(rows), *f = ints(left);
     int64_t *sl = slots.defined() ? static_cast<int64_t *>(slots.data_ptr()) : nullptr;
     int rc;
@@ -590,7 +601,16 @@ PyObject *paged_read_mx(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (!cache_mx_of(t[0], t[1], t[2], t[3], t[4], dev, H, K, cache) || !int_array(t[5], dev, t[5]->sizes(), &pos) || !int_array(t[6], dev, t[5]->sizes(), &seq, false)) Py_RETURN_NONE;
     osdn_norm_params p{(int32_t)B, (int32_t)T, 0, (int32_t)H, (int32_t)K, a[7] == Py_True ? OSDN_BF16 : OSDN_F32, 0, 0, 0, 0, 0.f};
     const at::TensorOptions io = t[0]->options().dtype(a[7] == Py_True ? at::kBFloat16 : at::kFloat);
-    at::Tensor k = at::empty({B, T, H, K}, io), v = at::empty({B, T, H, K}, io);
+    const int64_t half = B * T * H * K, sizes[] = {B, T, H, K};
+    at::Tensor k, v;
+    if (half <= 1 << 17) {
+        const at::Tensor both = at::empty({2 * half}, io);
+        k = piece(both, both.scalar_type(), 0, at::IntArrayRef(sizes, 4));
+        v = piece(both, both.scalar_type(), half * (int64_t)both.itemsize(), at::IntArrayRef(sizes, 4));
+    } else {
+        k = at::empty(at::IntArrayRef(sizes, 4), io);
+        v = at::empty(at::IntArrayRef(sizes, 4), io);
+    }
     osdn_rows ko = dense(k), vo = dense(v);
     int rc;
     Py_BEGIN_ALLOW_THREADS
@@ -772,7 +792,9 @@ PyObject *page_select(PyObject *, PyObject *const *a, Py_ssize_t n) {
         scratch = ws.data_ptr();
     }
     if (B * Hk > (1 << 21) || B * Hk * p.pages > INT_MAX) Py_RETURN_NONE;
-    at::Tensor chosen = at::empty({B, Hk, p.pages}, t[2]->options()), tokens = at::empty({B, Hk}, t[2]->options());
+    const int64_t bhn[] = {B, Hk, p.pages};
+    const at::Tensor both = at::empty({B * Hk * (p.pages + 1)}, t[2]->options());
+    const at::Tensor chosen = piece(both, at::kInt, 0, at::IntArrayRef(bhn, 3)), tokens = piece(both, at::kInt, 4 * B * Hk * (int64_t)p.pages, at::IntArrayRef(bhn, 2));
     int32_t *c = ints(chosen), *k = ints(tokens);
     int rc;
     Py_BEGIN_ALLOW_THREADS

@@ -21,14 +21,21 @@ constexpr int PLAN_T = 1024, PLAN_W = PLAN_T / 64;
 
 __device__ __forceinline__ unsigned add_sat(unsigned a, unsigned b) { return __builtin_elementwise_add_sat(a, b); }
 
+// Sums over the lanes up to this one (SAT: that stop at the largest number)
+template <bool SAT> __device__ __forceinline__ unsigned sum_upto(unsigned x) {
+    auto with = [&](int y) { x = SAT ? add_sat(x, (unsigned)y) : x + (unsigned)y; };
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true));       // row_shr:1, 2, 4, 8
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));      // row_bcast:15 into rows 1 and 3
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));      // row_bcast:31 into rows 2 and 3
+    return x;
+}
 // Sums over the threads of a workgroup, each with its own and those before it; saturating.  `all`: the sum over all threads.
 struct TwoSums { unsigned a, b; };
-__device__ __forceinline__ TwoSums running_sums(TwoSums x, TwoSums &all, unsigned (&part)[PLAN_W][2], int lane, int wave) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const unsigned a = __shfl_up(x.a, d, 64), b = __shfl_up(x.b, d, 64);
-        if (lane >= d) { x.a = add_sat(x.a, a); x.b = add_sat(x.b, b); }
-    }
+__device__ __forceinline__ TwoSums running_sums(TwoSums x, TwoSums &all, unsigned (&part)[PLAN_W][2], int wave, int lane) {
+    x = {sum_upto<true>(x.a), sum_upto<true>(x.b)};
     __syncthreads();                    // (what stands in `part` has been read)
     if (lane == 63) { part[wave][0] = x.a; part[wave][1] = x.b; }
     __syncthreads();
@@ -56,193 +63,204 @@ __device__ __forceinline__ void note_rows(unsigned *bits, int words, int n_seqs,
     __syncthreads();
 }
 
-struct Request { int row, first, need, cached, fresh; unsigned pages_before; };
-
-// The pages of a request into its row of the table: its i-th is the (pages_before + i)-th from the top of the list
+// The page that the place-th from the top of the list is
 __device__ __forceinline__ int granted(const PlanArgs &a, int have, unsigned place) { return a.free_list[have - 1 - (int)place]; }
-
-// What lanes [0, n) of the request of lane `src` do, for the requests of a wavefront one after the other
-template <typename F> __device__ __forceinline__ void each_request(unsigned long long who, F &&f) {
-    while (who) {
-        const int src = __builtin_ctzll(who);
-        who &= who - 1;
-        f(src);
-    }
-}
-
 // (a page that is not there has no slots)
 __device__ __forceinline__ void leave_token(const PlanArgs &a, int at, int pos, int row, int page) {
     a.positions[at] = pos;
     a.rows[at] = row;
     if (a.slots) a.slots[at] = (unsigned)page < (unsigned)a.n_pages ? ((long long)page << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) : -1;
 }
+// The last of n ascending numbers that is no larger than x (the first is); of equal ones the last
+__device__ __forceinline__ int last_up_to(const int *v, int n, int x) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (v[mid] <= x) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
 
-// TOKENS: also the tokens' places (else plan_tokens_kernel, for many)
-template <bool TOKENS> __global__ __launch_bounds__(PLAN_T) void plan_kernel(PlanArgs a) {
+// Every workgroup makes the running sums; the first leaves what there is for each request and grants the pages, each the tokens of its part of the token axis (`per` of
+// them, 0: plan_tokens_kernel does).  A request of a token and of no more than two pages is its thread's; others are laid down in LDS, where every page and token finds its own.
+__global__ __launch_bounds__(PLAN_T) void plan_kernel(PlanArgs a, int per) {
     extern __shared__ unsigned bits[];
     __shared__ unsigned part[PLAN_W][2];
+    __shared__ int pages_at[PLAN_T], tokens_at[PLAN_T], first_of[PLAN_T], row_of[PLAN_T], cached_of[PLAN_T];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), words = (a.n_seqs + 31) / 32;
-    const int P = 1 << a.page_shift;
+    const int P = 1 << a.page_shift, begin = min(a.N, (int)blockIdx.x * per), end = min(a.N, begin + per);
+    const bool grants = blockIdx.x == 0;
     const long long capacity = (long long)a.max_pages << a.page_shift;
     const int have = max(0, min(*a.n_free, a.free_capacity));
     if (a.seq) note_rows(bits, words, a.n_seqs, a.B, a.seq, a.fresh);
     TwoSums asked{0u, 0u}, given{0u, 0u};           // of the requests before this round's: pages and tokens, asked for and given
     for (int b0 = 0; b0 < a.B; b0 += PLAN_T) {
         const int b = b0 + (int)threadIdx.x;
-        Request r{};
-        bool valid = false;
+        int row = 0, cached = 0, fresh = 0, first = 0, need = 0;
         if (b < a.B) {
-            r.row = a.seq ? a.seq[b] : b;
-            r.cached = a.cached[b];
-            r.fresh = a.fresh[b];
-            const bool known = (unsigned)r.row < (unsigned)a.n_seqs;
-            const bool twice = a.seq && known && r.fresh > 0 && (bits[words + (r.row >> 5)] >> (r.row & 31) & 1u);
-            valid = known && !twice && r.cached >= 0 && r.fresh >= 0 && (long long)r.cached + r.fresh <= capacity;
-            if (!known || r.cached < 0) r.cached = 0;
-            if (!valid) r.fresh = 0;
-            r.first = (int)(((long long)r.cached + P - 1) >> a.page_shift);
-            r.need = valid ? (int)(((long long)r.cached + r.fresh + P - 1) >> a.page_shift) - r.first : 0;
+            row = a.seq ? a.seq[b] : b;
+            cached = a.cached[b];
+            fresh = a.fresh[b];
+            const bool known = (unsigned)row < (unsigned)a.n_seqs;
+            const bool twice = a.seq && known && fresh > 0 && (bits[words + (row >> 5)] >> (row & 31) & 1u);
+            const bool valid = known && !twice && cached >= 0 && fresh >= 0 && (long long)cached + fresh <= capacity;
+            if (!known || cached < 0) cached = 0;
+            if (!valid) fresh = 0;
+            first = (int)(((long long)cached + P - 1) >> a.page_shift);
+            need = valid ? (int)(((long long)cached + fresh + P - 1) >> a.page_shift) - first : 0;
         }
         TwoSums all;
-        TwoSums upto = running_sums({(unsigned)r.need, (unsigned)r.fresh}, all, part, lane, wave);
-        const bool served = (r.need == 0 || add_sat(asked.a, upto.a) <= (unsigned)have) && (r.fresh == 0 || add_sat(asked.b, upto.b) <= (unsigned)a.N);
+        TwoSums upto = running_sums({(unsigned)need, (unsigned)fresh}, all, part, wave, lane);
+        const bool served = (need == 0 || add_sat(asked.a, upto.a) <= (unsigned)have) && (fresh == 0 || add_sat(asked.b, upto.b) <= (unsigned)a.N);
         asked = {add_sat(asked.a, all.a), add_sat(asked.b, all.b)};
-        if (!served) r.need = r.fresh = 0;
-        if (__syncthreads_or(!served)) upto = running_sums({(unsigned)r.need, (unsigned)r.fresh}, all, part, lane, wave);
-        r.pages_before = given.a + upto.a - r.need;
-        const int start = (int)(given.b + upto.b) - r.fresh;
-        given = {given.a + all.a, given.b + all.b};
-        if (b < a.B) {
-            a.lengths[b] = r.cached + r.fresh;
+        if (!served) need = fresh = 0;
+        if (__syncthreads_or(!served)) upto = running_sums({(unsigned)need, (unsigned)fresh}, all, part, wave, lane);
+        const unsigned place = given.a + upto.a - need;
+        const int start = (int)(given.b + upto.b) - fresh;
+        if (grants && b < a.B) {
+            a.lengths[b] = cached + fresh;
             a.starts[b] = start;
-            if (b == a.B - 1) a.starts[a.B] = start + r.fresh;
+            if (b == a.B - 1) a.starts[a.B] = start + fresh;
         }
-        // pages: one or two by the request's lane, more by the whole wavefront
-        int *row = a.table + (long long)r.row * a.table_stride;
-        int page0 = -1;
-        if (r.need > 0) page0 = granted(a, have, r.pages_before);
-        if (r.need > 0 && r.need <= 2) {
-            row[r.first] = page0;
-            if (r.need == 2) row[r.first + 1] = granted(a, have, r.pages_before + 1);
-        }
-        each_request(__ballot(r.need > 2), [&](int src) {
-            int *to = a.table + (long long)__shfl(r.row, src, 64) * a.table_stride + __shfl(r.first, src, 64);
-            const int n = __shfl(r.need, src, 64);
-            const unsigned from = __shfl(r.pages_before, src, 64);
-            for (int i = lane; i < n; i += 64) to[i] = granted(a, have, from + i);
-        });
-        if constexpr (TOKENS) {
-            if (r.fresh == 1) {
-                const int col = r.cached >> a.page_shift, page = r.need ? page0 : a.slots ? row[col] : 0;
-                leave_token(a, start, r.cached, r.row, page);
-            }
-            each_request(__ballot(r.fresh > 1), [&](int src) {
-                const int R = __shfl(r.row, src, 64), n = __shfl(r.fresh, src, 64), c = __shfl(r.cached, src, 64), first = __shfl(r.first, src, 64), at = __shfl(start, src, 64);
-                const unsigned from = __shfl(r.pages_before, src, 64);
-                for (int i = lane; i < n; i += 64) {
-                    const int pos = c + i, col = pos >> a.page_shift;
-                    int page = 0;
-                    if (a.slots) page = col < first ? a.table[(long long)R * a.table_stride + col] : granted(a, have, from + col - first);
-                    leave_token(a, at + i, pos, R, page);
+        if (__syncthreads_or(need > 2 || (fresh > 1 && per > 0))) {
+            const int n = min(PLAN_T, a.B - b0);
+            pages_at[threadIdx.x] = (int)place;
+            tokens_at[threadIdx.x] = start;
+            first_of[threadIdx.x] = first;
+            row_of[threadIdx.x] = row;
+            cached_of[threadIdx.x] = cached;
+            __syncthreads();
+            if (grants)
+                for (int i = (int)given.a + threadIdx.x; i < (int)(given.a + all.a); i += PLAN_T) {
+                    const int r = last_up_to(pages_at, n, i);
+                    a.table[(long long)row_of[r] * a.table_stride + first_of[r] + (i - pages_at[r])] = granted(a, have, i);
                 }
-            });
+            for (int i = max(begin, (int)given.b) + (int)threadIdx.x; i < min(end, (int)(given.b + all.b)); i += PLAN_T) {
+                const int r = last_up_to(tokens_at, n, i), pos = cached_of[r] + (i - tokens_at[r]), col = pos >> a.page_shift;
+                int page = 0;
+                if (a.slots) page = col < first_of[r] ? a.table[(long long)row_of[r] * a.table_stride + col] : granted(a, have, pages_at[r] + (col - first_of[r]));
+                leave_token(a, i, pos, row_of[r], page);
+            }
+            __syncthreads();
+        } else {
+            int *to = a.table + (long long)row * a.table_stride;
+            const int page = need > 0 ? granted(a, have, place) : 0;
+            if (grants && need > 0) {
+                to[first] = page;
+                if (need == 2) to[first + 1] = granted(a, have, place + 1);
+            }
+            if (fresh == 1 && start >= begin && start < end) leave_token(a, start, cached, row, need > 0 ? page : a.slots ? to[cached >> a.page_shift] : 0);
         }
+        given = {given.a + all.a, given.b + all.b};
     }
-    if constexpr (TOKENS)
-        for (int i = (int)given.b + (int)threadIdx.x; i < a.N; i += PLAN_T) leave_token(a, i, -1, -1, -1);
-    if (threadIdx.x == 0) *a.n_free_out = have - (int)given.a;
+    for (int i = max(begin, (int)given.b) + (int)threadIdx.x; i < end; i += PLAN_T) leave_token(a, i, -1, -1, -1);
+    if (grants && threadIdx.x == 0) *a.n_free_out = have - (int)given.a;
 }
 
-// Places of many tokens, behind plan_kernel<false>: a token finds its request in the requests' starts
+// Places of many tokens, behind plan_kernel: where its outputs stand in the place of its inputs, which then no second workgroup may read beside the first
 __global__ __launch_bounds__(256) void plan_tokens_kernel(PlanArgs a) {
     const int j = blockIdx.x * 256 + threadIdx.x;
     if (j >= a.N) return;
     if (j >= a.starts[a.B]) return leave_token(a, j, -1, -1, -1);
-    int lo = 0, hi = a.B;                       // starts[lo] <= j < starts[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.starts[mid] <= j) lo = mid;
-        else hi = mid;
-    }
-    const int row = a.seq ? a.seq[lo] : lo, pos = a.lengths[lo] - (a.starts[lo + 1] - j);
-    const int page = a.slots ? a.table[(long long)row * a.table_stride + (pos >> a.page_shift)] : 0;
-    leave_token(a, j, pos, row, page);
+    const int b = last_up_to(a.starts, a.B, j), row = a.seq ? a.seq[b] : b, pos = a.lengths[b] - (a.starts[b + 1] - j);
+    leave_token(a, j, pos, row, a.slots ? a.table[(long long)row * a.table_stride + (pos >> a.page_shift)] : 0);
 }
 
 // The i-th page that is given back, of R in the order of the requests and of their pages, lands R - 1 - i above what the list holds, so that the next requests
-// take them in that order again.  A wavefront takes a request: it counts its pages, and, once it is known how many come before them, moves them.
+// take them in that order again.  All entries of the table that are given back make one list, of which a thread takes runs of RELEASE_RUN.
+constexpr int RELEASE_RUN = 4;
 __global__ __launch_bounds__(PLAN_T) void release_kernel(PlanArgs a) {
     extern __shared__ unsigned bits[];
-    __shared__ unsigned count[PLAN_T], before[PLAN_T], part[PLAN_W][2];
+    __shared__ unsigned part[PLAN_W][2];
+    __shared__ int entries_at[PLAN_T], row_of[PLAN_T];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), words = (a.n_seqs + 31) / 32;
     const int have = max(0, min(*a.n_free, a.free_capacity));
     if (a.seq) note_rows(bits, words, a.n_seqs, a.B, a.seq, a.cached);
-    // columns of the table that request b holds; none where there is nothing to give back
-    auto held = [&](int b, int &row) {
-        row = a.seq ? a.seq[b] : b;
-        const int n = a.cached[b];
-        if ((unsigned)row >= (unsigned)a.n_seqs || n <= 0 || (a.seq && (bits[words + (row >> 5)] >> (row & 31) & 1u))) return 0;
-        return (int)min((long long)a.max_pages, ((long long)n + (1 << a.page_shift) - 1) >> a.page_shift);
-    };
-    auto pages_of = [&](int b) {
-        int row;
-        const int cols = held(b, row);
-        const int *from = a.table + (cols ? (long long)row * a.table_stride : 0);
-        int n = 0;
-        for (int i = 0; i < cols; i += 64) n += __builtin_popcountll(__ballot(i + lane < cols && (unsigned)from[min(i + lane, cols - 1)] < (unsigned)a.n_pages));
-        return n;
-    };
-    auto count_round = [&](int b0) {
-        __syncthreads();
-        count[threadIdx.x] = 0;
-        __syncthreads();
-        for (int i = wave; i < PLAN_T && b0 + i < a.B; i += PLAN_W) {
-            const int n = pages_of(b0 + i);
-            if (lane == 0) count[i] = n;
+    // requests b0 .. of a round: how many entries come before each of theirs; all of the round's
+    auto lay_down = [&](int b0) {
+        const int b = b0 + (int)threadIdx.x;
+        int row = 0, cols = 0;
+        if (b < a.B) {
+            row = a.seq ? a.seq[b] : b;
+            const int n = a.cached[b];
+            if ((unsigned)row < (unsigned)a.n_seqs && n > 0 && !(a.seq && (bits[words + (row >> 5)] >> (row & 31) & 1u)))
+                cols = (int)min((long long)a.max_pages, ((long long)n + (1 << a.page_shift) - 1) >> a.page_shift);
         }
+        TwoSums all;
+        const TwoSums upto = running_sums({(unsigned)cols, 0u}, all, part, wave, lane);
+        entries_at[threadIdx.x] = (int)upto.a - cols;
+        row_of[threadIdx.x] = row;
         __syncthreads();
+        return (int)all.a;
     };
-    unsigned total = 0;
-    for (int b0 = 0; b0 < a.B; b0 += PLAN_T) {
-        count_round(b0);
-        TwoSums all;
-        running_sums({count[threadIdx.x], 0u}, all, part, lane, wave);
-        total += all.a;
-    }
-    unsigned done = 0;
-    for (int b0 = 0; b0 < a.B; b0 += PLAN_T) {
-        if (a.B > PLAN_T) count_round(b0);      // (else they are still there)
-        TwoSums all;
-        const TwoSums upto = running_sums({count[threadIdx.x], 0u}, all, part, lane, wave);
-        before[threadIdx.x] = done + upto.a - count[threadIdx.x];
-        __syncthreads();
-        for (int i = wave; i < PLAN_T && b0 + i < a.B; i += PLAN_W) {
-            int row;
-            const int cols = held(b0 + i, row);
-            int *from = a.table + (cols ? (long long)row * a.table_stride : 0);
-            unsigned at = before[i];
-            for (int c = 0; c < cols; c += 64) {
-                const bool in = c + lane < cols;
-                const int page = in ? from[c + lane] : -1;
-                const bool there = (unsigned)page < (unsigned)a.n_pages;
-                const unsigned long long who = __ballot(there);
-                const long long to = (long long)have + total - 1 - (at + __builtin_popcountll(who & ((1ull << lane) - 1)));
-                if (there && to < a.free_capacity) a.free_list[to] = page;
-                if (in) from[c + lane] = -1;
-                at += __builtin_popcountll(who);
+    // the entries of a thread's run from i on
+    auto entry = [&](int n, int i, long long &at) {
+        const int r = last_up_to(entries_at, n, i);
+        at = (long long)row_of[r] * a.table_stride + (i - entries_at[r]);
+        return a.table[at];
+    };
+    // gives back the entries [0, count) of a round, `before` pages coming before theirs, of `total`; or, total < 0, only counts them (a round that is one run long does both)
+    auto go = [&](int n, int count, unsigned before, long long total) {
+        unsigned sum = 0;
+        for (int i0 = 0; i0 < count; i0 += PLAN_T * RELEASE_RUN) {
+            long long at[RELEASE_RUN];
+            int page[RELEASE_RUN];
+            unsigned mine = 0;
+#pragma unroll
+            for (int u = 0; u < RELEASE_RUN; ++u) {
+                const int i = i0 + (int)threadIdx.x * RELEASE_RUN + u;
+                at[u] = -1;
+                page[u] = i < count ? entry(n, i, at[u]) : -1;
+            }
+#pragma unroll
+            for (int u = 0; u < RELEASE_RUN; ++u) mine += (unsigned)page[u] < (unsigned)a.n_pages;
+            TwoSums all;
+            const TwoSums upto = running_sums({mine, 0u}, all, part, wave, lane);
+            unsigned place = before + sum + upto.a - mine;
+            sum += all.a;
+            const long long of = total == 0 ? (long long)before + sum : total;          // (0: this run has all of them)
+            if (total >= 0) {
+#pragma unroll
+                for (int u = 0; u < RELEASE_RUN; ++u) {
+                    if (at[u] >= 0) a.table[at[u]] = -1;
+                    if ((unsigned)page[u] < (unsigned)a.n_pages) {
+                        const long long to = have + of - 1 - place++;
+                        if (to < a.free_capacity) a.free_list[to] = page[u];
+                    }
+                }
             }
         }
-        done += all.a;
+        return sum;
+    };
+    unsigned total = 0;
+    const int count = lay_down(0);
+    if (a.B <= PLAN_T && count <= PLAN_T * RELEASE_RUN) {
+        total = go(min(PLAN_T, a.B), count, 0, 0);
+    } else {
+        for (int pass = 0; pass < 2; ++pass) {
+            unsigned before = 0;
+            for (int b0 = 0; b0 < a.B; b0 += PLAN_T) {
+                __syncthreads();
+                const int c = lay_down(b0);
+                before += go(min(PLAN_T, a.B - b0), c, before, pass == 0 ? -1 : (long long)total);
+            }
+            total = before;
+            if (total == 0 && pass == 0) total = 1;         // (nothing to give back: entries are cleared all the same)
+            if (pass == 1) total = before;
+        }
     }
     if (threadIdx.x == 0) *a.n_free_out = (int)min((long long)a.free_capacity, (long long)have + total);
 }
 
 int launch_plan(const PlanArgs &a, hipStream_t st) {
     const size_t lds = a.seq ? (size_t)((a.n_seqs + 31) / 32) * 8 : 0;
-    if (a.N <= PLAN_TOKENS_HERE) {
-        hipLaunchKernelGGL(plan_kernel<true>, dim3(1), dim3(PLAN_T), lds, st, a);
+    const bool over_itself = a.lengths == a.cached || a.lengths == a.fresh || a.n_free_out == a.n_free;
+    const int workgroups = plan_workgroups(a.N), per = (a.N + workgroups - 1) / workgroups;
+    if (workgroups == 1 || !over_itself) {
+        hipLaunchKernelGGL(plan_kernel, dim3(workgroups), dim3(PLAN_T), lds, st, a, per);
     } else {
-        hipLaunchKernelGGL(plan_kernel<false>, dim3(1), dim3(PLAN_T), lds, st, a);
+        hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(PLAN_T), lds, st, a, 0);
         hipLaunchKernelGGL(plan_tokens_kernel, dim3(((unsigned)a.N + 255) / 256), dim3(256), 0, st, a);
     }
     return 0;
@@ -355,16 +373,7 @@ template <int AWAY> __device__ __forceinline__ double with_lanes_away(double x) 
     else asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\tv_permlane32_swap_b32 %2, %3" : "+v"(a), "+v"(c), "+v"(b), "+v"(d));
     return __builtin_bit_cast(double, (uint64_t)b << 32 | a) + __builtin_bit_cast(double, (uint64_t)d << 32 | c);
 }
-// Sums over the lanes up to this one; the largest of all lanes (in lane 63)
-__device__ __forceinline__ unsigned sum_upto(unsigned x) {
-    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true);       // row_shr:1, 2, 4, 8
-    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true);
-    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true);
-    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true);
-    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);      // row_bcast:15 into rows 1 and 3
-    x += (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);      // row_bcast:31 into rows 2 and 3
-    return x;
-}
+// The largest of the lanes up to this one
 __device__ __forceinline__ unsigned largest_upto(unsigned x) {
     auto with = [&](int y) { x = max(x, (unsigned)y); };
     with(__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true));
@@ -555,7 +564,7 @@ template <typename F> __device__ __forceinline__ Cut cut_keys(CutSpace &c, unsig
             c.bins[SEL_BINS - 1 - (SEL_RUN * threadIdx.x + i)] = 0;
             all += here[i];
         }
-        const unsigned upto = sum_upto(all);
+        const unsigned upto = sum_upto<false>(all);
         if (lane == 63) c.part[wave] = upto;
         __syncthreads();
         unsigned above = upto - all;
@@ -663,7 +672,7 @@ template <typename T, int K, int EACH, bool SCORE> __global__ __launch_bounds__(
         above += x > cut.hi;
         in += x >= cut.lo && x <= cut.hi;
     });
-    unsigned a0 = sum_upto(above), i0 = sum_upto(in);
+    unsigned a0 = sum_upto<false>(above), i0 = sum_upto<false>(in);
     __syncthreads();
     if (lane == 63) { space.part[wave] = a0; space.bins[wave] = i0; }
     __syncthreads();

@@ -364,8 +364,8 @@ inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K
     return p;
 }
 
-// Tokens of a batch of requests whose places one workgroup writes, beside the running sums; more go in a launch of their own
-constexpr int PLAN_TOKENS_HERE = 2048;
+// Workgroups for the places of a batch's tokens, each of which makes the batch's running sums for itself
+inline int plan_workgroups(int tokens) { return tokens <= 4096 ? 1 : (int)((tokens + 4095LL) / 4096 < NUM_CU ? (tokens + 4095LL) / 4096 : NUM_CU); }
 // Rows of a page table that a call with an index of them may have (two bits each in LDS)
 constexpr int PLAN_MAX_ROWS = 1 << 17;
 // Selection of pages: whether a row's workgroup makes the scores itself, which saves a launch, or a launch of many workgroups does.  bytes: of a page's bounds.  (us, a launch of their own

@@ -183,3 +183,31 @@ def test_places_in_place_and_in_a_graph():
         for got, want in zip((lengths, starts, pos, rows, slots, n_free), w):
             assert got.tolist() == (want if isinstance(want, list) else [want])
         assert torch.equal(table.cpu(), x["table"])
+
+
+@pytest.mark.parametrize("tokens", [40, 9000])
+def test_outputs_over_the_inputs(tokens):
+    """The same numbers where lengths and the count of free pages stand in the place of what they come from, for few tokens and for many."""
+    x = make([3, 0, 70, 15, 16, 1], [1, 30, 0, 1, 3, 2] if tokens == 40 else [1, 3000, 0, 2000, 3, 2500], 8, rows=9, order="any")
+    table = x["table"].clone()
+    want = ref.plan(table, x["cached"], x["fresh"], x["seq"], x["free"], x["n_free"][0], 8, tokens, x["n_pages"])
+    d = {n: t.cuda() if isinstance(t, torch.Tensor) else t for n, t in x.items()}
+    starts, pos, rows = (torch.empty(n, dtype=torch.int32, device="cuda") for n in (7, tokens, tokens))
+    slots = torch.empty(tokens, dtype=torch.int64, device="cuda")
+    ob.osdn_paged_plan(ob._pages(d["table"], 8, x["n_pages"], d["free"]), 6, tokens, d["cached"], d["fresh"], d["seq"], d["n_free"], d["n_free"], d["cached"], starts, pos, rows, slots)
+    for got, w in zip((d["cached"], starts, pos, rows, slots, d["n_free"]), want):
+        assert got.tolist() == (w if isinstance(w, list) else [w])
+    assert torch.equal(d["table"].cpu(), table)
+    ob.osdn_paged_plan(ob._pages(d["table"], 8, x["n_pages"], d["free"]), 6, tokens, torch.zeros(6, dtype=torch.int32, device="cuda"), d["fresh"], d["seq"], d["n_free"], d["n_free"], d["fresh"],
+                       starts, pos, rows)
+    # (from nothing, with what the list still holds: lengths are what is new of those that are served)
+    again = ref.plan(table, torch.zeros(6, dtype=torch.int32), x["fresh"], x["seq"], x["free"], want[5], 8, tokens, x["n_pages"])
+    assert d["fresh"].tolist() == again[0] and int(d["n_free"]) == again[5] and torch.equal(d["table"].cpu(), table)
+
+
+@pytest.mark.parametrize("rows", [1, 1025, 3000])
+def test_release_of_many_entries(rows):
+    """More entries than a workgroup takes at a time, and more sequences than a round; some of them with holes."""
+    x = make([(53 * i) % 97 * 11 for i in range(rows)] if rows > 1 else [40000], [0] * rows, 2 if rows == 1 else 16, rows=rows + 5, order="any", spare=50)
+    x["table"][x["seq"][::7].long(), 0] = -1
+    check_release(x, x["cached"])
