@@ -932,7 +932,7 @@ def paged_read_mx(cache, page_table, positions, seq=None, dtype=torch.bfloat16):
     return tuple(out)
 
 
-def _decode_in_parts(q, most, lengths, bytes_of, call, per_head, workspace, want_lse):
+def _decode_in_parts(q, most, bytes_of, call, per_head, workspace, want_lse):
     """Calls of at most `most` queries each; per_head: what goes with a query."""
     B, Hq, _ = q.shape
     most = most if B <= most else -(-B // -(-B // most))
@@ -974,7 +974,7 @@ def paged_decode_mx(q, cache, page_table, lengths, seq=None, scale=None, window:
         if seq is None:
             seq = torch.arange(B, dtype=torch.int32, device=q.device)
     params = lambda n: make_decode_params(n, Hq, Hk, K, q.dtype == torch.bfloat16, max_length, scale, window)
-    return _decode_in_parts(q, most, lengths, lambda n: osdn_paged_decode_mx_workspace_bytes(params(n)),
+    return _decode_in_parts(q, most, lambda n: osdn_paged_decode_mx_workspace_bytes(params(n)),
                             lambda n, q, lengths, seq, o, lse, ws: osdn_paged_decode_mx(params(n), q, cache, page_table, lengths, seq, o, lse, ws), (lengths, seq), workspace, want_lse)
 
 
@@ -1087,6 +1087,8 @@ def page_select(q, bounds, page_table, lengths, page_size: int, pages: int, seq=
     p = make_select_params(B, Hq, Hk, K, q.dtype == torch.bfloat16, max_length, pages=pages, first=first, last=last)
     if p.pages < 1:
         raise OsdnError(-5)
+    if B * Hk * p.pages > 2**31 - 1:                        # (before they are allocated)
+        raise OsdnError(OSDN_ERR_SHAPE)
     new = lambda *shape: torch.empty(*shape, dtype=torch.int32, device=q.device)
     chosen, tokens = new(B, Hk, p.pages), new(B, Hk)
     if workspace is None:
@@ -1108,7 +1110,7 @@ def _decode_pages(q, cache, Hk, page_size, chosen, tokens, scale, max_length, wa
         _array(tokens, torch.int32, (B, Hk), "tokens")
     params = lambda n: make_decode_params(n, Hq, Hk, K, q.dtype == torch.bfloat16, max_length, scale)
     call = osdn_paged_decode_pages_mx if mx else osdn_paged_decode_pages
-    return _decode_in_parts(q, most, tokens, lambda n: _pages_bytes(params(n), mx),
+    return _decode_in_parts(q, most, lambda n: _pages_bytes(params(n), mx),
                             lambda n, q, chosen, tokens, o, lse, ws: call(params(n), q, *cache, chosen, tokens, o, lse, ws), (chosen, tokens), workspace, want_lse)
 
 
