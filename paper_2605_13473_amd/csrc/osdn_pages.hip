@@ -432,20 +432,28 @@ template <typename T, int K> struct ScoreRow {
 #pragma unroll
         for (int v = 0; v < VPL; ++v) raw[v] = *reinterpret_cast<const u32x4 *>(from + v * LANES * VE);
     }
-    // the score, in every lane of the row
-    __device__ __forceinline__ double score(const u32x4 (&raw)[VPL]) const {
+    __device__ __forceinline__ double sum(const u32x4 (&raw)[VPL]) const {
         double s = 0.0;
 #pragma unroll
         for (int v = 0; v < VPL; ++v)
 #pragma unroll
             for (int e = 0; e < VE; ++e) s = __builtin_fma(w[v][e], (double)vec_get<T>(raw[v], e), s);
-        s += moved<0xB1>(s);                    // quad_perm [1,0,3,2]
-        s += moved<0x4E>(s);                    // quad_perm [2,3,0,1]
-        s += moved<0x141>(s);                   // row_half_mirror
-        s += moved<0x140>(s);                   // row_mirror (a row has 16 lanes at least)
-        if constexpr (LANES > 16) s = with_lanes_away<16>(s);
-        if constexpr (LANES > 32) s = with_lanes_away<32>(s);
         return s;
+    }
+    // the scores of four pages, of page u in the row's lanes that are u modulo 4 (a row has 16 lanes at least): the first two exchanges halve what there is to add
+    __device__ __forceinline__ double scores(const u32x4 (&raw)[4][VPL], int lane) const {
+        double s[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s[u] = sum(raw[u]);
+        const bool odd = lane & 1, upper = lane & 2;
+        const double s01 = (odd ? s[1] : s[0]) + moved<0xB1>(odd ? s[0] : s[1]);            // quad_perm [1,0,3,2]
+        const double s23 = (odd ? s[3] : s[2]) + moved<0xB1>(odd ? s[2] : s[3]);
+        double x = (upper ? s23 : s01) + moved<0x4E>(upper ? s01 : s23);                    // quad_perm [2,3,0,1]
+        x += moved<0x124>(x);                   // row_ror:4
+        x += moved<0x128>(x);                   // row_ror:8
+        if constexpr (LANES > 16) x = with_lanes_away<16>(x);
+        if constexpr (LANES > 32) x = with_lanes_away<32>(x);
+        return x;
     }
 };
 __device__ __forceinline__ Seen pages_seen(const SelectArgs &a, int b) {
@@ -470,32 +478,26 @@ __device__ __forceinline__ void score_pages(const SelectArgs &a, const ScoreRow<
     const int sub = HEADS ? 0 : lane / R::LANES;
     for (int p = p0; p < p1; p += STEPS * stride) {
         if (p > p0) own = P::ask(a, table, p, stride, lane);
-        int page[4];
         u32x4 raw[4][R::VPL];
         auto ask = [&](int i) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                page[u] = __shfl(own, STEP * i + u * SIDE + sub, 64);
-                R::ask(a, (unsigned)page[u] < (unsigned)a.n_pages ? page[u] : 0, h, lane, raw[u]);
+                const int page = __shfl(own, STEP * i + u * SIDE + sub, 64);
+                R::ask(a, (unsigned)page < (unsigned)a.n_pages ? page : 0, h, lane, raw[u]);
             }
         };
         ask(0);
         for (int i = 0; i < STEPS && p + i * stride < p1; ++i) {
             u32x4 now[4][R::VPL];
-            bool there[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                there[u] = (unsigned)page[u] < (unsigned)a.n_pages;
+            for (int u = 0; u < 4; ++u)
 #pragma unroll
                 for (int v = 0; v < R::VPL; ++v) now[u][v] = raw[u][v];
-            }
+            const int mine = __shfl(own, STEP * i + (lane & 3) * SIDE + sub, 64);
             if (i + 1 < STEPS && p + (i + 1) * stride < p1) ask(i + 1);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const double s = r.score(now[u]);
-                const int at = p + i * stride + u * SIDE + sub;
-                if (at < p1) leave(at, there[u] ? score_key(s) : ~0ull);
-            }
+            const unsigned long long key = score_key(r.scores(now, lane));
+            const int at = p + i * stride + (lane & 3) * SIDE + sub;
+            if (at < p1 && lane % R::LANES < 4) leave(at, (unsigned)mine < (unsigned)a.n_pages ? key : ~0ull);
         }
     }
 }
@@ -515,7 +517,7 @@ template <typename T, int K> __global__ __launch_bounds__(256) void score_kernel
     if (have <= a.pages || first >= have - a.last) return;              // (all of them are taken)
     unsigned long long *keys = a.keys + ((long long)b * a.Hk + hh) * a.max_pages_seen;
     score_pages<T, K, true>(a, r, table, hh, own, first, have - a.last, stride, lane, [&](int p, unsigned long long key) {
-        if (lane % R::LANES == 0 && h < a.Hk) keys[p] = key;
+        if (h < a.Hk) keys[p] = key;
     });
 }
 
@@ -644,7 +646,7 @@ template <typename T, int K, int EACH, bool SCORE> __global__ __launch_bounds__(
     const unsigned long long *keys = a.keys + (long long)blockIdx.x * a.max_pages_seen + begin;
     if constexpr (SCORE) {
         score_pages<T, K, false>(a, r, table, h, own, begin + wave * P::STEP, end, STRIDE, lane, [&](int p, unsigned long long key) {
-            if (lane % R::LANES == 0) made[p - begin] = key;
+            made[p - begin] = key;
         });
         __syncthreads();
         keys = made;
