@@ -587,7 +587,8 @@ static int check_decode(const osdn_decode_params *p, bool mx, bool heads_togethe
     a.head_tiles = (a.group + 15) / 16;
     a.part_heads = a.group < 16 ? a.group : 16;
     const int rows = a.Hk * a.head_tiles;
-    const DecodePlan plan = decode_plan(a.B, rows, p->max_length, p->window, p->K, p->io_dtype == OSDN_BF16, a.part_heads, (heads_together && !pages) || a.head_tiles > 1, p->shares, mx);
+    const DecodePlan plan = decode_plan(a.B, rows, p->max_length, p->window, p->K, p->io_dtype == OSDN_BF16, a.part_heads,
+                                        (pages ? mx : heads_together) || a.head_tiles > 1, p->shares, mx);
     const long long groups = (long long)a.B * rows / plan.row_group;
     if (groups * plan.units > 0x7fffffffLL) return OSDN_ERR_SHAPE;     // (units are counted in 32 bits)
     a.row_group = plan.row_group;

@@ -131,8 +131,8 @@ template <typename IO, int W, bool C = false> struct RowTile {
 // A row of K elements is K / 2 bytes of codes and K / 32 scales.  Its four lanes take K / 4 adjacent elements each, whole words of eight codes, which one
 // instruction a pair turns into the bf16 numbers that they stand for, exactly; the order of a row's elements is the same on both sides of
 // the first product, so nothing is passed between lanes.  Values go through LDS as bf16.  fp32 queries and weights are sums of three bf16 numbers, which hold all their digits.
-// REGULAR (fp4_regular): a row's place in all four arrays comes of one offset.
-template <typename IO, int W, bool REGULAR, bool C = false> struct Fp4Tile {
+// REGULAR (fp4_regular): a row's place in all four arrays comes of one offset.  ONCE (decode_mx_once): the codes are loaded past the caches.
+template <typename IO, int W, bool REGULAR, bool C = false, bool ONCE = false> struct Fp4Tile {
     using T = IO;
     using V = bf16;                                     // of the values in LDS
     static constexpr int K = W;
@@ -207,7 +207,7 @@ template <typename IO, int W, bool REGULAR, bool C = false> struct Fp4Tile {
         } else {
 #pragma unroll
             for (int w = 0; w < WORDS; w += 4) {
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(codes + 4 * w);
+                const u32x4 *at = reinterpret_cast<const u32x4 *>(codes + 4 * w), x = ONCE ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) c.word[w + e] = x[e];
             }

@@ -340,11 +340,18 @@ inline long long decode_span(int max_length, int window) {
 //  - four rows together from two rows a CU on: a share then begins fewer rows (uneven 512 x 4096, one by one 145, so 128; 64 x 8192 x 8 76.5 and 65.8; but 1 x 131072 x 8, whose rows all
 //    shares cut, 34.8 and 37.1).
 //  - two shares a CU, four for rows of 64 elements and where there is about a row for each (uneven 64 x 4096 x 8, K = 64, 256, 512, 768 and 1024 34.4, 27.4, 26.7, 25.5; 40 x 4000 x 8,
-//    K = 256, 84.3, 65.1, 58.8, 55.9; but 1 x 131072 x 8 44.6, 34.8, 37.8, 37.1; 16 x 8192 x 8 42.1, 34.7, 38.1, 37.5).
+//    K = 256, 84.3, 65.1, 58.8, 55.9; but 1 x 131072 x 8 44.6, 34.8, 37.8, 37.1; 16 x 8192 x 8 42.1, 34.7, 38.1, 37.5); three for many rows of 128 whose heads lie apart, the codes past the caches (512, 768, 1024: uneven
+//    512 x 4096 119, 115.5, 118.7, 64 x 4096 x 4 33.9, 27.9, 29.9, fp32 256 x 4096 x 8 128, 121, 131, even 64 x 8192 x 8 107, 107.5, 104; heads side by side uneven 512 x 4096 140.5, 145, 146).
 inline bool decode_mx_each(long long span, long long all, int K) {
     return span <= (all >= 2 * NUM_CU ? 3000 : all >= NUM_CU ? 2048 : K == 256 ? 384 : 768);
 }
 struct DecodePlan { int row_group, shares; long long units; };
+// Whether a call over a cache in 4 bits (K = 128) loads its codes past the caches: rows of a head lie next to each other, so that one load takes whole lines of 128 bytes, and the rows that it may
+// read are more than 64 MB, a quarter of the memory-side cache, from which a program that comes back to less of them soon would have them (us, through the caches and past them: uneven
+// 512 x 4096 x 4 heads 131 and 121, 512 x 1000 x 4 59.8 and 57.2, 64 x 4096 x 4 39.7 and 36.1, 4 x 32768 x 8 38.1 and 35.3, 1 x 131072 x 8 38.2 and 37.5; but 512 x 200 x 4, called again on
+// what the memory-side cache holds, 18.7 and 21.0, 1 x 32768 x 8 16.4 and 17.0; heads side by side, whose lines two wavefronts share, uneven 512 x 4096 x 4 142 and 148.  K = 64, of whose lines a load
+// takes eight bytes a lane, 26.7 and 31.0, K = 256, half lines, 62.6 and 66.0.)
+constexpr bool decode_mx_once(long long rows, long long token_step) { return token_step == 64 && rows * 136 > 64LL << 20; }
 inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K, bool bf16, int part_heads, bool heads_together, int asked, bool mx = false) {
     const long long span = decode_span(max_length, window), all = (long long)B * rows;
     const int tile = mx ? DECODE_MX_TILE : decode_tile(K, bf16), alone = mx ? decode_mx_unit(1) : decode_unit(K, bf16, 1), held = (mx ? decode_mx_per_cu(K, bf16) : decode_per_cu(K, bf16)) * NUM_CU;
@@ -358,7 +365,7 @@ inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K
     const int unit = mx ? decode_mx_unit(p.row_group) : decode_unit(K, bf16, p.row_group);
     p.units = span < 1 ? 1 : (span + unit - 1) / unit;
     const long long groups = all / p.row_group;
-    const int per_cu = mx ? (K == 64 || (all >= NUM_CU && all < 2 * NUM_CU) ? 4 : 2) : all <= 16 || (K == 256 && !bf16) || (K == 128 && bf16 && p.row_group == 4 && span > 1024) ? 1 : K == 64 && p.row_group < 4 ? 3 : 2;
+    const int per_cu = mx ? (K == 128 && !heads_together && all >= NUM_CU ? 3 : K == 64 || (all >= NUM_CU && all < 2 * NUM_CU) ? 4 : 2) : all <= 16 || (K == 256 && !bf16) || (K == 128 && bf16 && p.row_group == 4 && span > 1024) ? 1 : K == 64 && p.row_group < 4 ? 3 : 2;
     const long long worth = groups * span / (16 * part_heads), most = per_cu * NUM_CU < worth ? per_cu * NUM_CU : worth > NUM_CU ? worth : NUM_CU;
     p.shares = each ? 0 : asked > 0 ? asked : (int)(groups * p.units < most ? groups * p.units : most);
     return p;

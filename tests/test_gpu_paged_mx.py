@@ -291,6 +291,15 @@ def test_decode(case):
     compare(x, *call(x, max_length=x["longest"] + 777 if x["longest"] + 777 <= x["table"].shape[1] * page else x["longest"]))
 
 
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [1, 4, 20])
+def test_rows_that_may_be_many(io, group):
+    """A bound of the lengths beyond 2^19 rows of 128 elements: their codes are loaded past the caches, in shares and a row each; the lengths themselves stay small."""
+    for B, lengths in ((3, [1531, 0, 77]), (130, [1 + 37 * b % 530 for b in range(130)])):
+        x = make_decode(lengths, 4 * group, 4, 128, 16, io)
+        compare(x, *call(x, max_length=65536 if B == 3 else 2000))
+
+
 def test_decode_slices_several_queries_and_scale():
     x = make_decode([200, 33], 8, 2, 128, 16)
     wide = torch.randn(2, 12, 128, device="cuda").bfloat16()
