@@ -652,7 +652,10 @@ static int decode_impl(const osdn_decode_params *p, const Cache *cache, const os
         a.info = reinterpret_cast<int *>(a.part_ml + parts * 2);
     }
     take_cache(&c, a.cache_k, a.cache_v, a.scale_k, a.scale_v);
-    if constexpr (mx) a.regular = fp4_regular(a);
+    if constexpr (mx) {
+        a.regular = fp4_regular(a);
+        a.side_by_side = c.k_head < c.k_token;
+    }
     a.table = c.table; a.table_stride = c.table_stride; a.lengths = lengths; a.seq = seq; a.lse = lse;
     a.n_pages = c.n_pages; a.n_seqs = c.n_seqs; a.max_pages = c.max_pages;
     hipStream_t st = static_cast<hipStream_t>(stream);

@@ -115,6 +115,14 @@ template <bool CHOSEN> __device__ __forceinline__ Entry entry_of(const DecodeArg
     return {i, b - i * a.table_heads};
 }
 
+// Blocks go to the eight XCDs in turn.  The block whose work number w does so that the `of` of a sequence are on one XCD, and the sequences (but for the last few) go round: heads side by
+// side share lines of 128 bytes, which then cross to one L2.  (us, in the order of their numbers and so: 512 x 1000 tokens, four heads of K = 128 in 4 bits side by side 91.2 and 69.7, uneven
+// 51.6 and 46.0, 32 x 2000 x 8 28.5 and 20.8, uneven 300 x 1500 x 8, K = 64, 79 and 58; 8 heads' own 32 of at most 128 pages of 32 tokens 23.8 and 21.1.  Heads apart: 57.8 and 57.9.)
+__device__ __forceinline__ int by_sequence(int w, int of) {
+    const int x = w & 7, i = w >> 3, s = i / (unsigned)of;
+    return w < (int)(gridDim.x - gridDim.x % (8u * of)) ? (8 * s + x) * of + (i - s * of) : w;
+}
+
 // SHARED: even shares; else a workgroup takes one group of rows, whole (short ones, or many: no search and no second kernel)
 template <typename D, int R, bool SHARED>
 __global__ __launch_bounds__(DEC_T, D::PER_CU) void decode_kernel(DecodeArgs a) {
@@ -128,7 +136,10 @@ __global__ __launch_bounds__(DEC_T, D::PER_CU) void decode_kernel(DecodeArgs a) 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     ask_arguments(a);
     D::ask_arguments(a);
-    const int groups = a.Hk * a.head_tiles / R, w = blockIdx.x;     // groups of rows of a sequence
+    const int groups = a.Hk * a.head_tiles / R;                     // groups of rows of a sequence
+    int w = blockIdx.x;
+    if constexpr (D::BY_SEQUENCE && !SHARED)
+        if (a.side_by_side) w = by_sequence(w, groups * a.table_heads);
     const int turn = wave % WPR;                                    // this wavefront's among those of its row
     // This workgroup's share: units [at, until), the first of them of sequence b, whose units start at `base`
     int b, base, at, until, total = 0;

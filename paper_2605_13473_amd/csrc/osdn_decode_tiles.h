@@ -12,7 +12,7 @@ template <typename IO, int W, bool C = false> struct RowTile {
     using T = IO;
     using V = IO;                                       // of the values in LDS
     static constexpr int K = W;
-    static constexpr bool CHOSEN = C;                   // a table for each key head
+    static constexpr bool CHOSEN = C, BY_SEQUENCE = false;      // CHOSEN: a table for each key head; BY_SEQUENCE: see by_sequence
     static constexpr bool BF = sizeof(T) == 2;
     static constexpr int PER_CU = decode_per_cu(K, BF);
     static constexpr int TT = decode_tile(K, BF);       // tokens: the depth of the second product's matrix instruction (fp32: four of them)
@@ -136,7 +136,7 @@ template <typename IO, int W, bool REGULAR, bool C = false, bool ONCE = false> s
     using T = IO;
     using V = bf16;                                     // of the values in LDS
     static constexpr int K = W;
-    static constexpr bool CHOSEN = C;
+    static constexpr bool CHOSEN = C, BY_SEQUENCE = true;
     static constexpr bool BF = sizeof(T) == 2;
     static constexpr int PER_CU = decode_mx_per_cu(K, BF);
     static constexpr int TT = DECODE_MX_TILE;

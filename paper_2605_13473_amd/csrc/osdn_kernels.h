@@ -290,7 +290,7 @@ struct DecodeArgs {
     int *info;
     // a cache in 4 bits, its steps in bytes (last: a cache of whole rows does not ask for them); regular: see fp4_regular
     HeadRows scale_k, scale_v;
-    bool regular;
+    bool regular, side_by_side;             // side_by_side: the heads of a token lie next to each other
 };
 int launch_paged_decode(const DecodeArgs &a, bool bf16_io, hipStream_t st);
 int launch_paged_decode_mx(const DecodeArgs &a, bool bf16_io, hipStream_t st);

@@ -495,7 +495,8 @@ PyObject *paged_plan(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const at::Tensor all = at::empty({slot_bytes + 4 * (2 * N + 2 * B + 2)}, t[0]->options().dtype(at::kByte));
     const auto take = [&](int64_t at, at::IntArrayRef sizes) { return piece(all, at::kInt, slot_bytes + 4 * at, sizes); };
     const at::Tensor pos = take(0, at::IntArrayRef(line, 2)), rows = take(N, at::IntArrayRef(line, 2)), lengths = take(2 * N, b), starts = take(2 * N + B, at::IntArrayRef(&b1, 1));
-    at::Tensor left = at::empty({1}, t[0]->options()), slots;           // (kept from call to call: not with the rest)
+    const at::Tensor left = take(2 * N + 2 * B + 1, at::IntArrayRef(&one, 1));
+    at::Tensor slots;
     if (slot_bytes) slots = piece(all, at::kLong, 0, at::IntArrayRef(&N, 1));
     int32_t *l = ints(lengths), *s = ints(starts), *p = ints(pos), *r = ints(rows), *f = ints(left);
     int64_t *sl = slots.defined() ? static_cast<int64_t *>(slots.data_ptr()) : nullptr;

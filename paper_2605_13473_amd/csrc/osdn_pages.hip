@@ -256,8 +256,8 @@ __global__ __launch_bounds__(PLAN_T) void release_kernel(PlanArgs a) {
 int launch_plan(const PlanArgs &a, hipStream_t st) {
     const size_t lds = a.seq ? (size_t)((a.n_seqs + 31) / 32) * 8 : 0;
     const bool over_itself = a.lengths == a.cached || a.lengths == a.fresh || a.n_free_out == a.n_free;
-    const int workgroups = plan_workgroups(a.N), per = (a.N + workgroups - 1) / workgroups;
-    if (workgroups == 1 || !over_itself) {
+    const int workgroups = over_itself ? 1 : plan_workgroups(a.N), per = (a.N + workgroups - 1) / workgroups;
+    if (!over_itself || a.N <= 4096) {
         hipLaunchKernelGGL(plan_kernel, dim3(workgroups), dim3(PLAN_T), lds, st, a, per);
     } else {
         hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(PLAN_T), lds, st, a, 0);

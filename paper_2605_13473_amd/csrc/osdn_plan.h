@@ -371,8 +371,9 @@ inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K
     return p;
 }
 
-// Workgroups for the places of a batch's tokens, each of which makes the batch's running sums for itself
-inline int plan_workgroups(int tokens) { return tokens <= 4096 ? 1 : (int)((tokens + 4095LL) / 4096 < NUM_CU ? (tokens + 4095LL) / 4096 : NUM_CU); }
+// Workgroups for the places of a batch's tokens, each of which makes the batch's running sums for itself (us, of 4096, 2048 and 1024 tokens each: 96 requests of 683 7.2, 6.1, 5.9, 2000 of 30
+// 13.1, 11.5, 10.8, 32 of 128 6.3, 5.1, 4.7)
+inline int plan_workgroups(int tokens) { return tokens <= 1024 ? 1 : (int)((tokens + 1023LL) / 1024 < NUM_CU ? (tokens + 1023LL) / 1024 : NUM_CU); }
 // Rows of a page table that a call with an index of them may have (two bits each in LDS)
 constexpr int PLAN_MAX_ROWS = 1 << 17;
 // Selection of pages: whether a row's workgroup makes the scores itself, which saves a launch, or a launch of many workgroups does.  bytes: of a page's bounds.  (us, a launch of their own

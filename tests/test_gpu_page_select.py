@@ -130,6 +130,7 @@ SELECT = [
     dict(lengths=[9000, 40], Hq=6, Hk=3, K=64, page=2, n=33, order="page_inside"),
     dict(lengths=[700, 701], Hq=9, Hk=9, K=64, page=16, n=5, first=2, last=3),
     dict(lengths=[50, 20], Hq=4, Hk=2, K=128, page=16, n=60),
+    dict(lengths=[(97 * b) % 260 for b in range(19)], Hq=6, Hk=3, K=64, page=8, n=9, order="token"),
 ]
 
 

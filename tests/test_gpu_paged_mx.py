@@ -300,6 +300,15 @@ def test_rows_that_may_be_many(io, group):
         compare(x, *call(x, max_length=65536 if B == 3 else 2000))
 
 
+@pytest.mark.parametrize("Hq,Hk,K", [(6, 3, 64), (8, 4, 128), (18, 1, 64), (4, 4, 256), (40, 2, 128)])
+def test_heads_side_by_side(Hq, Hk, K):
+    """More sequences than XCDs, and some over: the workgroups of a sequence on one of them."""
+    x = make_decode([(97 * b) % 260 for b in range(19)], Hq, Hk, K, 8, order="token")
+    compare(x, *call(x))
+    x = make_decode([(97 * b) % 260 for b in range(16)], Hq, Hk, K, 8, order="token", shares=-1)
+    compare(x, *call(x))
+
+
 def test_decode_slices_several_queries_and_scale():
     x = make_decode([200, 33], 8, 2, 128, 16)
     wide = torch.randn(2, 12, 128, device="cuda").bfloat16()

@@ -185,7 +185,7 @@ def test_places_in_place_and_in_a_graph():
         assert torch.equal(table.cpu(), x["table"])
 
 
-@pytest.mark.parametrize("tokens", [40, 9000])
+@pytest.mark.parametrize("tokens", [40, 3500, 9000])
 def test_outputs_over_the_inputs(tokens):
     """The same numbers where lengths and the count of free pages stand in the place of what they come from, for few tokens and for many."""
     x = make([3, 0, 70, 15, 16, 1], [1, 30, 0, 1, 3, 2] if tokens == 40 else [1, 3000, 0, 2000, 3, 2500], 8, rows=9, order="any")

@@ -61,9 +61,9 @@ def test_attention_over_4_bits(rule):
 
 
 def test_places_of_many_tokens(rule):
-    asked = [(n,) for n in (1, 256, 4096, 4097, 8192, 65536, 10 ** 6, 2 ** 20, 2 ** 21, 2 ** 31 - 1)]
+    asked = [(n,) for n in (1, 256, 1024, 1025, 4096, 4097, 8192, 65536, 10 ** 6, 2 ** 20, 2 ** 21, 2 ** 31 - 1)]
     for (n,), (w,) in zip(asked, rule("plan", asked)):
-        assert 1 <= w <= 256 and (w == 1) == (n <= 4096)
+        assert 1 <= w <= 256 and (w == 1) == (n <= 1024)
         per = -(-n // w)
         assert (w - 1) * per < n <= w * per and w * per < 2 ** 31 + 256             # every part begins inside
 
