@@ -10,7 +10,7 @@ template <int K> using Fp4Bf16Any = Fp4Tile<bf16, K, false>;
 template <int K> using Fp4F32Any = Fp4Tile<float, K, false>;
 int launch_paged_decode_mx(const DecodeArgs &a, bool bf16_io, hipStream_t st) {
     const int span = a.window && a.window < a.max_length ? a.window : a.max_length;
-    if (a.regular && a.K == 128 && decode_mx_once((long long)a.B * a.Hk * span, a.cache_k.token)) {
+    if (a.regular && a.K == 128 && decode_mx_once((long long)a.B * a.Hk * span, a.cache_k.token, false)) {
         if (bf16_io) decode_of<Fp4Tile<bf16, 128, true, false, true>>(a, st);
         else decode_of<Fp4Tile<float, 128, true, false, true>>(a, st);
         return 0;

@@ -148,6 +148,17 @@ def test_select_and_attend(case, form):
     check_choice(x, bounds, n, first, last, max_length=x["longest"] + 555 if -(-(x["longest"] + 555) // x["page"]) <= x["table"].shape[1] else None)
 
 
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_chosen_rows_that_may_be_many(io):
+    """A bound of the tokens that makes them 2^19 rows of 128 elements in 4 bits: their codes are loaded past the caches."""
+    x = make([700, 41, 0, 260], 6, 3, 128, 8, io, "token", mx=True)
+    chosen, tokens = check_choice(x, bounds_of(x), 20)
+    check_attention(x, chosen, tokens, max_length=1 << 17)
+    x = make([700, 41, 0, 260], 6, 3, 128, 8, io, mx=True)
+    chosen, tokens = check_choice(x, bounds_of(x), 20)
+    check_attention(x, chosen, tokens, max_length=1 << 17)
+
+
 def test_equal_scores_go_to_the_earlier_page():
     x = make([640, 640], 4, 2, 64, 8)
     b = bounds_of(x)
