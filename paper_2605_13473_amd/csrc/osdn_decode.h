@@ -10,7 +10,7 @@
 // The visible tokens of all groups of R rows make one list that is cut into even shares, one a workgroup, whatever the lengths; a share is
 // a part of a group, or the end of one, whole ones and the beginning of the last.  Rows that a share does not hold whole go to a second
 // kernel, which joins their parts in their order.
-// 2.1 GB of keys and values of 512 sequences of 1 to 4096 tokens: 371 us, 5.8 TB/s (cut into pieces of 1024 tokens, a workgroup each, 22 more); 0.54 GB of
+// Rows of bf16: 2.1 GB of keys and values of 512 sequences of 1 to 4096 tokens: 371 us, 5.8 TB/s (cut into pieces of 1024 tokens, a workgroup each, 22 more); 0.54 GB of
 // one sequence 97 us, 5.5 TB/s; reading alone reaches 5.9.  (Calls among others.)  The second kernel takes 3 to 6 us; the fence that a join inside the
 // first would take after every part costs more (900 and 180 us).
 //

@@ -378,10 +378,10 @@ inline int plan_workgroups(int tokens) { return tokens <= 1024 ? 1 : (int)((toke
 // Rows of a page table that a call with an index of them may have (two bits each in LDS)
 constexpr int PLAN_MAX_ROWS = 1 << 17;
 // Selection of pages: whether a row's workgroup makes the scores itself, which saves a launch, or a launch of many workgroups does.  bytes: of a page's bounds.  (us, a launch of their own
-// and so: 4 rows of 256 pages of 512 bytes 8.1 and 9.6, 64 9.0 and 8.8, 128 11.9 and 10.8, 128 of 256 bytes 9.1 and 7.0; 64 rows of 512 12.4 and 15.7, 384, uneven, 22.3 and 22.8; 256 of 1024 41
-// and 35; 512, uneven, of 128 14.5 and 11.3; 8 of 4096 16 and 85.)
+// and so, pages of 512 bytes: 4 rows of 128 8.0 and 6.8, of 256 7.7 and 8.1, 8 of 4096 14.6 and 60; 64 rows of 256 9.4 and 8.9, of 512 12.1 and 12.2, of 768 14.3 and 16.4, of 1024 in fp32
+// 14.8 and 16.2; 128 of 512 14.7 and 12.8, uneven 13.2 and 12.4; 256 of 1024 38.5 and 33.9, of 4096 124 and 109; uneven 384 of 512 19.1 and 18.0, 512 of 128 13.5 and 10.1.)
 inline bool select_scores_itself(long long rows, int pages, int bytes) {
-    return pages <= 4096 && (rows >= NUM_CU || (long long)pages * bytes <= (rows >= 64 ? 1 << 17 : 1 << 16));
+    return pages <= 4096 && (rows >= NUM_CU || (long long)pages * bytes <= (rows >= 64 ? 1 << 18 : 1 << 16));
 }
 // Workgroups (four wavefronts, four pages each at a time) for the scores of a sequence's pages of one group of key heads
 inline unsigned select_chunks(int B, int Hk, int heads, int pages) {
