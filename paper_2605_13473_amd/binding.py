@@ -7,7 +7,8 @@ streams only), check dtype / contiguity / device, and pass raw pointers.  Every 
 the computation runs in the HIP library; there is no fallback of any kind: if the shared
 object is missing this module raises.
 
-``forward`` / ``backward`` are conveniences that allocate the outputs and the workspace.
+``forward`` / ``backward`` are conveniences that allocate the outputs and the workspace; ``qk_norm``, ``paged_append``, ``paged_decode`` and the operators on
+a cache's pages (``paged_plan`` .. ``paged_decode_pages_mx``) are, too.
 """
 from __future__ import annotations
 
