@@ -396,7 +396,7 @@ typedef struct {
  *   positions, rows   [tokens] int32 out: position and sequence of every token (-1 and -1 behind the last), as osdn_paged_append takes them
  *   slots             [tokens] int64 out or NULL: page * page_size + place in the page; -1 behind the last, and where the page is not there
  * Not served either, and without a part in the sums: a request whose sequence is not in the table, whose cached or fresh is negative or whose
- * tokens its row of the table does not hold; and those that bring tokens to a sequence that another one brings some too.
+ * tokens its row of the table or 31 bits do not hold; and those that bring tokens to a sequence that another one brings some too.
  * (lengths: 0 where the sequence is not in the table or cached is negative.)  B is at most 65535, tokens at least 1;
  * with seq, n_seqs is at most 131072.
  */
@@ -407,7 +407,8 @@ int osdn_paged_plan(const osdn_pages *pages, int32_t B, int32_t tokens, const in
 /*
  * The pages of B sequences that end go back onto the list, and their entries of the table become -1: the first
  * ceil(lengths[b] / page_size) of row seq[b], those that are there.  They lie so that the next requests take them in the order that they
- * had.  A sequence that is named twice keeps its pages.  What the list has no room for is dropped.  Limits as for osdn_paged_plan, and
+ * had.  A sequence that is named twice keeps its pages; a page that stands in two rows goes back with each of them (pages that sequences
+ * share are the caller's to keep track of).  What the list has no room for is dropped.  Limits as for osdn_paged_plan, and
  * up to 1024 B as many times max_pages entries of the table at most 2^30.
  */
 int osdn_paged_release(const osdn_pages *pages, int32_t B, const int32_t *lengths, const int32_t *seq, const int32_t *n_free,

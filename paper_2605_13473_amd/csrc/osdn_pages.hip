@@ -94,7 +94,7 @@ __global__ __launch_bounds__(PLAN_T) void plan_kernel(PlanArgs a, int per) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), words = (a.n_seqs + 31) / 32;
     const int P = 1 << a.page_shift, begin = min(a.N, (int)blockIdx.x * per), end = min(a.N, begin + per);
     const bool grants = blockIdx.x == 0;
-    const long long capacity = (long long)a.max_pages << a.page_shift;
+    const long long capacity = min((long long)a.max_pages << a.page_shift, 0x7fffffffLL);
     const int have = max(0, min(*a.n_free, a.free_capacity));
     if (a.seq) note_rows(bits, words, a.n_seqs, a.B, a.seq, a.fresh);
     TwoSums asked{0u, 0u}, given{0u, 0u};           // of the requests before this round's: pages and tokens, asked for and given

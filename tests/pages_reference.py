@@ -15,7 +15,7 @@ def plan(table, cached, fresh, seq, free, n_free, page, tokens, n_pages):
     lengths, starts, pos, rows, slots = [], [0], [], [], []
     for s, c, f in zip(seq.tolist(), cached.tolist(), fresh.tolist()):
         known = 0 <= s < n_seqs
-        valid = known and c >= 0 and f >= 0 and c + f <= max_pages * page and not (f > 0 and names.count(s) > 1)
+        valid = known and c >= 0 and f >= 0 and c + f <= min(max_pages * page, 2 ** 31 - 1) and not (f > 0 and names.count(s) > 1)
         c = c if known and c >= 0 else 0
         f = f if valid else 0
         first = -(-c // page)

@@ -237,3 +237,21 @@ def test_several_queries_of_a_sequence_and_more_than_a_launch_takes():
         assert torch.equal(c, chosen[s]) and torch.equal(t, tokens[s])
         y_o, y_lse = check_attention(y, c, t)
         assert torch.allclose(o[s].float(), y_o.float(), atol=2.0 ** -7, rtol=2.0 ** -7)
+
+
+def test_bounds_past_32_bits():
+    """2^21 + 64 pages, whose bounds are 4.3 GB: those of the last ones, selected as from a small array."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    far, Hk, K = 1 << 21, 4, 128
+    keys = torch.zeros(far + 64, 1, Hk, K, dtype=torch.bfloat16, device="cuda")
+    keys[far:] = rnd(g, 64, 1, Hk, K).bfloat16()
+    table = torch.randperm(64, device="cuda", generator=g).int()[None]
+    q, n, none = rnd(g, 1, 8, K).bfloat16(), i32([60]).cuda(), i32([0]).cuda()
+    small, large = ob.alloc_page_bounds(64, Hk, K).zero_(), torch.zeros(far + 64, Hk, 2, K, dtype=torch.bfloat16, device="cuda")
+    ob.page_bounds(keys[far:], table, none, n, small)
+    ob.page_bounds(keys, table + far, none, n, large)
+    assert torch.equal(large[far:], small) and not bool(large[:1000].any())
+    a, b = ob.page_select(q, small, table, n, 1, 7), ob.page_select(q, large, table + far, n, 1, 7)
+    assert torch.equal(a[0] + far, b[0]) and torch.equal(a[1], b[1])
+    got, want = ob.paged_decode_pages(q, keys, keys, *b), ob.paged_decode_pages(q, keys[far:], keys[far:], *a)
+    assert torch.equal(got, want)

@@ -408,3 +408,25 @@ def test_append_read_and_attend_in_a_graph(io):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
         assert all(torch.equal(a, b) for a, b in zip(eager, graphed))
+
+
+@pytest.mark.parametrize("step", [3 << 30, 5 << 30])
+def test_offsets_past_32_bits(step):
+    """Pages 3 (one rule finds a row's place in all four arrays) and 5 GiB apart: what is appended, read and attended to is that of a small cache, to the bit."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    far = [torch.zeros(2 * s + 2048, dtype=torch.uint8, device="cuda").as_strided((3, 8, 2, n), (s, 2 * n, n, 1)) for n, s in ((64, step), (64, step), (4, step // 16), (4, step // 16))]
+    near = [t.clone() for t in make_cache(g, 3, 8, 2, 128, "token")]
+    for a, b in zip(far, near):
+        a.copy_(b)
+    table = torch.tensor([[2, 0, 1]], dtype=torch.int32, device="cuda")
+    k, v, q = rnd(g, 1, 21, 2, 128).bfloat16(), rnd(g, 1, 21, 2, 128).bfloat16(), rnd(g, 1, 4, 128).bfloat16()
+    pos, n = torch.arange(2, 23, dtype=torch.int32, device="cuda")[None], torch.tensor([23], dtype=torch.int32, device="cuda")
+    got = []
+    for cache in (tuple(near), tuple(far)):
+        ob.paged_append_mx(k, v, cache, table, pos, hp=ob.NormHyper("rms"))
+        bounds = ob.alloc_page_bounds(3, 2, 128).zero_()
+        ob.page_bounds((cache[0], cache[2]), table, torch.zeros_like(n), n, bounds)
+        chosen, tokens = ob.page_select(q, bounds, table, n, 8, 2)
+        got.append([*ob.paged_read_mx(cache, table, pos), ob.paged_decode_mx(q, cache, table, n), bounds, chosen, ob.paged_decode_pages_mx(q, cache, chosen, tokens)])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)

@@ -65,6 +65,16 @@ def test_plan(case, extra):
     check_plan(x, max(1, sum(case["fresh"]) + extra), use_seq=case.get("order") == "any")
 
 
+def test_lengths_that_31_bits_do_not_hold():
+    """A row of the table that holds more than 2^31 tokens: the request that would pass them is not served, one that ends at them is."""
+    top = 2 ** 31 - 1
+    for fresh in ([5, 1, 0], [4, 1, 3]):
+        x = make([0, 0, 0], fresh, 2 ** 16, spare=9, max_pages=2 ** 15 + 4)
+        x["cached"] = i32([top - 4, 7, top])
+        check_plan(x, 40)
+        check_plan(x, 4000)
+
+
 @pytest.mark.parametrize("spare", [0, 1, 2, 5, 11])
 def test_pages_that_do_not_do_for_all(spare):
     x = make([3, 0, 8, 15, 16, 1], [1, 30, 8, 1, 40, 2], 8, spare=spare)
