@@ -397,7 +397,7 @@ typedef struct {
  *   slots             [tokens] int64 out or NULL: page * page_size + place in the page; -1 behind the last, and where the page is not there
  * Not served either, and without a part in the sums: a request whose sequence is not in the table, whose cached or fresh is negative or whose
  * tokens its row of the table or 31 bits do not hold; and those that bring tokens to a sequence that another one brings some too.
- * (lengths: 0 where the sequence is not in the table or cached is negative.)  B is at most 65535, tokens at least 1;
+ * (lengths: 0 where the sequence is not in the table or cached is negative.)  B is at most 65535, tokens from 1 to 2^30;
  * with seq, n_seqs is at most 131072.
  */
 int osdn_paged_plan(const osdn_pages *pages, int32_t B, int32_t tokens, const int32_t *cached, const int32_t *fresh, const int32_t *seq,

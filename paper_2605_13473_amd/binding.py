@@ -815,7 +815,7 @@ def paged_plan(page_table, cached, fresh, free_pages, n_free, page_size: int, to
     B, N = _requests(cached, "cached"), int(tokens)
     g = _pages(page_table, page_size, free_pages.numel() if n_pages is None and isinstance(free_pages, torch.Tensor) else n_pages or 0, free_pages)
     new = lambda *shape, dtype=torch.int32: torch.empty(*shape, dtype=dtype, device=page_table.device)
-    if N < 0 or N > 2**31 - 1:
+    if N < 0 or N > 2**30:
         raise OsdnError(OSDN_ERR_SHAPE)
     r = {"lengths": new(B), "starts": new(B + 1), "positions": new(1, N), "seq": new(1, N), "n_free": new(1),
          "slots": new(N, dtype=torch.int64) if want_slots else None}
@@ -1053,7 +1053,7 @@ def osdn_paged_decode_pages_mx(params, q, cache, chosen, tokens, o, lse, workspa
 def page_bounds(keys, page_table, cached, lengths, bounds, seq=None, max_new=None):
     """Keep the bounds of the pages up with what was appended: the tokens cached[b] <= i < lengths[b] of sequence seq[b] (None: b).  keys: those of
     a cache [n_pages, page_size, Hk, K], or (codes, scales) of one in 4 bits.  bounds [n_pages, Hk, 2, K] are written in place.
-    max_new: no sequence gets more new tokens (None: what a row of the table can hold)."""
+    max_new: no sequence gets more new tokens (None: what a row of the table can hold; the launch is sized by it)."""
     mx = isinstance(keys, (tuple, list))
     k = keys[0] if mx and len(keys) == 2 else keys
     if _rows_native is not None and type(bounds) is torch.Tensor and bounds.is_cuda and (not mx or len(keys) == 2):

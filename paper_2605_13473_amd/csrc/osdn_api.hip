@@ -707,7 +707,7 @@ int osdn_paged_plan(const osdn_pages *pages, int32_t B, int32_t tokens, const in
     int shift = 0;
     const int rc = check_pages(pages, true, seq != nullptr, shift);
     if (rc != OSDN_OK) return rc;
-    if (B < 1 || B > 65535 || tokens < 1) return OSDN_ERR_SHAPE;
+    if (B < 1 || B > 65535 || tokens < 1 || tokens > 1 << 30) return OSDN_ERR_SHAPE;
     if (!cached || !fresh || !n_free || !n_free_out || !lengths || !starts || !positions || !rows) return OSDN_ERR_NULL;
     PlanArgs a = plan_args(pages, B, shift);
     a.N = tokens; a.cached = cached; a.fresh = fresh; a.seq = seq; a.n_free = n_free; a.n_free_out = n_free_out;

@@ -484,7 +484,7 @@ PyObject *paged_plan(PyObject *, PyObject *const *a, Py_ssize_t n) {
     int32_t tokens;
     const int32_t *cached, *fresh, *seq, *n_free;
     if (n != 12 || !ordinary() || !tensors(a, 6, t) || !device_and_stream(a[10], a[11], dev, stream) || !t[1] || t[1]->dim() != 1 || !PyBool_Check(a[9]) ||
-        !int_of(a[7], tokens) || tokens < 1 || !pages_of(t[0], t[3], a[6], a[8], dev, g))
+        !int_of(a[7], tokens) || tokens < 1 || tokens > 1 << 30 || !pages_of(t[0], t[3], a[6], a[8], dev, g))
         Py_RETURN_NONE;
     const int64_t B = t[1]->size(0), one = 1;
     const at::IntArrayRef b(&B, 1);

@@ -462,7 +462,7 @@ template <typename T, int K> struct ScoreRow {
 __device__ __forceinline__ Seen pages_seen(const SelectArgs &a, int b) {
     return seen_tokens(a.lengths[b], a.seq ? a.seq[b] : b, a.n_seqs, a.max_length, 0, a.page_shift, a.max_pages);
 }
-__device__ __forceinline__ int pages_of(const SelectArgs &a, const Seen &see) { return (see.end + (1 << a.page_shift) - 1) >> a.page_shift; }
+__device__ __forceinline__ int pages_of(const SelectArgs &a, const Seen &see) { return see.end > 0 ? ((see.end - 1) >> a.page_shift) + 1 : 0; }
 
 // Keys of the pages p0 + l (l < 4 ROWS or, HEADS: 4) + stride i of a table's row, below p1, for one head (lanes of a wavefront: ROWS pages next to each other) or, HEADS, for ROWS heads next
 // to each other.  The numbers of the pages of 16 steps (64 / (4 ROWS) if that is less) are on their way at once, the bounds of a step while those of the one before are summed.

@@ -239,6 +239,23 @@ def test_several_queries_of_a_sequence_and_more_than_a_launch_takes():
         assert torch.allclose(o[s].float(), y_o.float(), atol=2.0 ** -7, rtol=2.0 ** -7)
 
 
+def test_lengths_near_31_bits():
+    """Pages of 2^22 tokens, and of so many that the length and a page are more than 31 bits hold: the choice of the definition, and nothing beside it is written."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    for page, last in ((2 ** 22, 2 ** 31 - 257), (2 ** 22, 2 ** 31 - 2 ** 22), (2 ** 22, 2 ** 31 - 2 ** 22 + 1), (2 ** 30, 2 ** 30 + 1), (2 ** 30, 2 ** 31 - 300)):
+        n, have = i32([last]), -(-last // page)
+        q, bounds, table = rnd(g, 1, 4, 64).bfloat16(), rnd(g, 600, 2, 2, 64).bfloat16().sort(2).values, torch.randperm(600, device="cuda", generator=g).int()[None, :have + 1]
+        pages_taken = 9 if page < 2 ** 30 else 1
+        p = ob.make_select_params(1, 4, 2, 64, True, 2 ** 31 - 256, pages=pages_taken, first=0)
+        held = torch.full((3, 1, 2, pages_taken), -5, dtype=torch.int32, device="cuda")
+        tokens = torch.empty(1, 2, dtype=torch.int32, device="cuda")
+        size = ob.osdn_page_select_workspace_bytes(p, page)
+        ob.osdn_page_select(p, ob._pages(table, page, 600), q, bounds, n.cuda(), None, held[1], tokens, torch.empty(size, dtype=torch.uint8, device="cuda") if size else None)
+        want = pages.select(ref.f64(q), ref.f64(bounds), table.cpu(), n, torch.arange(1), page, pages_taken, 0, 1, 2 ** 31 - 256)
+        assert torch.equal(held[1].cpu(), want[0]) and torch.equal(tokens.cpu(), want[1])
+        assert bool((held[0] == -5).all()) and bool((held[2] == -5).all())
+
+
 def test_bounds_past_32_bits():
     """2^21 + 64 pages, whose bounds are 4.3 GB: those of the last ones, selected as from a small array."""
     g = torch.Generator(device="cuda").manual_seed(3)

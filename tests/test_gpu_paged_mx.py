@@ -171,6 +171,17 @@ def test_values_at_the_ends(io):
     assert torch.equal(nan, want) and bool(torch.isfinite(kr[0, :, 0].cpu()[~want]).all())
 
 
+@pytest.mark.parametrize("T,Hq,Hk,K", [(1, 1, 1, 64), (37, 7, 3, 128), (300, 5, 2, 256)])
+def test_queries_in_place(T, Hq, Hk, K):
+    """q_out may be q: the same rows as into an array of their own."""
+    x = make_append(2, T, Hq, Hk, K, 16, norm="rms", rotary=K)
+    q = x["q"].clone()
+    want = ob.paged_append_mx(x["k"], x["v"], x["cache"], x["table"], x["pos"], q=q, rotary=x["rotary"], hp=ob.NormHyper("rms"))
+    p = ob._params_of(q, x["k"], ob.NormHyper("rms"), x["rotary"])
+    ob.osdn_paged_append_mx(p, q, x["k"], x["v"], x["cache"], x["table"], None, None, x["rotary"], x["pos"], None, q)
+    assert torch.equal(q, want) and not torch.equal(q, x["q"])
+
+
 def test_rows_past_what_fp32_squares():
     """Keys whose squares leave the range of fp32: in 64 bits they have a norm; a row with an infinity is NaN in its blocks that hold one and zero in the others."""
     k = torch.full((1, 3, 1, 128), 1e30, device="cuda")

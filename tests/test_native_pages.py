@@ -95,7 +95,7 @@ def test_what_is_out_of_the_ordinary_goes_through_python():
     plan = lambda **kw: ob.paged_plan(**{**dict(page_table=t, cached=a["cached"], fresh=a["fresh"], free_pages=a["free"], n_free=a["n_free"], page_size=4, tokens=23), **kw})
     for kw, error in [(dict(cached=a["cached"].long()), TypeError), (dict(fresh=a["fresh"][:2]), ValueError), (dict(page_table=t.long()), TypeError), (dict(page_table=t.t()), ValueError),
                       (dict(page_table=t[0]), ValueError), (dict(page_table=t.cpu()), TypeError), (dict(n_free=a["n_free"].repeat(2)), ValueError), (dict(free_pages=a["free"][::2]), ValueError),
-                      (dict(seq=a["fresh"].float()), TypeError), (dict(page_size=3), ob.OsdnError), (dict(tokens=0), ob.OsdnError), (dict(tokens=2 ** 31), ob.OsdnError), (dict(tokens=-1), ob.OsdnError),
+                      (dict(seq=a["fresh"].float()), TypeError), (dict(page_size=3), ob.OsdnError), (dict(tokens=0), ob.OsdnError), (dict(tokens=2 ** 31), ob.OsdnError), (dict(tokens=2 ** 30 + 1), ob.OsdnError), (dict(tokens=-1), ob.OsdnError),
                       (dict(n_pages=0), ob.OsdnError), (dict(page_table=t[:1].expand(3, 6)), ob.OsdnError), (dict(cached=a["cached"][:0], fresh=a["fresh"][:0]), ob.OsdnError)]:
         with pytest.raises(error):
             plan(**kw)

@@ -57,7 +57,7 @@ def test_pages(kw, status):
 def test_requests():
     for B in (0, -1, 65536):
         assert plan(pages(), B=B) == SHAPE and release(pages(), B=B) == SHAPE
-    for tokens in (0, -5):
+    for tokens in (0, -5, 2 ** 30 + 1, 2 ** 31 - 1):
         assert plan(pages(), tokens=tokens) == SHAPE
     for n in ("cached", "fresh", "n_free", "n_free_out", "lengths", "starts", "positions", "rows"):
         assert plan(pages(), missing=n) == NULL
