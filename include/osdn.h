@@ -386,8 +386,8 @@ typedef struct {
 /*
  * Places for the new tokens of B requests.  Request b brings fresh[b] tokens to sequence seq[b], which has cached[b]: it needs
  * ceil((cached + fresh) / page_size) - ceil(cached / page_size) more pages.  Requests are looked at in their order: one is served if it
- * needs no page or the needs up to it are no more than the list holds, and if it brings no token or those up to it are no more
- * than `tokens`.  The i-th page that is granted is the i-th from the end of the list.
+ * needs no page or the needs up to it (served or not) are no more than the list holds, and if it brings no token or those up to it
+ * are no more than `tokens`.  The i-th page that is granted is the i-th from the end of the list.
  *   cached, fresh     [B] int32
  *   seq               [B] int32 or NULL (=> b)
  *   n_free            [1] int32: how many pages the list holds;  n_free_out [1] int32 out: and how many it holds then (may be n_free)

@@ -803,7 +803,7 @@ def paged_plan(page_table, cached, fresh, free_pages, n_free, page_size: int, to
     needs come off the end of free_pages, of which n_free [1] are in the list, into page_table; both are written in place.  tokens: the length of
     the token axis, at least the sum of fresh.  n_pages: of the cache (None: as many as the list has room for).  Returns a dict: lengths [B], starts [B + 1],
     positions and seq [1, tokens] as ``paged_append`` takes them, n_free [1] (for the next call) and, if wanted, slots [tokens] int64.  A request that
-    finds no pages is not served: its length stays, its tokens have no places, and starts[b + 1] == starts[b]."""
+    finds no pages is not served, nor is a later one that needs some: its length stays, its tokens have no places, and starts[b + 1] == starts[b]."""
     if _rows_native is not None and type(page_table) is torch.Tensor and page_table.is_cuda:
         dev = torch._C._cuda_getDevice()
         r = _rows_native.paged_plan(page_table, cached, fresh, free_pages, n_free, seq, page_size, tokens, n_pages, want_slots, dev,
