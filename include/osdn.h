@@ -417,9 +417,9 @@ int osdn_paged_release(const osdn_pages *pages, int32_t B, const int32_t *length
 /*
  * A paged cache in 4 bits (the microscaling format with 4-bit floats): blocks of 32 adjacent elements of a row share a scale 2^e, kept
  * as the byte e + 127, and every element is a code of four bits: a sign (8) and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6.  The byte 255 makes all of a
- * block NaN.  A row is K / 2 bytes of codes, two to a byte (the first in the lower bits), and K / 32 bytes of scales, which stand
- * apart.  Steps are in bytes; rows of codes start on 16 bytes, rows of scales, for K = 256, on 2.  The page table is as
- * in osdn_cache.
+ * block NaN; what fp32 does not hold is infinite (4 * 2^126 and more, which no append leaves).  A row is K / 2 bytes of codes, two to a
+ * byte (the first in the lower bits), and K / 32 bytes of scales, which stand apart.  Steps are in bytes; rows of codes start on 16 bytes,
+ * rows of scales, for K = 256, on 2.  The page table is as in osdn_cache.
  */
 typedef struct {
     void *k, *v;                                    /* codes */

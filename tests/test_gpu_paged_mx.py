@@ -197,6 +197,26 @@ def test_rows_past_what_fp32_squares():
     assert bool(torch.isfinite(kr[0, 2]).all())
 
 
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_every_scale_and_code(io):
+    """All sixteen codes under all scales, those that no append leaves among them, as read and as the bounds of a page.  (4 * 2^126 and more, under the scales 253 and 254, is
+    more than the type holds: infinite, as rounded to it.)"""
+    codes = torch.tensor([(2 * i % 16) | ((2 * i + 1) % 16) << 4 for i in range(32)], dtype=torch.uint8).expand(256, 1, 1, 32)
+    scales = torch.stack([torch.arange(256), 255 - torch.arange(256)], dim=-1).to(torch.uint8)[:, None, None]
+    cache = tuple(t.contiguous().cuda() for t in (codes, codes.flip(-1), scales, scales))
+    table, pos = torch.arange(256, dtype=torch.int32, device="cuda")[None], torch.arange(256, dtype=torch.int32, device="cuda")[None]
+    dt = torch.bfloat16 if io == "bf16" else torch.float32
+    got = ob.paged_read_mx(cache, table, pos, dtype=dt)
+    for x, i in zip(got, range(2)):
+        want = pages.values(cache[i].cpu(), cache[i + 2].cpu())[:, 0].to(dt).double()
+        assert torch.equal(x[0].double().cpu().nan_to_num(1e300), want.nan_to_num(1e300))
+    bounds = ob.alloc_page_bounds(256, 1, 64, dt).zero_()
+    ob.page_bounds((cache[0], cache[2]), table, torch.zeros(1, dtype=torch.int32, device="cuda"), torch.tensor([256], dtype=torch.int32, device="cuda"), bounds)
+    want = pages.values(cache[0].cpu(), cache[2].cpu())[:, 0, 0].to(dt).double()
+    for side in range(2):
+        assert torch.equal(bounds[:, 0, side].double().cpu().nan_to_num(1e300), want.nan_to_num(1e300))
+
+
 def test_tokens_without_a_place():
     """No token, a sequence or a page that is not there, a position past the table: not appended, nothing else touched; read as zeros and NaN."""
     x = make_append(2, 6, 4, 2, 128, 8, norm="rms", rotary=128)
