@@ -338,7 +338,8 @@ inline long long decode_span(int max_length, int window) {
 //    11.9; but 1 x 1200 x 8 11.9 and 8.7, 4 x 700, K = 256, 12.7 and 12.5; up to 2048 where every CU has a row (32 x 2000 x 8 18.7 and 21.8, uneven 17.9 and 25.5; 32 x 3000 x 8 uneven 24.1
 //    and 22.4), and to 3000 where it has two (64 x 3000 x 8 42.6 and 51.5, uneven 31.5 and 37.4; 512 x 3000 151 and 160; but uneven 64 x 8192 x 8 75.3 and 65.8).
 //  - four rows together from two rows a CU on: a share then begins fewer rows (uneven 512 x 4096, one by one 145, so 128; 64 x 8192 x 8 76.5 and 65.8; but 1 x 131072 x 8, whose rows all
-//    shares cut, 34.8 and 37.1).
+//    shares cut, 34.8 and 37.1); of heads side by side, whose lines they then share, also of 32 rows and 64 MB on, two shares a CU (4 x 32000 x 8 62.7 and 44, K = 64 52.6 and 32; 16 x 4096 x 8
+//    33.4 and 26.9; 50 x 8000 x 8 157 and 114, K = 64 137 and 80; but 16 x 8000 x 4 26.8 and 27.5, 1 x 131072 x 8 42.7 and 43.6).
 //  - two shares a CU, four for rows of 64 elements and where there is about a row for each (uneven 64 x 4096 x 8, K = 64, 256, 512, 768 and 1024 34.4, 27.4, 26.7, 25.5; 40 x 4000 x 8,
 //    K = 256, 84.3, 65.1, 58.8, 55.9; but 1 x 131072 x 8 44.6, 34.8, 37.8, 37.1; 16 x 8192 x 8 42.1, 34.7, 38.1, 37.5); three for many rows of 128 whose heads lie apart, the codes past the caches (512, 768, 1024: uneven
 //    512 x 4096 119, 115.5, 118.7, 64 x 4096 x 4 33.9, 27.9, 29.9, fp32 256 x 4096 x 8 128, 121, 131, even 64 x 8192 x 8 107, 107.5, 104; heads side by side uneven 512 x 4096 140.5, 145, 146).
@@ -352,7 +353,9 @@ struct DecodePlan { int row_group, shares; long long units; };
 // 1 x 131072 x 8 38.2 and 37.5; but 512 x 200 x 4, called again on what the memory-side cache holds, 18.7 and 21.0, 1 x 32768 x 8 16.4 and 17.0; heads side by side, whose lines two wavefronts
 // share, uneven 512 x 4096 x 4 142 and 148.  K = 64, of whose lines a load takes eight bytes a lane, 26.7 and 31.0, K = 256, half lines, 62.6 and 66.0.  Chosen pages of 48 x 8 heads, 32 of 64
 // tokens, side by side 51.4 and 47.6, apart 29.7 and 28.8, of 96 x 8, 128 of 16 tokens, 79.0 and 75.1, apart 46.0 and 41.4; of 300 x 2 side by side, one line for both, 112 and 115.)
-constexpr bool decode_mx_once(long long rows, long long token_step, bool chosen) { return (chosen || token_step == 64) && rows * 136 > 64LL << 20; }
+// (rows of more than 64 MB)
+constexpr bool decode_mx_large(long long rows, int K) { return rows * (K + K / 16) > 64LL << 20; }
+constexpr bool decode_mx_once(long long rows, long long token_step, bool chosen) { return (chosen || token_step == 64) && decode_mx_large(rows, 128); }
 inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K, bool bf16, int part_heads, bool heads_together, int asked, bool mx = false) {
     const long long span = decode_span(max_length, window), all = (long long)B * rows;
     const int tile = mx ? DECODE_MX_TILE : decode_tile(K, bf16), alone = mx ? decode_mx_unit(1) : decode_unit(K, bf16, 1), held = (mx ? decode_mx_per_cu(K, bf16) : decode_per_cu(K, bf16)) * NUM_CU;
@@ -360,13 +363,13 @@ inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K
     const bool few_units = span <= (K == 64 ? 4 : bf16 ? 3 : 2) * alone || (span <= 4 * alone && all >= NUM_CU / 2);
     const bool full = all >= held && held > NUM_CU && span <= (beside || K == 256 ? 512 : 1024);
     const bool each = asked < 0 || (asked == 0 && (mx ? decode_mx_each(span, all, K) : few_units || full));
-    const bool together = each ? (span <= tile && all > held) || (span <= 4 * tile && 2 * all > 3 * held) : mx ? all >= 2 * NUM_CU : beside || (K == 64 && bf16);
+    const bool together = each ? (span <= tile && all > held) || (span <= 4 * tile && 2 * all > 3 * held) : mx ? all >= 2 * NUM_CU || (heads_together && K <= 128 && all >= 32 && decode_mx_large(all * span, K)) : beside || (K == 64 && bf16);
     DecodePlan p{};
     p.row_group = together && rows % 4 == 0 ? 4 : together && rows % 2 == 0 ? 2 : 1;
     const int unit = mx ? decode_mx_unit(p.row_group) : decode_unit(K, bf16, p.row_group);
     p.units = span < 1 ? 1 : (span + unit - 1) / unit;
     const long long groups = all / p.row_group;
-    const int per_cu = mx ? (K == 128 && !heads_together && all >= NUM_CU ? 3 : K == 64 || (all >= NUM_CU && all < 2 * NUM_CU) ? 4 : 2) : all <= 16 || (K == 256 && !bf16) || (K == 128 && bf16 && p.row_group == 4 && span > 1024) ? 1 : K == 64 && p.row_group < 4 ? 3 : 2;
+    const int per_cu = mx ? (heads_together && p.row_group > 1 ? 2 : K == 128 && !heads_together && all >= NUM_CU ? 3 : K == 64 || (all >= NUM_CU && all < 2 * NUM_CU) ? 4 : 2) : all <= 16 || (K == 256 && !bf16) || (K == 128 && bf16 && p.row_group == 4 && span > 1024) ? 1 : K == 64 && p.row_group < 4 ? 3 : 2;
     const long long worth = groups * span / (16 * part_heads), most = per_cu * NUM_CU < worth ? per_cu * NUM_CU : worth > NUM_CU ? worth : NUM_CU;
     p.shares = each ? 0 : asked > 0 ? asked : (int)(groups * p.units < most ? groups * p.units : most);
     return p;
