@@ -342,7 +342,7 @@ inline long long decode_span(int max_length, int window) {
 //    33.4 and 26.9; 50 x 8000 x 8 157 and 114, K = 64 137 and 80; but 16 x 8000 x 4 26.8 and 27.5, 1 x 131072 x 8 42.7 and 43.6).
 //  - two shares a CU, four for rows of 64 elements and where there is about a row for each (uneven 64 x 4096 x 8, K = 64, 256, 512, 768 and 1024 34.4, 27.4, 26.7, 25.5; 40 x 4000 x 8,
 //    K = 256, 84.3, 65.1, 58.8, 55.9; but 1 x 131072 x 8 44.6, 34.8, 37.8, 37.1; 16 x 8192 x 8 42.1, 34.7, 38.1, 37.5); three for many rows of 128 whose heads lie apart, the codes past the caches (512, 768, 1024: uneven
-//    512 x 4096 119, 115.5, 118.7, 64 x 4096 x 4 33.9, 27.9, 29.9, fp32 256 x 4096 x 8 128, 121, 131, even 64 x 8192 x 8 107, 107.5, 104; heads side by side uneven 512 x 4096 140.5, 145, 146).
+//    512 x 4096 119, 115.5, 118.7, 64 x 4096 x 4 33.9, 27.9, 29.9, fp32 256 x 4096 x 8 128, 121, 131, even 64 x 8192 x 8 107, 107.5, 104, 28 x 8192 x 8 52.4, 48.9, 45.9, even 55.3, 54.3, 55.1, but 16 x 8192 x 8 33.6, 36.1, 37.2; heads side by side uneven 512 x 4096 140.5, 145, 146).
 inline bool decode_mx_each(long long span, long long all, int K) {
     return span <= (all >= 2 * NUM_CU ? 3000 : all >= NUM_CU ? 2048 : K == 256 ? 384 : 768);
 }
@@ -369,7 +369,7 @@ inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K
     const int unit = mx ? decode_mx_unit(p.row_group) : decode_unit(K, bf16, p.row_group);
     p.units = span < 1 ? 1 : (span + unit - 1) / unit;
     const long long groups = all / p.row_group;
-    const int per_cu = mx ? (heads_together && p.row_group > 1 ? 2 : K == 128 && !heads_together && all >= NUM_CU ? 3 : K == 64 || (all >= NUM_CU && all < 2 * NUM_CU) ? 4 : 2) : all <= 16 || (K == 256 && !bf16) || (K == 128 && bf16 && p.row_group == 4 && span > 1024) ? 1 : K == 64 && p.row_group < 4 ? 3 : 2;
+    const int per_cu = mx ? (heads_together && p.row_group > 1 ? 2 : K == 128 && !heads_together && all >= 3 * NUM_CU / 4 ? 3 : K == 64 || (all >= NUM_CU && all < 2 * NUM_CU) ? 4 : 2) : all <= 16 || (K == 256 && !bf16) || (K == 128 && bf16 && p.row_group == 4 && span > 1024) ? 1 : K == 64 && p.row_group < 4 ? 3 : 2;
     const long long worth = groups * span / (16 * part_heads), most = per_cu * NUM_CU < worth ? per_cu * NUM_CU : worth > NUM_CU ? worth : NUM_CU;
     p.shares = each ? 0 : asked > 0 ? asked : (int)(groups * p.units < most ? groups * p.units : most);
     return p;
