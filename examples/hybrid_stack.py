@@ -130,7 +130,8 @@ class Serving:
         return self.attend(self.mix(x[None], row), positions, seq, at + T, before, row)[0]
 
     def token(self, x, longest):
-        """One new token x [B,width] of every sequence; returns the outputs [B,width].  longest: no sequence is longer afterwards."""
+        """One new token x [B,width] of every sequence; returns the outputs [B,width].  longest: no sequence is longer afterwards.  (The pool has to
+        hold a page for each that needs one: the tokens of those that are served stand side by side, and are the rows of x only if all are.)"""
         positions, seq, before = self.places(torch.ones_like(self.lengths), x.shape[0])
         return self.attend(self.mix(x[:, None]), positions.view(-1, 1), seq.view(-1, 1), longest, before)[:, 0]
 
