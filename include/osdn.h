@@ -488,9 +488,10 @@ int osdn_page_bounds_mx(const osdn_select_params *p, const osdn_cache_mx *cache,
 /*
  * The pages that a query reads.  For key head h and page g the score is sum over its query heads and the elements of
  *     max(q_i lo_i, q_i hi_i),
- * which no key of the page passes (computed in 64 bits).  Of the pages that the sequence has, the first `first`, the last `last` and
- * those of the largest scores are chosen, p->pages in all or as many as there are; equal scores: the earlier page.  A page that is not
- * there, and one whose score is NaN, come before all others.
+ * which no key of the page passes (computed in 64 bits, as sum of Q-_i lo_i + Q+_i hi_i, Q- and Q+ the sums over the query heads of min(q, 0) and
+ * max(q, 0)).  Of the pages that the sequence has, the first `first`, the last `last` and those of the largest scores are chosen, p->pages in
+ * all or as many as there are; equal scores: the earlier page.  A page that is not there, and one whose score is NaN, come before all
+ * others; so does one with an infinite bound where its Q is zero.
  *   q                 [B,Hq,K] rows (token is not used)
  *   lengths, seq      as for osdn_paged_decode
  *   chosen            [B,Hk,pages] int32 out: page numbers in the order of their tokens, -1 behind the last (and for one that is not there)

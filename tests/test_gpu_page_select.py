@@ -196,6 +196,22 @@ def test_scores_that_are_not_numbers_and_pages_that_are_not_there():
     assert bool(torch.isnan(o[1]).all()) and bool(torch.isnan(o[2]).all()) and not bool(torch.isnan(o[4]).any())
 
 
+def test_infinite_bounds_come_first_or_last():
+    """Bounds that infinite keys leave: an infinite score, of either sign, and one whose Q is zero, which is read before the finite ones."""
+    x = make([160, 160, 160], 4, 2, 64, 8)
+    b, t = bounds_of(x), x["table"]
+    x["q"][:, :, 3] = torch.tensor([2.0, 1.0, 3.0, 0.5], device="cuda")
+    for at, (lo, hi) in enumerate(((-math.inf, 1.0), (-math.inf, -math.inf), (1.0, math.inf))):
+        b[int(t[at, 11]), :, 0, 3], b[int(t[at, 11]), :, 1, 3] = lo, hi
+    for n in (3, 19):
+        chosen, _ = ob.page_select(x["q"], b, t, x["lengths"], 8, n)
+        for at in range(3):
+            assert all((int(t[at, 11]) in row) for row in chosen[at].tolist())
+    b[int(t[1, 11]), :, 0, 3] = -3e38                           # (Q- is zero there: with a finite bound the largest is minus infinity, and the score too)
+    chosen, _ = ob.page_select(x["q"], b, t, x["lengths"], 8, 19)
+    assert all((int(t[1, 11]) not in row) for row in chosen[1].tolist())
+
+
 def test_all_pages_are_the_whole_sequence():
     """As many pages as there are: the bits of attention over all of it, over either kind of cache."""
     for form in FORMS:
