@@ -9,10 +9,11 @@ template <int K> using Fp4Bf16 = Fp4Tile<bf16, K, true, true>;
 template <int K> using Fp4F32 = Fp4Tile<float, K, true, true>;
 template <int K> using Fp4Bf16Any = Fp4Tile<bf16, K, false, true>;
 template <int K> using Fp4F32Any = Fp4Tile<float, K, false, true>;
+template <typename T, int K> using Once = Fp4Tile<T, K, true, true, true>;
 int launch_chosen_decode_mx(const DecodeArgs &a, bool bf16_io, hipStream_t st) {
-    if (a.regular && a.K == 128 && decode_mx_once((long long)a.B * a.Hk * a.max_length, a.cache_k.token, true)) {
-        if (bf16_io) decode_of<Fp4Tile<bf16, 128, true, true, true>>(a, st);
-        else decode_of<Fp4Tile<float, 128, true, true, true>>(a, st);
+    if (a.regular && decode_mx_once((long long)a.B * a.Hk * a.max_length, a.K, a.cache_k.token, true)) {
+        if (a.K == 64) bf16_io ? decode_of<Once<bf16, 64>>(a, st) : decode_of<Once<float, 64>>(a, st);
+        else bf16_io ? decode_of<Once<bf16, 128>>(a, st) : decode_of<Once<float, 128>>(a, st);
         return 0;
     }
     if (a.regular) return bf16_io ? decode_by_width<Fp4Bf16>(a, st) : decode_by_width<Fp4F32>(a, st);

@@ -202,7 +202,7 @@ template <typename IO, int W, bool REGULAR, bool C = false, bool ONCE = false> s
     static __device__ __forceinline__ Codes fetch(const char *codes, const unsigned char *scale) {
         Codes c;
         if constexpr (WORDS == 2) {
-            const u32x2 x = *reinterpret_cast<const u32x2 *>(codes);
+            const u32x2 *at = reinterpret_cast<const u32x2 *>(codes), x = ONCE ? __builtin_nontemporal_load(at) : *at;
             c.word[0] = x[0];
             c.word[1] = x[1];
         } else {

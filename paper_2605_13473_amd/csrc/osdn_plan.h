@@ -347,15 +347,17 @@ inline bool decode_mx_each(long long span, long long all, int K) {
     return span <= (all >= 2 * NUM_CU ? 3000 : all >= NUM_CU ? 2048 : K == 256 ? 384 : 768);
 }
 struct DecodePlan { int row_group, shares; long long units; };
-// Whether a call over a cache in 4 bits (K = 128) loads its codes past the caches: rows of a head lie next to each other (or are chosen ones), so that a load takes whole lines of 128 bytes
-// which no other wants, and those that it may read are more than 64 MB, a quarter of the memory-side cache, from which a program that comes back to less of them soon would have them
-// (us, through the caches and past them: uneven 512 x 4096 x 4 heads 131 and 121, 512 x 1000 x 4 59.8 and 57.2, 64 x 4096 x 4 39.7 and 36.1, 4 x 32768 x 8 38.1 and 35.3,
-// 1 x 131072 x 8 38.2 and 37.5; but 512 x 200 x 4, called again on what the memory-side cache holds, 18.7 and 21.0, 1 x 32768 x 8 16.4 and 17.0; heads side by side, whose lines two wavefronts
-// share, uneven 512 x 4096 x 4 142 and 148.  K = 64, of whose lines a load takes eight bytes a lane, 26.7 and 31.0, K = 256, half lines, 62.6 and 66.0.  Chosen pages of 48 x 8 heads, 32 of 64
-// tokens, side by side 51.4 and 47.6, apart 29.7 and 28.8, of 96 x 8, 128 of 16 tokens, 79.0 and 75.1, apart 46.0 and 41.4; of 300 x 2 side by side, one line for both, 112 and 115.)
-// (rows of more than 64 MB)
+// Rows of more than 64 MB, a quarter of the memory-side cache, from which a program that comes back to less of them soon would have them
 constexpr bool decode_mx_large(long long rows, int K) { return rows * (K + K / 16) > 64LL << 20; }
-constexpr bool decode_mx_once(long long rows, long long token_step, bool chosen) { return (chosen || token_step == 64) && decode_mx_large(rows, 128); }
+// Whether a call over a cache in 4 bits loads its codes past the caches: rows of a head lie next to each other (K = 128: or are chosen ones), so that a load takes whole lines of 128 bytes which no
+// other wants, and those that it may read are many (us, through the caches and past them: uneven 512 x 4096 x 4 heads 131 and 121, K = 64 84.1 and 79.7, 512 x 1000 x 4 59.8 and 57.2, K = 64
+// 42.3 and 40.7, 64 x 4096 x 4 39.7 and 36.1, 4 x 32768 x 8 38.1 and 35.3, K = 64 29.5 and 28.6, 1 x 131072 x 8 38.2 and 37.5, K = 64 29.0 and 28.1; but 512 x 200 x 4, called again on
+// what the memory-side cache holds, 18.7 and 21.0, 1 x 32768 x 8 16.4 and 17.0; heads side by side, whose lines wavefronts share, uneven 512 x 4096 x 4 142 and 148, K = 64 97.5 and
+// 112; K = 256, half a line a load, 62.6 and 66.0.  Chosen pages of 48 x 8 heads, 32 of 64 tokens, side by side 51.4 and 47.6, apart 29.7 and 28.8, of 96 x 8, 128 of 16 tokens, 79.0 and 75.1,
+// apart 46.0 and 41.4, K = 64 59.0 and 59.8, apart 32.6 and 31.0; of 300 x 2 side by side, one line for both, 112 and 115.)
+constexpr bool decode_mx_once(long long rows, int K, long long token_step, bool chosen) {
+    return K <= 128 && (token_step == K / 2 || (chosen && K == 128)) && decode_mx_large(rows, K);
+}
 inline DecodePlan decode_plan(int B, int rows, int max_length, int window, int K, bool bf16, int part_heads, bool heads_together, int asked, bool mx = false) {
     const long long span = decode_span(max_length, window), all = (long long)B * rows;
     const int tile = mx ? DECODE_MX_TILE : decode_tile(K, bf16), alone = mx ? decode_mx_unit(1) : decode_unit(K, bf16, 1), held = (mx ? decode_mx_per_cu(K, bf16) : decode_per_cu(K, bf16)) * NUM_CU;

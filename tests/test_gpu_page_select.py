@@ -154,9 +154,10 @@ def test_chosen_rows_that_may_be_many(io):
     x = make([700, 41, 0, 260], 6, 3, 128, 8, io, "token", mx=True)
     chosen, tokens = check_choice(x, bounds_of(x), 20)
     check_attention(x, chosen, tokens, max_length=1 << 17)
-    x = make([700, 41, 0, 260], 6, 3, 128, 8, io, mx=True)
-    chosen, tokens = check_choice(x, bounds_of(x), 20)
-    check_attention(x, chosen, tokens, max_length=1 << 17)
+    for K in (64, 128):
+        x = make([700, 41, 0, 260], 6, 3, K, 8, io, mx=True)
+        chosen, tokens = check_choice(x, bounds_of(x), 20)
+        check_attention(x, chosen, tokens, max_length=1 << 17)
 
 
 def test_equal_scores_go_to_the_earlier_page():

@@ -325,10 +325,11 @@ def test_decode(case):
 @pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("group", [1, 4, 20])
 def test_rows_that_may_be_many(io, group):
-    """A bound of the lengths beyond 2^19 rows of 128 elements: their codes are loaded past the caches, in shares and a row each; the lengths themselves stay small."""
+    """A bound of the lengths beyond 64 MB of rows: their codes are loaded past the caches, in shares and a row each; the lengths themselves stay small."""
     for B, lengths in ((3, [1531, 0, 77]), (130, [1 + 37 * b % 530 for b in range(130)])):
-        x = make_decode(lengths, 4 * group, 4, 128, 16, io)
-        compare(x, *call(x, max_length=65536 if B == 3 else 2000))
+        for K in (64, 128):
+            x = make_decode(lengths, 4 * group, 4, K, 16, io)
+            compare(x, *call(x, max_length=1 << 17 if B == 3 else 2000 * 128 // K))
 
 
 @pytest.mark.parametrize("Hq,Hk,K", [(6, 3, 64), (8, 4, 128), (18, 1, 64), (4, 4, 256), (40, 2, 128)])
