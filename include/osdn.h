@@ -492,6 +492,7 @@ int osdn_page_bounds_mx(const osdn_select_params *p, const osdn_cache_mx *cache,
  * max(q, 0)).  Of the pages that the sequence has, the first `first`, the last `last` and those of the largest scores are chosen, p->pages in
  * all or as many as there are; equal scores: the earlier page.  A page that is not there, and one whose score is NaN, come before all
  * others; so does one with an infinite bound where its Q is zero.
+ * max_length is no more than 2^30 pages, and p->pages no more than that.
  *   q                 [B,Hq,K] rows (token is not used)
  *   lengths, seq      as for osdn_paged_decode
  *   chosen            [B,Hk,pages] int32 out: page numbers in the order of their tokens, -1 behind the last (and for one that is not there)

@@ -785,8 +785,9 @@ static int check_choice(const osdn_select_params *p, int page_size, long long &s
     const int rc = check_select(p);
     if (rc != OSDN_OK) return rc;
     if (p->Hq < p->Hk || p->Hq % p->Hk != 0 || p->Hq > 65535 || p->max_length < 0 || p->max_length > 0x7fffff00 || page_size < 1) return OSDN_ERR_SHAPE;
-    if (p->first < 0 || p->last < 1 || p->pages < 1 || (long long)p->first + p->last > p->pages || (long long)p->pages * page_size > 0x7fffff00) return OSDN_ERR_PARAM;
+    if (p->first < 0 || p->last < 1 || p->pages < 1 || p->pages > SELECT_MAX_PAGES || (long long)p->first + p->last > p->pages || (long long)p->pages * page_size > 0x7fffff00) return OSDN_ERR_PARAM;
     seen = ((long long)p->max_length + page_size - 1) / page_size;
+    if (seen > SELECT_MAX_PAGES) return OSDN_ERR_SHAPE;
     return (long long)p->B * p->Hk * seen > 0x7fffffffLL || (long long)p->B * p->Hk * p->pages > 0x7fffffffLL ? OSDN_ERR_SHAPE : OSDN_OK;
 }
 size_t osdn_page_select_workspace_bytes(const osdn_select_params *p, int32_t page_size) {

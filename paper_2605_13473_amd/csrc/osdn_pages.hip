@@ -468,6 +468,7 @@ __device__ __forceinline__ int pages_of(const SelectArgs &a, const Seen &see) { 
 // to each other.  The numbers of the pages of 16 steps (64 / (4 ROWS) if that is less) are on their way at once, the bounds of a step while those of the one before are summed.
 template <typename T, int K, bool HEADS> struct PageSteps {
     static constexpr int SIDE = HEADS ? 1 : ScoreRow<T, K>::ROWS, STEP = 4 * SIDE, STEPS = 64 / STEP;
+    static_assert(STEPS <= SELECT_STEPS, "the page counter's steps");
     // the lane STEP i + l: page l of step i from p on (what stands behind the last page is looked at, and left out in the end)
     static __device__ __forceinline__ int ask(const SelectArgs &a, const int *table, int p, int stride, int lane) {
         return table[min((long long)p + (long long)(lane / STEP) * stride + lane % STEP, (long long)a.max_pages - 1)];
