@@ -31,9 +31,11 @@ int main() {
                         if (end > worst) worst = end;
                     }
                 }
-    for (int pages : {most, most - 1})              // a run of a thread, and where it starts
-        for (int threads : {512})
-            if ((long long)pages + threads - 1 + (long long)threads * ((pages + threads - 1) / threads) > worst) worst = (long long)pages + threads - 1 + (long long)threads * ((pages + threads - 1) / threads);
+    for (long long count : {(long long)most, most - 1LL}) {             // select_kernel: the runs of 512 threads
+        const long long run = (count + 511) / 512;
+        for (long long end : {count + 511, 511 * run})
+            if (end > worst) worst = end;
+    }
     std::printf("%d %lld\n", most, worst);
 }
 """
