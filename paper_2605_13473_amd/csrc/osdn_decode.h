@@ -297,7 +297,9 @@ __global__ __launch_bounds__(DEC_T, D::PER_CU) void decode_kernel(DecodeArgs a) 
             if (alone) {
                 const float inv = L == 0.f ? 0.f : 1.f / L;
                 int again = b;
-                asm volatile("" : "+s"(again));     // (found once more: kept from the start it would cost registers that the loop wants)
+                // (SHARED: found once more, as kept from the start it would cost registers that the loop wants.  Else not, as stores that follow it wait for it: 266 x 1 x 16, a
+                // row each, 12.95 us, K = 256, and 14.4 so, K = 128 9.24 and 9.62)
+                if constexpr (SHARED) asm volatile("" : "+s"(again));
                 const Entry of = entry_of<D::CHOSEN>(a, again);
                 T *dst = static_cast<T *>(a.o.data) + of.b * a.o.batch + (D::CHOSEN ? of.head * a.group + h0 + h : h0 + h) * a.o.head + d;
 #pragma unroll
