@@ -243,7 +243,8 @@ template <typename T, int K, bool VEC, int ROT> __global__ __launch_bounds__(HEA
                 for (int e = 0; e < VE; ++e) {
                     most = __builtin_fmaxf(most, __builtin_fabsf(z[e]) + off[e]);
                     least = __builtin_fmaxf(least, __builtin_fabsf(z[e]) - off[e]);
-                    sure = sure && off[e] < 0x1p100f;                   // (not so of NaN)
+                    // (not so of NaN; and what cancels below its error could have either sign)
+                    sure = sure && off[e] < 0x1p100f && !(off[e] > 0.f && __builtin_fabsf(z[e]) <= off[e]);
                 }
                 int byte = fp4_byte(max_block(__builtin_bit_cast(int, most), 32 / VE));
                 sure = sure && byte == fp4_byte(max_block(__builtin_bit_cast(int, least), 32 / VE));
