@@ -233,9 +233,14 @@ template <typename T, int K, bool VEC, int ROT> __global__ __launch_bounds__(HEA
         }
         if (first < a.Hq + a.Hk) {
             const RowWeights<VE> w = weights_of<T, K, ROT>(a.weight_k, turn, lane);
+            // (the factor of a row is at least 2^-50 where its sum is far from where fp32 ends: times such a weight it has all its digits)
+            uint32_t least_weight = ~0u;            // twice the bits of its magnitude, less one: of zero the largest
+#pragma unroll
+            for (int e = 0; e < VE; ++e) least_weight = min(least_weight, 2 * __builtin_bit_cast(uint32_t, w.own[e]) - 1u);
+            const bool whole_digits = least_weight >= 2 * __builtin_bit_cast(uint32_t, 0x1p-60f) - 1u || a.norm == 0;
             rows(a.k, max(first, a.Hq) - a.Hq, min(last, a.Hq + a.Hk) - a.Hq, [&](int h, const u32x4 &raw, const float (&x)[VE]) {
                 float z[VE], off[VE];
-                bool sure = row_ready<T, K, ROT, true>(a, turn, w, raw, x, c, s, off_table, z, off);
+                bool sure = row_ready<T, K, ROT, true>(a, turn, w, raw, x, c, s, off_table, z, off) && whole_digits;
                 // the elements as large and as small as they may be: the same byte, the same codes
                 auto moved = [&](int e, float by) { return __builtin_copysignf(__builtin_fmaxf(__builtin_fmaf(off[e], by, __builtin_fabsf(z[e])), 0.f), z[e]); };
                 float most = 0.f, least = 0.f;

@@ -40,3 +40,17 @@ def test_signs_of_elements_that_cancel(K, interleaved):
     got, want, z = append(k[None, :, None].cuda(), torch.cat([c, s], dim=1).cuda(), interleaved=interleaved)
     assert torch.equal(z[0, :, 0, 0::2] if interleaved else z[0, :, 0, :half], sums)
     assert torch.equal(got[1], want[1]) and torch.equal(got[0], want[0])
+
+
+@pytest.mark.parametrize("rotary", [0, 64])
+@pytest.mark.parametrize("size,weight", [(48, -95), (49, -85), (-20, -125), (0, -60), (0, -61)])
+def test_weights_next_to_the_smallest_numbers(size, weight, rotary):
+    """The factor of a row times a weight is below 2^-126 in fp32, where a product keeps a few of its digits."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k = torch.randn(1, 64, 4, 64, device="cuda", generator=g) * 2.0 ** size
+    w = (1 + torch.randn(64, device="cuda", generator=g) / 8) * 2.0 ** weight
+    w[5] = 0.0
+    got, want, z = append(k, ob.rotary_table(64, rotary) if rotary else None, w, "rms")
+    # (size -20: eps, 2^-20, makes the factor of a row 2^10, and keys of 2^-135 are below the least scale's codes)
+    assert (float(z.abs().amax()) > 2.0 ** -118 and int((got[0] & 7).sum()) > 0) == (size >= 0)
+    assert torch.equal(got[1], want[1]) and torch.equal(got[0], want[0])
