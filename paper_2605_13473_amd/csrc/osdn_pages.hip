@@ -295,62 +295,64 @@ template <typename T, int K, bool MX> struct KeyRow {
 __device__ __forceinline__ float least(float x, float y) { return __builtin_elementwise_minimum(x, y); }
 __device__ __forceinline__ float greatest(float x, float y) { return __builtin_elementwise_maximum(x, y); }
 
-// A wavefront takes one page that got new tokens, for one head: its new rows, 64 / LANES at a time, and, where it had tokens before, its bounds.
+// A wavefront takes one page that got new tokens, for one head: its new rows, 64 / LANES at a time, and, where it had tokens before, its bounds.  (More pages than a launch has wavefronts:
+// one after the other.)
 template <typename T, int K, bool MX> __global__ __launch_bounds__(256) void bounds_kernel(BoundsArgs a) {
     using R = KeyRow<T, K, MX>;
     constexpr int VE = R::VE, ROWS = 64 / R::LANES, PER = 16 / sizeof(T);
     const int lane = threadIdx.x & 63, sub = lane / R::LANES, e0 = lane % R::LANES * VE;
-    const long long item = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int h = (int)(item % a.Hk);
-    const long long rest = item / a.Hk;
-    const int nth = (int)(rest % a.touched);
-    if (rest / a.touched >= a.B) return;
-    const int b = (int)(rest / a.touched);
-    const int from = max(0, a.cached[b]), end = (int)min((long long)a.lengths[b], (long long)from + a.max_new), row = a.seq ? a.seq[b] : b;
-    const int col = (from >> a.page_shift) + nth;
-    const long long begin = (long long)col << a.page_shift;
-    if (begin >= end || from >= end || col >= a.max_pages || (unsigned)row >= (unsigned)a.n_seqs) return;
-    const int page = a.table[(long long)row * a.table_stride + col];
-    if ((unsigned)page >= (unsigned)a.n_pages) return;
-    const int s0 = (int)(max((long long)from, begin) - begin), s1 = (int)min((long long)1 << a.page_shift, end - begin);
-    T *out = static_cast<T *>(a.bounds) + ((long long)page * a.Hk + h) * 2 * K + e0;
-    float lo[VE], hi[VE];
+    const long long items = (long long)a.B * a.touched * a.Hk;
+    for (long long item = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items; item += 4LL * gridDim.x) {
+        const int h = (int)(item % a.Hk);
+        const long long rest = item / a.Hk;
+        const int nth = (int)(rest % a.touched);
+        const int b = (int)(rest / a.touched);
+        const int from = max(0, a.cached[b]), end = (int)min((long long)a.lengths[b], (long long)from + a.max_new), row = a.seq ? a.seq[b] : b;
+        const int col = (from >> a.page_shift) + nth;
+        const long long begin = (long long)col << a.page_shift;
+        if (begin >= end || from >= end || col >= a.max_pages || (unsigned)row >= (unsigned)a.n_seqs) continue;
+        const int page = a.table[(long long)row * a.table_stride + col];
+        if ((unsigned)page >= (unsigned)a.n_pages) continue;
+        const int s0 = (int)(max((long long)from, begin) - begin), s1 = (int)min((long long)1 << a.page_shift, end - begin);
+        T *out = static_cast<T *>(a.bounds) + ((long long)page * a.Hk + h) * 2 * K + e0;
+        float lo[VE], hi[VE];
 #pragma unroll
-    for (int e = 0; e < VE; ++e) { lo[e] = INFINITY; hi[e] = -INFINITY; }
-    if (s0 > 0) {                       // (tokens from before)
-        auto old = [&](const T *at, float (&x)[VE]) {
+        for (int e = 0; e < VE; ++e) { lo[e] = INFINITY; hi[e] = -INFINITY; }
+        if (s0 > 0) {                       // (tokens from before)
+            auto old = [&](const T *at, float (&x)[VE]) {
 #pragma unroll
-            for (int v = 0; v < VE / PER; ++v) {
-                const u32x4 raw = *reinterpret_cast<const u32x4 *>(at + v * PER);
+                for (int v = 0; v < VE / PER; ++v) {
+                    const u32x4 raw = *reinterpret_cast<const u32x4 *>(at + v * PER);
 #pragma unroll
-                for (int e = 0; e < PER; ++e) x[v * PER + e] = vec_get<T>(raw, e);
-            }
-        };
-        old(out, lo);
-        old(out + K, hi);
-    }
-    for (int s = s0 + sub; s < s1; s += ROWS) {
-        float x[VE];
-        R::load(a, page, s, h, e0, x);
+                    for (int e = 0; e < PER; ++e) x[v * PER + e] = vec_get<T>(raw, e);
+                }
+            };
+            old(out, lo);
+            old(out + K, hi);
+        }
+        for (int s = s0 + sub; s < s1; s += ROWS) {
+            float x[VE];
+            R::load(a, page, s, h, e0, x);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) { lo[e] = least(lo[e], x[e]); hi[e] = greatest(hi[e], x[e]); }
-    }
+            for (int e = 0; e < VE; ++e) { lo[e] = least(lo[e], x[e]); hi[e] = greatest(hi[e], x[e]); }
+        }
 #pragma unroll
-    for (int d = R::LANES; d < 64; d <<= 1)
+        for (int d = R::LANES; d < 64; d <<= 1)
 #pragma unroll
-        for (int e = 0; e < VE; ++e) { lo[e] = least(lo[e], __shfl_xor(lo[e], d, 64)); hi[e] = greatest(hi[e], __shfl_xor(hi[e], d, 64)); }
-    if (sub == 0) {
-        auto leave = [&](T *at, const float (&x)[VE]) {
+            for (int e = 0; e < VE; ++e) { lo[e] = least(lo[e], __shfl_xor(lo[e], d, 64)); hi[e] = greatest(hi[e], __shfl_xor(hi[e], d, 64)); }
+        if (sub == 0) {
+            auto leave = [&](T *at, const float (&x)[VE]) {
 #pragma unroll
-            for (int v = 0; v < VE / PER; ++v) {
-                float y[PER];
+                for (int v = 0; v < VE / PER; ++v) {
+                    float y[PER];
 #pragma unroll
-                for (int e = 0; e < PER; ++e) y[e] = x[v * PER + e];
-                store_vec_t(at + v * PER, y);
-            }
-        };
-        leave(out, lo);
-        leave(out + K, hi);
+                    for (int e = 0; e < PER; ++e) y[e] = x[v * PER + e];
+                    store_vec_t(at + v * PER, y);
+                }
+            };
+            leave(out, lo);
+            leave(out + K, hi);
+        }
     }
 }
 
@@ -710,7 +712,7 @@ template <typename F> int by_width(int K, F &&f) {
 }
 template <typename T> int bounds_of(const BoundsArgs &a, bool mx, hipStream_t st) {
     const long long items = (long long)a.B * a.touched * a.Hk;
-    const dim3 g((unsigned)((items + 3) / 4)), t(256);
+    const dim3 g(bounds_workgroups(items)), t(256);
     return by_width(a.K, [&](auto k) {
         if (mx) hipLaunchKernelGGL((bounds_kernel<T, decltype(k)::value, true>), g, t, 0, st, a);
         else hipLaunchKernelGGL((bounds_kernel<T, decltype(k)::value, false>), g, t, 0, st, a);

@@ -388,6 +388,8 @@ constexpr int PLAN_MAX_ROWS = 1 << 17;
 inline bool select_scores_itself(long long rows, int pages, int bytes) {
     return pages <= 4096 && (rows >= NUM_CU || (long long)pages * bytes <= (rows >= 64 ? 1 << 18 : 1 << 16));
 }
+// Workgroups (four wavefronts, a page and head each) for the bounds of pages: a launch has less than 2^32 threads
+inline unsigned bounds_workgroups(long long items) { return (unsigned)(items < 4LL << 22 ? (items + 3) / 4 : 1 << 22); }
 // Pages of a sequence that are counted, and that a query may choose: a step of the counter, SELECT_STEPS times 16 pages for each of up to 4 NUM_CU workgroups, then stays in 32 bits
 constexpr int SELECT_MAX_PAGES = 1 << 30, SELECT_STEPS = 16;
 // Workgroups (four wavefronts, four pages each at a time) for the scores of a sequence's pages of one group of key heads

@@ -61,3 +61,13 @@ def test_more_pages_than_are_counted_are_not_chosen():
     g = pages(page_size=1, max_pages=2 ** 31 - 1, table_stride=2 ** 31 - 1, n_seqs=1)
     for n in (2 ** 30 + 1, 2 ** 31 - 256):
         assert select(choice(B=1, Hq=1, Hk=1, pages=n), g, chosen=None) == PARAM
+
+
+def test_bounds_of_more_pages_than_a_launch_has_wavefronts(tmp_path):
+    """All pages that B sequences may hold, as page_bounds takes them where it is not told how many tokens are new."""
+    (tmp_path / "main.cpp").write_text('#include "osdn_plan.h"\n#include <cstdio>\nint main() { long long n; while (std::scanf("%lld", &n) == 1) std::printf("%u\\n", osdn::bounds_workgroups(n)); }\n')
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", CSRC, "-o", str(tmp_path / "workgroups"), str(tmp_path / "main.cpp")], check=True)
+    asked = [1, 4, 5, 1000, 2 ** 24 - 1, 2 ** 24, 2 ** 24 + 1, 2048 * 4096 * 8, 2 ** 31 - 1]
+    got = subprocess.run([str(tmp_path / "workgroups")], input="\n".join(map(str, asked)), capture_output=True, text=True, check=True).stdout.split()
+    for n, w in zip(asked, map(int, got)):
+        assert 1 <= w and 256 * w < 2 ** 32 and (4 * w >= n or w == 2 ** 22)
