@@ -1071,13 +1071,15 @@ def page_bounds(keys, page_table, cached, lengths, bounds, seq=None, max_new=Non
 
 def page_select(q, bounds, page_table, lengths, page_size: int, pages: int, seq=None, first: int = 1, last: int = 1, max_length=None, workspace=None):
     """The pages that queries [B,Hq,K] read: of every key head the first, the last and those of the largest bounds of a score, at most `pages`.
-    Returns (chosen [B,Hk,pages], tokens [B,Hk]) for ``paged_decode_pages``."""
+    Returns (chosen [B,Hk,pages], tokens [B,Hk]) for ``paged_decode_pages``.  More queries than a launch takes go in several."""
     if _rows_native is not None and type(q) is torch.Tensor and q.is_cuda:
         dev = torch._C._cuda_getDevice()
         r = _rows_native.page_select(q, bounds, page_table, lengths, seq, workspace, page_size, pages, first, last, max_length, dev,
                                      torch._C._cuda_getCurrentRawStream(dev))
-        if r is not None:
-            return r if type(r) is tuple else _check(r)
+        if type(r) is tuple:
+            return r
+        if r is not None and r != OSDN_ERR_SHAPE:           # (too many queries are that, too)
+            _check(r)
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(bounds, torch.Tensor) or bounds.dim() != 4:
         raise TypeError("expected q [B,Hq,K] and bounds [n_pages, Hk, 2, K] as CUDA/HIP torch tensors")
     B, Hq, K = q.shape
@@ -1085,17 +1087,31 @@ def page_select(q, bounds, page_table, lengths, page_size: int, pages: int, seq=
     g = _pages(page_table, page_size, n_pages)
     if max_length is None:
         max_length = min(g.max_pages * max(int(page_size), 0), 0x7fffff00)
-    p = make_select_params(B, Hq, Hk, K, q.dtype == torch.bfloat16, max_length, pages=pages, first=first, last=last)
+    of = lambda n: make_select_params(n, Hq, Hk, K, q.dtype == torch.bfloat16, max_length, pages=pages, first=first, last=last)
+    p = of(B)
     if p.pages < 1:
         raise OsdnError(-5)
-    if B * Hk * p.pages > 2**31 - 1:                        # (before they are allocated)
+    rows = max(Hk, 1) * max(p.pages, -(-p.max_length // max(g.page_size, 1)))               # pages of a query that are written, or have a score
+    most = min(65535, (1 << 21) // max(Hk, 1), (2**31 - 1) // rows) or 1
+    if Hk * p.pages > 2**31 - 1:                            # (before they are allocated)
         raise OsdnError(OSDN_ERR_SHAPE)
+    if B > most:
+        if not q.is_cuda:
+            raise TypeError("q: expected a CUDA/HIP torch tensor")
+        _array(lengths, torch.int32, (B,), "lengths")
+        _array(seq, torch.int32, (B,), "seq")
+        if seq is None:
+            seq = torch.arange(B, dtype=torch.int32, device=q.device)
+        most = -(-B // -(-B // most))
     new = lambda *shape: torch.empty(*shape, dtype=torch.int32, device=q.device)
     chosen, tokens = new(B, Hk, p.pages), new(B, Hk)
-    if workspace is None:
-        n = osdn_page_select_workspace_bytes(p, page_size)
-        workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-    osdn_page_select(p, g, q, bounds, lengths, seq, chosen, tokens, workspace)
+    part = (lambda t, i: t) if B <= most else (lambda t, i: None if t is None else t[i:i + most])
+    for i in range(0, max(B, 1), most):
+        p, ws = of(min(most, B - i)), workspace
+        if ws is None:
+            n = osdn_page_select_workspace_bytes(p, page_size)
+            ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+        osdn_page_select(p, g, part(q, i), bounds, part(lengths, i), part(seq, i), part(chosen, i), part(tokens, i), ws)
     return chosen, tokens
 
 
