@@ -492,12 +492,17 @@ PyObject *paged_plan(PyObject *, PyObject *const *a, Py_ssize_t n) {
         !int_array(t[4], dev, at::IntArrayRef(&one, 1), &n_free))
         Py_RETURN_NONE;
     const int64_t N = tokens, line[] = {1, N}, b1 = B + 1, slot_bytes = a[9] == Py_True ? 8 * N : 0;
-    const at::Tensor all = at::empty({slot_bytes + 4 * (2 * N + 2 * B + 2)}, t[0]->options().dtype(at::kByte));
-    const auto take = [&](int64_t at, at::IntArrayRef sizes) { return piece(all, at::kInt, slot_bytes + 4 * at, sizes); };
-    const at::Tensor pos = take(0, at::IntArrayRef(line, 2)), rows = take(N, at::IntArrayRef(line, 2)), lengths = take(2 * N, b), starts = take(2 * N + B, at::IntArrayRef(&b1, 1));
-    const at::Tensor left = take(2 * N + 2 * B + 1, at::IntArrayRef(&one, 1));
+    // One allocation for all, but where there are many tokens: what a server keeps of a step (lengths, starts, n_free) then does not hold their places, too
+    const int64_t of_tokens = slot_bytes + 8 * N, of_requests = 4 * (2 * B + 2);
+    const bool apart = of_tokens > 1 << 16;
+    const at::TensorOptions bytes = t[0]->options().dtype(at::kByte);
+    const at::Tensor places = at::empty({of_tokens + (apart ? 0 : of_requests)}, bytes), kept = apart ? at::empty({of_requests}, bytes) : places;
+    const auto take = [&](int64_t at, at::IntArrayRef sizes) { return piece(places, at::kInt, slot_bytes + 4 * at, sizes); };
+    const auto keep = [&](int64_t at, at::IntArrayRef sizes) { return piece(kept, at::kInt, (apart ? 0 : of_tokens) + 4 * at, sizes); };
+    const at::Tensor pos = take(0, at::IntArrayRef(line, 2)), rows = take(N, at::IntArrayRef(line, 2)), lengths = keep(0, b), starts = keep(B, at::IntArrayRef(&b1, 1));
+    const at::Tensor left = keep(2 * B + 1, at::IntArrayRef(&one, 1));
     at::Tensor slots;
-    if (slot_bytes) slots = piece(all, at::kLong, 0, at::IntArrayRef(&N, 1));
+    if (slot_bytes) slots = piece(places, at::kLong, 0, at::IntArrayRef(&N, 1));
     int32_t *l = ints(lengths), *s = ints(starts), *p = ints(pos), *r = ints(rows), *f = ints(left);
     int64_t *sl = slots.defined() ? static_cast<int64_t *>(slots.data_ptr()) : nullptr;
     int rc;
