@@ -12,6 +12,7 @@ time of a token and how far the outputs lie from those of the whole text at once
 backward of the recurrence with the norm in front of it.
 """
 import argparse
+import math
 import os
 import sys
 import time
@@ -72,15 +73,16 @@ class Serving:
         self.S = torch.zeros(sequences, c.heads, c.head_width, c.head_width, device=device)
         self.d = torch.ones(sequences, c.heads, c.head_width, device=device)
 
-    def mix(self, x, row=None):
-        """The recurrence over x [1,T,width] of sequence `row`, or over one token x [B,1,width] of each sequence."""
+    def mix(self, x, row=None, served=None):
+        """The recurrence over x [1,T,width] of sequence `row`, or over one token x [B,1,width] of each sequence; served [B]: of those that it is true for."""
         c, w = self.c, self.w
         q, k, v = split(x @ w["mix_in"], c.heads, c.heads, c.heads)
         gates = (x @ w["mix_gates"]).float()
         beta, log_alpha = torch.sigmoid(gates[..., : c.heads]).contiguous(), -torch.nn.functional.softplus(gates[..., c.heads:] - 2).contiguous()
         q, k = ob.qk_norm(q, k, hp=UNIT)
         if row is None:
-            o, self.S, self.d = ob.step(q, k, v.contiguous(), beta, log_alpha, None, self.d, self.S, in_place=True)
+            o, S, d = ob.step(q, k, v.contiguous(), beta, log_alpha, None, self.d, self.S, in_place=served is None)
+            self.S, self.d = (S, d) if served is None else (torch.where(served[:, None, None, None], S, self.S), torch.where(served[:, None, None], d, self.d))
         else:
             o, self.S[row], self.d[row], _ = ob.forward(q, k, v.contiguous(), beta, log_alpha, None, self.d[row:row + 1], self.S[row:row + 1])
         return x + o.flatten(2) @ w["mix_out"]
@@ -124,16 +126,22 @@ class Serving:
         return x + o.view(*x.shape[:2], -1) @ w["att_out"]
 
     def prompt(self, row, x):
-        """A prompt x [T,width] of one sequence; returns the outputs [T,width]."""
+        """A prompt x [T,width] of one sequence; returns the outputs [T,width].  MemoryError: the pool has no pages for it, nothing has changed."""
         T, at = x.shape[0], int(self.lengths[row])
         positions, seq, before = self.places(torch.full((1,), T, dtype=torch.int32, device=x.device), T, row)
+        if int(self.lengths[row]) != at + T:
+            raise MemoryError(f"no pages for {T} tokens of sequence {row}")
         return self.attend(self.mix(x[None], row), positions, seq, at + T, before, row)[0]
 
     def token(self, x, longest):
-        """One new token x [B,width] of every sequence; returns the outputs [B,width].  longest: no sequence is longer afterwards.  (The pool has to
-        hold a page for each that needs one: the tokens of those that are served stand side by side, and are the rows of x only if all are.)"""
-        positions, seq, before = self.places(torch.ones_like(self.lengths), x.shape[0])
-        return self.attend(self.mix(x[:, None]), positions.view(-1, 1), seq.view(-1, 1), longest, before)[:, 0]
+        """One new token x [B,width] of every sequence; returns the outputs [B,width].  longest: no sequence is longer afterwards.  A sequence that needs a page which the pool
+        does not have keeps its length and its state, and its outputs are NaN; nothing is asked of the host."""
+        _, _, before = self.places(torch.ones_like(self.lengths), x.shape[0])
+        served = self.lengths > before
+        # (the plan's tokens are those of the served sequences, side by side: here every row of x keeps its place)
+        positions, seq = torch.where(served, before, -1)[:, None], torch.arange(len(before), dtype=torch.int32, device=x.device)[:, None]
+        y = self.attend(self.mix(x[:, None], served=served), positions, seq, longest, before)[:, 0]
+        return torch.where(served[:, None], y, math.nan)
 
 
 def mixer_step(q, k, v, beta, log_alpha, dO, hp=ob.Hyper()):
