@@ -376,7 +376,7 @@ int osdn_paged_decode(const osdn_decode_params *p, const osdn_cache *cache, cons
  * captured into a graph.  A list holds the pages that are not in use: entries [0, n_free) of free_list, taken from its end.
  */
 typedef struct {
-    int32_t *table;                 /* [n_seqs, max_pages], rows table_stride entries apart; NULL where a call only reads lengths */
+    int32_t *table;                 /* [n_seqs, max_pages], rows table_stride entries apart */
     int64_t table_stride;
     int32_t *free_list;             /* [free_capacity] page numbers */
     int32_t free_capacity;
@@ -454,6 +454,8 @@ int osdn_paged_read_mx(const osdn_norm_params *p, const osdn_cache_mx *cache, co
  * osdn_paged_decode over a cache in 4 bits: the same with the values that the codes stand for (io_dtype: of q and o).  Products are of bf16
  * numbers with fp32 sums: the cache's values are exact in bf16; with bf16 I/O weights are the sum of two such numbers, with fp32 I/O
  * queries and weights that of three, which hold all digits of a float.
+ * How a call is cut, and whether codes are loaded past the caches, hangs on p->max_length, as lengths are not known to the host: a bound that is far above
+ * them gives the same results in more time (512 sequences of 200 tokens, four heads: bounds of 200, 2048, 4096 and 131072 18.7, 18.8, 30.9 and 30.3 us).
  */
 size_t osdn_paged_decode_mx_workspace_bytes(const osdn_decode_params *p);
 int osdn_paged_decode_mx(const osdn_decode_params *p, const osdn_cache_mx *cache, const osdn_rows *q, const int32_t *lengths,
@@ -474,7 +476,8 @@ typedef struct {
 /*
  * The smallest and the largest key of every page, for each head and element, kept up with what is appended: those of the pages that the
  * tokens cached[b] <= i < lengths[b] of sequence seq[b] stand in.  A page that had tokens before keeps their bounds, one that begins
- * with these tokens gets new ones.  NaN among the keys makes the element's bounds NaN.
+ * with these tokens gets new ones.  NaN among the keys makes the element's bounds NaN.  B is at most 65535, B Hk at most 2^21, and that times the pages
+ * that max_new tokens of a sequence may lie in (no more than max_pages) less than 2^31; the launch is sized by it.
  *   cache             the keys alone are looked at (v may be NULL)
  *   cached, lengths   [B] int32 (as osdn_paged_plan leaves them); nothing to do where cached >= lengths
  *   seq               [B] int32 or NULL (=> b).  No sequence twice
@@ -492,7 +495,9 @@ int osdn_page_bounds_mx(const osdn_select_params *p, const osdn_cache_mx *cache,
  * max(q, 0)).  Of the pages that the sequence has, the first `first`, the last `last` and those of the largest scores are chosen, p->pages in
  * all or as many as there are; equal scores: the earlier page.  A page that is not there, and one whose score is NaN, come before all
  * others; so does one with an infinite bound where its Q is zero.
- * max_length is no more than 2^30 pages, and p->pages no more than that.
+ * B is at most 65535, B Hk at most 2^21, Hq at most 65535; p->pages and the pages of max_length tokens are at most 2^30 and, times B Hk, less than 2^31; p->pages
+ * hold at most 2^31 - 256 tokens.  Who makes the scores hangs on max_length (64 sequences of 8192 tokens in pages of 16, one head of 64: bounds of 8192 and 131072 tokens 9.3
+ * and 15.6 us).
  *   q                 [B,Hq,K] rows (token is not used)
  *   lengths, seq      as for osdn_paged_decode
  *   chosen            [B,Hk,pages] int32 out: page numbers in the order of their tokens, -1 behind the last (and for one that is not there)

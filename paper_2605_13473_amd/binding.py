@@ -951,7 +951,7 @@ def _decode_in_parts(q, most, bytes_of, call, per_head, workspace, want_lse):
 
 
 def paged_decode_mx(q, cache, page_table, lengths, seq=None, scale=None, window: int = 0, max_length=None, want_lse: bool = False, workspace=None):
-    """``paged_decode`` over a cache in 4 bits."""
+    """``paged_decode`` over a cache in 4 bits.  max_length: no length is above it; the nearer to the longest, the better the call is cut."""
     if _rows_native is not None and type(q) is torch.Tensor and q.is_cuda and type(cache) is tuple and len(cache) == 4:
         dev = torch._C._cuda_getDevice()
         r = _rows_native.paged_decode_mx(q, *cache, page_table, lengths, seq, workspace, scale, window, max_length, want_lse, dev,

@@ -1,5 +1,6 @@
-// Attention over chosen pages of a cache in 4 bits.  Bound by the lines that it fetches: with heads side by side a row of 64 bytes is half of one, whose other half another head wants only if it chose
-// the page too (48 sequences, 32 pages of 64 tokens for each of 8 heads: 107 MB asked for, 190 fetched, 44 us; heads apart 28).
+// Attention over chosen pages of a cache in 4 bits.  Bound by its loads where heads lie side by side: a row of 64 bytes is half of a line, whose other half another head wants only if it
+// chose the page too (48 sequences, 32 pages of 64 tokens for each of 8 heads, 107 MB: 44 us; heads apart, where a load takes whole lines, 28).  What of it the halves cost and what the
+// scales, 4 bytes of a line a row, was not measured apart.
 #include "osdn_decode_tiles.h"
 #include "osdn_plan.h"
 

@@ -132,7 +132,7 @@ template <typename IO, int W, bool C = false> struct RowTile {
 // A row of K elements is K / 2 bytes of codes and K / 32 scales.  Its four lanes take K / 4 adjacent elements each, whole words of eight codes, which one
 // instruction a pair turns into the bf16 numbers that they stand for, exactly; the order of a row's elements is the same on both sides of
 // the first product, so nothing is passed between lanes.  Values go through LDS as bf16.  Bound by memory where there is enough: 573 MB of 512 sequences of 1 to 4096 tokens, four heads of 128,
-// 114 us, 5.0 TB/s (in bf16 2.1 GB, 371); 142 MB of one sequence 32, its second kernel 4 of them; one of 1531 tokens 10.3, two launches.  fp32 queries and weights are sums of three bf16 numbers, which hold all their digits.
+// 114 us, 5.0 TB/s (in bf16 2.1 GB, 371); 142 MB of one sequence 32, its second kernel 4 of them; one of 1531 tokens 9.5, two launches.  fp32 queries and weights are sums of three bf16 numbers, which hold all their digits.
 // REGULAR (fp4_regular): a row's place in all four arrays comes of one offset.  ONCE (decode_mx_once): the codes are loaded past the caches.
 template <typename IO, int W, bool REGULAR, bool C = false, bool ONCE = false> struct Fp4Tile {
     using T = IO;

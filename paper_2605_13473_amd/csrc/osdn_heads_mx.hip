@@ -2,8 +2,8 @@
 //
 // A wavefront takes 64 / LANES tokens next to each other, the lanes of a row one of them each, and walks the heads of their queries, keys and values: what does not depend on the head
 // (position, page, angles, the rows' addresses) is found once for all of them, and the codes of adjacent tokens, which a cache that holds a page head
-// after head has side by side, leave together.  Bound by memory: 65536 tokens of 16 + 4 + 4 heads of 128 in bf16 appended 154 us, 4.6 TB/s (a token a wavefront 205: 80 MB more are written,
-// as rows of 64 and 4 bytes leave one by one), and read back 29 us, 5.9 TB/s (43).
+// after head has side by side, leave together.  Bound by memory: 65536 tokens of 16 + 4 + 4 heads of 128 in bf16 appended 147 us, 4.8 TB/s (a token a wavefront 205: 80 MB more are written,
+// as rows of 64 and 4 bytes leave one by one), and read back 31 us, 5.6 TB/s (43).  (Append: calls in a loop; read back: the smallest of twelve launches in a kernel trace.)
 #include "osdn_heads.h"
 
 namespace osdn {
@@ -11,8 +11,9 @@ namespace osdn {
 // A block of 32 elements, VE of them a lane, becomes codes and a scale 2^e, e the least (from -120 to 125) with the largest element no more than 7 * 2^e: what lies
 // between 6 and 7 is off by no more than what lies between 4 and 6 may be.  The codes are the nearest values, ties to the even code.
 // Which code that is must not hang on a rounding before.  Values come as they are.  Keys are computed in fp32 with a bound of their error, and where an element with
-// its error either way could get another code or its block another scale, which one block of rows in hundreds has, once more in 64 bits.  (All of them in 64 bits,
-// a wavefront a token: 65536 tokens of 16 + 4 + 4 heads of 128 in bf16 293 us, so 201.)
+// its error either way could get another code or sign, or its block another scale, once more in 64 bits.  (All of them in 64 bits, a wavefront a token: 65536 tokens of 16 + 4 + 4 heads of 128
+// in bf16 293 us, so 201.)  Of normed or rotated keys one block of rows in hundreds goes that way.  Keys of bf16 that come as they are mostly do: they have no error, but get its bound all
+// the same, and one of their elements in ninety stands on a border of two codes.  The same tokens without norm and rotation take 143 us, as memory is what they wait for.
 __device__ __forceinline__ int max_block(int x, int lanes) {
     auto with = [&](int y) { x = max(x, y); };
     with(__builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, true));         // quad_perm [1,0,3,2]

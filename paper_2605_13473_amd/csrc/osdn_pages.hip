@@ -9,12 +9,13 @@
 //            <Q-, lo> + <Q+, hi>  with  Q- = sum of min(q, 0), Q+ = sum of max(q, 0):
 //            one row of 2 K products per page and key head, however many query heads there are.  The pages of the largest sums are taken.
 //
-// plan and release are bound by latency: a launch, the lengths, the list, the table, one after the other (256 requests of a token 3.8 us, 96 prompts of 65536 tokens 5.9, whose positions, rows and
-// slots are 1 MB; 64 sequences of 24 pages back 5.0).  A workgroup of 16 wavefronts holds the running sums, which every one of many makes for itself rather than wait for another's.
-// bounds reads the new rows and the bounds of the pages that had some before (8 heads of one token 3.7 us, of 48 in 4 bits 4.7).
-// select is bound by the bounds that it reads where there are many: 4096 pages of 8 heads 15.4 us, of which the scores are 7.4 (17 MB), 384 rows of up to 512 pages 18.0 (44 MB, and half of
+// plan and release are bound by latency: a launch, the lengths, the list, the table, one after the other (256 requests of a token 4.3 us, 96 prompts of 65536 tokens 6.3, whose positions,
+// rows and slots are 1 MB; 64 sequences of 24 pages back 5.1).  A workgroup of 16 wavefronts holds the running sums, which every one of many makes for itself rather than wait for another's.
+// bounds reads the new rows and the bounds of the pages that had some before (8 heads of one token 3.3 us, of 48 sequences in 4 bits 4.3).
+// select is bound by the bounds that it reads where there are many: 4096 pages of 8 heads 13.7 us, of which the scores are 7.0 (17 MB), 384 rows of up to 512 pages 17.1 (44 MB, and half of
 // the vector instructions' time), 256 of 4096 109 (537 MB, 4.9 TB/s).  Sums of select are in 64 bits: the products of bf16 numbers are exact there and so, but for a spread of more than
 // 2^25 between them, are their sums, so that which page wins does not hang on their order.
+// (The smallest of twelve launches in a kernel trace; 256 of 4096 pages: calls in a loop.)
 #include "osdn_kernels.h"
 #include "osdn_plan.h"
 

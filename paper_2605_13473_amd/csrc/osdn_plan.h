@@ -332,17 +332,30 @@ inline long long decode_span(int max_length, int window) {
 //    18.7, 18.3, 20.3, 21.8, bf16 2 x 58831 x 2 16.2, 16.1, 18.8, 20.9, K = 128, 4 x 32768 x 1 25.5, 22.1, 22.8, 24.4; but 8 x 4096 x 4 18.4, 19.4, 18.2, 17.5).
 //  - and not so many that the parts (an fp32 row of each query head) outweigh what a share reads: 8 x 8000 x 2 with 32 query heads each, 256 and 512
 //    shares 31.6 and 35.3.
-// Over a cache in 4 bits, whose rows are a quarter as long, what is the same for every row and every call weighs more, and so does the join (us, as above, four heads of K = 128 in
-// bf16 unless said):
-//  - a row each up to 768 tokens (K = 256: 384), where the second kernel costs more than what it makes shorter: 1 x 500 x 8 7.1 and 8.7, 16 x 800 9.7 and 11.0, 4 x 300, K = 256, 8.8 and
-//    11.9; but 1 x 1200 x 8 11.9 and 8.7, 4 x 700, K = 256, 12.7 and 12.5; up to 2048 where every CU has a row (32 x 2000 x 8 18.7 and 21.8, uneven 17.9 and 25.5; 32 x 3000 x 8 uneven 24.1
-//    and 22.4), and to 3000 where it has two (64 x 3000 x 8 42.6 and 51.5, uneven 31.5 and 37.4; 512 x 3000 151 and 160; but uneven 64 x 8192 x 8 75.3 and 65.8).
-//  - four rows together from two rows a CU on: a share then begins fewer rows (uneven 512 x 4096, one by one 145, so 128; 64 x 8192 x 8 76.5 and 65.8; but 1 x 131072 x 8, whose rows all
-//    shares cut, 34.8 and 37.1); of heads side by side, whose lines they then share, also of 32 rows and 64 MB on, two shares a CU (4 x 32000 x 8 62.7 and 44, K = 64 52.6 and 32; 16 x 4096 x 8
-//    33.4 and 26.9; 50 x 8000 x 8 157 and 114, K = 64 137 and 80; but 16 x 8000 x 4 26.8 and 27.5, 1 x 131072 x 8 42.7 and 43.6).
-//  - two shares a CU, four for rows of 64 elements and where there is about a row for each (uneven 64 x 4096 x 8, K = 64, 256, 512, 768 and 1024 34.4, 27.4, 26.7, 25.5; 40 x 4000 x 8,
-//    K = 256, 84.3, 65.1, 58.8, 55.9; but 1 x 131072 x 8 44.6, 34.8, 37.8, 37.1; 16 x 8192 x 8 42.1, 34.7, 38.1, 37.5); three for many rows of 128 whose heads lie apart, the codes past the caches (512, 768, 1024: uneven
-//    512 x 4096 119, 115.5, 118.7, 64 x 4096 x 4 33.9, 27.9, 29.9, fp32 256 x 4096 x 8 128, 121, 131, even 64 x 8192 x 8 107, 107.5, 104, 28 x 8192 x 8 52.4, 48.9, 45.9, even 55.3, 54.3, 55.1, but 16 x 8192 x 8 33.6, 36.1, 37.2; heads side by side uneven 512 x 4096 140.5, 145, 146).
+// Over a cache in 4 bits, whose rows are a quarter as long, what is the same for every row and every call weighs more, and so does the join (us, as above, four heads of
+// K = 128 in bf16 unless said):
+//  - a row each up to 768 tokens (K = 256: 384), where the second kernel costs more than what it makes shorter.  A row each and shares:
+//        1 x 500 x 8             7.1   8.7        16 x 800              9.7  11.0        4 x 300, K = 256      8.8  11.9
+//        1 x 1200 x 8           11.9   8.7                                               4 x 700, K = 256     12.7  12.5
+//    up to 2048 where every CU has a row:
+//        32 x 2000 x 8          18.7  21.8        uneven               17.9  25.5        32 x 3000 x 8 uneven 24.1  22.4
+//    and to 3000 where it has two:
+//        64 x 3000 x 8          42.6  51.5        uneven               31.5  37.4        512 x 3000            151   160
+//        64 x 8192 x 8 uneven   75.3  65.8
+//  - four rows together from two rows a CU on, as a share then begins fewer rows.  One by one and together:
+//        512 x 4096 uneven       145   128        64 x 8192 x 8        76.5  65.8        1 x 131072 x 8       34.8  37.1 (all shares cut its rows)
+//    of heads side by side, whose lines they then share, also from 32 rows and 64 MB on, with two shares a CU:
+//        4 x 32000 x 8          62.7  44          K = 64               52.6  32          16 x 4096 x 8        33.4  26.9
+//        50 x 8000 x 8           157   114        K = 64                137  80
+//        16 x 8000 x 4          26.8  27.5        1 x 131072 x 8       42.7  43.6
+//  - two shares a CU, four for rows of 64 elements and where there is about a row for each.  256, 512, 768 and 1024 shares:
+//        64 x 4096 x 8, K = 64, uneven            34.4  27.4  26.7  25.5                  40 x 4000 x 8, K = 256   84.3  65.1  58.8  55.9
+//        1 x 131072 x 8                           44.6  34.8  37.8  37.1                  16 x 8192 x 8            42.1  34.7  38.1  37.5
+//    three from 192 rows of 128 on whose heads lie apart, the codes past the caches.  512, 768 and 1024 shares:
+//        512 x 4096 uneven                         119   115.5 118.7                      64 x 4096 x 4            33.9  27.9  29.9
+//        256 x 4096 x 8, fp32                      128   121   131                        64 x 8192 x 8            107   107.5 104
+//        28 x 8192 x 8 even                       55.3  54.3  55.1                        uneven                   52.4  48.9  45.9 (here four would be better)
+//        16 x 8192 x 8                            33.6  36.1  37.2                        512 x 4096 uneven, heads side by side   140.5  145  146
 inline bool decode_mx_each(long long span, long long all, int K) {
     return span <= (all >= 2 * NUM_CU ? 3000 : all >= NUM_CU ? 2048 : K == 256 ? 384 : 768);
 }
