@@ -1,4 +1,4 @@
-"""Selection for more queries than a launch takes."""
+"""Selection for more queries than a launch takes, and of all pages."""
 import pytest
 import torch
 
@@ -28,3 +28,19 @@ def test_more_queries_than_a_launch_takes(B, max_length):
     for bad in (lengths[:5], lengths.long()):
         with pytest.raises((TypeError, ValueError)):
             ob.page_select(q, b, x["table"], bad, 8, 4, seq=seq, max_length=max_length)
+
+
+@pytest.mark.parametrize("form", [dict(io="bf16"), dict(io="f32"), dict(io="bf16", mx=True), dict(io="f32", mx=True)], ids=str)
+def test_all_pages_cut_alike_are_the_bits_of_the_whole_sequence(form):
+    """As many pages as there are, a row to a workgroup on both sides: the same sums in the same order."""
+    x = make([300, 47, 0, 16], 8, 2, 128, 16, **form)
+    chosen, tokens = ob.page_select(x["q"], bounds_of(x), x["table"], x["lengths"], 16, 25)
+    p = ob.make_decode_params(4, 8, 2, 128, x["dt"] == torch.bfloat16, 400, shares=-1)
+    out = [(torch.empty_like(x["q"]), torch.empty(4, 8, device="cuda")) for _ in range(2)]
+    if x["mx"]:
+        ob.osdn_paged_decode_pages_mx(p, x["q"], x["cache"], chosen, tokens, *out[0])
+        ob.osdn_paged_decode_mx(p, x["q"], x["cache"], x["table"], x["lengths"], None, *out[1])
+    else:
+        ob.osdn_paged_decode_pages(p, x["q"], *x["cache"], chosen, tokens, *out[0])
+        ob.osdn_paged_decode(p, x["q"], *x["cache"], x["table"], x["lengths"], None, *out[1])
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
