@@ -149,7 +149,10 @@ __device__ __forceinline__ bool row_ready(const HeadsArgs &a, const Turn<T, K, R
         for (int e = 0; e < VE; ++e) {
             const float own = x[e] * (r * w.own[e]), other = y[e] * (r * w.partner[e]);
             z[e] = __builtin_fmaf(own, c[e], other * s[e]);
-            if constexpr (KEY) off[e] = __builtin_fmaf(__builtin_fabsf(own), __builtin_fabsf(c[e]), __builtin_fabsf(other * s[e])) * KEY_OFF;
+            if constexpr (KEY) {                // (and where products are next to the smallest numbers no less than all of them)
+                const float both = __builtin_fmaf(__builtin_fabsf(own), __builtin_fabsf(c[e]), __builtin_fabsf(other * s[e]));
+                off[e] = __builtin_fmaf(both, KEY_OFF, __builtin_fminf(both, 0x1p-140f));
+            }
         }
     }
     return sure;

@@ -54,3 +54,22 @@ def test_weights_next_to_the_smallest_numbers(size, weight, rotary):
     # (size -20: eps, 2^-20, makes the factor of a row 2^10, and keys of 2^-135 are below the least scale's codes)
     assert (float(z.abs().amax()) > 2.0 ** -118 and int((got[0] & 7).sum()) > 0) == (size >= 0)
     assert torch.equal(got[1], want[1]) and torch.equal(got[0], want[0])
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("least", [0, -100, -130, -145])
+def test_signs_of_the_smallest_elements_that_cancel(least, interleaved):
+    """Products that fp32 rounds to a multiple of 2^-149 or to zero: the sign of what is left of two of them."""
+    g = torch.Generator().manual_seed(11)
+    T, half = 40, 32
+    x, c, s = (torch.rand(T, half, generator=g) + 0.5 for _ in range(3))
+    x = torch.ldexp(x, torch.tensor(float(least))).float()
+    y = (x.double() * c.double() / s.double()).float()
+    y[:, 0] = 0.25                                                      # (a block that is not small)
+    y[::2, 1::4], x[1::2, 2::4] = 0.0, 0.0                              # nothing to cancel, and nothing at all
+    x[::2, 1::8] = 0.0
+    sums = x.double() * c.double() - y.double() * s.double()
+    k = torch.stack([x, y], dim=-1).flatten(1) if interleaved else torch.cat([x, y], dim=1)
+    got, want, z = append(k[None, :, None].cuda(), torch.cat([c, s], dim=1).cuda(), interleaved=interleaved)
+    assert torch.equal(z[0, :, 0, 0::2] if interleaved else z[0, :, 0, :half], sums)
+    assert torch.equal(got[1], want[1]) and torch.equal(got[0], want[0])
