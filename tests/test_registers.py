@@ -1,8 +1,8 @@
 """What the kernels of attention over a cache take of a CU's registers, as the built library says it of itself: so many workgroups are held side by side."""
 import re
 import struct
+import subprocess
 
-import msgpack
 import pytest
 
 from paper_2605_13473_amd import binding as ob
@@ -24,32 +24,26 @@ def code_objects(blob):
         at = blob.find(MAGIC, at + 1)
 
 
-def kernels_of(elf):
-    start, = struct.unpack_from("<Q", elf, 40)                  # the sections: e_shoff, e_shentsize, e_shnum
-    step, count = struct.unpack_from("<HH", elf, 58)
-    for i in range(count):
-        kind, _, _, offset, size = struct.unpack_from("<IQQQQ", elf, start + i * step + 4)
-        while kind == 7 and size > 12:                          # notes
-            name, words, what = struct.unpack_from("<III", elf, offset)
-            begin = offset + 12 + (name + 3) // 4 * 4
-            if what == 32:
-                yield from msgpack.unpackb(elf[begin:begin + words])["amdhsa.kernels"]
-            used = begin - offset + (words + 3) // 4 * 4
-            offset, size = offset + used, size - used
+def kernels_of(elf, path):
+    path.write_bytes(elf)
+    notes = subprocess.run(["/opt/rocm/llvm/bin/llvm-readelf", "--notes", str(path)], capture_output=True, text=True, check=True).stdout
+    for k in re.findall(r"- \.agpr_count:.*?\.vgpr_count: +\d+", notes, re.S):
+        number = lambda name: int(re.search(rf"\.{name}: +(\d+)", k)[1])
+        yield re.search(r"\.symbol: +'?(\w+)\.kd", k)[1], number("agpr_count") + number("vgpr_count"), number("private_segment_fixed_size")
 
 
 @pytest.fixture(scope="module")
-def decode_kernels():
+def decode_kernels(tmp_path_factory):
     """(rows' format, element, K, chosen pages, R, shares) of every instance of decode_kernel: (registers, scratch)."""
     ob.lib()
-    found = {}
+    found, path = {}, tmp_path_factory.mktemp("code") / "code.elf"
     with open(hb.LIB, "rb") as f:
         for elf in code_objects(f.read()):
-            for k in kernels_of(elf):
-                m = re.match(r"_ZN4osdn13decode_kernelINS_7(RowTile|Fp4Tile)I(f|DF16b)Li(\d+)ELb([01])E(?:Lb([01])ELb[01]E)?EELi([124])ELb([01])E", k[".name"])
+            for name, registers, scratch in kernels_of(elf, path):
+                m = re.match(r"_ZN4osdn13decode_kernelINS_7(RowTile|Fp4Tile)I(f|DF16b)Li(\d+)ELb([01])E(?:Lb([01])ELb[01]E)?EELi([124])ELb([01])E", name)
                 if m:
                     tile, io, K, first, second, R, shared = m.groups()
-                    found[tile, io, int(K), (second if tile == "Fp4Tile" else first) == "1", int(R), shared == "1", k[".name"]] = (k[".vgpr_count"] + k.get(".agpr_count", 0), k[".private_segment_fixed_size"])
+                    found[tile, io, int(K), (second if tile == "Fp4Tile" else first) == "1", int(R), shared == "1", name] = (registers, scratch)
     assert len([k for k in found if k[0] == "RowTile"]) == 2 * 3 * 2 * 3 * 2 and len(found) > 144
     return found
 
